@@ -1,0 +1,4 @@
+// Attention over the 8-bit cache, heads of 192 channels.
+#include "br_kv_attend.h"
+
+void br_kv_launch_attend_192(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st) { br_kv_attend_dim<192>(p, tile, fp8, cus, st); }

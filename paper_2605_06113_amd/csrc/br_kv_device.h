@@ -1,0 +1,107 @@
+// Device-side parameters and helpers of the worker's part (include/br_kv.h): tables, 8-bit cache, attention over it.
+#ifndef BR_KV_DEVICE_H
+#define BR_KV_DEVICE_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "br_kv.h"
+
+#define BR_KV_SPLIT_WGS 768  // most blocks of an attention launch that split rows' tokens among them
+#define BR_KV_TILE 64        // cached tokens of an attention tile
+
+// The tables of all workers, inside the context's workspace.
+struct BrKvTables {
+  int W, B, shift, n_blocks, max_blocks, words;  // words: 32-bit words of a worker's used bits
+  int *lens;                                     // [W][B]
+  int *table;                                    // [W][B][max_blocks]
+  unsigned *used;                                // [W][words]
+};
+
+struct BrKvStep {
+  const int *keep, *add;
+  int *slot, *pos, *start, *count, *status;
+  long long *stats;
+  int cap;
+};
+
+// One layer's cache and what indexes it.
+struct BrKvCache {
+  unsigned char *k, *v;
+  float *ks, *vs;
+  int shift, n_blocks, heads, dim;
+};
+
+struct BrKvTokens {
+  void *k, *v;
+  const int *slot;
+  long long k_token, k_head, v_token, v_head;
+  int n, W, dtype;
+};
+
+struct BrKvAttend {
+  const unsigned short *q;
+  unsigned short *out;
+  float *lse;
+  const int *start, *count, *lens, *table;
+  const unsigned char *k, *v;
+  const float *ks, *vs;
+  float *part;  // sums of the pieces of split rows, see br_kv_attend.h
+  float *ml;    // their maxima and sums of weights
+  int *desc;    // per block: the split piece that begins in it
+  long long q_token, q_head, out_token, out_head;
+  int n_rows, rows, n_tokens, window, group, kv_heads, shift, n_blocks, max_blocks;
+  int bf16, q_wide, out_wide;  // wide: rows of q (out) can be read (written) 16 (8) bytes at a time
+  float scale2;                // scale * log2(e)
+};
+
+void br_kv_launch_clear(const BrKvTables &t, hipStream_t st);
+void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, hipStream_t st);
+void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st);
+void br_kv_launch_append(const BrKvCache &c, const BrKvTokens &t, bool fp8, hipStream_t st);
+void br_kv_launch_read(const BrKvCache &c, const BrKvTokens &t, bool fp8, hipStream_t st);
+
+// br_kv_attend_*.hip, one per head width
+enum { BR_KV_TILE_16 = 0, BR_KV_TILE_32 = 1, BR_KV_TILE_128 = 2 };  // rows of queries of a block's tile
+void br_kv_launch_attend_64(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_attend_96(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_attend_128(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_attend_192(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_attend_256(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+
+#ifdef __HIPCC__
+typedef _Float16 br_h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 br_h8 __attribute__((ext_vector_type(8)));
+typedef float br_f4 __attribute__((ext_vector_type(4)));
+
+// 4 codes to f16, exactly (e4m3 has 4 significant bits, int8 has 8, f16 has 11).  int8: a code plus 128 is put into the mantissa of
+// 1024, 1152 is taken off.
+template <bool FP8>
+__device__ __forceinline__ void br_kv_decode4(unsigned c, br_h2 &lo, br_h2 &hi) {
+  if constexpr (FP8) {
+    lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, 1.0f, false);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, 1.0f, true);
+  } else {
+    c ^= 0x80808080u;
+    const unsigned a = __builtin_amdgcn_perm(0x64646464u, c, 0x04010400u), b = __builtin_amdgcn_perm(0x64646464u, c, 0x04030402u);
+    const br_h2 off = {(_Float16)1152.0f, (_Float16)1152.0f};
+    lo = __builtin_bit_cast(br_h2, a) - off;
+    hi = __builtin_bit_cast(br_h2, b) - off;
+  }
+}
+
+template <bool FP8>
+__device__ __forceinline__ br_h8 br_kv_decode8(unsigned c0, unsigned c1) {
+  br_h2 a, b, c, d;
+  br_kv_decode4<FP8>(c0, a, b);
+  br_kv_decode4<FP8>(c1, c, d);
+  return br_h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ __forceinline__ float br_kv_bf16(unsigned short u) { return __uint_as_float((unsigned)u << 16); }
+__device__ __forceinline__ float br_kv_f16(unsigned short u) { return (float)__builtin_bit_cast(_Float16, u); }
+__device__ __forceinline__ unsigned short br_kv_to_bf16(float x) { return __builtin_bit_cast(unsigned short, (__bf16)x); }
+__device__ __forceinline__ unsigned short br_kv_to_f16(float x) { return __builtin_bit_cast(unsigned short, (_Float16)x); }
+#endif
+
+#endif

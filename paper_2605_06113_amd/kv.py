@@ -1,0 +1,291 @@
+"""Binding over the worker's part of the C-ABI HIP library (include/br_kv.h): block tables, the 8-bit cache of keys and
+values, attention over it.
+
+As in `binding`: argument marshalling only, every step runs in the library's kernels, PyTorch supplies device memory and
+the stream, and nothing falls back to the CPU.  All `*_device` calls enqueue on the cache's stream and return; they check
+types, shapes, strides and devices, since the C ABI takes bare pointers.
+
+    cfg = kv.KvConfig(rows=96, n_blocks=4096, max_blocks=512, n_kv_heads=8, n_q_heads=32, head_dim=128, fmt="fp8")
+    cache = kv.KvCache(cfg)
+    layers = [cache.new_layer() for _ in range(n_layers)]
+    step = cache.alloc_step(token_cap=8192)
+    ...
+    cache.step_device(keep, add, step)                        # tables and slots of this decode step
+    for layer in layers:
+        cache.append_device(layer, k, v, step["slot"])        # k, v [token_cap, n_kv_heads, head_dim]
+        cache.attend_device(layer, q, out, start=step["start"], count=step["count"], max_count=longest)
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+from dataclasses import dataclass
+from typing import Dict, Optional
+
+from .binding import BR_OK, BrError, load as _load
+
+FMT = dict(int8=0, fp8=1)
+NSTATS = 8
+ST = dict(tokens=0, used=1, free=2, rows=3, added=4, refused=5, no_blocks=6, taken=7)
+STATUS = dict(taken=0, no_blocks=1, too_long=2, no_room=3)
+EXPORTS = ("br_kv_workspace_bytes", "br_kv_init", "br_kv_step", "br_kv_append", "br_kv_read", "br_kv_attend", "br_kv_free",
+           "br_kv_last_hip_error", "br_kv_get_layout")
+
+_P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
+
+
+class _Config(C.Structure):
+    _fields_ = [(k, _I) for k in ("n_workers", "rows", "block_tokens", "n_blocks", "max_blocks", "n_kv_heads", "n_q_heads", "head_dim", "fmt", "pad")] + \
+               [("stream", _P), ("workspace", _P), ("workspace_bytes", C.c_uint64)]
+
+
+class _State(C.Structure):
+    _fields_ = [("lens", _P), ("table", _P)]
+
+
+class _Lengths(C.Structure):
+    _fields_ = [("keep", _P), ("add", _P)]
+
+
+class _StepOut(C.Structure):
+    _fields_ = [(k, _P) for k in ("slot", "pos", "start", "count", "status", "stats")] + [("token_cap", _I), ("pad", _I)]
+
+
+class _Layer(C.Structure):
+    _fields_ = [(k, _P) for k in ("k", "v", "k_scale", "v_scale")]
+
+
+class _Tokens(C.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("slot", _P)] + [(k, _L) for k in ("k_token", "k_head", "v_token", "v_head")] + [("n_tokens", _I), ("dtype", _I)]
+
+
+class _Attention(C.Structure):
+    _fields_ = [(k, _P) for k in ("q", "out", "lse", "start", "count", "lens", "table")] + [(k, _L) for k in ("q_token", "q_head", "out_token", "out_head")] + \
+               [("n_tokens", _I), ("max_count", _I), ("window", _I), ("dtype", _I), ("scale", C.c_float), ("pad", _I)]
+
+
+class _Layout(C.Structure):
+    _fields_ = [("lens", C.c_uint64), ("table", C.c_uint64), ("total_bytes", C.c_uint64)]
+
+
+_lib = None
+
+
+def load():
+    """The library with the symbols of include/br_kv.h bound (raises if one is missing)."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = _load()
+    for name in EXPORTS:
+        getattr(lib, name).restype = C.c_int32
+    lib.br_kv_workspace_bytes.restype = C.c_uint64
+    lib.br_kv_workspace_bytes.argtypes = [C.POINTER(_Config)]
+    lib.br_kv_init.argtypes = [C.POINTER(_Config), C.POINTER(_State), C.POINTER(_P)]
+    lib.br_kv_step.argtypes = [_P, C.POINTER(_Lengths), C.POINTER(_StepOut)]
+    lib.br_kv_append.argtypes = [_P, C.POINTER(_Layer), C.POINTER(_Tokens)]
+    lib.br_kv_read.argtypes = [_P, C.POINTER(_Layer), C.POINTER(_Tokens)]
+    lib.br_kv_attend.argtypes = [_P, C.POINTER(_Layer), C.POINTER(_Attention)]
+    lib.br_kv_free.restype = None
+    lib.br_kv_free.argtypes = [_P]
+    lib.br_kv_last_hip_error.argtypes = [_P]
+    lib.br_kv_get_layout.argtypes = [_P, C.POINTER(_Layout)]
+    _lib = lib
+    return lib
+
+
+@dataclass(frozen=True)
+class KvConfig:
+    """Sizes of a cache (limits and meanings: br_kv_config)."""
+
+    rows: int                 # requests a worker may hold: the router's slot limit B
+    n_blocks: int             # blocks of each worker
+    max_blocks: int           # entries of a row's table
+    block_tokens: int = 16
+    n_workers: int = 1
+    n_kv_heads: int = 1
+    n_q_heads: int = 1
+    head_dim: int = 64
+    fmt: str = "int8"         # "int8" or "fp8" (e4m3)
+
+
+def _config(cfg: KvConfig, stream=0, workspace=0, workspace_bytes=0) -> _Config:
+    return _Config(n_workers=cfg.n_workers, rows=cfg.rows, block_tokens=cfg.block_tokens, n_blocks=cfg.n_blocks, max_blocks=cfg.max_blocks,
+                   n_kv_heads=cfg.n_kv_heads, n_q_heads=cfg.n_q_heads, head_dim=cfg.head_dim, fmt=FMT.get(cfg.fmt, -1), stream=stream, workspace=workspace,
+                   workspace_bytes=workspace_bytes)
+
+
+def workspace_bytes(cfg: KvConfig) -> int:
+    return int(load().br_kv_workspace_bytes(C.byref(_config(cfg))))
+
+
+class KvLayer:
+    """One layer's cache: codes k [n_workers * n_blocks, n_kv_heads, block_tokens, head_dim] and v [.., head_dim, block_tokens]
+    (uint8), scales k_scale, v_scale [n_workers * n_blocks, n_kv_heads] (float32)."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.struct = _Layer(k=k.data_ptr(), v=v.data_ptr(), k_scale=k_scale.data_ptr(), v_scale=v_scale.data_ptr())
+        self.ref = C.byref(self.struct)
+
+
+class KvCache:
+    """Owns a workspace tensor and a br_kv_ctx; all methods only marshal arguments."""
+
+    def __init__(self, cfg: KvConfig, lens=None, table=None, device="cuda:0", stream=None):
+        """lens [n_workers, rows], table [n_workers, rows, max_blocks] (int32): requests held at the start."""
+        import torch
+        self.torch, self.lib, self.cfg = torch, load(), cfg
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._dtypes = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+        W, B = cfg.n_workers, cfg.rows
+        nbytes = workspace_bytes(cfg)
+        if nbytes == 0:
+            raise BrError("invalid configuration")
+        if (lens is None) != (table is None):
+            raise BrError("lens and table come together")
+        state = None
+        if lens is not None:
+            self._check(lens, "lens", (W, B), torch.int32)
+            self._check(table, "table", (W, B, cfg.max_blocks), torch.int32)
+            state = C.byref(_State(lens=lens.data_ptr(), table=table.data_ptr()))
+        self.ws = torch.empty(nbytes // 4 + 64, dtype=torch.int32, device=self.device)
+        assert self.ws.data_ptr() % 256 == 0
+        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        c = _config(cfg, stream=self.stream.cuda_stream, workspace=self.ws.data_ptr(), workspace_bytes=self.ws.numel() * 4)
+        ctx = _P()
+        with torch.cuda.device(self.device):
+            self._done(self.lib.br_kv_init(C.byref(c), state, C.byref(ctx)), "br_kv_init")
+        self.ctx = ctx
+        self._init = (lens, table)  # alive until they have been copied
+        lay = _Layout()
+        self._done(self.lib.br_kv_get_layout(ctx, C.byref(lay)), "br_kv_get_layout")
+        #: cached tokens of every row and the block tables, as they are on the device: [n_workers, rows] and [n_workers, rows, max_blocks]
+        self.lens = self.ws[lay.lens // 4:lay.lens // 4 + W * B].view(W, B)
+        self.table = self.ws[lay.table // 4:lay.table // 4 + W * B * cfg.max_blocks].view(W, B, cfg.max_blocks)
+
+    # -- checks ---------------------------------------------------------------
+    def _done(self, rc: int, what: str) -> None:
+        if rc != BR_OK:
+            ctx = getattr(self, "ctx", None)
+            raise BrError(f"{what} failed: rc={rc} hip_error={self.lib.br_kv_last_hip_error(ctx) if ctx else 0}")
+
+    def _check(self, x, name: str, shape, dtype) -> None:
+        """A contiguous tensor of that shape and type on this device."""
+        if tuple(x.shape) != tuple(shape) or x.dtype != dtype or x.device != self.device or not x.is_contiguous():
+            raise BrError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}")
+
+    def _tokens(self, x, name: str, n, heads: int) -> int:
+        """The type code of keys, values, queries or outputs [n, heads, head_dim] with contiguous channels."""
+        shape = (x.shape[0] if n is None and x.dim() else n, heads, self.cfg.head_dim)
+        if tuple(x.shape) != shape or x.device != self.device or (x.stride(2) != 1 and x.numel()):
+            raise BrError(f"{name} must have shape {shape} with contiguous channels on {self.device}")
+        dtype = self._dtypes.get(x.dtype)
+        if dtype is None:
+            raise BrError(f"{name} must be float16, bfloat16 or float32, not {x.dtype}")
+        return dtype
+
+    # -- memory ---------------------------------------------------------------
+    def layer(self, k, v, k_scale, v_scale) -> KvLayer:
+        """A layer over memory that is there (16-byte aligned)."""
+        t, c = self.torch, self.cfg
+        n, H, b, D = c.n_workers * c.n_blocks, c.n_kv_heads, c.block_tokens, c.head_dim
+        self._check(k, "k", (n, H, b, D), t.uint8)
+        self._check(v, "v", (n, H, D, b), t.uint8)
+        self._check(k_scale, "k_scale", (n, H), t.float32)
+        self._check(v_scale, "v_scale", (n, H), t.float32)
+        return KvLayer(k, v, k_scale, v_scale)
+
+    def new_layer(self) -> KvLayer:
+        t, c = self.torch, self.cfg
+        n, H, b, D = c.n_workers * c.n_blocks, c.n_kv_heads, c.block_tokens, c.head_dim
+        e = lambda shape, dtype: t.empty(shape, dtype=dtype, device=self.device)
+        return self.layer(e((n, H, b, D), t.uint8), e((n, H, D, b), t.uint8), e((n, H), t.float32), e((n, H), t.float32))
+
+    def alloc_step(self, token_cap: int) -> Dict[str, object]:
+        """Output arrays of step_device, with room for token_cap new tokens per worker."""
+        t, W, B = self.torch, self.cfg.n_workers, self.cfg.rows
+        e = lambda *shape: t.empty(shape, dtype=t.int32, device=self.device)
+        return dict(slot=e(W, token_cap), pos=e(W, token_cap), start=e(W, B), count=e(W, B), status=e(W, B),
+                    stats=t.empty((W, NSTATS), dtype=t.int64, device=self.device))
+
+    # -- calls ----------------------------------------------------------------
+    def step_device(self, keep, add, out) -> None:
+        """Tables of the next step (br_kv_step): keep, add [n_workers, rows] int32; out: alloc_step's arrays."""
+        i32, W, B = self.torch.int32, self.cfg.n_workers, self.cfg.rows
+        self._check(keep, "keep", (W, B), i32)
+        self._check(add, "add", (W, B), i32)
+        slot = out["slot"]
+        if slot.dim() != 2:
+            raise BrError("slot must have shape (n_workers, token_cap)")
+        cap = slot.shape[1]
+        self._check(slot, "slot", (W, cap), i32)
+        self._check(out["pos"], "pos", (W, cap), i32)
+        for name in ("start", "count", "status"):
+            self._check(out[name], name, (W, B), i32)
+        self._check(out["stats"], "stats", (W, NSTATS), self.torch.int64)
+        a = _Lengths(keep=keep.data_ptr(), add=add.data_ptr())
+        o = _StepOut(slot=slot.data_ptr(), pos=out["pos"].data_ptr(), start=out["start"].data_ptr(), count=out["count"].data_ptr(),
+                     status=out["status"].data_ptr(), stats=out["stats"].data_ptr(), token_cap=cap)
+        self._done(self.lib.br_kv_step(self.ctx, C.byref(a), C.byref(o)), "br_kv_step")
+
+    def _token_struct(self, k, v, slot) -> _Tokens:
+        W = self.cfg.n_workers
+        n = slot.numel()
+        if n % W or slot.dtype != self.torch.int32 or slot.device != self.device or not slot.is_contiguous():
+            raise BrError(f"slot must be a contiguous int32 tensor on {self.device} with the same number of tokens for each worker")
+        dtype = self._tokens(k, "k", n, self.cfg.n_kv_heads)
+        if self._tokens(v, "v", n, self.cfg.n_kv_heads) != dtype:
+            raise BrError("k and v must have one type")
+        return _Tokens(k=k.data_ptr(), v=v.data_ptr(), slot=slot.data_ptr(), k_token=k.stride(0), k_head=k.stride(1), v_token=v.stride(0),
+                       v_head=v.stride(1), n_tokens=n // W, dtype=dtype)
+
+    def append_device(self, layer: KvLayer, k, v, slot) -> None:
+        """Tokens into the cache (br_kv_append): k, v [tokens, n_kv_heads, head_dim], slot [tokens] (step_device's, or alike)."""
+        a = self._token_struct(k, v, slot)
+        self._done(self.lib.br_kv_append(self.ctx, layer.ref, C.byref(a)), "br_kv_append")
+
+    def read_device(self, layer: KvLayer, slot, k, v) -> None:
+        """Tokens out of the cache into k, v [tokens, n_kv_heads, head_dim] (br_kv_read)."""
+        a = self._token_struct(k, v, slot)
+        self._done(self.lib.br_kv_read(self.ctx, layer.ref, C.byref(a)), "br_kv_read")
+
+    def attend_device(self, layer: KvLayer, q, out, lse=None, start=None, count=None, max_count: int = 1, scale: Optional[float] = None, window: int = 0,
+                      lens=None, table=None) -> None:
+        """Attention of q [tokens, n_q_heads, head_dim] over the rows' cached tokens into out (br_kv_attend).
+
+        start, count [n_workers, rows] (step_device's): a row's query tokens; none: token r belongs to row r.  lse [tokens, n_q_heads] float32.
+        scale: 1 / sqrt(head_dim) if not given.  lens, table: instead of the cache's own."""
+        c, t = self.cfg, self.torch
+        dtype = self._tokens(q, "q", None, c.n_q_heads)
+        n = q.shape[0]
+        if dtype == 2:
+            raise BrError("q must be float16 or bfloat16")
+        if self._tokens(out, "out", n, c.n_q_heads) != dtype:
+            raise BrError("q and out must have one type")
+        rows = (c.n_workers, c.rows)
+        if (start is None) != (count is None):
+            raise BrError("start and count come together")
+        for x, name, shape, kind in ((lse, "lse", (n, c.n_q_heads), t.float32), (start, "start", rows, t.int32), (count, "count", rows, t.int32),
+                                     (lens, "lens", rows, t.int32), (table, "table", rows + (c.max_blocks,), t.int32)):
+            if x is not None and (x.numel() != math.prod(shape) or x.dtype != kind or x.device != self.device or not x.is_contiguous()):
+                raise BrError(f"{name} must be a contiguous {kind} tensor of shape {shape} on {self.device}")
+        p = lambda x: None if x is None else x.data_ptr()
+        a = _Attention(q=q.data_ptr(), out=out.data_ptr(), lse=p(lse), start=p(start), count=p(count), lens=p(lens), table=p(table), q_token=q.stride(0),
+                       q_head=q.stride(1), out_token=out.stride(0), out_head=out.stride(1), n_tokens=n, max_count=int(max_count), window=int(window),
+                       dtype=dtype, scale=c.head_dim ** -0.5 if scale is None else float(scale))
+        self._done(self.lib.br_kv_attend(self.ctx, layer.ref, C.byref(a)), "br_kv_attend")
+
+    def close(self) -> None:
+        if getattr(self, "ctx", None):
+            self.stream.synchronize()
+            self.lib.br_kv_free(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
