@@ -30,7 +30,7 @@ bool config_ok(const br_kv_config *c) {
 }
 
 struct Places {
-  uint64_t lens, table, used, part, ml, desc, total;
+  uint64_t lens, table, used, part, ml, arrived, total;
 };
 
 Places make_layout(const br_kv_config &c) {
@@ -49,7 +49,7 @@ Places make_layout(const br_kv_config &c) {
   const uint64_t pieces = 2ull * BR_KV_SPLIT_WGS * 128;
   l.part = take(pieces * c.head_dim);
   l.ml = take(pieces * 2);
-  l.desc = take(4ull * BR_KV_SPLIT_WGS);
+  l.arrived = take(BR_KV_SPLIT_WGS);
   l.total = off;
   return l;
 }
@@ -137,7 +137,7 @@ int32_t br_kv_init(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx *
   t.lens = (int *)(base + at.lens);
   t.table = (int *)(base + at.table);
   t.used = (unsigned *)(base + at.used);
-  int32_t rc = enqueue(ctx, [&] { br_kv_launch_clear(t, ctx->st); });
+  int32_t rc = enqueue(ctx, [&] { br_kv_launch_clear(t, (int *)(base + at.arrived), ctx->st); });
   if (rc == BR_OK && init) rc = enqueue(ctx, [&] { br_kv_launch_load(t, init->lens, init->table, ctx->st); });
   if (rc != BR_OK) {
     delete ctx;
@@ -190,7 +190,7 @@ int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_atten
   p.k = layer->k, p.v = layer->v, p.ks = layer->k_scale, p.vs = layer->v_scale;
   p.part = (float *)(base + ctx->at.part);
   p.ml = (float *)(base + ctx->at.ml);
-  p.desc = (int *)(base + ctx->at.desc);
+  p.arrived = (int *)(base + ctx->at.arrived);
   p.q_token = a->q_token, p.q_head = a->q_head, p.out_token = a->out_token, p.out_head = a->out_head;
   p.n_rows = c.n_workers * c.rows, p.rows = c.rows, p.n_tokens = a->n_tokens, p.window = a->window;
   p.group = group, p.kv_heads = c.n_kv_heads, p.shift = ctx->t.shift, p.n_blocks = c.n_blocks, p.max_blocks = c.max_blocks;

@@ -4,8 +4,9 @@
 // codes, ks_j, vs_j the scales of j's block and head.  One pass over the tokens with a running m.
 //
 // Work: a tile is 64 cached tokens of one row and key head against TQ query rows (query tokens x heads of the group).  All tiles
-// of the call, in the order (row, key head, query tile, token tile), are dealt to the blocks in equal runs, whatever the lengths: a
-// block's run may end inside a row and head, whose pieces are then joined by br_kv_k_join in the order of their tokens.
+// of the call, in the order (row, key head, query tile, token tile), are dealt to the waves in equal runs, whatever the lengths.  A
+// run may end inside a query tile's tokens: pieces of a block's waves are joined in LDS at its end, pieces of several blocks go to
+// memory, where the last block to arrive joins them in the order of their tokens, so that the result does not depend on who that was.
 //
 // A wave's tile on the matrix units, 16x16x32 in f16 (codes are exact there; the queries are scaled to 1..2 by a power of two per
 // row, so they are too unless they span more than f16's exponents):
@@ -58,6 +59,14 @@ __device__ __forceinline__ long long br_kv_row_tiles(const BrKvAttend &p, const 
   return s;
 }
 
+// 16 codes; ONCE: that nobody else of the launch reads
+template <bool ONCE>
+__device__ __forceinline__ uint4 br_kv_load16(const unsigned char *at) {
+  typedef unsigned u4 __attribute__((ext_vector_type(4)));
+  const u4 x = ONCE ? __builtin_nontemporal_load((const u4 *)at) : *(const u4 *)at;
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
 __device__ __forceinline__ unsigned br_kv_pack(float a, float b, int bf16) {
   return bf16 ? (unsigned)br_kv_to_bf16(a) | (unsigned)br_kv_to_bf16(b) << 16 : (unsigned)br_kv_to_f16(a) | (unsigned)br_kv_to_f16(b) << 16;
 }
@@ -81,389 +90,643 @@ __device__ __forceinline__ void br_kv_store_lse(const BrKvAttend &p, const BrKvR
   p.lse[(long long)t * p.kv_heads * p.group + h * p.group + ri - i * p.group] = l == 0.0f ? BR_KV_NEG : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
 
-// D channels, NQ groups of 16 query rows a wave; the block's four waves share the query rows and deal the token tiles (WQ = 1) or
-// have query rows of their own (WQ = 4).
-template <int D, int NQ, int WQ, bool FP8>
-__global__ __launch_bounds__(256, 2) void br_kv_k_attend(BrKvAttend p) {
-  constexpr int TQ = 16 * NQ * WQ, WT = 4 / WQ, NI = D / 64, REST = D % 64 / 32, NK = 2 * NI + REST, ND = D / 16;
-  __shared__ long long before[257], wave_sum[4];
-  __shared__ br_f4 red[WQ == 1 ? 4 * ND * 64 : 1];
-  __shared__ float red_m[4][16], red_l[4][16], red_c[4];
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, n = lane & 15, g = lane >> 4;
-  const int wq = WQ == 1 ? 0 : wv, wt = WQ == 1 ? wv : 0;
+// Pieces go from block to block past the L2s that the XCDs do not share, 8 bytes at a time; the writer waits for its stores before it
+// says that it has delivered.  (Plain stores between fences of the device cost more than the attention: the fences empty
+// whole L2s, 144 rows 390 us.)
+__device__ __forceinline__ void br_kv_put2(float *at, float x, float y) {
+  __hip_atomic_store((unsigned long long *)at, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
-  // the division of the work: tiles before each thread's rows
-  const int per = (p.n_rows + 255) / 256;
-  long long mine = 0;
-  for (int r = tid * per; r < min(p.n_rows, (tid + 1) * per); ++r) {
-    const BrKvRow w = br_kv_row(p, r);
-    if (w.n > 0) mine += br_kv_row_tiles<TQ>(p, w) * p.kv_heads;
-  }
-  long long sum = mine;
-  for (int d = 1; d < 64; d <<= 1) {
-    const long long o = __shfl_up(sum, d, 64);
-    if (lane >= d) sum += o;
-  }
-  if (lane == 63) wave_sum[wv] = sum;
-  __syncthreads();
-  for (int k = 0; k < wv; ++k) sum += wave_sum[k];
-  before[tid + 1] = sum;
-  if (tid == 0) before[0] = 0;
-  __syncthreads();
-  const long long all = before[256];
-  const long long G = max(1ll, min((long long)gridDim.x, all / WT));
-  const int wg = blockIdx.x;
-  if (wg >= G) {
-    if (tid == 0) p.desc[4 * wg + 3] = 0;
-    return;
-  }
-  long long u = all * wg / G;
-  const long long end = all * (wg + 1) / G;
-  int split_r = 0, split_h = 0, split_q = 0, split_n = 0;  // the piece that begins here and ends in another block
+__device__ __forceinline__ float2 br_kv_get2(const float *at) {
+  const unsigned long long x = __hip_atomic_load((const unsigned long long *)at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((unsigned)x), __uint_as_float((unsigned)(x >> 32)));
+}
 
-  if (u < end) {
-    int lo = 0, hi = 255;
+__device__ __forceinline__ void br_kv_stores_done() {
+  __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+__device__ __forceinline__ long long br_kv_div(long long x, long long y) {  // of what is not negative
+  return (x | y) >> 31 ? x / y : (long long)((unsigned)x / (unsigned)y);
+}
+
+// Sums of one wave over some tokens of 16 NQ query rows: o [channel 16 d + 4 g + j][row 16 x + n] (to be multiplied by c), l the sum of
+// weights, both of e^(s - m), m in powers of two (0 where nothing was seen).
+template <int D, int NQ>
+struct BrKvSums {
+  br_f4 o[NQ][D / 16];
+  float m[NQ], l[NQ], c;
+};
+
+// Over the four lanes of a query row: the exchanges of 16 and 32 lanes stay in the vector registers.
+__device__ __forceinline__ float br_kv_max4(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+__device__ __forceinline__ float br_kv_sum4(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Token tiles t .. stop - 1 of row r and key head h for the query rows from row0 on, whose positions lie in first_pos .. last_pos.
+template <int D, int NQ, bool FP8, bool ONCE>
+__device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int r, int h, int row0, int first_pos, int last_pos, int t, int stop,
+                                            BrKvSums<D, NQ> &sums) {
+  constexpr int NI = D / 64, REST = D % 64 / 32, NK = 2 * NI + REST, ND = D / 16;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  // (what is the same for the wave, in scalar registers)
+  auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  w0.n = scalar(w0.n), w0.len = scalar(w0.len), w0.start = scalar(w0.start);
+  r = scalar(r), h = scalar(h), row0 = scalar(row0), first_pos = scalar(first_pos), last_pos = scalar(last_pos), t = scalar(t), stop = scalar(stop);
+  const BrKvRow &w = w0;
+  auto &o = sums.o;
+  auto &m = sums.m;
+  auto &l = sums.l;
+  // queries: channels 64 i + 16 g .. + 15 of its row for each lane, then 8 g .. + 7 of the last 32
+  br_h8 qf[NQ][NK];
+  float qs[NQ];
+  int pos[NQ];
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    const int ri = row0 + 16 * x + n, i = ri / p.group, t = w.start + i;
+    const bool in = i < w.n && t >= 0 && t < p.n_tokens;
+    pos[x] = in ? w.len - w.n + i : -1;
+    const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(h * p.group + ri - i * p.group) * p.q_head : 0);
+    float f[NK * 8], top = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NK; ++c) {
+      const int d = c < 2 * NI ? (c / 2) * 64 + g * 16 + (c & 1) * 8 : NI * 64 + g * 8;
+      unsigned short e[8];
+      if (p.q_wide) {
+        *(uint4 *)e = *(const uint4 *)(at + d);
+      } else {
+        for (int j = 0; j < 8; ++j) e[j] = at[d + j];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float y = in ? (p.bf16 ? br_kv_bf16(e[j]) : br_kv_f16(e[j])) : 0.0f;
+        f[8 * c + j] = y;
+        top = fmaxf(top, fabsf(y));
+      }
+    }
+    top = br_kv_max4(top);
+    // the power of two at or below `top`; not below 2^-100, where its inverse would leave the range
+    const int ex = max((int)(__float_as_uint(top) >> 23), 27);
+    const float inv = __uint_as_float((unsigned)(254 - min(ex, 253)) << 23);
+    qs[x] = top > 3.0e38f && top * 0.0f != 0.0f ? __builtin_nanf("") : __uint_as_float((unsigned)min(ex, 253) << 23) * p.scale2;
+#pragma unroll
+    for (int c = 0; c < NK; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) qf[x][c][j] = (_Float16)(f[8 * c + j] * inv);
+  }
+
+  float cmax = 0.0f, cinv = 0.0f;  // c and its inverse
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    m[x] = BR_KV_NEG, l[x] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) o[x][d] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  const int worker = r / p.rows;
+  const int *table = p.table + (long long)r * p.max_blocks;
+  const int last_block = max(0, (w.len - 1) >> p.shift);
+  const long long cache0 = (long long)worker * p.n_blocks;
+  const int mask = (1 << p.shift) - 1;
+  const int kg = n >> 2, kr = n & 3;  // the token group, and the place in fours, of the lane's row of K
+
+  uint4 kc[4][NI + (NI == 0)];
+  uint2 kx[4];
+  uint4 vc[ND];
+  // block of a lane's 16 tokens, as the table has it; where it is read, one that does not exist is block 0
+  auto id_of = [&](int token) { return table[min(token >> p.shift, last_block)]; };
+  auto there = [&](int id) { return (unsigned)id < (unsigned)p.n_blocks; };
+  auto load_k = [&](int t, int id, bool live) {
+    const unsigned char *at =
+        live ? p.k + ((((cache0 + (there(id) ? id : 0)) * p.kv_heads + h) << p.shift) + ((t * BR_KV_TILE + 16 * kg) & mask) + kr) * D : p.k;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) kc[s][i] = br_kv_load16<ONCE>(at + 4 * s * D + 64 * i + 16 * g);
+      if (REST) kx[s] = *(const uint2 *)(at + 4 * s * D + 64 * NI + 8 * g);
+    }
+  };
+
+  // Codes of K are asked for a tile ahead, scales too, ids two ahead, always, behind a wave's last tile for the cache's first
+  // lines: loads under a branch would make every wait one for all of them (144 rows of 8 key heads, 666 MB: 195 us).
+  int kid1 = 0, vid = 0, vid1 = 0;
+  float ks1 = 0.0f, vs1 = 0.0f;
+  auto load_scales = [&](int id) {
+    const long long at = (cache0 + (there(id) ? id : 0)) * p.kv_heads + h;
+    ks1 = p.ks[at], vs1 = p.vs[at];
+  };
+  if (t < stop) {
+    const int next = t + 1 < stop ? t + 1 : t;
+    const int kid = id_of(t * BR_KV_TILE + 16 * kg);
+    vid = id_of(t * BR_KV_TILE + 16 * g);
+    kid1 = id_of(next * BR_KV_TILE + 16 * kg), vid1 = id_of(next * BR_KV_TILE + 16 * g);
+    load_k(t, kid, true);
+    load_scales(vid);
+  }
+  for (; t < stop; ++t) {
+    const int token = t * BR_KV_TILE + 16 * g;  // of the lane's first weight
+    {
+      const unsigned char *at = p.v + ((((cache0 + (there(vid) ? vid : 0)) * p.kv_heads + h) * D + n) << p.shift) + (token & mask);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) vc[d] = br_kv_load16<ONCE>(at + ((16 * d) << p.shift));
+    }
+    const float ks = there(vid) ? ks1 : 0.0f, vs = there(vid) ? vs1 : 0.0f;
+    const int have = there(vid) ? min(max(w.len - token, 0), 16) : 0;  // of the lane's tokens, those that exist
+
+    br_f4 s[NQ][4];
+#pragma unroll
+    for (int x = 0; x < NQ; ++x)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) s[x][y] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        br_h8 kf;
+        if (c < 2 * NI) kf = c & 1 ? br_kv_decode8<FP8>(kc[y][c / 2].z, kc[y][c / 2].w) : br_kv_decode8<FP8>(kc[y][c / 2].x, kc[y][c / 2].y);
+        else kf = br_kv_decode8<FP8>(kx[y].x, kx[y].y);
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[x][c], s[x][y], 0, 0, 0);
+      }
+    }
+    const int next = t + 1 < stop ? t + 1 : t, after = next + 1 < stop ? next + 1 : next;
+    load_k(next, kid1, t + 1 < stop);
+    load_scales(vid1);
+    kid1 = id_of(after * BR_KV_TILE + 16 * kg);
+    const int vid2 = id_of(after * BR_KV_TILE + 16 * g);
+
+
+    // (a block that no query of the tile sees has no say in c)
+    float top = have > 0 && token <= last_pos && (p.window == 0 || token + 15 > first_pos - p.window) ? fabsf(vs) : 0.0f;
+    top = br_kv_max4(top);
+    float cf = 1.0f;
+    if (top > 8.0f * cmax) {
+      const unsigned e = min(max(__float_as_uint(top) >> 23, 20u), 252u) + 1;
+      cinv = __uint_as_float((254u - e) << 23);
+      cf = cmax * cinv;
+      cmax = __uint_as_float(e << 23);
+    }
+    const float wgt = vs * (256.0f * cinv);
+    // inside: every query of the tile sees all of its tokens, and all exist
+    const bool inside = t * BR_KV_TILE + BR_KV_TILE - 1 <= first_pos && (p.window == 0 || t * BR_KV_TILE > last_pos - p.window) && !__any(!there(vid));
+    br_h8 pf[NQ][2];
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      const float f = qs[x] * ks;
+      float z[16], mx = BR_KV_NEG;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        z[j] = s[x][j >> 2][j & 3] * f;
+        if (!inside && !(j < have && token + j <= pos[x] && (p.window == 0 || token + j > pos[x] - p.window))) z[j] = BR_KV_NEG;
+        mx = fmaxf(mx, z[j]);
+      }
+      mx = br_kv_max4(mx);
+      const bool up = mx > m[x] + 4.0f;
+      if (__any(up || cf != 1.0f)) {
+        const float to = up ? mx : m[x];
+        const float al = m[x] == BR_KV_NEG ? (l[x] != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m[x] - to), ao = al * cf;
+        m[x] = to;
+        l[x] *= al;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[x][d][j] *= ao;
+      }
+      const float ref = m[x] == BR_KV_NEG ? 0.0f : m[x];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float e = __builtin_amdgcn_exp2f(z[j] - ref);
+        l[x] += e;
+        // (a token that is not seen has no weight, whatever its block's scale)
+        pf[x][j >> 3][j & 7] = (_Float16)(!inside && z[j] == BR_KV_NEG ? 0.0f : e * wgt);
+      }
+    }
+    // bytes behind the row's end are whatever memory held: an 8-bit float may be a NaN there
+    if (FP8 && __any(have < 16)) {
+      const unsigned long long full = ~0ull;
+      const unsigned long long m0 = have >= 8 ? full : ~(full << (8 * have));
+      const unsigned long long m1 = have >= 16 ? full : have <= 8 ? 0ull : ~(full << (8 * (have - 8)));
+#pragma unroll
+      for (int d = 0; d < ND; ++d) vc[d].x &= (unsigned)m0, vc[d].y &= (unsigned)(m0 >> 32), vc[d].z &= (unsigned)m1, vc[d].w &= (unsigned)(m1 >> 32);
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      const br_h8 v0 = br_kv_decode8<FP8>(vc[d].x, vc[d].y), v1 = br_kv_decode8<FP8>(vc[d].z, vc[d].w);
+#pragma unroll
+      for (int x = 0; x < NQ; ++x) {
+        o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[x][0], o[x][d], 0, 0, 0);
+        o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[x][1], o[x][d], 0, 0, 0);
+      }
+    }
+    vid = vid1, vid1 = vid2;
+  }
+  sums.c = cmax * (1.0f / 256.0f);
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    l[x] = br_kv_sum4(l[x]);
+    if (m[x] == BR_KV_NEG) m[x] = 0.0f;
+  }
+}
+
+// Joins the pieces of a query tile, of blocks first .. first + parts - 1, into its result (all of the block's threads).
+template <int D, int TQ, int NT>
+__device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int rows_q, int first, int parts, br_f4 *sums, float2 *total) {
+  constexpr int PER = NT / TQ >= 64 ? 64 : NT / TQ >= 32 ? 32 : NT / TQ >= 16 ? 16 : NT / TQ >= 8 ? 8 : 2;
+  static_assert(PER * TQ <= NT, "threads for every row");
+  const int tid = threadIdx.x;
+  auto piece = [&](int k) { return (long long)(k ? 2 * (first + k) : 2 * first + 1) * TQ; };
+  {
+    const int row = tid / PER;  // (threads beyond TQ rows have none)
+    float m = BR_KV_NEG, l = 0.0f;
+    if (row < rows_q) {
+#pragma unroll 4
+      for (int k = tid % PER; k < parts; k += PER) {
+        const float2 x = br_kv_get2(p.ml + (piece(k) + row) * 2);
+        m = x.y != 0.0f ? fmaxf(m, x.x) : m;
+      }
+    }
+    for (int d = 1; d < PER; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    if (row < rows_q) {
+#pragma unroll 4
+      for (int k = tid % PER; k < parts; k += PER) {
+        const float2 x = br_kv_get2(p.ml + (piece(k) + row) * 2);
+        l += x.y != 0.0f ? x.y * __builtin_amdgcn_exp2f(x.x - m) : 0.0f;
+      }
+    }
+    for (int d = 1; d < PER; d <<= 1) l += __shfl_xor(l, d, 64);
+    __syncthreads();
+    if (tid % PER == 0 && row < TQ) {
+      total[row] = make_float2(m, l);
+      if (row < rows_q) br_kv_store_lse(p, w, h, qi * TQ + row, l != 0.0f ? m : 0.0f, l);
+    }
+    __syncthreads();
+  }
+  // four channels of a row per thread; where those are less than half of the threads, the pieces are shared out as well
+  const int items = rows_q * (D / 4), S = items < NT ? max(1, NT / items) : 1;
+  for (int at = tid; at < max(items, NT); at += NT) {
+    const int it = at % items, k0 = at / items, row = it / (D / 4), d = it % (D / 4) * 4;
+    const float2 ml = total[row];
+    br_f4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (k0 < S) {
+#pragma unroll 4
+      for (int k = k0; k < parts; k += S) {
+        const float2 x = br_kv_get2(p.ml + (piece(k) + row) * 2);
+        const float2 v0 = br_kv_get2(p.part + (piece(k) + row) * D + d), v1 = br_kv_get2(p.part + (piece(k) + row) * D + d + 2);
+        const br_f4 v = {v0.x, v0.y, v1.x, v1.y};
+        const float e = x.y != 0.0f ? __builtin_amdgcn_exp2f(x.x - ml.x) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] += e != 0.0f ? v[j] * e : 0.0f;
+      }
+    }
+    if (S > 1) {
+      sums[tid] = y;
+      __syncthreads();
+      if (k0 == 0)
+        for (int k = 1; k < S; ++k) {
+          const br_f4 v = sums[tid + k * items];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] += v[j];
+        }
+    }
+    const float inv = ml.y != 0.0f ? 1.0f / ml.y : 0.0f;
+    if (k0 == 0) br_kv_store4(p, w, h, qi * TQ + row, d, br_f4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv});
+  }
+}
+
+// The division of a call's tiles: `workers` of them (waves or blocks) get runs that differ by one tile at most.
+template <int TQ, int NT>
+struct BrKvRuns {
+  struct Shared {
+    long long before[NT + 1], wave_sum[NT / 64];
+    int4 row[NT];
+  };
+  Shared &s;
+  long long all, share, more;
+  int per, workers;
+
+  __device__ __forceinline__ BrKvRuns(const BrKvAttend &p, Shared &sh, int most) : s(sh) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    per = (p.n_rows + NT - 1) / NT;
+    long long mine = 0;
+    for (int r = tid * per; r < min(p.n_rows, (tid + 1) * per); ++r) {
+      const BrKvRow w = br_kv_row(p, r);
+      if (w.n > 0) mine += br_kv_row_tiles<TQ>(p, w) * p.kv_heads;
+      s.row[tid] = make_int4(w.n, w.len, w.start, 0);
+    }
+    long long sum = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+      const long long o = __shfl_up(sum, d, 64);
+      if (lane >= d) sum += o;
+    }
+    if (lane == 63) s.wave_sum[tid >> 6] = sum;
+    __syncthreads();
+    for (int k = 0; k < (tid >> 6); ++k) sum += s.wave_sum[k];
+    s.before[tid + 1] = sum;
+    if (tid == 0) s.before[0] = 0;
+    __syncthreads();
+    all = s.before[NT];
+    workers = (int)max(1ll, min((long long)most, all));
+    share = br_kv_div(all, workers);
+    more = all - share * workers;  // the first `more` have one tile more
+  }
+  __device__ __forceinline__ long long begin_of(int k) const {
+    k = min(k, workers);
+    return k * share + min((long long)k, more);
+  }
+  __device__ __forceinline__ int owner_of(long long x) const {
+    const long long y = x - more * (share + 1);
+    return (int)(y < 0 ? br_kv_div(x, share + 1) : more + br_kv_div(y, share));
+  }
+  __device__ __forceinline__ BrKvRow row_of(const BrKvAttend &p, int r) const {
+    if (per > 1) return br_kv_row(p, r);
+    const int4 x = s.row[r];
+    return BrKvRow{x.x, x.y, x.z};
+  }
+};
+
+// Where a run stands: query tile qi of row r and key head h, tiles t0 .. t1 - 1 of its tokens, the first of which is tile `seg` of the call.
+template <int TQ, int NT>
+struct BrKvPlace {
+  BrKvRow w;
+  long long base, seg, tiles;
+  int r, h, qi, size, t0, t1;
+
+  __device__ __forceinline__ bool find(const BrKvAttend &p, const BrKvRuns<TQ, NT> &runs, long long u) {
+    int lo = 0, hi = NT - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (before[mid] <= u) lo = mid;
+      if (runs.s.before[mid] <= u) lo = mid;
       else hi = mid - 1;
     }
-    int r = lo * per;
-    long long base = before[lo], tiles = 0;
-    BrKvRow w;
+    r = lo * runs.per;
+    base = runs.s.before[lo];
     for (; r < p.n_rows; ++r) {
-      w = br_kv_row(p, r);
+      w = runs.row_of(p, r);
       tiles = w.n > 0 ? br_kv_row_tiles<TQ>(p, w) : 0;
       if (u < base + tiles * p.kv_heads) break;
       base += tiles * p.kv_heads;
     }
-    if (r >= p.n_rows) return;  // (only if lengths were changed under the launch)
-    int h = (int)((u - base) / tiles), qi = 0, t0, t1;
-    long long seg = base + h * tiles;  // first tile of the query tile
-    int size = br_kv_span<TQ>(p, w, 0, t0, t1);
+    if (r >= p.n_rows) return false;  // (only if lengths were changed under the launch)
+    h = (int)br_kv_div(u - base, tiles);
+    qi = 0;
+    seg = base + h * tiles;
+    size = br_kv_span<TQ>(p, w, 0, t0, t1);
     while (u >= seg + size) seg += size, size = br_kv_span<TQ>(p, w, ++qi, t0, t1);
+    return true;
+  }
+  __device__ __forceinline__ bool next(const BrKvAttend &p, const BrKvRuns<TQ, NT> &runs) {
+    seg += size;
+    if (seg < base + (h + 1) * tiles) {
+      ++qi;
+    } else {
+      qi = 0;
+      if (++h == p.kv_heads) {
+        h = 0;
+        base += tiles * p.kv_heads;
+        while (++r < p.n_rows) {
+          w = runs.row_of(p, r);
+          tiles = w.n > 0 ? br_kv_row_tiles<TQ>(p, w) : 0;
+          if (tiles > 0) break;
+        }
+        if (r >= p.n_rows) return false;
+      }
+    }
+    size = br_kv_span<TQ>(p, w, qi, t0, t1);
+    return true;
+  }
+  __device__ __forceinline__ int rows_q(const BrKvAttend &p) const { return (int)min((long long)TQ, (long long)w.n * p.group - (long long)qi * TQ); }
+  // positions of the first and the last query of rows a .. b of the tile
+  __device__ __forceinline__ int pos_of(const BrKvAttend &p, int row) const { return w.len - w.n + min(w.n - 1, (qi * TQ + row) / p.group); }
+};
 
+// A wave's result of query rows row.. of the tile, to its place, or as piece `piece` to memory
+template <int D, int NQ, int TQ>
+__device__ __forceinline__ void br_kv_result(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int row, int rows_q, const BrKvSums<D, NQ> &s) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    const int at = row + 16 * x + n;
+    if (at >= rows_q) continue;
+    const float inv = s.l[x] != 0.0f ? s.c / s.l[x] : 0.0f;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) br_kv_store4(p, w, h, qi * TQ + at, 16 * d + 4 * g, br_f4{s.o[x][d][0] * inv, s.o[x][d][1] * inv, s.o[x][d][2] * inv, s.o[x][d][3] * inv});
+    if (g == 0) br_kv_store_lse(p, w, h, qi * TQ + at, s.m[x], s.l[x]);
+  }
+}
+
+template <int D, int NQ, int TQ>
+__device__ __forceinline__ void br_kv_piece(const BrKvAttend &p, int piece, int row, int rows_q, const BrKvSums<D, NQ> &s) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    const int at = row + 16 * x + n;
+    if (at >= rows_q) continue;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) {
+      float *to = p.part + ((long long)piece * TQ + at) * D + 16 * d + 4 * g;
+      br_kv_put2(to, s.o[x][d][0] * s.c, s.o[x][d][1] * s.c);
+      br_kv_put2(to + 2, s.o[x][d][2] * s.c, s.o[x][d][3] * s.c);
+    }
+    if (g == 0) br_kv_put2(p.ml + ((long long)piece * TQ + at) * 2, s.m[x], s.l[x]);
+  }
+}
+
+// What the block has to say of a query tile that other blocks have pieces of: the first of them, their number, and whose it is.
+struct BrKvShare {
+  int on, first, parts, r, h, qi;
+};
+
+// Few query rows: a wave for itself, NW waves to a block.  A wave keeps the sums of a query tile that goes on in the next wave; those of one
+// that it takes up in the middle wait in LDS until the block's end.
+template <int D, int NQ, bool FP8, int NW, int WAVES>
+__global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
+  constexpr int TQ = 16 * NQ, NT = 64 * NW, ND = D / 16;
+  __shared__ typename BrKvRuns<TQ, NT>::Shared shared;
+  __shared__ br_f4 kept[NW * NQ * ND * 64];
+  __shared__ float2 kept_ml[NW * NQ * 16];
+  __shared__ int goes_on[NW];
+  __shared__ BrKvShare out[2];
+  __shared__ int arrived[2];
+  __shared__ float2 total[TQ];
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const BrKvRuns<TQ, NT> runs(p, shared, gridDim.x * NW);
+  // runs that follow each other go to one XCD (blocks go round them), which has what they share in its L2
+  const int blocks = (runs.workers + NW - 1) / NW, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
+  if (wg >= blocks) return;
+  if (tid < 2) out[tid].on = 0;
+  const int me = wg * NW + wv;
+  long long u = runs.begin_of(me);
+  const long long end = runs.begin_of(me + 1);
+
+  BrKvPlace<TQ, NT> at;
+  BrKvSums<D, NQ> s;
+  bool tail = false, open = false;  // a query tile that goes on in the next wave, begun here or before
+  if (u < end && at.find(p, runs, u)) {
     for (;;) {
-      const int a = (int)(u - seg), b = (int)min((long long)size, end - seg);
-      const bool whole = a == 0 && b == size;
-      const int first_pos = w.len - w.n + qi * TQ / p.group, last_pos = w.len - w.n + min(w.n - 1, (qi * TQ + TQ - 1) / p.group);
-
-      // queries: channels 64 i + 16 g .. + 15 of its row for each lane, then 8 g .. + 7 of the last 32
-      br_h8 qf[NQ][NK];
-      float qs[NQ];
-      int pos[NQ];
-#pragma unroll
-      for (int x = 0; x < NQ; ++x) {
-        const int ri = qi * TQ + (wq * NQ + x) * 16 + n, i = ri / p.group, t = w.start + i;
-        const bool in = i < w.n && t >= 0 && t < p.n_tokens;
-        pos[x] = in ? w.len - w.n + i : -1;
-        const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(h * p.group + ri - i * p.group) * p.q_head : 0);
-        float f[NK * 8], top = 0.0f;
-#pragma unroll
-        for (int c = 0; c < NK; ++c) {
-          const int d = c < 2 * NI ? (c / 2) * 64 + g * 16 + (c & 1) * 8 : NI * 64 + g * 8;
-          unsigned short e[8];
-          if (p.q_wide) {
-            *(uint4 *)e = *(const uint4 *)(at + d);
-          } else {
-            for (int j = 0; j < 8; ++j) e[j] = at[d + j];
-          }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float y = in ? (p.bf16 ? br_kv_bf16(e[j]) : br_kv_f16(e[j])) : 0.0f;
-            f[8 * c + j] = y;
-            top = fmaxf(top, fabsf(y));
-          }
-        }
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        // the power of two at or below `top`; not below 2^-100, where its inverse would leave the range
-        const int ex = max((int)(__float_as_uint(top) >> 23), 27);
-        const float inv = __uint_as_float((unsigned)(254 - min(ex, 253)) << 23);
-        qs[x] = top > 3.0e38f && top * 0.0f != 0.0f ? __builtin_nanf("") : __uint_as_float((unsigned)min(ex, 253) << 23) * p.scale2;
-#pragma unroll
-        for (int c = 0; c < NK; ++c)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) qf[x][c][j] = (_Float16)(f[8 * c + j] * inv);
-      }
-
-      br_f4 o[NQ][ND];
-      float m[NQ], l[NQ], cmax = 0.0f, cinv = 0.0f;  // c and its inverse
-#pragma unroll
-      for (int x = 0; x < NQ; ++x) {
-        m[x] = BR_KV_NEG, l[x] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) o[x][d] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
-      }
-
-      const int worker = r / p.rows;
-      const int *table = p.table + (long long)r * p.max_blocks;
-      const int last_block = max(0, (w.len - 1) >> p.shift);
-      const long long cache0 = (long long)worker * p.n_blocks;
-      const int mask = (1 << p.shift) - 1;
-      const int kg = n >> 2, kr = n & 3;  // the token group, and the place in fours, of the lane's row of K
-
-      uint4 kc[4][NI + (NI == 0)];
-      uint2 kx[4];
-      uint4 vc[ND];
-      const int rows_q = (int)min((long long)TQ, (long long)w.n * p.group - (long long)qi * TQ);  // query rows of the tile
-      const int stop = wq * NQ * 16 < rows_q ? min(t0 + b, t1) : 0;
-      // block of a lane's 16 tokens, -1: none
-      auto block_of = [&](int token) {
-        const int id = table[min(token >> p.shift, last_block)];
-        return id >= 0 && id < p.n_blocks ? id : -1;
-      };
-      auto load_k = [&](int t, int id) {
-        const unsigned char *at = p.k + ((((cache0 + max(id, 0)) * p.kv_heads + h) << p.shift) + ((t * BR_KV_TILE + 16 * kg) & mask) + kr) * D;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-#pragma unroll
-          for (int i = 0; i < NI; ++i) kc[s][i] = *(const uint4 *)(at + 4 * s * D + 64 * i + 16 * g);
-          if (REST) kx[s] = *(const uint2 *)(at + 4 * s * D + 64 * NI + 8 * g);
-        }
-      };
-
-      int t = t0 + a + wt;
-      int kid = 0, vid = 0, kid1 = 0, vid1 = 0;
-      if (t < stop) {
-        kid = block_of(t * BR_KV_TILE + 16 * kg), vid = block_of(t * BR_KV_TILE + 16 * g);
-        if (t + WT < stop) kid1 = block_of((t + WT) * BR_KV_TILE + 16 * kg), vid1 = block_of((t + WT) * BR_KV_TILE + 16 * g);
-        load_k(t, kid);
-      }
-      for (; t < stop; t += WT) {
-        const int token = t * BR_KV_TILE + 16 * g;  // of the lane's first weight
-        const long long vb = (cache0 + max(vid, 0)) * p.kv_heads + h;
-        {
-          const unsigned char *at = p.v + (((vb * D + n) << p.shift) + (token & mask));
-#pragma unroll
-          for (int d = 0; d < ND; ++d) vc[d] = *(const uint4 *)(at + ((16 * d) << p.shift));
-        }
-        const float ks = vid < 0 ? 0.0f : p.ks[vb], vs = vid < 0 ? 0.0f : p.vs[vb];
-        const int have = vid < 0 ? 0 : min(max(w.len - token, 0), 16);  // of the lane's tokens, those that exist
-        int kid2 = 0, vid2 = 0;
-        if (t + 2 * WT < stop) kid2 = block_of((t + 2 * WT) * BR_KV_TILE + 16 * kg), vid2 = block_of((t + 2 * WT) * BR_KV_TILE + 16 * g);
-
-        br_f4 s[NQ][4];
-#pragma unroll
-        for (int x = 0; x < NQ; ++x)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) s[x][y] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-#pragma unroll
-          for (int c = 0; c < NK; ++c) {
-            br_h8 kf;
-            if (c < 2 * NI) kf = c & 1 ? br_kv_decode8<FP8>(kc[y][c / 2].z, kc[y][c / 2].w) : br_kv_decode8<FP8>(kc[y][c / 2].x, kc[y][c / 2].y);
-            else kf = br_kv_decode8<FP8>(kx[y].x, kx[y].y);
-#pragma unroll
-            for (int x = 0; x < NQ; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[x][c], s[x][y], 0, 0, 0);
-          }
-        }
-        if (t + WT < stop) load_k(t + WT, kid1);
-
-        // (a block that no query of the tile sees has no say in c)
-        float top = have > 0 && token <= last_pos && (p.window == 0 || token + 15 > first_pos - p.window) ? fabsf(vs) : 0.0f;
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        float cf = 1.0f;
-        if (top > 8.0f * cmax) {
-          const unsigned e = min(max(__float_as_uint(top) >> 23, 20u), 252u) + 1;
-          cinv = __uint_as_float((254u - e) << 23);
-          cf = cmax * cinv;
-          cmax = __uint_as_float(e << 23);
-        }
-        const float wgt = vs * (256.0f * cinv);
-        // inside: every query of the tile sees all of its tokens, and all exist
-        const bool inside = t * BR_KV_TILE + BR_KV_TILE - 1 <= first_pos && (p.window == 0 || t * BR_KV_TILE > last_pos - p.window) && !__any(vid < 0);
-        br_h8 pf[NQ][2];
+      const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg), rows_q = at.rows_q(p);
+      br_kv_tiles<D, NQ, FP8, true>(p, at.w, at.r, at.h, at.qi * TQ, at.pos_of(p, 0), at.pos_of(p, TQ - 1), at.t0 + a, min(at.t0 + b, at.t1), s);
+      if (a > 0) {
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
-          const float f = qs[x] * ks;
-          float z[16], mx = BR_KV_NEG;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            z[j] = s[x][j >> 2][j & 3] * f;
-            if (!inside && !(j < have && token + j <= pos[x] && (p.window == 0 || token + j > pos[x] - p.window))) z[j] = BR_KV_NEG;
-            mx = fmaxf(mx, z[j]);
+          for (int d = 0; d < ND; ++d) {
+            br_f4 y = s.o[x][d];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] *= s.c;
+            kept[((wv * NQ + x) * ND + d) * 64 + lane] = y;
           }
-          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-          const bool up = mx > m[x] + 4.0f;
-          if (__any(up || cf != 1.0f)) {
-            const float to = up ? mx : m[x];
-            const float al = m[x] == BR_KV_NEG ? (l[x] != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m[x] - to), ao = al * cf;
-            m[x] = to;
-            l[x] *= al;
-#pragma unroll
-            for (int d = 0; d < ND; ++d)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) o[x][d][j] *= ao;
-          }
-          const float ref = m[x] == BR_KV_NEG ? 0.0f : m[x];
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float e = __builtin_amdgcn_exp2f(z[j] - ref);
-            l[x] += e;
-            // (a token that is not seen has no weight, whatever its block's scale)
-            pf[x][j >> 3][j & 7] = (_Float16)(!inside && z[j] == BR_KV_NEG ? 0.0f : e * wgt);
-          }
+          if (g == 0) kept_ml[(wv * NQ + x) * 16 + n] = make_float2(s.m[x], s.l[x]);
         }
-        // bytes behind the row's end are whatever memory held: an 8-bit float may be a NaN there
-        if (FP8 && __any(have < 16)) {
-          const unsigned long long full = ~0ull;
-          const unsigned long long m0 = have >= 8 ? full : ~(full << (8 * have));
-          const unsigned long long m1 = have >= 16 ? full : have <= 8 ? 0ull : ~(full << (8 * (have - 8)));
-#pragma unroll
-          for (int d = 0; d < ND; ++d) vc[d].x &= (unsigned)m0, vc[d].y &= (unsigned)(m0 >> 32), vc[d].z &= (unsigned)m1, vc[d].w &= (unsigned)(m1 >> 32);
+        open = b < at.size;
+        if (wv == 0 && lane == 0) {
+          const int first = runs.owner_of(at.seg) / NW;
+          out[0] = BrKvShare{1, first, runs.owner_of(at.seg + at.size - 1) / NW - first + 1, at.r, at.h, at.qi};
         }
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          const br_h8 v0 = br_kv_decode8<FP8>(vc[d].x, vc[d].y), v1 = br_kv_decode8<FP8>(vc[d].z, vc[d].w);
-#pragma unroll
-          for (int x = 0; x < NQ; ++x) {
-            o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[x][0], o[x][d], 0, 0, 0);
-            o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[x][1], o[x][d], 0, 0, 0);
-          }
-        }
-        vid = vid1;
-        kid1 = kid2, vid1 = vid2;
-      }
-      cmax *= 1.0f / 256.0f;
-#pragma unroll
-      for (int x = 0; x < NQ; ++x) {
-        l[x] += __shfl_xor(l[x], 16, 64);
-        l[x] += __shfl_xor(l[x], 32, 64);
-        if (m[x] == BR_KV_NEG) m[x] = 0.0f;
-      }
-
-      // the pieces of a split row: the one that begins in this block in the second place, others in the first
-      const int piece = 2 * wg + (a == 0 ? 1 : 0);
-      auto put = [&](int row, int d, br_f4 x, float inv) {  // row: of the query tile
-        if (row >= rows_q) return;
-        if (whole) br_kv_store4(p, w, h, qi * TQ + row, d, br_f4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv});
-        else *(br_f4 *)(p.part + ((long long)piece * TQ + row) * D + d) = x;
-      };
-      auto put_ml = [&](int row, float mm, float ll) {
-        if (row >= rows_q) return;
-        if (whole) br_kv_store_lse(p, w, h, qi * TQ + row, mm, ll);
-        else *(float2 *)(p.ml + ((long long)piece * TQ + row) * 2) = make_float2(mm, ll);
-      };
-      if constexpr (WQ == 1) {
-#pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-          __syncthreads();
-#pragma unroll
-          for (int d = 0; d < ND; ++d) red[(wv * ND + d) * 64 + lane] = o[x][d];
-          if (g == 0) red_m[wv][n] = m[x], red_l[wv][n] = l[x];
-          if (lane == 0) red_c[wv] = cmax;
-          __syncthreads();
-          float mm = BR_KV_NEG, ll = 0.0f, f[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (red_l[k][n] != 0.0f) mm = fmaxf(mm, red_m[k][n]);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float e = red_l[k][n] != 0.0f ? __builtin_amdgcn_exp2f(red_m[k][n] - mm) : 0.0f;
-            ll += red_l[k][n] * e;
-            f[k] = e * red_c[k];
-          }
-          const float inv = ll != 0.0f ? 1.0f / ll : 0.0f;
-          for (int d = wv; d < ND; d += 4) {
-            br_f4 y = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const br_f4 v = red[(k * ND + d) * 64 + lane];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) y[j] += v[j] * f[k];
-            }
-            put(16 * x + n, 16 * d + 4 * g, y, inv);
-          }
-          if (wv == 0 && g == 0) put_ml(16 * x + n, ll != 0.0f ? mm : 0.0f, ll);
-        }
+      } else if (b == at.size) {
+        br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, 0, rows_q, s);
       } else {
-#pragma unroll
-        for (int x = 0; x < NQ; ++x) {
-          const int row = (wq * NQ + x) * 16 + n;
-          const float inv = l[x] != 0.0f ? 1.0f / l[x] : 0.0f;
-#pragma unroll
-          for (int d = 0; d < ND; ++d) put(row, 16 * d + 4 * g, br_f4{o[x][d][0] * cmax, o[x][d][1] * cmax, o[x][d][2] * cmax, o[x][d][3] * cmax}, inv);
-          if (g == 0) put_ml(row, m[x], l[x]);
-        }
+        tail = true;
+        break;
       }
-
-      if (a == 0 && b < size) {
-        const long long last = ((seg + size) * G - 1) / all;  // the block of the piece's last tile
-        split_r = r, split_h = h, split_q = qi, split_n = (int)(last - wg + 1);
-      }
-      u = seg + b;
-      if (u >= end) break;
-      seg += size;
-      if (seg < base + (h + 1) * tiles) {
-        ++qi;
-      } else {
-        qi = 0;
-        if (++h == p.kv_heads) {
-          h = 0;
-          base += tiles * p.kv_heads;
-          while (++r < p.n_rows) {
-            w = br_kv_row(p, r);
-            tiles = w.n > 0 ? br_kv_row_tiles<TQ>(p, w) : 0;
-            if (tiles > 0) break;
-          }
-          if (r >= p.n_rows) break;
-        }
-      }
-      size = br_kv_span<TQ>(p, w, qi, t0, t1);
+      u = at.seg + b;
+      if (u >= end || !at.next(p, runs)) break;
     }
   }
-  if (tid == 0) *(int4 *)(p.desc + 4 * wg) = make_int4(split_r, split_h, split_q, split_n);
-}
+  if (lane == 0) goes_on[wv] = open;
+  __syncthreads();
 
-// Joins the pieces of the query tile that block `blockIdx.x` of the attention has begun and others have gone on with.
-template <int D, int TQ>
-__global__ __launch_bounds__(256) void br_kv_k_join(BrKvAttend p) {
-  const int wg = blockIdx.x, parts = p.desc[4 * wg + 3];
-  if (parts < 2) return;
-  const int r = p.desc[4 * wg], h = p.desc[4 * wg + 1], qi = p.desc[4 * wg + 2];
-  const BrKvRow w = br_kv_row(p, r);
-  const int rows_q = (int)min((long long)TQ, (long long)w.n * p.group - (long long)qi * TQ);
-  for (int at = threadIdx.x; at < rows_q * (D / 4); at += 256) {
-    const int row = at / (D / 4), d = at % (D / 4) * 4;
-    float m = BR_KV_NEG, l = 0.0f;
-    for (int k = 0; k < parts; ++k) {
-      const float2 x = *(const float2 *)(p.ml + ((long long)(k ? 2 * (wg + k) : 2 * wg + 1) * TQ + row) * 2);
-      if (x.y != 0.0f) m = fmaxf(m, x.x);
-    }
-    br_f4 y = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 0; k < parts; ++k) {
-      const long long piece = (long long)(k ? 2 * (wg + k) : 2 * wg + 1) * TQ + row;
-      const float2 x = *(const float2 *)(p.ml + piece * 2);
-      const br_f4 v = *(const br_f4 *)(p.part + piece * D + d);
-      if (x.y == 0.0f) continue;
-      const float e = __builtin_amdgcn_exp2f(x.x - m);
-      l += x.y * e;
+  // adds what wave k has kept
+  auto add = [&](int k) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] += v[j] * e;
+    for (int x = 0; x < NQ; ++x) {
+      const float2 ml = kept_ml[(k * NQ + x) * 16 + n];
+      const float top = s.l[x] == 0.0f ? ml.x : ml.y == 0.0f ? s.m[x] : fmaxf(s.m[x], ml.x);
+      const float e0 = s.l[x] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(s.m[x] - top), e1 = ml.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
+      s.m[x] = top;
+      s.l[x] = s.l[x] * e0 + ml.y * e1;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const br_f4 y = kept[((k * NQ + x) * ND + d) * 64 + lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s.o[x][d][j] = s.o[x][d][j] * (s.c * e0) + y[j] * e1;
+      }
     }
-    const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-    br_kv_store4(p, w, h, qi * TQ + row, d, br_f4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv});
-    if (d == 0) br_kv_store_lse(p, w, h, qi * TQ + row, l != 0.0f ? m : 0.0f, l);
+    s.c = 1.0f;
+  };
+  if (tail) {
+    bool done = false;
+    for (int k = wv + 1; k < NW && !done; ++k) add(k), done = !goes_on[k];
+    if (done) {
+      br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, 0, at.rows_q(p), s);
+    } else {
+      br_kv_piece<D, NQ, TQ>(p, 2 * wg + 1, 0, at.rows_q(p), s);
+      if (lane == 0) out[1] = BrKvShare{1, wg, runs.owner_of(at.seg + at.size - 1) / NW - wg + 1, at.r, at.h, at.qi};
+    }
+  }
+  if (wv == 0 && out[0].on) {
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      s.m[x] = s.l[x] = 0.0f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) s.o[x][d] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    s.c = 1.0f;
+    for (int k = 0; k < NW; ++k) {
+      add(k);
+      if (!goes_on[k]) break;
+    }
+    br_kv_piece<D, NQ, TQ>(p, 2 * wg, 0, TQ, s);
+  }
+  br_kv_stores_done();
+  __syncthreads();
+  if (tid < 2 && out[tid].on) arrived[tid] = __hip_atomic_fetch_add(&p.arrived[out[tid].first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (!out[k].on || arrived[k] != out[k].parts - 1) continue;
+    const BrKvRow w = runs.row_of(p, out[k].r);
+    br_kv_join<D, TQ, NT>(p, w, out[k].h, out[k].qi, (int)min((long long)TQ, (long long)w.n * p.group - (long long)out[k].qi * TQ), out[k].first, out[k].parts, kept, total);
+    if (tid == 0) p.arrived[out[k].first] = 0;  // (for the next launch)
+    __syncthreads();
   }
 }
 
-template <int D, int NQ, int WQ>
-void br_kv_attend_tile(const BrKvAttend &p, bool fp8, int blocks, hipStream_t st) {
-  if (fp8) br_kv_k_attend<D, NQ, WQ, true><<<blocks, 256, 0, st>>>(p);
-  else br_kv_k_attend<D, NQ, WQ, false><<<blocks, 256, 0, st>>>(p);
-  br_kv_k_join<D, 16 * NQ * WQ><<<blocks, 256, 0, st>>>(p);
+// Many query rows: the block's four waves have 16 NQ each and go over the same tokens.
+template <int D, int NQ, bool FP8, int WAVES>
+__global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) {
+  constexpr int TQ = 64 * NQ, NT = 256;
+  __shared__ typename BrKvRuns<TQ, NT>::Shared shared;
+  __shared__ br_f4 sums[NT];
+  __shared__ float2 total[TQ];
+  __shared__ int arrived;
+  const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const BrKvRuns<TQ, NT> runs(p, shared, gridDim.x);
+  const int blocks = runs.workers, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
+  if (wg >= blocks) return;
+  long long u = runs.begin_of(wg);
+  const long long end = runs.begin_of(wg + 1);
+  BrKvPlace<TQ, NT> at;
+  if (u >= end || !at.find(p, runs, u)) return;
+  for (;;) {
+    const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg), rows_q = at.rows_q(p), row = 16 * NQ * wv;
+    const bool whole = a == 0 && b == at.size;
+    BrKvSums<D, NQ> s;
+    const int last_pos = at.pos_of(p, row + 16 * NQ - 1);
+    // (tiles behind a wave's own last query have nothing for it)
+    const int stop = row < rows_q ? min(min(at.t0 + b, at.t1), last_pos / BR_KV_TILE + 1) : 0;
+    br_kv_tiles<D, NQ, FP8, false>(p, at.w, at.r, at.h, at.qi * TQ + row, at.pos_of(p, row), last_pos, at.t0 + a, stop, s);
+    if (whole) {
+      br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, row, rows_q, s);
+    } else {
+      const int first = runs.owner_of(at.seg), parts = runs.owner_of(at.seg + at.size - 1) - first + 1;
+      br_kv_piece<D, NQ, TQ>(p, 2 * wg + (a == 0 ? 1 : 0), row, rows_q, s);
+      br_kv_stores_done();
+      __syncthreads();
+      if (tid == 0) arrived = __hip_atomic_fetch_add(&p.arrived[first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __syncthreads();
+      if (arrived == parts - 1) {
+        br_kv_join<D, TQ, NT>(p, at.w, at.h, at.qi, rows_q, first, parts, sums, total);
+        if (tid == 0) p.arrived[first] = 0;  // (for the next launch)
+      }
+      __syncthreads();
+    }
+    u = at.seg + b;
+    if (u >= end || !at.next(p, runs)) break;
+  }
+}
+
+// WAVES on a SIMD, by the registers that the tile needs; PER blocks of NW waves on a compute unit
+template <int D, int NQ, int NW, int WAVES>
+void br_kv_attend_few(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
+  constexpr int PER = 4 * WAVES / NW;
+  const int blocks = PER * cus < BR_KV_SPLIT_WGS ? PER * cus : BR_KV_SPLIT_WGS;
+  if (fp8) br_kv_k_attend<D, NQ, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+  else br_kv_k_attend<D, NQ, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+}
+
+template <int D, int NQ, int WAVES>
+void br_kv_attend_rows(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
+  const int blocks = WAVES * cus < BR_KV_SPLIT_WGS ? WAVES * cus : BR_KV_SPLIT_WGS;
+  if (fp8) br_kv_k_attend_rows<D, NQ, true, WAVES><<<blocks, 256, 0, st>>>(p);
+  else br_kv_k_attend_rows<D, NQ, false, WAVES><<<blocks, 256, 0, st>>>(p);
 }
 
 template <int D>
 void br_kv_attend_dim(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st) {
-  const int blocks = 2 * cus < BR_KV_SPLIT_WGS ? 2 * cus : BR_KV_SPLIT_WGS;
-  if (tile == BR_KV_TILE_16) br_kv_attend_tile<D, 1, 1>(p, fp8, blocks, st);
-  else if (tile == BR_KV_TILE_32) br_kv_attend_tile<D, 2, 1>(p, fp8, blocks, st);
-  else br_kv_attend_tile<D, 2, 4>(p, fp8, blocks, st);
+  if (tile == BR_KV_TILE_16) br_kv_attend_few<D, 1, D <= 96 ? 12 : D <= 128 ? 8 : 4, D <= 96 ? 3 : D <= 128 ? 2 : 1>(p, fp8, cus, st);
+  else if (tile == BR_KV_TILE_32) br_kv_attend_few<D, 2, D <= 64 ? 8 : 4, D <= 64 ? 2 : 1>(p, fp8, cus, st);
+  else br_kv_attend_rows<D, 2, D <= 96 ? 2 : 1>(p, fp8, cus, st);
 }
 
 #endif

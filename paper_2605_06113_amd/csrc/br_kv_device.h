@@ -48,14 +48,14 @@ struct BrKvAttend {
   const float *ks, *vs;
   float *part;  // sums of the pieces of split rows, see br_kv_attend.h
   float *ml;    // their maxima and sums of weights
-  int *desc;    // per block: the split piece that begins in it
+  int *arrived; // per block: blocks that have delivered a piece of the query tile that is split and begins in it; 0 between launches
   long long q_token, q_head, out_token, out_head;
   int n_rows, rows, n_tokens, window, group, kv_heads, shift, n_blocks, max_blocks;
   int bf16, q_wide, out_wide;  // wide: rows of q (out) can be read (written) 16 (8) bytes at a time
   float scale2;                // scale * log2(e)
 };
 
-void br_kv_launch_clear(const BrKvTables &t, hipStream_t st);
+void br_kv_launch_clear(const BrKvTables &t, int *arrived, hipStream_t st);
 void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, hipStream_t st);
 void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st);
 void br_kv_launch_append(const BrKvCache &c, const BrKvTokens &t, bool fp8, hipStream_t st);

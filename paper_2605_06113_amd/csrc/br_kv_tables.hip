@@ -1,8 +1,8 @@
 // Block tables and slot maps of a step (br_kv_step), and the kernels that set a context up.
 #include "br_kv_device.h"
 
-// Every row empty, every block free.
-__global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t) {
+// Every row empty, every block free; nothing begun.
+__global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t, int *arrived) {
   const long long n = (long long)t.W * t.B * t.max_blocks, rows = (long long)t.W * t.B, words = (long long)t.W * t.words;
   const long long step = (long long)gridDim.x * 256;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
@@ -10,6 +10,7 @@ __global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t) {
     if (i < rows) t.lens[i] = 0;
   }
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < words; i += step) t.used[i] = 0;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < BR_KV_SPLIT_WGS; i += step) arrived[i] = 0;
 }
 
 // The rows held at the start (behind br_kv_k_clear).
@@ -203,8 +204,8 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
 
 static int grid_for(long long n) { return (int)(n < 1 ? 1 : n > 4096ll * 256 ? 4096 : (n + 255) / 256); }
 
-void br_kv_launch_clear(const BrKvTables &t, hipStream_t st) {
-  br_kv_k_clear<<<grid_for((long long)t.W * t.B * t.max_blocks), 256, 0, st>>>(t);
+void br_kv_launch_clear(const BrKvTables &t, int *arrived, hipStream_t st) {
+  br_kv_k_clear<<<grid_for((long long)t.W * t.B * t.max_blocks), 256, 0, st>>>(t, arrived);
 }
 
 void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, hipStream_t st) {
