@@ -194,12 +194,14 @@ int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_atten
   p.q_token = a->q_token, p.q_head = a->q_head, p.out_token = a->out_token, p.out_head = a->out_head;
   p.n_rows = c.n_workers * c.rows, p.rows = c.rows, p.n_tokens = a->n_tokens, p.window = a->window;
   p.group = group, p.kv_heads = c.n_kv_heads, p.shift = ctx->t.shift, p.n_blocks = c.n_blocks, p.max_blocks = c.max_blocks;
+  p.group_shift = (unsigned)log2_of(group);
+  p.group_mul = (unsigned)((((uint64_t)1 << 32) * (((uint64_t)1 << p.group_shift) - group)) / group + 1);
   p.bf16 = a->dtype == BR_KV_BF16;
   p.q_wide = ((uintptr_t)a->q & 15u) == 0 && ((a->q_token | a->q_head) & 7) == 0;
   p.out_wide = ((uintptr_t)a->out & 7u) == 0 && ((a->out_token | a->out_head) & 3) == 0;
   p.scale2 = a->scale * 1.4426950408889634f;
   const int64_t rows = (int64_t)a->max_count * group;
-  const int tile = rows <= 16 ? BR_KV_TILE_16 : rows <= 64 ? BR_KV_TILE_32 : BR_KV_TILE_128;
+  const int tile = rows <= 16 || (rows <= 64 && c.head_dim > 128) ? BR_KV_TILE_16 : rows <= 64 ? BR_KV_TILE_32 : BR_KV_TILE_128;
   const bool fp8 = c.fmt == BR_KV_E4M3;
   return enqueue(ctx, [&] {
     switch (c.head_dim) {

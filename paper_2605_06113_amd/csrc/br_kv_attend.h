@@ -36,11 +36,14 @@ __device__ __forceinline__ BrKvRow br_kv_row(const BrKvAttend &p, int r) {
   return w;
 }
 
+// Query token of a query row: row / group, by a multiplication.
+__device__ __forceinline__ int br_kv_token(const BrKvAttend &p, int row) { return (int)((__umulhi(p.group_mul, (unsigned)row) + (unsigned)row) >> p.group_shift); }
+
 // First token tile of a query tile, one past the last, and what it counts in the division of the work: a tile that sees nothing still has
 // zeros to write.
 template <int TQ>
 __device__ __forceinline__ int br_kv_span(const BrKvAttend &p, const BrKvRow &w, int qi, int &t0, int &t1) {
-  const int i0 = qi * TQ / p.group, i1 = min(w.n - 1, (qi * TQ + TQ - 1) / p.group), at = w.len - w.n;
+  const int i0 = br_kv_token(p, qi * TQ), i1 = min(w.n - 1, br_kv_token(p, qi * TQ + TQ - 1)), at = w.len - w.n;
   const int hi = max(0, at + i1 + 1), lo = p.window > 0 ? max(0, at + i0 - p.window + 1) : 0;
   t0 = lo / BR_KV_TILE;
   t1 = max(t0, (hi + BR_KV_TILE - 1) / BR_KV_TILE);
@@ -67,25 +70,40 @@ __device__ __forceinline__ uint4 br_kv_load16(const unsigned char *at) {
   return make_uint4(x[0], x[1], x[2], x[3]);
 }
 
-__device__ __forceinline__ unsigned br_kv_pack(float a, float b, int bf16) {
-  return bf16 ? (unsigned)br_kv_to_bf16(a) | (unsigned)br_kv_to_bf16(b) << 16 : (unsigned)br_kv_to_f16(a) | (unsigned)br_kv_to_f16(b) << 16;
+// Two values in 16 bits each
+template <class T>
+__device__ __forceinline__ unsigned br_kv_pair(float a, float b) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef T t2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{a, b}), t2));
 }
 
-// 4 channels of one query row, final
-__device__ __forceinline__ void br_kv_store4(const BrKvAttend &p, const BrKvRow &w, int h, int ri, int d, br_f4 x) {
-  const int i = ri / p.group, t = w.start + i;
+// One query row's place in the output: its 4 N channels d, d + 16, ..., of the lane, times inv.
+template <int N>
+__device__ __forceinline__ void br_kv_store(const BrKvAttend &p, const BrKvRow &w, int h, int ri, int d, const br_f4 (&x)[N], float inv) {
+  const int i = br_kv_token(p, ri), t = w.start + i;
   if (i >= w.n || t < 0 || t >= p.n_tokens) return;
   unsigned short *at = p.out + (long long)t * p.out_token + (long long)(h * p.group + ri - i * p.group) * p.out_head + d;
-  const unsigned a = br_kv_pack(x[0], x[1], p.bf16), b = br_kv_pack(x[2], x[3], p.bf16);
-  if (p.out_wide) {
-    *(uint2 *)at = make_uint2(a, b);
+  uint2 y[N];
+  if (p.bf16) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) y[k] = make_uint2(br_kv_pair<__bf16>(x[k][0] * inv, x[k][1] * inv), br_kv_pair<__bf16>(x[k][2] * inv, x[k][3] * inv));
   } else {
-    at[0] = (unsigned short)a, at[1] = (unsigned short)(a >> 16), at[2] = (unsigned short)b, at[3] = (unsigned short)(b >> 16);
+#pragma unroll
+    for (int k = 0; k < N; ++k) y[k] = make_uint2(br_kv_pair<_Float16>(x[k][0] * inv, x[k][1] * inv), br_kv_pair<_Float16>(x[k][2] * inv, x[k][3] * inv));
+  }
+  if (p.out_wide) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) *(uint2 *)(at + 16 * k) = y[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      at[16 * k] = (unsigned short)y[k].x, at[16 * k + 1] = (unsigned short)(y[k].x >> 16), at[16 * k + 2] = (unsigned short)y[k].y, at[16 * k + 3] = (unsigned short)(y[k].y >> 16);
   }
 }
 
 __device__ __forceinline__ void br_kv_store_lse(const BrKvAttend &p, const BrKvRow &w, int h, int ri, float m, float l) {
-  const int i = ri / p.group, t = w.start + i;
+  const int i = br_kv_token(p, ri), t = w.start + i;
   if (!p.lse || i >= w.n || t < 0 || t >= p.n_tokens) return;
   p.lse[(long long)t * p.kv_heads * p.group + h * p.group + ri - i * p.group] = l == 0.0f ? BR_KV_NEG : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
@@ -104,10 +122,6 @@ __device__ __forceinline__ float2 br_kv_get2(const float *at) {
 
 __device__ __forceinline__ void br_kv_stores_done() {
   __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
-}
-
-__device__ __forceinline__ long long br_kv_div(long long x, long long y) {  // of what is not negative
-  return (x | y) >> 31 ? x / y : (long long)((unsigned)x / (unsigned)y);
 }
 
 // Sums of one wave over some tokens of 16 NQ query rows: o [channel 16 d + 4 g + j][row 16 x + n] (to be multiplied by c), l the sum of
@@ -147,44 +161,6 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   auto &o = sums.o;
   auto &m = sums.m;
   auto &l = sums.l;
-  // queries: channels 64 i + 16 g .. + 15 of its row for each lane, then 8 g .. + 7 of the last 32
-  br_h8 qf[NQ][NK];
-  float qs[NQ];
-  int pos[NQ];
-#pragma unroll
-  for (int x = 0; x < NQ; ++x) {
-    const int ri = row0 + 16 * x + n, i = ri / p.group, t = w.start + i;
-    const bool in = i < w.n && t >= 0 && t < p.n_tokens;
-    pos[x] = in ? w.len - w.n + i : -1;
-    const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(h * p.group + ri - i * p.group) * p.q_head : 0);
-    float f[NK * 8], top = 0.0f;
-#pragma unroll
-    for (int c = 0; c < NK; ++c) {
-      const int d = c < 2 * NI ? (c / 2) * 64 + g * 16 + (c & 1) * 8 : NI * 64 + g * 8;
-      unsigned short e[8];
-      if (p.q_wide) {
-        *(uint4 *)e = *(const uint4 *)(at + d);
-      } else {
-        for (int j = 0; j < 8; ++j) e[j] = at[d + j];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float y = in ? (p.bf16 ? br_kv_bf16(e[j]) : br_kv_f16(e[j])) : 0.0f;
-        f[8 * c + j] = y;
-        top = fmaxf(top, fabsf(y));
-      }
-    }
-    top = br_kv_max4(top);
-    // the power of two at or below `top`; not below 2^-100, where its inverse would leave the range
-    const int ex = max((int)(__float_as_uint(top) >> 23), 27);
-    const float inv = __uint_as_float((unsigned)(254 - min(ex, 253)) << 23);
-    qs[x] = top > 3.0e38f && top * 0.0f != 0.0f ? __builtin_nanf("") : __uint_as_float((unsigned)min(ex, 253) << 23) * p.scale2;
-#pragma unroll
-    for (int c = 0; c < NK; ++c)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) qf[x][c][j] = (_Float16)(f[8 * c + j] * inv);
-  }
-
   float cmax = 0.0f, cinv = 0.0f;  // c and its inverse
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
@@ -225,14 +201,65 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     const long long at = (cache0 + (there(id) ? id : 0)) * p.kv_heads + h;
     ks1 = p.ks[at], vs1 = p.vs[at];
   };
-  if (t < stop) {
+  const bool t_any = t < stop;
+  int kid = 0;
+  if (t_any) {
     const int next = t + 1 < stop ? t + 1 : t;
-    const int kid = id_of(t * BR_KV_TILE + 16 * kg);
-    vid = id_of(t * BR_KV_TILE + 16 * g);
+    kid = id_of(t * BR_KV_TILE + 16 * kg), vid = id_of(t * BR_KV_TILE + 16 * g);
     kid1 = id_of(next * BR_KV_TILE + 16 * kg), vid1 = id_of(next * BR_KV_TILE + 16 * g);
+  }
+  auto load_first = [&]() {
     load_k(t, kid, true);
     load_scales(vid);
+  };
+  // queries: channels 64 i + 16 g .. + 15 of its row for each lane, then 8 g .. + 7 of the last 32
+  br_h8 qf[NQ][NK];
+  float qs[NQ];
+  int pos[NQ];
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    const int ri = row0 + 16 * x + n, i = br_kv_token(p, ri), t = w.start + i;
+    const bool in = i < w.n && t >= 0 && t < p.n_tokens;
+    pos[x] = in ? w.len - w.n + i : -1;
+    const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(h * p.group + ri - i * p.group) * p.q_head : 0);
+    uint4 e[NK];
+    auto channel = [&](int c) { return c < 2 * NI ? (c / 2) * 64 + g * 16 + (c & 1) * 8 : NI * 64 + g * 8; };
+    if (p.q_wide) {
+#pragma unroll
+      for (int c = 0; c < NK; ++c) e[c] = *(const uint4 *)(at + channel(c));
+    } else {
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        const unsigned short *y = at + channel(c);
+        e[c] = make_uint4(y[0] | (unsigned)y[1] << 16, y[2] | (unsigned)y[3] << 16, y[4] | (unsigned)y[5] << 16, y[6] | (unsigned)y[7] << 16);
+      }
+    }
+    if (x == 0 && t_any) load_first();  // (while the queries are on their way)
+    float f[NK * 8], top = 0.0f;
+    auto half = [&](int c) {
+      const uint4 y = e[c / 8];
+      const unsigned z = c % 8 < 2 ? y.x : c % 8 < 4 ? y.y : c % 8 < 6 ? y.z : y.w;
+      return (unsigned short)(c & 1 ? z >> 16 : z);
+    };
+    if (p.bf16) {
+#pragma unroll
+      for (int c = 0; c < 8 * NK; ++c) f[c] = br_kv_bf16(half(c));
+    } else {
+#pragma unroll
+      for (int c = 0; c < 8 * NK; ++c) f[c] = br_kv_f16(half(c));
+    }
+    // (a row of the tile that is none takes the first one's values: its results go nowhere)
+#pragma unroll
+    for (int c = 0; c < 8 * NK; ++c) top = fmaxf(top, fabsf(f[c]));
+    top = br_kv_max4(top);
+    // the power of two at or below `top`; not below 2^-100, where its inverse would leave the range
+    const int ex = max((int)(__float_as_uint(top) >> 23), 27);
+    const float inv = __uint_as_float((unsigned)(254 - min(ex, 253)) << 23);
+    qs[x] = top > 3.0e38f && top * 0.0f != 0.0f ? __builtin_nanf("") : __uint_as_float((unsigned)min(ex, 253) << 23) * p.scale2;
+#pragma unroll
+    for (int c = 0; c < 8 * NK; ++c) qf[x][c / 8][c % 8] = (_Float16)(f[c] * inv);
   }
+
   for (; t < stop; ++t) {
     const int token = t * BR_KV_TILE + 16 * g;  // of the lane's first weight
     {
@@ -283,13 +310,17 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       const float f = qs[x] * ks;
-      float z[16], mx = BR_KV_NEG;
+      float z[16], mx = BR_KV_NEG, wx = wgt;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        z[j] = s[x][j >> 2][j & 3] * f;
-        if (!inside && !(j < have && token + j <= pos[x] && (p.window == 0 || token + j > pos[x] - p.window))) z[j] = BR_KV_NEG;
-        mx = fmaxf(mx, z[j]);
+      for (int j = 0; j < 16; ++j) z[j] = s[x][j >> 2][j & 3] * f;
+      if (!inside) {  // of the lane's tokens, those from `lo` on, `seen` of them
+        const int lo = p.window > 0 ? max(pos[x] - p.window + 1 - token, 0) : 0, seen = max(min(have, pos[x] + 1 - token) - lo, 0);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) z[j] = (unsigned)(j - lo) < (unsigned)seen ? z[j] : BR_KV_NEG;
+        wx = seen > 0 ? wgt : 0.0f;  // (a block that is not seen has no weight, whatever its scale)
       }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) mx = fmaxf(mx, z[j]);
       mx = br_kv_max4(mx);
       const bool up = mx > m[x] + 4.0f;
       if (__any(up || cf != 1.0f)) {
@@ -307,8 +338,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
       for (int j = 0; j < 16; ++j) {
         const float e = __builtin_amdgcn_exp2f(z[j] - ref);
         l[x] += e;
-        // (a token that is not seen has no weight, whatever its block's scale)
-        pf[x][j >> 3][j & 7] = (_Float16)(!inside && z[j] == BR_KV_NEG ? 0.0f : e * wgt);
+        pf[x][j >> 3][j & 7] = (_Float16)(e * wx);
       }
     }
     // bytes behind the row's end are whatever memory held: an 8-bit float may be a NaN there
@@ -338,68 +368,74 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   }
 }
 
-// Joins the pieces of a query tile, of blocks first .. first + parts - 1, into its result (all of the block's threads).
+// Joins the pieces of a query tile, of blocks first .. first + parts - 1, into its result (all of the block's threads; sums and ml: NT of
+// each in LDS).  A thread has four channels of a row; where those are less than half of the threads the pieces are shared out as
+// well.  One way to memory and back: each thread weighs its pieces against the largest maximum among them.
 template <int D, int TQ, int NT>
-__device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int rows_q, int first, int parts, br_f4 *sums, float2 *total) {
-  constexpr int PER = NT / TQ >= 64 ? 64 : NT / TQ >= 32 ? 32 : NT / TQ >= 16 ? 16 : NT / TQ >= 8 ? 8 : 2;
-  static_assert(PER * TQ <= NT, "threads for every row");
-  const int tid = threadIdx.x;
-  auto piece = [&](int k) { return (long long)(k ? 2 * (first + k) : 2 * first + 1) * TQ; };
-  {
-    const int row = tid / PER;  // (threads beyond TQ rows have none)
-    float m = BR_KV_NEG, l = 0.0f;
-    if (row < rows_q) {
-#pragma unroll 4
-      for (int k = tid % PER; k < parts; k += PER) {
-        const float2 x = br_kv_get2(p.ml + (piece(k) + row) * 2);
-        m = x.y != 0.0f ? fmaxf(m, x.x) : m;
-      }
-    }
-    for (int d = 1; d < PER; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-    if (row < rows_q) {
-#pragma unroll 4
-      for (int k = tid % PER; k < parts; k += PER) {
-        const float2 x = br_kv_get2(p.ml + (piece(k) + row) * 2);
-        l += x.y != 0.0f ? x.y * __builtin_amdgcn_exp2f(x.x - m) : 0.0f;
-      }
-    }
-    for (int d = 1; d < PER; d <<= 1) l += __shfl_xor(l, d, 64);
-    __syncthreads();
-    if (tid % PER == 0 && row < TQ) {
-      total[row] = make_float2(m, l);
-      if (row < rows_q) br_kv_store_lse(p, w, h, qi * TQ + row, l != 0.0f ? m : 0.0f, l);
-    }
-    __syncthreads();
-  }
-  // four channels of a row per thread; where those are less than half of the threads, the pieces are shared out as well
-  const int items = rows_q * (D / 4), S = items < NT ? max(1, NT / items) : 1;
+__device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int rows_q, int first, int parts, br_f4 *sums, float2 *ml) {
+  constexpr int AT_ONCE = 8;
+  const int tid = threadIdx.x, items = rows_q * (D / 4), S = items < NT ? max(1, NT / items) : 1;
   for (int at = tid; at < max(items, NT); at += NT) {
     const int it = at % items, k0 = at / items, row = it / (D / 4), d = it % (D / 4) * 4;
-    const float2 ml = total[row];
     br_f4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+    float m = 0.0f, l = 0.0f;
     if (k0 < S) {
-#pragma unroll 4
-      for (int k = k0; k < parts; k += S) {
-        const float2 x = br_kv_get2(p.ml + (piece(k) + row) * 2);
-        const float2 v0 = br_kv_get2(p.part + (piece(k) + row) * D + d), v1 = br_kv_get2(p.part + (piece(k) + row) * D + d + 2);
-        const br_f4 v = {v0.x, v0.y, v1.x, v1.y};
-        const float e = x.y != 0.0f ? __builtin_amdgcn_exp2f(x.x - ml.x) : 0.0f;
+      for (int k = k0; k < parts; k += S * AT_ONCE) {
+        float2 x[AT_ONCE], v0[AT_ONCE], v1[AT_ONCE];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] += e != 0.0f ? v[j] * e : 0.0f;
+        for (int j = 0; j < AT_ONCE; ++j) {
+          const int kk = min(k + j * S, parts - 1);
+          const long long piece = (long long)(kk ? 2 * (first + kk) : 2 * first + 1) * TQ + row;
+          x[j] = br_kv_get2(p.ml + piece * 2);
+          v0[j] = br_kv_get2(p.part + piece * D + d), v1[j] = br_kv_get2(p.part + piece * D + d + 2);
+        }
+        float top = l != 0.0f ? m : BR_KV_NEG;
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+          if (k + j * S >= parts) x[j].y = 0.0f;
+          if (x[j].y != 0.0f) top = fmaxf(top, x[j].x);
+        }
+        const float e0 = l != 0.0f ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
+        l *= e0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] *= e0;
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+          if (x[j].y == 0.0f) continue;
+          const float e = __builtin_amdgcn_exp2f(x[j].x - top);
+          l += x[j].y * e;
+          y[0] = __builtin_fmaf(v0[j].x, e, y[0]), y[1] = __builtin_fmaf(v0[j].y, e, y[1]), y[2] = __builtin_fmaf(v1[j].x, e, y[2]), y[3] = __builtin_fmaf(v1[j].y, e, y[3]);
+        }
+        m = top == BR_KV_NEG ? 0.0f : top;
       }
     }
     if (S > 1) {
-      sums[tid] = y;
+      sums[tid] = y, ml[tid] = make_float2(m, l);
       __syncthreads();
-      if (k0 == 0)
-        for (int k = 1; k < S; ++k) {
+      if (k0 == 0) {
+        float top = BR_KV_NEG;
+        for (int k = 0; k < S; ++k)
+          if (ml[tid + k * items].y != 0.0f) top = fmaxf(top, ml[tid + k * items].x);
+        y = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
+        l = 0.0f;
+        for (int k = 0; k < S; ++k) {
+          const float2 x = ml[tid + k * items];
+          if (x.y == 0.0f) continue;
+          const float e = __builtin_amdgcn_exp2f(x.x - top);
           const br_f4 v = sums[tid + k * items];
+          l += x.y * e;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) y[j] += v[j];
+          for (int c = 0; c < 4; ++c) y[c] += v[c] * e;
         }
+        m = top;
+      }
     }
-    const float inv = ml.y != 0.0f ? 1.0f / ml.y : 0.0f;
-    if (k0 == 0) br_kv_store4(p, w, h, qi * TQ + row, d, br_f4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv});
+    if (k0 == 0) {
+      const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+      const br_f4 one[1] = {y};
+      br_kv_store<1>(p, w, h, qi * TQ + row, d, one, inv);
+      if (d == 0) br_kv_store_lse(p, w, h, qi * TQ + row, m, l);
+    }
   }
 }
 
@@ -411,7 +447,8 @@ struct BrKvRuns {
     int4 row[NT];
   };
   Shared &s;
-  long long all, share, more;
+  long long all;
+  unsigned share, more;
   int per, workers;
 
   __device__ __forceinline__ BrKvRuns(const BrKvAttend &p, Shared &sh, int most) : s(sh) {
@@ -435,17 +472,35 @@ struct BrKvRuns {
     if (tid == 0) s.before[0] = 0;
     __syncthreads();
     all = s.before[NT];
+    // all / most where there is a tile for each, by the reciprocal (exact behind the step up or down); else a tile each
     workers = (int)max(1ll, min((long long)most, all));
-    share = br_kv_div(all, workers);
-    more = all - share * workers;  // the first `more` have one tile more
+    share = 1, more = 0;
+    if (all >= most) {
+      long long q = (long long)((double)all * (1.0 / most)), left = all - q * most;
+      if (left < 0) --q, left += most;
+      if (left >= most) ++q, left -= most;
+      share = (unsigned)q, more = (unsigned)left;  // the first `more` have one tile more
+    }
   }
   __device__ __forceinline__ long long begin_of(int k) const {
     k = min(k, workers);
-    return k * share + min((long long)k, more);
+    return min((unsigned long long)all, (unsigned long long)(unsigned)k * share + min((unsigned)k, more));
   }
-  __device__ __forceinline__ int owner_of(long long x) const {
-    const long long y = x - more * (share + 1);
-    return (int)(y < 0 ? br_kv_div(x, share + 1) : more + br_kv_div(y, share));
+  // The thread in whose rows tile u is: every lane looks at NT / 64 threads' ends, then at one of them.
+  __device__ __forceinline__ int find(long long u) const {
+    constexpr int PER_LANE = NT / 64;
+    const int lane = threadIdx.x & 63;
+    const int chunk = __popcll(__ballot(s.before[(lane + 1) * PER_LANE] <= u)) * PER_LANE;
+    return chunk + __popcll(__ballot(lane < PER_LANE && s.before[min(chunk + lane + 1, NT)] <= u));
+  }
+  __device__ __forceinline__ int owner_of(long long x) const {  // (a search: 64-bit divisions are long code, and cold when they run)
+    int lo = 0, hi = workers - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (begin_of(mid) <= x) lo = mid;
+      else hi = mid - 1;
+    }
+    return lo;
   }
   __device__ __forceinline__ BrKvRow row_of(const BrKvAttend &p, int r) const {
     if (per > 1) return br_kv_row(p, r);
@@ -462,12 +517,7 @@ struct BrKvPlace {
   int r, h, qi, size, t0, t1;
 
   __device__ __forceinline__ bool find(const BrKvAttend &p, const BrKvRuns<TQ, NT> &runs, long long u) {
-    int lo = 0, hi = NT - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (runs.s.before[mid] <= u) lo = mid;
-      else hi = mid - 1;
-    }
+    const int lo = runs.find(u);
     r = lo * runs.per;
     base = runs.s.before[lo];
     for (; r < p.n_rows; ++r) {
@@ -477,7 +527,9 @@ struct BrKvPlace {
       base += tiles * p.kv_heads;
     }
     if (r >= p.n_rows) return false;  // (only if lengths were changed under the launch)
-    h = (int)br_kv_div(u - base, tiles);
+    h = (int)((float)(u - base) * __builtin_amdgcn_rcpf((float)tiles));
+    while (h > 0 && u - base < h * tiles) --h;
+    while (u - base >= (h + 1) * tiles) ++h;
     qi = 0;
     seg = base + h * tiles;
     size = br_kv_span<TQ>(p, w, 0, t0, t1);
@@ -506,7 +558,7 @@ struct BrKvPlace {
   }
   __device__ __forceinline__ int rows_q(const BrKvAttend &p) const { return (int)min((long long)TQ, (long long)w.n * p.group - (long long)qi * TQ); }
   // positions of the first and the last query of rows a .. b of the tile
-  __device__ __forceinline__ int pos_of(const BrKvAttend &p, int row) const { return w.len - w.n + min(w.n - 1, (qi * TQ + row) / p.group); }
+  __device__ __forceinline__ int pos_of(const BrKvAttend &p, int row) const { return w.len - w.n + min(w.n - 1, br_kv_token(p, qi * TQ + row)); }
 };
 
 // A wave's result of query rows row.. of the tile, to its place, or as piece `piece` to memory
@@ -518,8 +570,7 @@ __device__ __forceinline__ void br_kv_result(const BrKvAttend &p, const BrKvRow 
     const int at = row + 16 * x + n;
     if (at >= rows_q) continue;
     const float inv = s.l[x] != 0.0f ? s.c / s.l[x] : 0.0f;
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) br_kv_store4(p, w, h, qi * TQ + at, 16 * d + 4 * g, br_f4{s.o[x][d][0] * inv, s.o[x][d][1] * inv, s.o[x][d][2] * inv, s.o[x][d][3] * inv});
+    br_kv_store<D / 16>(p, w, h, qi * TQ + at, 4 * g, s.o[x], inv);
     if (g == 0) br_kv_store_lse(p, w, h, qi * TQ + at, s.m[x], s.l[x]);
   }
 }
@@ -541,123 +592,129 @@ __device__ __forceinline__ void br_kv_piece(const BrKvAttend &p, int piece, int 
   }
 }
 
-// What the block has to say of a query tile that other blocks have pieces of: the first of them, their number, and whose it is.
+// A query tile that several of a block's waves have pieces of: whose it is, and the blocks that have (`parts` 1: this one alone).
 struct BrKvShare {
   int on, first, parts, r, h, qi;
 };
 
-// Few query rows: a wave for itself, NW waves to a block.  A wave keeps the sums of a query tile that goes on in the next wave; those of one
-// that it takes up in the middle wait in LDS until the block's end.
+// Few query rows: a run for each wave, NW waves to a block.  A wave's pieces (of a query tile that it takes up in the middle, and of one that
+// goes on in the next wave) wait in LDS until the block's end, where all waves join them, each its share of the channels.
 template <int D, int NQ, bool FP8, int NW, int WAVES>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   constexpr int TQ = 16 * NQ, NT = 64 * NW, ND = D / 16;
   __shared__ typename BrKvRuns<TQ, NT>::Shared shared;
-  __shared__ br_f4 kept[NW * NQ * ND * 64];
-  __shared__ float2 kept_ml[NW * NQ * 16];
-  __shared__ int goes_on[NW];
-  __shared__ BrKvShare out[2];
-  __shared__ int arrived[2];
-  __shared__ float2 total[TQ];
+  __shared__ br_f4 kept[2 * NW * NQ * ND * 64];  // piece 2 k: taken up by wave k, 2 k + 1: begun by it
+  __shared__ float2 kept_ml[2 * NW * NQ * 16];
+  __shared__ int goes_on[NW], arrived[2];
+  __shared__ BrKvShare chains[NW + 1];  // of the query tile that wave k has begun; the last: of one that an earlier block has
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const BrKvRuns<TQ, NT> runs(p, shared, gridDim.x * NW);
+  BrKvRuns<TQ, NT> runs(p, shared, gridDim.x * NW);
   // runs that follow each other go to one XCD (blocks go round them), which has what they share in its L2
   const int blocks = (runs.workers + NW - 1) / NW, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
   if (wg >= blocks) return;
-  if (tid < 2) out[tid].on = 0;
+  if (tid <= NW) chains[tid].on = 0;
+  __syncthreads();
   const int me = wg * NW + wv;
   long long u = runs.begin_of(me);
   const long long end = runs.begin_of(me + 1);
 
-  BrKvPlace<TQ, NT> at;
-  BrKvSums<D, NQ> s;
-  bool tail = false, open = false;  // a query tile that goes on in the next wave, begun here or before
-  if (u < end && at.find(p, runs, u)) {
-    for (;;) {
-      const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg), rows_q = at.rows_q(p);
-      br_kv_tiles<D, NQ, FP8, true>(p, at.w, at.r, at.h, at.qi * TQ, at.pos_of(p, 0), at.pos_of(p, TQ - 1), at.t0 + a, min(at.t0 + b, at.t1), s);
-      if (a > 0) {
+  bool open = false;  // the query tile that was taken up goes on in the next wave
+  {
+    BrKvPlace<TQ, NT> at;
+    BrKvSums<D, NQ> s;
+    if (u < end && at.find(p, runs, u)) {
+      for (;;) {
+        const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg);
+        br_kv_tiles<D, NQ, FP8, true>(p, at.w, at.r, at.h, at.qi * TQ, at.pos_of(p, 0), at.pos_of(p, TQ - 1), at.t0 + a, min(at.t0 + b, at.t1), s);
+        if (a == 0 && b == at.size) {
+          br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, 0, at.rows_q(p), s);
+        } else {
+          const int piece = 2 * wv + (a == 0);
 #pragma unroll
-        for (int x = 0; x < NQ; ++x) {
+          for (int x = 0; x < NQ; ++x) {
 #pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            br_f4 y = s.o[x][d];
+            for (int d = 0; d < ND; ++d) {
+              br_f4 y = s.o[x][d];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] *= s.c;
-            kept[((wv * NQ + x) * ND + d) * 64 + lane] = y;
+              for (int j = 0; j < 4; ++j) y[j] *= s.c;
+              kept[((piece * NQ + x) * ND + d) * 64 + lane] = y;
+            }
+            if (g == 0) kept_ml[(piece * NQ + x) * 16 + n] = make_float2(s.m[x], s.l[x]);
           }
-          if (g == 0) kept_ml[(wv * NQ + x) * 16 + n] = make_float2(s.m[x], s.l[x]);
+          open = a > 0 && b < at.size;
+          if (a == 0 || (wv == 0 && at.seg < u)) {
+            BrKvShare c = {1, wg, 1, at.r, at.h, at.qi};
+            if (a > 0 || at.seg + at.size > runs.begin_of((wg + 1) * NW)) c.first = runs.owner_of(at.seg) / NW, c.parts = runs.owner_of(at.seg + at.size - 1) / NW - c.first + 1;
+            if (lane == 0) chains[a == 0 ? wv : NW] = c;
+          }
         }
-        open = b < at.size;
-        if (wv == 0 && lane == 0) {
-          const int first = runs.owner_of(at.seg) / NW;
-          out[0] = BrKvShare{1, first, runs.owner_of(at.seg + at.size - 1) / NW - first + 1, at.r, at.h, at.qi};
-        }
-      } else if (b == at.size) {
-        br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, 0, rows_q, s);
-      } else {
-        tail = true;
-        break;
+        u = at.seg + b;
+        if (u >= end || !at.next(p, runs)) break;
       }
-      u = at.seg + b;
-      if (u >= end || !at.next(p, runs)) break;
     }
   }
   if (lane == 0) goes_on[wv] = open;
   __syncthreads();
 
-  // adds what wave k has kept
-  auto add = [&](int k) {
+#pragma unroll 1
+  for (int c = 0; c <= NW; ++c) {
+    const BrKvShare chain = chains[c];
+    if (!chain.on) continue;
+    const int k0 = c < NW ? c + 1 : 0;  // the chain: piece 2 c + 1 (c < NW), then the pieces taken up by waves k0 .. k1
+    int k1 = min(k0, NW - 1);
+    while (k1 < NW - 1 && goes_on[k1]) ++k1;
+    auto member = [&](int k) { return k < k0 ? 2 * c + 1 : 2 * k; };
+    const int begin = c < NW ? k0 - 1 : k0;
+    const BrKvRow w = runs.row_of(p, chain.r);
+    const int rows_q = (int)min((long long)TQ, (long long)w.n * p.group - (long long)chain.qi * TQ);
+    for (int it = wv; it < NQ * ND; it += NW) {
+      const int x = it / ND, d = it - x * ND, row = 16 * x + n;
+      float top = BR_KV_NEG, l = 0.0f;
+      for (int k = begin; k <= k1; ++k) {
+        const float2 ml = kept_ml[(member(k) * NQ + x) * 16 + n];
+        if (ml.y != 0.0f) top = fmaxf(top, ml.x);
+      }
+      br_f4 y[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll 2
+      for (int k = begin; k <= k1; ++k) {
+        const float2 ml = kept_ml[(member(k) * NQ + x) * 16 + n];
+        const br_f4 v = kept[((member(k) * NQ + x) * ND + d) * 64 + lane];
+        const float e = ml.y != 0.0f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
+        l += ml.y * e;
 #pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-      const float2 ml = kept_ml[(k * NQ + x) * 16 + n];
-      const float top = s.l[x] == 0.0f ? ml.x : ml.y == 0.0f ? s.m[x] : fmaxf(s.m[x], ml.x);
-      const float e0 = s.l[x] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(s.m[x] - top), e1 = ml.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
-      s.m[x] = top;
-      s.l[x] = s.l[x] * e0 + ml.y * e1;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        const br_f4 y = kept[((k * NQ + x) * ND + d) * 64 + lane];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s.o[x][d][j] = s.o[x][d][j] * (s.c * e0) + y[j] * e1;
+        for (int j = 0; j < 4; ++j) y[0][j] = __builtin_fmaf(v[j], e, y[0][j]);
+      }
+      if (row >= rows_q) continue;
+      if (top == BR_KV_NEG) top = 0.0f;
+      if (chain.parts == 1) {
+        br_kv_store<1>(p, w, chain.h, chain.qi * TQ + row, 16 * d + 4 * g, y, l != 0.0f ? 1.0f / l : 0.0f);
+        if (d == 0 && g == 0) br_kv_store_lse(p, w, chain.h, chain.qi * TQ + row, top, l);
+      } else {
+        const long long piece = (long long)(2 * wg + (c < NW)) * TQ + row;
+        br_kv_put2(p.part + piece * D + 16 * d + 4 * g, y[0][0], y[0][1]);
+        br_kv_put2(p.part + piece * D + 16 * d + 4 * g + 2, y[0][2], y[0][3]);
+        if (d == 0 && g == 0) br_kv_put2(p.ml + piece * 2, top, l);
       }
     }
-    s.c = 1.0f;
-  };
-  if (tail) {
-    bool done = false;
-    for (int k = wv + 1; k < NW && !done; ++k) add(k), done = !goes_on[k];
-    if (done) {
-      br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, 0, at.rows_q(p), s);
-    } else {
-      br_kv_piece<D, NQ, TQ>(p, 2 * wg + 1, 0, at.rows_q(p), s);
-      if (lane == 0) out[1] = BrKvShare{1, wg, runs.owner_of(at.seg + at.size - 1) / NW - wg + 1, at.r, at.h, at.qi};
-    }
-  }
-  if (wv == 0 && out[0].on) {
-#pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-      s.m[x] = s.l[x] = 0.0f;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) s.o[x][d] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    s.c = 1.0f;
-    for (int k = 0; k < NW; ++k) {
-      add(k);
-      if (!goes_on[k]) break;
-    }
-    br_kv_piece<D, NQ, TQ>(p, 2 * wg, 0, TQ, s);
   }
   br_kv_stores_done();
   __syncthreads();
-  if (tid < 2 && out[tid].on) arrived[tid] = __hip_atomic_fetch_add(&p.arrived[out[tid].first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // the query tiles that other blocks have pieces of: at most one of an earlier block, and one that goes on in a later one
+  const unsigned long long going = __ballot(lane < NW && chains[min(lane, NW - 1)].on && chains[min(lane, NW - 1)].parts > 1);
+  const bool goes = going != 0;
+  const int which = goes ? __ffsll(going) - 1 : 0;
+  if (!goes && !chains[NW].on) return;
+  if (tid == 0 && chains[NW].on) arrived[0] = __hip_atomic_fetch_add(&p.arrived[chains[NW].first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (tid == 1 && goes) arrived[1] = __hip_atomic_fetch_add(&p.arrived[chains[which].first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
-#pragma unroll
+#pragma unroll 1
   for (int k = 0; k < 2; ++k) {
-    if (!out[k].on || arrived[k] != out[k].parts - 1) continue;
-    const BrKvRow w = runs.row_of(p, out[k].r);
-    br_kv_join<D, TQ, NT>(p, w, out[k].h, out[k].qi, (int)min((long long)TQ, (long long)w.n * p.group - (long long)out[k].qi * TQ), out[k].first, out[k].parts, kept, total);
-    if (tid == 0) p.arrived[out[k].first] = 0;  // (for the next launch)
+    const BrKvShare c = chains[k ? which : NW];
+    if ((k ? !goes : !c.on) || arrived[k] != c.parts - 1) continue;
+    const BrKvRow w = runs.row_of(p, c.r);
+    br_kv_join<D, TQ, NT>(p, w, c.h, c.qi, (int)min((long long)TQ, (long long)w.n * p.group - (long long)c.qi * TQ), c.first, c.parts, kept, (float2 *)(kept + NT));
+    if (tid == 0) p.arrived[c.first] = 0;  // (for the next launch)
     __syncthreads();
   }
 }
@@ -668,10 +725,10 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
   constexpr int TQ = 64 * NQ, NT = 256;
   __shared__ typename BrKvRuns<TQ, NT>::Shared shared;
   __shared__ br_f4 sums[NT];
-  __shared__ float2 total[TQ];
+  __shared__ float2 total[NT];
   __shared__ int arrived;
   const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const BrKvRuns<TQ, NT> runs(p, shared, gridDim.x);
+  BrKvRuns<TQ, NT> runs(p, shared, gridDim.x);
   const int blocks = runs.workers, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
   if (wg >= blocks) return;
   long long u = runs.begin_of(wg);
@@ -724,9 +781,11 @@ void br_kv_attend_rows(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
 
 template <int D>
 void br_kv_attend_dim(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st) {
-  if (tile == BR_KV_TILE_16) br_kv_attend_few<D, 1, D <= 96 ? 12 : D <= 128 ? 8 : 4, D <= 96 ? 3 : D <= 128 ? 2 : 1>(p, fp8, cus, st);
-  else if (tile == BR_KV_TILE_32) br_kv_attend_few<D, 2, D <= 64 ? 8 : 4, D <= 64 ? 2 : 1>(p, fp8, cus, st);
-  else br_kv_attend_rows<D, 2, D <= 96 ? 2 : 1>(p, fp8, cus, st);
+  if constexpr (D <= 128) {
+    if (tile == BR_KV_TILE_32) return br_kv_attend_few<D, 2, D <= 64 ? 8 : 4, D <= 64 ? 2 : 1>(p, fp8, cus, st);
+  }
+  if (tile == BR_KV_TILE_128) br_kv_attend_rows<D, 2, D <= 96 ? 2 : 1>(p, fp8, cus, st);
+  else br_kv_attend_few<D, 1, D <= 64 ? 12 : D <= 128 ? 8 : 4, D <= 64 ? 3 : D <= 128 ? 2 : 1>(p, fp8, cus, st);
 }
 
 #endif

@@ -52,6 +52,7 @@ struct BrKvAttend {
   long long q_token, q_head, out_token, out_head;
   int n_rows, rows, n_tokens, window, group, kv_heads, shift, n_blocks, max_blocks;
   int bf16, q_wide, out_wide;  // wide: rows of q (out) can be read (written) 16 (8) bytes at a time
+  unsigned group_mul, group_shift;  // x / group = (high word of group_mul x + x) >> group_shift for 0 <= x < 2^31
   float scale2;                // scale * log2(e)
 };
 
