@@ -657,13 +657,13 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   if (lane == 0) goes_on[wv] = open;
   __syncthreads();
 
+  const unsigned on = (unsigned)__ballot(lane <= NW && chains[min(lane, NW)].on), going_on = (unsigned)__ballot(lane < NW && goes_on[min(lane, NW - 1)]);
 #pragma unroll 1
-  for (int c = 0; c <= NW; ++c) {
+  for (unsigned left = on; left; left &= left - 1) {
+    const int c = __ffs(left) - 1;
     const BrKvShare chain = chains[c];
-    if (!chain.on) continue;
     const int k0 = c < NW ? c + 1 : 0;  // the chain: piece 2 c + 1 (c < NW), then the pieces taken up by waves k0 .. k1
-    int k1 = min(k0, NW - 1);
-    while (k1 < NW - 1 && goes_on[k1]) ++k1;
+    const int k1 = min(k0 + __ffs(~(going_on >> k0)) - 1, NW - 1);
     auto member = [&](int k) { return k < k0 ? 2 * c + 1 : 2 * k; };
     const int begin = c < NW ? k0 - 1 : k0;
     const BrKvRow w = runs.row_of(p, chain.r);
@@ -671,12 +671,13 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
     for (int it = wv; it < NQ * ND; it += NW) {
       const int x = it / ND, d = it - x * ND, row = 16 * x + n;
       float top = BR_KV_NEG, l = 0.0f;
+#pragma unroll 4
       for (int k = begin; k <= k1; ++k) {
         const float2 ml = kept_ml[(member(k) * NQ + x) * 16 + n];
         if (ml.y != 0.0f) top = fmaxf(top, ml.x);
       }
       br_f4 y[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
-#pragma unroll 2
+#pragma unroll 4
       for (int k = begin; k <= k1; ++k) {
         const float2 ml = kept_ml[(member(k) * NQ + x) * 16 + n];
         const br_f4 v = kept[((member(k) * NQ + x) * ND + d) * 64 + lane];
@@ -701,17 +702,17 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   br_kv_stores_done();
   __syncthreads();
   // the query tiles that other blocks have pieces of: at most one of an earlier block, and one that goes on in a later one
-  const unsigned long long going = __ballot(lane < NW && chains[min(lane, NW - 1)].on && chains[min(lane, NW - 1)].parts > 1);
-  const bool goes = going != 0;
-  const int which = goes ? __ffsll(going) - 1 : 0;
-  if (!goes && !chains[NW].on) return;
-  if (tid == 0 && chains[NW].on) arrived[0] = __hip_atomic_fetch_add(&p.arrived[chains[NW].first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const unsigned going = (unsigned)__ballot(lane < NW && chains[min(lane, NW - 1)].on && chains[min(lane, NW - 1)].parts > 1);
+  const bool goes = going != 0, came = on >> NW & 1;
+  const int which = goes ? __ffs(going) - 1 : 0;
+  if (!goes && !came) return;
+  if (tid == 0 && came) arrived[0] = __hip_atomic_fetch_add(&p.arrived[chains[NW].first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   if (tid == 1 && goes) arrived[1] = __hip_atomic_fetch_add(&p.arrived[chains[which].first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
 #pragma unroll 1
   for (int k = 0; k < 2; ++k) {
     const BrKvShare c = chains[k ? which : NW];
-    if ((k ? !goes : !c.on) || arrived[k] != c.parts - 1) continue;
+    if ((k ? !goes : !came) || arrived[k] != c.parts - 1) continue;
     const BrKvRow w = runs.row_of(p, c.r);
     br_kv_join<D, TQ, NT>(p, w, c.h, c.qi, (int)min((long long)TQ, (long long)w.n * p.group - (long long)c.qi * TQ), c.first, c.parts, kept, (float2 *)(kept + NT));
     if (tid == 0) p.arrived[c.first] = 0;  // (for the next launch)
