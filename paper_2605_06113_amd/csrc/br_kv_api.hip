@@ -103,6 +103,8 @@ BrKvTokens tokens_of(const br_kv_ctx *ctx, const br_kv_tokens *x) {
   t.k = x->k, t.v = x->v, t.slot = x->slot;
   t.k_token = x->k_token, t.k_head = x->k_head, t.v_token = x->v_token, t.v_head = x->v_head;
   t.n = x->n_tokens, t.W = ctx->cfg.n_workers, t.dtype = x->dtype;
+  const int64_t strides = x->k_token | x->k_head | x->v_token | x->v_head;
+  t.wide = (((uintptr_t)x->k | (uintptr_t)x->v) & 15u) == 0 && (strides & (x->dtype == BR_KV_F32 ? 3 : 7)) == 0;
   return t;
 }
 
@@ -161,13 +163,13 @@ int32_t br_kv_step(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out
 int32_t br_kv_append(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_tokens *in) {
   if (!ctx || !layer_ok(layer) || !tokens_ok(ctx, in)) return BR_EINVAL;
   if (in->n_tokens == 0) return BR_OK;
-  return enqueue(ctx, [&] { br_kv_launch_append(cache_of(ctx, layer), tokens_of(ctx, in), ctx->cfg.fmt == BR_KV_E4M3, ctx->st); });
+  return enqueue(ctx, [&] { br_kv_launch_append(cache_of(ctx, layer), tokens_of(ctx, in), ctx->cfg.rows, ctx->cfg.fmt == BR_KV_E4M3, ctx->st); });
 }
 
 int32_t br_kv_read(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_tokens *out) {
   if (!ctx || !layer_ok(layer) || !tokens_ok(ctx, out)) return BR_EINVAL;
   if (out->n_tokens == 0) return BR_OK;
-  return enqueue(ctx, [&] { br_kv_launch_read(cache_of(ctx, layer), tokens_of(ctx, out), ctx->cfg.fmt == BR_KV_E4M3, ctx->st); });
+  return enqueue(ctx, [&] { br_kv_launch_read(cache_of(ctx, layer), tokens_of(ctx, out), ctx->cfg.rows, ctx->cfg.fmt == BR_KV_E4M3, ctx->st); });
 }
 
 int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *a) {

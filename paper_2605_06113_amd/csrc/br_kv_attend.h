@@ -70,14 +70,6 @@ __device__ __forceinline__ uint4 br_kv_load16(const unsigned char *at) {
   return make_uint4(x[0], x[1], x[2], x[3]);
 }
 
-// Two values in 16 bits each
-template <class T>
-__device__ __forceinline__ unsigned br_kv_pair(float a, float b) {
-  typedef float f2 __attribute__((ext_vector_type(2)));
-  typedef T t2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{a, b}), t2));
-}
-
 // One query row's place in the output: its 4 N channels d, d + 16, ..., of the lane, times inv.
 template <int N>
 __device__ __forceinline__ void br_kv_store(const BrKvAttend &p, const BrKvRow &w, int h, int ri, int d, const br_f4 (&x)[N], float inv) {
@@ -131,14 +123,6 @@ struct BrKvSums {
   br_f4 o[NQ][D / 16];
   float m[NQ], l[NQ], c;
 };
-
-// Over the four lanes of a query row: the exchanges of 16 and 32 lanes stay in the vector registers.
-__device__ __forceinline__ float br_kv_max4(float x) {
-  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
 
 __device__ __forceinline__ float br_kv_sum4(float x) {
   auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);

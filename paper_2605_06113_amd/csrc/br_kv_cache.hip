@@ -1,33 +1,33 @@
 // Tokens into the 8-bit cache and out of it (br_kv_append, br_kv_read).
 //
-// A run: tokens that stand together in the call's list and in one block.  A wave takes a run and a head: nobody else writes that
-// block's codes or scales.
+// Bound by memory: values are read once (append: twice, the second time from a cache) and written once.  The unit of work is a run, tokens
+// that stand together in the call's list and in one block, with a key head: nobody else writes that block's codes or scales, so there
+// are no atomics.  Lists of single tokens (decode steps) take a wave per token and head, long ones a block per 16 to 64 tokens and
+// head, whose four waves share a run or take runs of their own.  Values lie with their tokens side by side: a thread has two channels
+// of 16 tokens, reads them token by token (lanes side by side) and moves 16 bytes of each channel.
 #include "br_kv_device.h"
 
 #define BR_KV_LEAST 27u  // biased exponent of 2^-100, the smallest scale
 
-__device__ __forceinline__ float br_kv_get(const void *x, long long at, int dtype) {
-  if (dtype == BR_KV_F32) return ((const float *)x)[at];
-  const unsigned short u = ((const unsigned short *)x)[at];
-  return dtype == BR_KV_BF16 ? br_kv_bf16(u) : br_kv_f16(u);
-}
+#define BR_KV_FEW 4      // tokens of a run that a wave takes one by one
 
-__device__ __forceinline__ void br_kv_set(void *x, long long at, int dtype, float y) {
-  if (dtype == BR_KV_F32) ((float *)x)[at] = y;
-  else ((unsigned short *)x)[at] = dtype == BR_KV_BF16 ? br_kv_to_bf16(y) : br_kv_to_f16(y);
-}
+typedef unsigned br_u4 __attribute__((ext_vector_type(4)));
 
 template <bool FP8>
-__device__ __forceinline__ float br_kv_value(unsigned char c) {
+__device__ __forceinline__ float br_kv_value(unsigned c) {  // of the lowest byte
   if constexpr (FP8) return __builtin_amdgcn_cvt_f32_fp8((int)c, 0);
   else return (float)(signed char)c;
 }
 
-// x of magnitude at most the format's top
+// Codes of four values of magnitude at most the format's top
 template <bool FP8>
-__device__ __forceinline__ unsigned char br_kv_code(float x) {
-  if constexpr (FP8) return (unsigned char)__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false);
-  else return (unsigned char)(int)__builtin_rintf(x);
+__device__ __forceinline__ unsigned br_kv_code4(float a, float b, float c, float d) {
+  if constexpr (FP8) {
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+  } else {
+    auto q = [](float x) { return (unsigned)(int)__builtin_rintf(x) & 255u; };
+    return q(a) | q(b) << 8 | q(c) << 16 | q(d) << 24;
+  }
 }
 
 // a * r rounded to odd: what is rounded to 8 bits next comes out as if from the exact product (a ratio of scales that is no power
@@ -37,6 +37,12 @@ __device__ __forceinline__ float br_kv_times(float a, float r) {
   const unsigned u = __float_as_uint(y);
   if (err == 0.0f || (u & 1u)) return y;
   return __uint_as_float((err > 0.0f) == (y > 0.0f) ? u + 1 : u - 1);
+}
+
+template <bool FP8>
+__device__ __forceinline__ unsigned br_kv_recode4(unsigned c, float r) {
+  return br_kv_code4<FP8>(br_kv_times(br_kv_value<FP8>(c), r), br_kv_times(br_kv_value<FP8>(c >> 8), r), br_kv_times(br_kv_value<FP8>(c >> 16), r),
+                          br_kv_times(br_kv_value<FP8>(c >> 24), r));
 }
 
 // Biased exponent of the least power of two s with top <= TOP s: TOP is 1.984375 2^6 or 1.75 2^8.
@@ -50,98 +56,379 @@ __device__ __forceinline__ unsigned br_kv_scale_exp(float top) {
 // 2^-(e - 127) of a biased exponent e in 27..253
 __device__ __forceinline__ float br_kv_inverse(unsigned e) { return __uint_as_float((254u - e) << 23); }
 
-// The run that begins with token t of a list of n: its tokens, or 0 if t begins none.
-__device__ __forceinline__ int br_kv_run(const int *slot, int t, int n, int slots, int b1) {
-  const int s = slot[t];
-  if (s < 0 || s >= slots) return 0;
-  if (t > 0 && (s & b1) != 0 && slot[t - 1] == s - 1) return 0;
-  int k = 1;
-  while (t + k < n && ((s + k) & b1) != 0 && slot[t + k] == s + k) ++k;
-  return k;
+template <int DT>
+__device__ __forceinline__ float br_kv_to_float(unsigned short u) {
+  return DT == BR_KV_BF16 ? br_kv_bf16(u) : br_kv_f16(u);
 }
 
-template <bool FP8, bool VALUES>
-__device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const void *x, long long x_token, long long x_head, int dtype, long long t, int run,
-                                                 int h, long long block, int off) {
-  const int lane = threadIdx.x & 63, D = c.dim, b = 1 << c.shift, n = run * D;
-  unsigned char *codes = (VALUES ? c.v : c.k) + ((block * D) << c.shift);
-  float *scale = (VALUES ? c.vs : c.ks) + block;
-  float top = 0.0f;
-  bool bad = false;
-  for (int i = lane; i < n; i += 64) {
-    const float y = fabsf(br_kv_get(x, (t + i / D) * x_token + (long long)h * x_head + i % D, dtype));
-    bad |= !(y < __builtin_inff());
-    top = fmaxf(top, y);
+// N = 8 or 2 neighbours of the caller's array as they lie there, and as floats; wide: they are aligned to their size
+template <int DT, int N>
+struct BrKvRaw {
+  static constexpr int WORDS = DT == BR_KV_F32 ? N : N / 2;
+  unsigned u[WORDS];
+
+  __device__ __forceinline__ void fetch(const void *x, long long at, int wide) {
+    if (wide) {
+      const unsigned *p = DT == BR_KV_F32 ? (const unsigned *)x + at : (const unsigned *)((const unsigned short *)x + at);
+      if constexpr (WORDS >= 4) {
+#pragma unroll
+        for (int k = 0; k < WORDS; k += 4) {
+          const uint4 y = *(const uint4 *)(p + k);
+          u[k] = y.x, u[k + 1] = y.y, u[k + 2] = y.z, u[k + 3] = y.w;
+        }
+      } else if constexpr (WORDS == 2) {
+        const uint2 y = *(const uint2 *)p;
+        u[0] = y.x, u[1] = y.y;
+      } else {
+        u[0] = *p;
+      }
+    } else if constexpr (DT == BR_KV_F32) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) u[k] = ((const unsigned *)x)[at + k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < WORDS; ++k) u[k] = ((const unsigned short *)x)[at + 2 * k] | (unsigned)((const unsigned short *)x)[at + 2 * k + 1] << 16;
+    }
   }
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-  bad = __any(bad);
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int k = 0; k < WORDS; ++k) u[k] = 0;
+  }
+  __device__ __forceinline__ float get(int j) const {
+    if constexpr (DT == BR_KV_F32) return __uint_as_float(u[j]);
+    else return br_kv_to_float<DT>((unsigned short)(j & 1 ? u[j / 2] >> 16 : u[j / 2]));
+  }
+  __device__ __forceinline__ void look(float &top, int &bad, int bit) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float y = fabsf(get(j));
+      top = fmaxf(top, y);
+      bad |= y < __builtin_inff() ? 0 : bit;
+    }
+  }
+};
+
+template <int DT, int N>
+__device__ __forceinline__ void br_kv_store_out(void *x, long long at, int wide, const float (&y)[N]) {
+  if constexpr (DT == BR_KV_F32) {
+    float *p = (float *)x + at;
+    if (wide) {
+      if constexpr (N == 8) {
+        *(float4 *)p = *(const float4 *)y;
+        *(float4 *)(p + 4) = *(const float4 *)(y + 4);
+      } else {
+        *(float2 *)p = *(const float2 *)y;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) p[j] = y[j];
+    }
+  } else {
+    unsigned short *p = (unsigned short *)x + at;
+    unsigned u[N / 2];
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) u[j] = DT == BR_KV_BF16 ? br_kv_pair<__bf16>(y[2 * j], y[2 * j + 1]) : br_kv_pair<_Float16>(y[2 * j], y[2 * j + 1]);
+    if (wide) {
+      if constexpr (N == 8) *(uint4 *)p = *(const uint4 *)u;
+      else *(unsigned *)p = u[0];
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) p[j] = (unsigned short)(j & 1 ? u[j / 2] >> 16 : u[j / 2]);
+    }
+  }
+}
+
+// A block's place for one key head, and what a run of n tokens from offset off on does there; t: the run's first token in the list.
+struct BrKvRun {
+  long long block, t;
+  int h, off, n;
+};
+
+// Over the wave: within rows of 16 lanes by their neighbours and mirrors, between rows by exchanges
+__device__ __forceinline__ float br_kv_max64(float x) {
+#define BR_KV_STEP(CTRL) x = fmaxf(x, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), CTRL, 0xf, 0xf, true)))
+  BR_KV_STEP(0xB1);   // lane ^ 1
+  BR_KV_STEP(0x4E);   // lane ^ 2
+  BR_KV_STEP(0x141);  // mirrored in 8
+  BR_KV_STEP(0x140);  // mirrored in 16
+#undef BR_KV_STEP
+  return br_kv_max4(x);
+}
+
+// The scale of the new tokens' block: `top` of them, `bad`: one is not finite.  r: what earlier codes are multiplied by.
+struct BrKvScale {
+  float inv, s, r;
+  bool bad;
+};
+
+template <bool FP8>
+__device__ __forceinline__ BrKvScale br_kv_scale(float top, bool bad, int off, float old) {
   unsigned e = br_kv_scale_exp<FP8>(bad ? 0.0f : top);
+  BrKvScale z = {0.0f, 0.0f, 1.0f, bad};
   if (off > 0) {
     // (a scale that is no power of two, in a cache that was written elsewhere, moves up to one)
-    const float old = *scale;
-    bad |= !(old >= 0.0f && old < 8.5e37f);
-    const unsigned u = bad ? 0u : __float_as_uint(old);
+    z.bad = z.bad || !(old >= 0.0f && old < 8.5e37f);
+    const unsigned u = z.bad ? 0u : __float_as_uint(old);
     e = max(e, (u >> 23) + ((u & 0x7fffffu) != 0));
-    const float r = old * br_kv_inverse(e);
-    if (!bad && r != 1.0f) {
-      for (int i = lane; i < off * D; i += 64) {
-        unsigned char *at = codes + (VALUES ? (i % D) * b + i / D : i);
-        *at = br_kv_code<FP8>(br_kv_times(br_kv_value<FP8>(*at), r));
+    z.r = z.bad ? 1.0f : old * br_kv_inverse(e);
+  }
+  z.inv = br_kv_inverse(e);
+  z.s = z.bad ? __builtin_nanf("") : __uint_as_float(e << 23);
+  return z;
+}
+
+// NT threads (a wave, or a block that is all here) write a run.  red: 16 floats of LDS.  The first AT_ONCE rows of keys and 16 x 2 values
+// of a thread (all, up to 64 tokens of 128 channels for a block) stay in registers between the maximum and the codes.
+template <bool FP8, int DT, int NT>
+__device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, int tid, float *red) {
+  constexpr int AT_ONCE = 4;
+  const int D = c.dim, b = 1 << c.shift, chunks = D >> 3, pairs = D >> 1;
+  unsigned char *kc = c.k + ((u.block * D) << c.shift), *vc = c.v + ((u.block * D) << c.shift);
+  const float old_k = u.off ? c.ks[u.block] : 0.0f, old_v = u.off ? c.vs[u.block] : 0.0f;
+  // keys: 8 channels from kd on of tokens kj, kj + kstep, ...
+  const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
+  const long long k0 = u.t * a.k_token + (long long)u.h * a.k_head + kd, v0 = u.t * a.v_token + (long long)u.h * a.v_head;
+  // values: channels vd and vd + 1 of the block's tokens 16 vg .. 16 vg + 15
+  const int vg0 = u.off >> 4, vitems = (((u.off + u.n - 1) >> 4) - vg0 + 1) * pairs;
+  float top_k = 0.0f, top_v = 0.0f;
+  int bad = 0;
+  BrKvRaw<DT, 8> rk[AT_ONCE];
+  BrKvRaw<DT, 2> rv[16];
+  auto fetch_v = [&](int i) {
+    const int g = vg0 + i / pairs, d = (i % pairs) * 2, lo = u.off - 16 * g, hi = u.off + u.n - 16 * g;
+    const long long at = v0 + (16 * g - u.off) * a.v_token + d;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      rv[j].zero();
+      if (j >= lo && j < hi) rv[j].fetch(a.v, at + j * a.v_token, a.wide);
+    }
+  };
+#pragma unroll
+  for (int m = 0; m < AT_ONCE; ++m) {
+    rk[m].zero();
+    if (kj + m * kstep < kn) rk[m].fetch(a.k, k0 + (kj + m * kstep) * a.k_token, a.wide);
+  }
+  // a decode step's few tokens: two channels of one token at a time
+  const bool few = NT == 64 && u.n <= BR_KV_FEW;
+  if (few) {
+    for (int i = tid; i < u.n * pairs; i += NT) {
+      const int j = i / pairs;
+      rv[0].fetch(a.v, v0 + j * a.v_token + (i - j * pairs) * 2, a.wide);
+      rv[0].look(top_v, bad, 2);
+    }
+  } else {
+    for (int i = tid; i < vitems; i += NT) {
+      fetch_v(i);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) rv[j].look(top_v, bad, 2);
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < AT_ONCE; ++m) rk[m].look(top_k, bad, 1);
+  for (int j = kj + AT_ONCE * kstep; j < kn; j += kstep) {
+    BrKvRaw<DT, 8> x;
+    x.fetch(a.k, k0 + j * a.k_token, a.wide);
+    x.look(top_k, bad, 1);
+  }
+  top_k = br_kv_max64(top_k), top_v = br_kv_max64(top_v);
+  bad = (__any(bad & 1) ? 1 : 0) | (__any(bad & 2) ? 2 : 0);
+  if constexpr (NT > 64) {
+    __syncthreads();
+    if ((tid & 63) == 0) red[tid >> 6] = top_k, red[4 + (tid >> 6)] = top_v, red[8 + (tid >> 6)] = __uint_as_float((unsigned)bad);
+    __syncthreads();
+    bad = 0;
+#pragma unroll
+    for (int k = 0; k < NT / 64; ++k) top_k = fmaxf(top_k, red[k]), top_v = fmaxf(top_v, red[4 + k]), bad |= (int)__float_as_uint(red[8 + k]);
+  }
+  const BrKvScale zk = br_kv_scale<FP8>(top_k, bad & 1, u.off, old_k), zv = br_kv_scale<FP8>(top_v, bad & 2, u.off, old_v);
+
+  if (zk.r != 1.0f) {  // earlier keys
+    for (int j = kj; j < (kj < kstep ? u.off : 0); j += kstep) {
+      uint2 *at = (uint2 *)(kc + (long long)j * D + kd);
+      *at = make_uint2(br_kv_recode4<FP8>(at->x, zk.r), br_kv_recode4<FP8>(at->y, zk.r));
+    }
+  }
+  auto put_k = [&](int j, const BrKvRaw<DT, 8> &x) {
+    auto q = [&](int m) { return zk.bad ? 0.0f : x.get(m) * zk.inv; };
+    *(uint2 *)(kc + (long long)(u.off + j) * D + kd) = make_uint2(br_kv_code4<FP8>(q(0), q(1), q(2), q(3)), br_kv_code4<FP8>(q(4), q(5), q(6), q(7)));
+  };
+#pragma unroll
+  for (int m = 0; m < AT_ONCE; ++m)
+    if (kj + m * kstep < kn) put_k(kj + m * kstep, rk[m]);
+  for (int j = kj + AT_ONCE * kstep; j < kn; j += kstep) {
+    BrKvRaw<DT, 8> x;
+    x.fetch(a.k, k0 + j * a.k_token, a.wide);
+    put_k(j, x);
+  }
+
+  if (zv.r != 1.0f) {  // earlier values: those in the first new group's 16 tokens too
+    for (int i = tid; i < (vg0 + 1) * D; i += NT) {
+      const int g = i / D, n = min(u.off - 16 * g, 16);
+      br_u4 *at = (br_u4 *)(vc + ((long long)(i - g * D) << c.shift) + 16 * g);
+      br_u4 x = *at;
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const unsigned before = n >= 4 * m + 4 ? ~0u : n <= 4 * m ? 0u : ~(~0u << (8 * (n - 4 * m)));
+        x[m] = (br_kv_recode4<FP8>(x[m], zv.r) & before) | (x[m] & ~before);
+      }
+      if (n > 0) *at = x;
+    }
+    if constexpr (NT > 64) __syncthreads();  // (other threads put new values beside them)
+    else __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  }
+  if (few) {
+    for (int i = tid; i < u.n * pairs; i += NT) {
+      const int j = i / pairs, d = (i - j * pairs) * 2;
+      if (u.n * pairs > NT) rv[0].fetch(a.v, v0 + j * a.v_token + d, a.wide);
+      const unsigned q = br_kv_code4<FP8>(zv.bad ? 0.0f : rv[0].get(0) * zv.inv, zv.bad ? 0.0f : rv[0].get(1) * zv.inv, 0.0f, 0.0f);
+      unsigned char *at = vc + ((long long)d << c.shift) + u.off + j;
+      at[0] = (unsigned char)q, at[b] = (unsigned char)(q >> 8);
+    }
+  }
+  const bool again = vitems > NT;
+  for (int i = tid; i < (few ? 0 : vitems); i += NT) {
+    if (again) fetch_v(i);
+    const int g = vg0 + i / pairs, d = (i % pairs) * 2, lo = max(u.off - 16 * g, 0), hi = min(u.off + u.n - 16 * g, 16);  // new ones: lo .. hi - 1
+    unsigned char *at = vc + ((long long)d << c.shift) + 16 * g;
+    br_u4 y[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        auto q = [&](int j) { return zv.bad ? 0.0f : rv[4 * m + j].get(k) * zv.inv; };
+        y[k][m] = br_kv_code4<FP8>(q(0), q(1), q(2), q(3));
+      }
+    if (hi - lo == 16) {
+      *(br_u4 *)at = y[0];
+      *(br_u4 *)(at + b) = y[1];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (j >= lo && j < hi) at[j] = (unsigned char)(y[0][j / 4] >> (8 * (j & 3))), at[b + j] = (unsigned char)(y[1][j / 4] >> (8 * (j & 3)));
+    }
+  }
+  if (tid == 0) c.ks[u.block] = zk.s, c.vs[u.block] = zv.s;
+}
+
+template <bool FP8, int DT, int NT>
+__device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, bool in, int tid) {
+  const int D = c.dim, b = 1 << c.shift, chunks = D >> 3, pairs = D >> 1;
+  const unsigned char *kc = c.k + ((u.block * D) << c.shift), *vc = c.v + ((u.block * D) << c.shift);
+  const float ks = c.ks[u.block], vs = c.vs[u.block];
+  const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
+  const long long k0 = u.t * a.k_token + (long long)u.h * a.k_head + kd, v0 = u.t * a.v_token + (long long)u.h * a.v_head;
+  const int vg0 = u.off >> 4, vitems = (((u.off + u.n - 1) >> 4) - vg0 + 1) * pairs;
+  br_u4 x0, x1;
+  auto fetch_v = [&](int i) {
+    const int g = vg0 + i / pairs, d = (i % pairs) * 2;
+    const unsigned char *at = vc + ((long long)d << c.shift) + 16 * g;
+    x0 = *(const br_u4 *)at, x1 = *(const br_u4 *)(at + b);
+  };
+  const bool few = NT == 64 && u.n <= BR_KV_FEW;
+  if (few) {
+    for (int i = tid; i < u.n * pairs; i += NT) {
+      const int j = i / pairs, d = (i - j * pairs) * 2;
+      const unsigned char *at = vc + ((long long)d << c.shift) + u.off + j;
+      const float y[2] = {in ? br_kv_value<FP8>(at[0]) * vs : 0.0f, in ? br_kv_value<FP8>(at[b]) * vs : 0.0f};
+      br_kv_store_out<DT, 2>(a.v, v0 + j * a.v_token + d, a.wide, y);
+    }
+  } else if (tid < vitems) {
+    fetch_v(tid);
+  }
+#pragma unroll 4
+  for (int j = kj; j < kn; j += kstep) {
+    const uint2 x = *(const uint2 *)(kc + (long long)(u.off + j) * D + kd);
+    float y[8];
+#pragma unroll
+    for (int m = 0; m < 8; ++m) y[m] = in ? br_kv_value<FP8>((m < 4 ? x.x : x.y) >> (8 * (m & 3))) * ks : 0.0f;
+    br_kv_store_out<DT, 8>(a.k, k0 + j * a.k_token, a.wide, y);
+  }
+  for (int i = tid; i < (few ? 0 : vitems); i += NT) {
+    if (i != tid) fetch_v(i);
+    const int g = vg0 + i / pairs, d = (i % pairs) * 2, lo = u.off - 16 * g, hi = u.off + u.n - 16 * g;
+    const long long at = v0 + (16 * g - u.off) * a.v_token + d;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if (j < lo || j >= hi) continue;
+      const float y[2] = {in ? br_kv_value<FP8>(x0[j / 4] >> (8 * (j & 3))) * vs : 0.0f, in ? br_kv_value<FP8>(x1[j / 4] >> (8 * (j & 3))) * vs : 0.0f};
+      br_kv_store_out<DT, 2>(a.v, at + j * a.v_token, a.wide, y);
+    }
+  }
+}
+
+// Which tokens of t .. t + 63 of a list of n begin a run (also those behind the list's end; bit k: token t + k).
+__device__ __forceinline__ unsigned long long br_kv_heads(const int *slot, int t, int n, int slots, int b1) {
+  const int at = t + (threadIdx.x & 63);
+  bool head = true;
+  if (at < n) {
+    const int s = slot[at], before = at > 0 ? slot[at - 1] : -1;
+    head = s < 0 || s >= slots || (s & b1) == 0 || before != s - 1;
+  }
+  return __ballot(head);
+}
+
+// `span` tokens of a list (at most 64) and a key head for a block, or one for a wave (WAVE).
+template <bool FP8, int DT, bool READ, bool WAVE>
+__global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a, int span) {
+  __shared__ float red[16];
+  if (WAVE) span = 1;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, b1 = (1 << c.shift) - 1, slots = c.n_blocks << c.shift;
+  const int spans = (a.n + span - 1) / span;
+  const long long units = (long long)a.W * spans * c.heads, step = WAVE ? (long long)gridDim.x * 4 : gridDim.x;
+  for (long long id = WAVE ? (long long)blockIdx.x * 4 + wv : blockIdx.x; id < units; id += step) {
+    const long long part = id / c.heads;
+    BrKvRun u;
+    u.h = (int)(id - part * c.heads);
+    const int w = (int)(part / spans), t0 = (int)(part - (long long)w * spans) * span;
+    const int *slot = a.slot + (long long)w * a.n;
+    // heads of the span's tokens, and of those that its last run may reach (a block's more)
+    unsigned long long heads[3] = {br_kv_heads(slot, t0, a.n, slots, b1), ~0ull, ~0ull};
+    if (span + b1 + 1 > 64) heads[1] = br_kv_heads(slot, t0 + 64, a.n, slots, b1);
+    if (span + b1 + 1 > 128) heads[2] = br_kv_heads(slot, t0 + 128, a.n, slots, b1);
+    unsigned long long left = heads[0] & (~0ull >> (64 - min(span, a.n - t0)));
+    const bool apart = !WAVE && __popcll(left) > 2;  // several short runs: one for each wave
+    int turn = 0;
+    for (; left; left &= left - 1, ++turn) {
+      if (apart && (turn & 3) != wv) continue;
+      const int k = __ffsll(left) - 1;
+      const unsigned long long rest = k < 63 ? heads[0] >> (k + 1) << (k + 1) : 0;
+      const int end = rest ? __ffsll(rest) - 1 : heads[1] ? 63 + __ffsll(heads[1]) : heads[2] ? 127 + __ffsll(heads[2]) : 192;
+      const int s = slot[t0 + k];
+      const bool in = s >= 0 && s < slots;
+      if (!READ && !in) continue;
+      u.t = (long long)w * a.n + t0 + k;
+      u.n = in ? min(end - k, b1 + 1) : 1;
+      u.off = in ? s & b1 : 0;
+      u.block = ((long long)w * c.n_blocks + (in ? s >> c.shift : 0)) * c.heads + u.h;
+      if constexpr (READ) {
+        if (WAVE || apart) br_kv_read_run<FP8, DT, 64>(c, a, u, in, lane);
+        else br_kv_read_run<FP8, DT, 256>(c, a, u, in, threadIdx.x);
+      } else {
+        if (WAVE || apart) br_kv_append_run<FP8, DT, 64>(c, a, u, lane, red);
+        else br_kv_append_run<FP8, DT, 256>(c, a, u, threadIdx.x, red);
       }
     }
   }
-  const float inv = br_kv_inverse(e);
-  for (int i = lane; i < n; i += 64) {
-    const int j = i / D, d = i % D;
-    const float y = br_kv_get(x, (t + j) * x_token + (long long)h * x_head + d, dtype);
-    codes[VALUES ? d * b + off + j : (off + j) * D + d] = bad ? 0 : br_kv_code<FP8>(y * inv);
-  }
-  if (lane == 0) *scale = bad ? __builtin_nanf("") : __uint_as_float(e << 23);
 }
 
-template <bool FP8>
-__global__ __launch_bounds__(256) void br_kv_k_append(BrKvCache c, BrKvTokens a) {
-  const int b1 = (1 << c.shift) - 1;
-  for (long long id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); id < (long long)a.W * a.n * c.heads; id += (long long)gridDim.x * 4) {
-    const long long t = id / c.heads;
-    const int h = (int)(id - t * c.heads), w = (int)(t / a.n);
-    const int run = br_kv_run(a.slot + (long long)w * a.n, (int)(t - (long long)w * a.n), a.n, c.n_blocks << c.shift, b1);
-    if (run == 0) continue;
-    const int s = a.slot[t];
-    const long long block = ((long long)w * c.n_blocks + (s >> c.shift)) * c.heads + h;
-    br_kv_append_run<FP8, false>(c, a.k, a.k_token, a.k_head, a.dtype, t, run, h, block, s & b1);
-    br_kv_append_run<FP8, true>(c, a.v, a.v_token, a.v_head, a.dtype, t, run, h, block, s & b1);
-  }
+template <bool FP8, int DT, bool READ>
+static void launch(const BrKvCache &c, const BrKvTokens &t, int rows, hipStream_t st) {
+  const long long tokens = (long long)t.W * t.n * c.heads;
+  auto grid = [](long long n) { return (unsigned)(n < 1 ? 1 : n > 1 << 20 ? 1 << 20 : n); };
+  // a wave for each token and head while they fit the chip about once; most waves of a longer list would begin no run.  A list of
+  // more than a few tokens a row has runs of whole blocks: 64 tokens are four runs of 16, one for each wave, or at most two longer ones
+  const int span = t.n > 4 * rows ? (c.shift == 5 ? 32 : 64) : 16;
+  if (tokens <= 16384) br_kv_k_tokens<FP8, DT, READ, true><<<grid((tokens + 3) / 4), 256, 0, st>>>(c, t, 1);
+  else br_kv_k_tokens<FP8, DT, READ, false><<<grid((long long)t.W * ((t.n + span - 1) / span) * c.heads), 256, 0, st>>>(c, t, span);
 }
 
-template <bool FP8>
-__global__ __launch_bounds__(256) void br_kv_k_read(BrKvCache c, BrKvTokens a) {
-  const int b = 1 << c.shift, D = c.dim, lane = threadIdx.x & 63;
-  for (long long id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); id < (long long)a.W * a.n * c.heads; id += (long long)gridDim.x * 4) {
-    const long long t = id / c.heads;
-    const int h = (int)(id - t * c.heads), w = (int)(t / a.n), s = a.slot[t];
-    const bool in = s >= 0 && s < c.n_blocks << c.shift;
-    const long long block = ((long long)w * c.n_blocks + (in ? s >> c.shift : 0)) * c.heads + h;
-    const int off = s & (b - 1);
-    const float ks = c.ks[block], vs = c.vs[block];
-    for (int d = lane; d < D; d += 64) {
-      const float k = br_kv_value<FP8>(c.k[((block << c.shift) + off) * D + d]) * ks, v = br_kv_value<FP8>(c.v[((block * D + d) << c.shift) + off]) * vs;
-      br_kv_set(a.k, t * a.k_token + h * a.k_head + d, a.dtype, in ? k : 0.0f);
-      br_kv_set(a.v, t * a.v_token + h * a.v_head + d, a.dtype, in ? v : 0.0f);
-    }
-  }
+template <bool READ>
+static void launch_type(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st) {
+  if (t.dtype == BR_KV_F32) fp8 ? launch<true, BR_KV_F32, READ>(c, t, rows, st) : launch<false, BR_KV_F32, READ>(c, t, rows, st);
+  else if (t.dtype == BR_KV_BF16) fp8 ? launch<true, BR_KV_BF16, READ>(c, t, rows, st) : launch<false, BR_KV_BF16, READ>(c, t, rows, st);
+  else fp8 ? launch<true, BR_KV_F16, READ>(c, t, rows, st) : launch<false, BR_KV_F16, READ>(c, t, rows, st);
 }
 
-void br_kv_launch_append(const BrKvCache &c, const BrKvTokens &t, bool fp8, hipStream_t st) {
-  const long long waves = (long long)t.W * t.n * c.heads;
-  const unsigned blocks = (unsigned)(waves + 3 < 4ll << 20 ? (waves + 3) / 4 : 1 << 20);
-  if (fp8) br_kv_k_append<true><<<blocks, 256, 0, st>>>(c, t);
-  else br_kv_k_append<false><<<blocks, 256, 0, st>>>(c, t);
-}
+void br_kv_launch_append(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st) { launch_type<false>(c, t, rows, fp8, st); }
 
-void br_kv_launch_read(const BrKvCache &c, const BrKvTokens &t, bool fp8, hipStream_t st) {
-  const long long waves = (long long)t.W * t.n * c.heads;
-  const unsigned blocks = (unsigned)(waves + 3 < 4ll << 20 ? (waves + 3) / 4 : 1 << 20);
-  if (fp8) br_kv_k_read<true><<<blocks, 256, 0, st>>>(c, t);
-  else br_kv_k_read<false><<<blocks, 256, 0, st>>>(c, t);
-}
+void br_kv_launch_read(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st) { launch_type<true>(c, t, rows, fp8, st); }

@@ -36,7 +36,7 @@ struct BrKvTokens {
   void *k, *v;
   const int *slot;
   long long k_token, k_head, v_token, v_head;
-  int n, W, dtype;
+  int n, W, dtype, wide;  // wide: 8 neighbouring channels can be moved at once
 };
 
 struct BrKvAttend {
@@ -59,8 +59,8 @@ struct BrKvAttend {
 void br_kv_launch_clear(const BrKvTables &t, int *arrived, hipStream_t st);
 void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, hipStream_t st);
 void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st);
-void br_kv_launch_append(const BrKvCache &c, const BrKvTokens &t, bool fp8, hipStream_t st);
-void br_kv_launch_read(const BrKvCache &c, const BrKvTokens &t, bool fp8, hipStream_t st);
+void br_kv_launch_append(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st);
+void br_kv_launch_read(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st);
 
 // br_kv_attend_*.hip, one per head width
 enum { BR_KV_TILE_16 = 0, BR_KV_TILE_32 = 1, BR_KV_TILE_128 = 2 };  // rows of queries of a block's tile
@@ -101,8 +101,22 @@ __device__ __forceinline__ br_h8 br_kv_decode8(unsigned c0, unsigned c1) {
 
 __device__ __forceinline__ float br_kv_bf16(unsigned short u) { return __uint_as_float((unsigned)u << 16); }
 __device__ __forceinline__ float br_kv_f16(unsigned short u) { return (float)__builtin_bit_cast(_Float16, u); }
-__device__ __forceinline__ unsigned short br_kv_to_bf16(float x) { return __builtin_bit_cast(unsigned short, (__bf16)x); }
-__device__ __forceinline__ unsigned short br_kv_to_f16(float x) { return __builtin_bit_cast(unsigned short, (_Float16)x); }
+
+// Over lanes n, n + 16, n + 32, n + 48: the exchanges of 16 and 32 lanes stay in the vector registers.
+__device__ __forceinline__ float br_kv_max4(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Two values in 16 bits each
+template <class T>
+__device__ __forceinline__ unsigned br_kv_pair(float a, float b) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef T t2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{a, b}), t2));
+}
 #endif
 
 #endif
