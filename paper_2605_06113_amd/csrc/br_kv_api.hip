@@ -30,7 +30,7 @@ bool config_ok(const br_kv_config *c) {
 }
 
 struct Places {
-  uint64_t lens, table, used, part, ml, arrived, total;
+  uint64_t lens, table, tail, used, runs, part, ml, arrived, total;
 };
 
 Places make_layout(const br_kv_config &c) {
@@ -44,7 +44,9 @@ Places make_layout(const br_kv_config &c) {
   Places l;
   l.lens = take(rows);
   l.table = take(rows * c.max_blocks);
+  l.tail = take(rows);
   l.used = take((uint64_t)c.n_workers * ((c.n_blocks + 31) / 32));
+  l.runs = take(2 * rows);
   // two pieces of a query tile's rows for each block of the attention's largest launch
   const uint64_t pieces = 2ull * BR_KV_SPLIT_WGS * 128;
   l.part = take(pieces * c.head_dim);
@@ -138,6 +140,7 @@ int32_t br_kv_init(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx *
   t.n_blocks = cfg->n_blocks, t.max_blocks = cfg->max_blocks, t.words = (cfg->n_blocks + 31) / 32;
   t.lens = (int *)(base + at.lens);
   t.table = (int *)(base + at.table);
+  t.tail = (int *)(base + at.tail);
   t.used = (unsigned *)(base + at.used);
   int32_t rc = enqueue(ctx, [&] { br_kv_launch_clear(t, (int *)(base + at.arrived), ctx->st); });
   if (rc == BR_OK && init) rc = enqueue(ctx, [&] { br_kv_launch_load(t, init->lens, init->table, ctx->st); });
@@ -156,7 +159,9 @@ int32_t br_kv_step(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out
   s.keep = in->keep, s.add = in->add;
   s.slot = out->slot, s.pos = out->pos, s.start = out->start, s.count = out->count, s.status = out->status;
   s.stats = (long long *)out->stats;
+  s.runs = (int2 *)((char *)ctx->cfg.workspace + ctx->at.runs);
   s.cap = out->token_cap;
+  s.wide = ((((uintptr_t)s.slot | (uintptr_t)s.pos) & 15u) | (s.cap & 3)) == 0;
   return enqueue(ctx, [&] { br_kv_launch_step(ctx->t, s, ctx->st); });
 }
 

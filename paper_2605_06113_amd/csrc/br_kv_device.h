@@ -8,6 +8,7 @@
 #include "br_kv.h"
 
 #define BR_KV_SPLIT_WGS 768  // most blocks of an attention launch that split rows' tokens among them
+#define BR_KV_LIST 4096      // places of a token list that are written with the tables; longer lists have a launch of their own
 #define BR_KV_TILE 64        // cached tokens of an attention tile
 
 // The tables of all workers, inside the context's workspace.
@@ -15,6 +16,7 @@ struct BrKvTables {
   int W, B, shift, n_blocks, max_blocks, words;  // words: 32-bit words of a worker's used bits
   int *lens;                                     // [W][B]
   int *table;                                    // [W][B][max_blocks]
+  int *tail;                                     // [W][B] each row's last block
   unsigned *used;                                // [W][words]
 };
 
@@ -22,7 +24,8 @@ struct BrKvStep {
   const int *keep, *add;
   int *slot, *pos, *start, *count, *status;
   long long *stats;
-  int cap;
+  int2 *runs;     // [W][B] workspace: each row's first place in the token list and first position there
+  int cap, wide;  // wide: four places of the lists can be written at once
 };
 
 // One layer's cache and what indexes it.

@@ -7,7 +7,7 @@ __global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t, int *arrived)
   const long long step = (long long)gridDim.x * 256;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
     t.table[i] = -1;
-    if (i < rows) t.lens[i] = 0;
+    if (i < rows) t.lens[i] = 0, t.tail[i] = -1;
   }
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < words; i += step) t.used[i] = 0;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < BR_KV_SPLIT_WGS; i += step) arrived[i] = 0;
@@ -25,28 +25,51 @@ __global__ __launch_bounds__(256) void br_kv_k_load(BrKvTables t, const int *len
     const int id = table[i];
     if (id < 0 || id >= t.n_blocks) continue;
     t.table[i] = id;
+    if (j == (len - 1) >> t.shift) t.tail[row] = id;
     atomicOr(&t.used[row / t.B * t.words + (id >> 5)], 1u << (id & 31));
   }
 }
 
-// Inclusive sum over the block's threads; *total: all of them.
-template <int NT>
-__device__ __forceinline__ int br_kv_scan(int x, int *part, int *total) {
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(x, d, 64);
-    if (lane >= d) x += o;
-  }
-  __syncthreads();
-  if (lane == 63) part[wv] = x;
-  __syncthreads();
-  int all = 0;
-  for (int k = 0; k < NT / 64; ++k) {
-    if (k < wv) x += part[k];
-    all += part[k];
-  }
-  *total = all;
+// Inclusive sum over the wave, in the vector registers: within rows of 16 lanes, then the rows' last ones handed on
+__device__ __forceinline__ int br_kv_wave_scan(int x) {
+#define BR_KV_STEP(CTRL, ROWS) x += __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false)
+  BR_KV_STEP(0x111, 0xf);  // from 1 lane below
+  BR_KV_STEP(0x112, 0xf);
+  BR_KV_STEP(0x114, 0xf);
+  BR_KV_STEP(0x118, 0xf);
+  BR_KV_STEP(0x142, 0xa);  // rows 1 and 3: the last of the row below
+  BR_KV_STEP(0x143, 0xc);  // rows 2 and 3: the last of row 1
+#undef BR_KV_STEP
   return x;
+}
+
+// Inclusive sums of K values each over the block's threads; total: all of them.  One barrier (part: 2 x K x NT / 64 words, used in turn).
+template <int NT, int K>
+__device__ __forceinline__ void br_kv_scan(int (&x)[K], int (&total)[K], int *part, int &turn) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+#pragma unroll
+  for (int k = 0; k < K; ++k) x[k] = br_kv_wave_scan(x[k]);
+  if constexpr (NT == 64) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) total[k] = __builtin_amdgcn_readlane(x[k], 63);
+  } else {
+    int *at = part + (turn & 1) * 8 * (NT / 64);
+    ++turn;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (lane == 63) at[k * (NT / 64) + wv] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      total[k] = 0;
+#pragma unroll
+      for (int v = 0; v < NT / 64; ++v) {
+        const int y = at[k * (NT / 64) + v];
+        if (v < wv) x[k] += y;
+        total[k] += y;
+      }
+    }
+  }
 }
 
 // Largest r in [0, n) with before[r] <= k (before ascending, before[0] = 0).
@@ -60,146 +83,209 @@ __device__ __forceinline__ int br_kv_find(const int *before, int n, int k) {
   return lo;
 }
 
-// One block of NT threads per worker; a thread has the RPT rows from tid * RPT on.  The used bits are in LDS.
-template <int NT, int RPT>
+// Places j0 .. j0 + 3 of a worker's token list: rows' tokens from before[r] on, at positions from kp[r] on.  tail: the block of the last
+// position before those (a decode step then reads no table: a line for each row would be more than all the rest, 16384 workers
+// of 144 rows 99 us), or null.
+__device__ __forceinline__ void br_kv_list4(const BrKvTables &t, const BrKvStep &s, long long list, const int *table, const int *before, const int *kp, const int *tail, int rows,
+                                            int total, int j0, int cap) {
+  int slot[4] = {-1, -1, -1, -1}, pos[4] = {-1, -1, -1, -1};
+  if (j0 < total) {
+    int r = br_kv_find(before, rows, j0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (j0 + k >= total) break;
+      while (r + 1 < rows && before[r + 1] <= j0 + k) ++r;
+      pos[k] = kp[r] + j0 + k - before[r];
+      const int id = tail && pos[k] >> t.shift == (kp[r] - 1) >> t.shift ? tail[r] : table[(long long)r * t.max_blocks + (pos[k] >> t.shift)];
+      slot[k] = id < 0 ? -1 : (id << t.shift) + (pos[k] & ((1 << t.shift) - 1));
+    }
+  }
+  if (s.wide) {
+    if (s.slot) *(int4 *)(s.slot + list + j0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+    if (s.pos) *(int4 *)(s.pos + list + j0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (j0 + k >= cap) break;
+      if (s.slot) s.slot[list + j0 + k] = slot[k];
+      if (s.pos) s.pos[list + j0 + k] = pos[k];
+    }
+  }
+}
+
+// One block of NT threads per worker; a thread has the RPT rows from tid * RPT on.  The used bits are in LDS.  LIST: writes the
+// token list as well; else leaves each row's first place in it and first position to br_kv_k_list.
+// A chain of dependent steps (rows, blocks given back, sums, free ids, lists), so its time is their latencies: barriers are few (the
+// sums of a step in which nothing is refused take one), scans stay in registers.
+template <int NT, int RPT, bool LIST>
 __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
+  constexpr int ROWS = NT * RPT, IDS = NT * 8;
   extern __shared__ unsigned used[];
-  __shared__ int part[NT / 64], give_n, need_before[NT * RPT], tok_before[NT * RPT], row_kp[NT * RPT], give[NT * RPT], ids[NT * 32];
+  __shared__ int part[16 * (NT / 64)], give_n, need_before[ROWS], tok_before[ROWS], row_kp[ROWS], give[ROWS], row_tail[ROWS], ids[IDS];
   const int w = blockIdx.x, tid = threadIdx.x, lane = tid & 63, B = t.B, b1 = (1 << t.shift) - 1;
+  int turn = 0;
   int *lens = t.lens + (long long)w * B;
   int *table = t.table + (long long)w * B * t.max_blocks;
+  int *tails = t.tail + (long long)w * B;
   unsigned *gused = t.used + (long long)w * t.words;
   if (tid == 0) give_n = 0;
+  int kp[RPT], have[RPT], why[RPT], held[RPT], want[RPT], tail[RPT];
+#pragma unroll
+  for (int i = 0; i < RPT; ++i) {
+    const int r = tid * RPT + i;
+    int keep = 0;
+    kp[i] = want[i] = 0, tail[i] = -1;
+    if (r < B) kp[i] = lens[r], tail[i] = tails[r], keep = s.keep[(long long)w * B + r], want[i] = s.add[(long long)w * B + r];
+    held[i] = (kp[i] + b1) >> t.shift;
+    kp[i] = keep < 0 ? kp[i] : min(keep, kp[i]);
+    want[i] = max(want[i], 0);
+  }
   for (int i = tid; i < t.words; i += NT) used[i] = gused[i];
   __syncthreads();
-
-  int kp[RPT], have[RPT], why[RPT], held[RPT];
-  long long want[RPT];
+  int long_ones = 0;
 #pragma unroll
   for (int i = 0; i < RPT; ++i) {
     const int r = tid * RPT + i;
-    kp[i] = have[i] = why[i] = held[i] = 0, want[i] = 0;
-    if (r < B) {
-      const int len = lens[r], keep = s.keep[(long long)w * B + r], add = s.add[(long long)w * B + r];
-      kp[i] = keep < 0 ? len : min(keep, len);
-      want[i] = max(add, 0);
-      have[i] = (kp[i] + b1) >> t.shift;
-      held[i] = (len + b1) >> t.shift;
-      if (held[i] > have[i]) give[atomicAdd(&give_n, 1)] = r;
-      if (want[i] > 0 && (kp[i] + want[i] + b1) >> t.shift > t.max_blocks) why[i] = BR_KV_TOO_LONG, want[i] = 0;
-      need_before[r] = have[i], tok_before[r] = held[i];
+    why[i] = 0;
+    have[i] = (kp[i] + b1) >> t.shift;
+    if (held[i] != have[i]) tail[i] = have[i] > 0 ? table[(long long)r * t.max_blocks + have[i] - 1] : -1;
+    // blocks given back: one here, of a longer run by a wave below
+    if (held[i] == have[i] + 1) {
+      int *at = table + (long long)r * t.max_blocks + have[i];
+      const int id = *at;
+      if (id >= 0) atomicAnd(&used[id >> 5], ~(1u << (id & 31)));
+      *at = -1;
+    } else if (held[i] > have[i]) {
+      give[atomicAdd(&give_n, 1)] = r, need_before[r] = have[i], tok_before[r] = held[i];
+    }
+    if ((long long)kp[i] + want[i] > (long long)t.max_blocks << t.shift) {
+      if (want[i] > 0) why[i] = BR_KV_TOO_LONG;
+      want[i] = 0;
     }
   }
   __syncthreads();
-  // blocks given back: a wave per row, in any order
-  for (int k = tid >> 6; k < give_n; k += NT / 64) {
-    const int r = give[k], from = need_before[r], to = tok_before[r];
-    for (int j = from + lane; j < to; j += 64) {
-      const int id = table[(long long)r * t.max_blocks + j];
-      if (id >= 0) atomicAnd(&used[id >> 5], ~(1u << (id & 31)));
-      table[(long long)r * t.max_blocks + j] = -1;
+  if (give_n > 0) {
+    for (int k = tid >> 6; k < give_n; k += NT / 64) {
+      const int r = give[k], from = need_before[r], to = tok_before[r];
+      for (int j = from + lane; j < to; j += 64) {
+        int *at = table + (long long)r * t.max_blocks + j;
+        const int id = *at;
+        if (id >= 0) atomicAnd(&used[id >> 5], ~(1u << (id & 31)));
+        *at = -1;
+      }
     }
+    __syncthreads();
   }
-  // tokens that find room in the list
-  int x = 0, total = 0;
-  long long sum = 0;
+
+  // sums, as if nothing were refused: tokens, blocks, and what is counted of them
+  int need[RPT], sum[6], all[6], nfree = 0;
+  auto count = [&]() {
 #pragma unroll
-  for (int i = 0; i < RPT; ++i) sum += want[i];
-  x = br_kv_scan<NT>((int)sum, part, &total);
-  int run = x - (int)sum;
+    for (int k = 0; k < 6; ++k) sum[k] = 0;
 #pragma unroll
-  for (int i = 0; i < RPT; ++i) {
-    run += (int)want[i];
-    if (want[i] > 0 && run > s.cap) why[i] = BR_KV_NO_ROOM, want[i] = 0;
-  }
-  // (the scans' barriers stand between the blocks given back and here)
-  int nfree = 0;
+    for (int i = 0; i < RPT; ++i) {
+      need[i] = ((kp[i] + want[i] + b1) >> t.shift) - have[i];
+      sum[0] += want[i], sum[1] += need[i], sum[2] += kp[i] + want[i];
+      sum[3] += kp[i] + want[i] > 0, sum[5] += (why[i] > 0) + (why[i] == BR_KV_NO_BLOCKS ? 1 << 16 : 0);
+    }
+    sum[4] = nfree;
+  };
   for (int i = tid; i < t.words; i += NT) nfree += 32 - __popc(used[i]);
-  br_kv_scan<NT>(nfree, part, &nfree);
-  nfree -= t.words * 32 - t.n_blocks;
-  int need[RPT], needs = 0, need_all;
+  count();
+  br_kv_scan<NT, 6>(sum, all, part, turn);
+  const int free_blocks = all[4] - (t.words * 32 - t.n_blocks);
+  if (all[0] > s.cap || all[1] > free_blocks) {
+    int run[1] = {sum[0]}, ignore[1];
 #pragma unroll
-  for (int i = 0; i < RPT; ++i) need[i] = (int)((kp[i] + want[i] + b1) >> t.shift) - have[i], needs += need[i];
-  x = br_kv_scan<NT>(needs, part, &need_all);
-  run = x - needs;
+    for (int i = 0; i < RPT; ++i) run[0] -= want[i];
 #pragma unroll
-  for (int i = 0; i < RPT; ++i) {
-    run += need[i];
-    if (need[i] > 0 && run > nfree) why[i] = BR_KV_NO_BLOCKS, want[i] = 0, need[i] = 0;
+    for (int i = 0; i < RPT; ++i) {
+      run[0] += want[i];
+      if (want[i] > 0 && run[0] > s.cap) why[i] = BR_KV_NO_ROOM, want[i] = 0;
+    }
+    count();
+    run[0] = sum[1];
+    br_kv_scan<NT, 1>(run, ignore, part, turn);
+    run[0] -= sum[1];
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+      run[0] += need[i];
+      if (need[i] > 0 && run[0] > free_blocks) why[i] = BR_KV_NO_BLOCKS, want[i] = 0;
+    }
+    count();
+    br_kv_scan<NT, 6>(sum, all, part, turn);
   }
-  int toks = 0;
-  needs = 0;
+  const int total = all[0], need_all = all[1];
+  int x = sum[1], y = sum[0];
 #pragma unroll
-  for (int i = 0; i < RPT; ++i) toks += (int)want[i], needs += need[i];
-  x = br_kv_scan<NT>(needs, part, &need_all) - needs;
-  int y = br_kv_scan<NT>(toks, part, &total) - toks;
-  int sums[5] = {0, 0, 0, 0, 0};
+  for (int i = 0; i < RPT; ++i) x -= need[i], y -= want[i];
 #pragma unroll
   for (int i = 0; i < RPT; ++i) {
     const int r = tid * RPT + i;
-    need_before[r] = x, tok_before[r] = y, row_kp[r] = kp[i];
-    const int len = kp[i] + (int)want[i];
+    need_before[r] = x, tok_before[r] = y, row_kp[r] = kp[i], row_tail[r] = tail[i];
     if (r < B) {
       const long long at = (long long)w * B + r;
-      lens[r] = len;
+      lens[r] = kp[i] + want[i];
+      if (held[i] != have[i] && need[i] == 0) tails[r] = tail[i];
       if (s.start) s.start[at] = w * s.cap + y;
-      if (s.count) s.count[at] = (int)want[i];
+      if (s.count) s.count[at] = want[i];
       if (s.status) s.status[at] = why[i];
-      sums[0] += len, sums[1] += len > 0, sums[2] += why[i] > 0, sums[3] += why[i] == BR_KV_NO_BLOCKS;
+      if (!LIST) s.runs[at] = make_int2(y, kp[i]);
     }
-    x += need[i], y += (int)want[i];
+    x += need[i], y += want[i];
   }
-  // blocks taken, lowest ids first
+  if (tid == 0 && s.stats) {
+    long long *o = s.stats + (long long)w * BR_KV_NSTATS;
+    const int n_used = t.n_blocks - free_blocks + need_all;
+    o[BR_KV_ST_TOKENS] = all[2], o[BR_KV_ST_USED] = n_used, o[BR_KV_ST_FREE] = t.n_blocks - n_used, o[BR_KV_ST_ROWS] = all[3];
+    o[BR_KV_ST_ADDED] = total, o[BR_KV_ST_REFUSED] = all[5] & 0xffff, o[BR_KV_ST_NO_BLOCKS] = all[5] >> 16, o[BR_KV_ST_TAKEN] = need_all;
+  }
+  // blocks taken, lowest ids first: NT words of used bits at a time, IDS ids at a time
   int taken = 0;
   for (int i0 = 0; taken < need_all && i0 < t.words; i0 += NT) {
     const int i = i0 + tid;
     unsigned bits = i < t.words ? ~used[i] : 0u;
     if (i == t.words - 1 && (t.n_blocks & 31)) bits &= (1u << (t.n_blocks & 31)) - 1;
-    int here;
-    int k = br_kv_scan<NT>(__popc(bits), part, &here) - __popc(bits);
+    int k[1] = {(int)__popc(bits)}, here[1];
+    const int mine = k[0];
+    br_kv_scan<NT, 1>(k, here, part, turn);
+    int at = k[0] - mine;
+    const int n = min(here[0], need_all - taken);
     unsigned got = 0;
-    for (; bits && taken + k < need_all; ++k, bits &= bits - 1) {
-      ids[k] = 32 * i + __ffs(bits) - 1;
-      got |= bits & -bits;
+    for (int from = 0; from < n; from += IDS) {
+      for (; bits && at < min(n, from + IDS); ++at, bits &= bits - 1) {
+        ids[at - from] = 32 * i + __ffs(bits) - 1;
+        got |= bits & -bits;
+      }
+      __syncthreads();
+      for (int j = tid; j < min(n - from, IDS); j += NT) {
+        const int q = taken + from + j, r = br_kv_find(need_before, ROWS, q);
+        table[(long long)r * t.max_blocks + ((row_kp[r] + b1) >> t.shift) + q - need_before[r]] = ids[j];
+        if (q + 1 == (r + 1 < ROWS ? need_before[r + 1] : need_all)) tails[r] = ids[j];
+      }
+      __syncthreads();
     }
     if (got) used[i] |= got;
-    __syncthreads();
-    here = min(here, need_all - taken);
-    for (int j = tid; j < here; j += NT) {
-      const int r = br_kv_find(need_before, NT * RPT, taken + j);
-      const int first = (row_kp[r] + b1) >> t.shift;
-      table[(long long)r * t.max_blocks + first + taken + j - need_before[r]] = ids[j];
-    }
-    taken += here;
+    taken += n;
   }
   __syncthreads();
   for (int i = tid; i < t.words; i += NT) gused[i] = used[i];
-  if (s.slot || s.pos) {
-    for (int j = tid; j < s.cap; j += NT) {
-      int pos = -1, slot = -1;
-      if (j < total) {
-        const int r = br_kv_find(tok_before, NT * RPT, j);
-        pos = row_kp[r] + j - tok_before[r];
-        const int id = table[(long long)r * t.max_blocks + (pos >> t.shift)];
-        slot = id < 0 ? -1 : (id << t.shift) + (pos & b1);
-      }
-      if (s.slot) s.slot[(long long)w * s.cap + j] = slot;
-      if (s.pos) s.pos[(long long)w * s.cap + j] = pos;
-    }
+  if (LIST && (s.slot || s.pos))
+    for (int j = 4 * tid; j < s.cap; j += 4 * NT) br_kv_list4(t, s, (long long)w * s.cap, table, tok_before, row_kp, row_tail, ROWS, total, j, s.cap);
+}
+
+// The token lists of a step, BR_KV_LIST places of a worker's for each block (behind br_kv_k_step).
+__global__ __launch_bounds__(256) void br_kv_k_list(BrKvTables t, BrKvStep s) {
+  __shared__ int before[BR_KV_MAX_ROWS], kp[BR_KV_MAX_ROWS], total;
+  const int parts = (s.cap + BR_KV_LIST - 1) / BR_KV_LIST, w = blockIdx.x / parts, j0 = (blockIdx.x - w * parts) * BR_KV_LIST, B = t.B;
+  for (int r = threadIdx.x; r < B; r += 256) {
+    const int2 x = s.runs[(long long)w * B + r];
+    before[r] = x.x, kp[r] = x.y;
+    if (r == B - 1) total = x.x + t.lens[(long long)w * B + r] - x.y;
   }
-  if (s.stats) {
-    int n_used = 0;
-    for (int i = tid; i < t.words; i += NT) n_used += __popc(used[i]);
-    int all[5];
-    sums[4] = n_used;
-#pragma unroll
-    for (int k = 0; k < 5; ++k) br_kv_scan<NT>(sums[k], part, &all[k]);
-    if (tid == 0) {
-      long long *o = s.stats + (long long)w * BR_KV_NSTATS;
-      o[BR_KV_ST_TOKENS] = all[0], o[BR_KV_ST_USED] = all[4], o[BR_KV_ST_FREE] = t.n_blocks - all[4], o[BR_KV_ST_ROWS] = all[1];
-      o[BR_KV_ST_ADDED] = total, o[BR_KV_ST_REFUSED] = all[2], o[BR_KV_ST_NO_BLOCKS] = all[3], o[BR_KV_ST_TAKEN] = need_all;
-    }
-  }
+  __syncthreads();
+  const int *table = t.table + (long long)w * B * t.max_blocks;
+  for (int j = j0 + 4 * threadIdx.x; j < min(s.cap, j0 + BR_KV_LIST); j += 1024) br_kv_list4(t, s, (long long)w * s.cap, table, before, kp, nullptr, B, total, j, s.cap);
 }
 
 static int grid_for(long long n) { return (int)(n < 1 ? 1 : n > 4096ll * 256 ? 4096 : (n + 255) / 256); }
@@ -212,8 +298,16 @@ void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, h
   br_kv_k_load<<<grid_for((long long)t.W * t.B * t.max_blocks), 256, 0, st>>>(t, lens, table);
 }
 
-void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st) {
+template <bool LIST>
+static void launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st) {
   const size_t lds = (size_t)t.words * 4;
-  if (t.B <= 256) br_kv_k_step<256, 1><<<t.W, 256, lds, st>>>(t, s);
-  else br_kv_k_step<256, 4><<<t.W, 256, lds, st>>>(t, s);
+  if (t.B <= 256) br_kv_k_step<256, 1, LIST><<<t.W, 256, lds, st>>>(t, s);
+  else br_kv_k_step<256, 4, LIST><<<t.W, 256, lds, st>>>(t, s);
+}
+
+void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st) {
+  const bool list = s.slot || s.pos;
+  if (!list || s.cap <= BR_KV_LIST) return launch_step<true>(t, s, st);
+  launch_step<false>(t, s, st);
+  br_kv_k_list<<<t.W * ((s.cap + BR_KV_LIST - 1) / BR_KV_LIST), 256, 0, st>>>(t, s);
 }
