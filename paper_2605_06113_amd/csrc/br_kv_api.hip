@@ -207,10 +207,11 @@ int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_atten
   p.q_wide = ((uintptr_t)a->q & 15u) == 0 && ((a->q_token | a->q_head) & 7) == 0;
   p.out_wide = ((uintptr_t)a->out & 7u) == 0 && ((a->out_token | a->out_head) & 3) == 0;
   p.scale2 = a->scale * 1.4426950408889634f;
+  // Rows of many queries share their block's token tiles, those of few have waves of their own: two launches where a call may have
+  // both (two chunks of 512 tokens beside 46 single ones: 375 us in one launch).
   const int64_t rows = (int64_t)a->max_count * group;
-  const int tile = rows <= 16 || (rows <= 64 && c.head_dim > 128) ? BR_KV_TILE_16 : rows <= 64 ? BR_KV_TILE_32 : BR_KV_TILE_128;
   const bool fp8 = c.fmt == BR_KV_E4M3;
-  return enqueue(ctx, [&] {
+  auto launch = [&](int tile) {
     switch (c.head_dim) {
       case 64: br_kv_launch_attend_64(p, tile, fp8, ctx->cus, ctx->st); break;
       case 96: br_kv_launch_attend_96(p, tile, fp8, ctx->cus, ctx->st); break;
@@ -218,7 +219,17 @@ int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_atten
       case 192: br_kv_launch_attend_192(p, tile, fp8, ctx->cus, ctx->st); break;
       default: br_kv_launch_attend_256(p, tile, fp8, ctx->cus, ctx->st); break;
     }
-  });
+  };
+  const bool both = rows > 64;
+  const int few = 16 / group;  // query tokens up to which a row of a mixed call goes with the few
+  p.least = 1, p.most = both ? few : INT32_MAX;
+  if (!both || few > 0) {
+    const int64_t most = both ? 16 : rows;
+    const int32_t rc = enqueue(ctx, [&] { launch(most <= 16 || c.head_dim > 128 ? BR_KV_TILE_16 : BR_KV_TILE_32); });
+    if (rc != BR_OK || !both) return rc;
+  }
+  p.least = few + 1, p.most = INT32_MAX;
+  return enqueue(ctx, [&] { launch(BR_KV_TILE_128); });
 }
 
 void br_kv_free(br_kv_ctx *ctx) { delete ctx; }

@@ -28,9 +28,11 @@ struct BrKvRow {
   int n, len, start;  // query tokens, cached tokens, first token
 };
 
+// (a row that is not this launch's has no queries here)
 __device__ __forceinline__ BrKvRow br_kv_row(const BrKvAttend &p, int r) {
   BrKvRow w;
   w.n = p.count ? min(max(p.count[r], 0), p.n_tokens) : 1;
+  if (w.n < p.least || w.n > p.most) w.n = 0;
   w.start = p.start ? p.start[r] : r;
   w.len = min(max(p.lens[r], 0), p.max_blocks << p.shift);
   return w;
@@ -238,8 +240,8 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     top = br_kv_max4(top);
     // the power of two at or below `top`; not below 2^-100, where its inverse would leave the range
     const int ex = max((int)(__float_as_uint(top) >> 23), 27);
-    const float inv = __uint_as_float((unsigned)(254 - min(ex, 253)) << 23);
-    qs[x] = top > 3.0e38f && top * 0.0f != 0.0f ? __builtin_nanf("") : __uint_as_float((unsigned)min(ex, 253) << 23) * p.scale2;
+    const float inv = __builtin_copysignf(__uint_as_float((unsigned)(254 - min(ex, 253)) << 23), p.scale2);
+    qs[x] = top > 3.0e38f && top * 0.0f != 0.0f ? __builtin_nanf("") : __uint_as_float((unsigned)min(ex, 253) << 23) * fabsf(p.scale2);
 #pragma unroll
     for (int c = 0; c < 8 * NK; ++c) qf[x][c / 8][c % 8] = (_Float16)(f[c] * inv);
   }
@@ -249,9 +251,9 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     {
       const unsigned char *at = p.v + ((((cache0 + (there(vid) ? vid : 0)) * p.kv_heads + h) * D + n) << p.shift) + (token & mask);
 #pragma unroll
-      for (int d = 0; d < ND; ++d) vc[d] = br_kv_load16<ONCE>(at + ((16 * d) << p.shift));
+      for (int d = 0; d < ND; ++d) vc[d] = br_kv_load16<false>(at + ((16 * d) << p.shift));
     }
-    const float ks = there(vid) ? ks1 : 0.0f, vs = there(vid) ? vs1 : 0.0f;
+    const float ks = there(vid) ? br_kv_sound(ks1) : 0.0f, vs = there(vid) ? br_kv_sound(vs1) : 0.0f;
     const int have = there(vid) ? min(max(w.len - token, 0), 16) : 0;  // of the lane's tokens, those that exist
 
     br_f4 s[NQ][4];
@@ -278,7 +280,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 
 
     // (a block that no query of the tile sees has no say in c)
-    float top = have > 0 && token <= last_pos && (p.window == 0 || token + 15 > first_pos - p.window) ? fabsf(vs) : 0.0f;
+    float top = have > 0 && token <= last_pos && (p.window == 0 || token + 15 > first_pos - p.window) ? vs : 0.0f;
     top = br_kv_max4(top);
     float cf = 1.0f;
     if (top > 8.0f * cmax) {
@@ -293,19 +295,20 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     br_h8 pf[NQ][2];
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-      const float f = qs[x] * ks;
+      float f = qs[x] * ks;  // (not below zero: the sign of the caller's scale is in the queries)
       float z[16], mx = BR_KV_NEG, wx = wgt;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) z[j] = s[x][j >> 2][j & 3] * f;
+      for (int j = 0; j < 16; ++j) z[j] = s[x][j >> 2][j & 3];
       if (!inside) {  // of the lane's tokens, those from `lo` on, `seen` of them
         const int lo = p.window > 0 ? max(pos[x] - p.window + 1 - token, 0) : 0, seen = max(min(have, pos[x] + 1 - token) - lo, 0);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) z[j] = (unsigned)(j - lo) < (unsigned)seen ? z[j] : BR_KV_NEG;
+        for (int j = 0; j < 16; ++j) z[j] = (unsigned)(j - lo) < (unsigned)seen ? z[j] * f : BR_KV_NEG;
+        f = 1.0f;
         wx = seen > 0 ? wgt : 0.0f;  // (a block that is not seen has no weight, whatever its scale)
       }
 #pragma unroll
       for (int j = 0; j < 16; ++j) mx = fmaxf(mx, z[j]);
-      mx = br_kv_max4(mx);
+      mx = br_kv_max4(mx * f);
       const bool up = mx > m[x] + 4.0f;
       if (__any(up || cf != 1.0f)) {
         const float to = up ? mx : m[x];
@@ -320,7 +323,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
       const float ref = m[x] == BR_KV_NEG ? 0.0f : m[x];
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
-        const float e = __builtin_amdgcn_exp2f(z[j] - ref);
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], f, -ref));
         l[x] += e;
         pf[x][j >> 3][j & 7] = (_Float16)(e * wx);
       }
@@ -766,10 +769,11 @@ void br_kv_attend_rows(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
 
 template <int D>
 void br_kv_attend_dim(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st) {
+  // (a tile's launch skips the rows of the other: least, most)
   if constexpr (D <= 128) {
     if (tile == BR_KV_TILE_32) return br_kv_attend_few<D, 2, D <= 64 ? 8 : 4, D <= 64 ? 2 : 1>(p, fp8, cus, st);
   }
-  if (tile == BR_KV_TILE_128) br_kv_attend_rows<D, 2, D <= 96 ? 2 : 1>(p, fp8, cus, st);
+  if (tile == BR_KV_TILE_128) br_kv_attend_rows<D, 2, D <= 128 ? 2 : 1>(p, fp8, cus, st);
   else br_kv_attend_few<D, 1, D <= 64 ? 12 : D <= 128 ? 8 : 4, D <= 64 ? 3 : D <= 128 ? 2 : 1>(p, fp8, cus, st);
 }
 

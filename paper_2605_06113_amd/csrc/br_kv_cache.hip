@@ -314,7 +314,7 @@ template <bool FP8, int DT, int NT>
 __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, bool in, int tid) {
   const int D = c.dim, b = 1 << c.shift, chunks = D >> 3, pairs = D >> 1;
   const unsigned char *kc = c.k + ((u.block * D) << c.shift), *vc = c.v + ((u.block * D) << c.shift);
-  const float ks = c.ks[u.block], vs = c.vs[u.block];
+  const float ks = br_kv_sound(c.ks[u.block]), vs = br_kv_sound(c.vs[u.block]);
   const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
   const long long k0 = u.t * a.k_token + (long long)u.h * a.k_head + kd, v0 = u.t * a.v_token + (long long)u.h * a.v_head;
   const int vg0 = u.off >> 4, vitems = (((u.off + u.n - 1) >> 4) - vg0 + 1) * pairs;

@@ -53,6 +53,7 @@ struct BrKvAttend {
   float *ml;    // their maxima and sums of weights
   int *arrived; // per block: blocks that have delivered a piece of the query tile that is split and begins in it; 0 between launches
   long long q_token, q_head, out_token, out_head;
+  int least, most;  // query tokens of the rows that this launch takes
   int n_rows, rows, n_tokens, window, group, kv_heads, shift, n_blocks, max_blocks;
   int bf16, q_wide, out_wide;  // wide: rows of q (out) can be read (written) 16 (8) bytes at a time
   unsigned group_mul, group_shift;  // x / group = (high word of group_mul x + x) >> group_shift for 0 <= x < 2^31
@@ -112,6 +113,9 @@ __device__ __forceinline__ float br_kv_max4(float x) {
   auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
+
+// A block's scale; one that is none (below zero or not finite) makes NaN of what is read with it.
+__device__ __forceinline__ float br_kv_sound(float s) { return s >= 0.0f && s < __builtin_inff() ? s : __builtin_nanf(""); }
 
 // Two values in 16 bits each
 template <class T>
