@@ -133,8 +133,127 @@ __device__ __forceinline__ float br_kv_sum4(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// The queries of 16 NQ rows from row0 on in f16, one row's to four lanes: channels 64 i + 16 g .. + 15 of its row for each lane, then
+// 8 g .. + 7 of the last 32; what their scores are multiplied by (in powers of two; never below zero), and their positions.
+template <int D, int NQ>
+struct BrKvQueries {
+  static constexpr int NI = D / 64, NK = D / 32;
+  br_h8 qf[NQ][NK];
+  float qs[NQ];
+  int pos[NQ];
+
+  template <class Fn>
+  __device__ __forceinline__ void load(const BrKvAttend &p, const BrKvRow &w, int h, int row0, Fn &&meanwhile) {
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      const int ri = row0 + 16 * x + n, i = br_kv_token(p, ri), t = w.start + i;
+      const bool in = i < w.n && t >= 0 && t < p.n_tokens;
+      pos[x] = in ? w.len - w.n + i : -1;
+      const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(h * p.group + ri - i * p.group) * p.q_head : 0);
+      uint4 e[NK];
+      auto channel = [&](int c) { return c < 2 * NI ? (c / 2) * 64 + g * 16 + (c & 1) * 8 : NI * 64 + g * 8; };
+      if (p.q_wide) {
+#pragma unroll
+        for (int c = 0; c < NK; ++c) e[c] = *(const uint4 *)(at + channel(c));
+      } else {
+#pragma unroll
+        for (int c = 0; c < NK; ++c) {
+          const unsigned short *y = at + channel(c);
+          e[c] = make_uint4(y[0] | (unsigned)y[1] << 16, y[2] | (unsigned)y[3] << 16, y[4] | (unsigned)y[5] << 16, y[6] | (unsigned)y[7] << 16);
+        }
+      }
+      if (x == 0) meanwhile();
+      float f[NK * 8], top = 0.0f;
+      auto half = [&](int c) {
+        const uint4 y = e[c / 8];
+        const unsigned z = c % 8 < 2 ? y.x : c % 8 < 4 ? y.y : c % 8 < 6 ? y.z : y.w;
+        return (unsigned short)(c & 1 ? z >> 16 : z);
+      };
+      if (p.bf16) {
+#pragma unroll
+        for (int c = 0; c < 8 * NK; ++c) f[c] = br_kv_bf16(half(c));
+      } else {
+#pragma unroll
+        for (int c = 0; c < 8 * NK; ++c) f[c] = br_kv_f16(half(c));
+      }
+      // (a row of the tile that is none takes the first one's values: its results go nowhere)
+#pragma unroll
+      for (int c = 0; c < 8 * NK; ++c) top = fmaxf(top, fabsf(f[c]));
+      top = br_kv_max4(top);
+      // the power of two at or below `top`; not below 2^-100, where its inverse would leave the range
+      const int ex = max((int)(__float_as_uint(top) >> 23), 27);
+      const float inv = __builtin_copysignf(__uint_as_float((unsigned)(254 - min(ex, 253)) << 23), p.scale2);
+      qs[x] = top > 3.0e38f && top * 0.0f != 0.0f ? __builtin_nanf("") : __uint_as_float((unsigned)min(ex, 253) << 23) * fabsf(p.scale2);
+#pragma unroll
+      for (int c = 0; c < 8 * NK; ++c) qf[x][c / 8][c % 8] = (_Float16)(f[c] * inv);
+    }
+  }
+};
+
+// Weights of a tile from its scores: s [16 tokens 4 y + i of the lane's group][query n of group x]; ks, vs the scales of the lane's tokens,
+// `have` of them; exist: all of the tile's blocks do.  Moves m and c, and the sums with them.
+template <int D, int NQ>
+__device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQueries<D, NQ> &q, const br_f4 (&s)[NQ][4], float ks, float vs, int have, int t, int first_pos,
+                                              int last_pos, bool exist, BrKvSums<D, NQ> &sums, float &cmax, float &cinv, br_h8 (&pf)[NQ][2]) {
+  constexpr int ND = D / 16;
+  const int token = t * BR_KV_TILE + 16 * ((threadIdx.x & 63) >> 4);
+  auto &o = sums.o;
+  auto &m = sums.m;
+  auto &l = sums.l;
+  // (a block that no query of the tile sees has no say in c)
+  float top = have > 0 && token <= last_pos && (p.window == 0 || token + 15 > first_pos - p.window) ? vs : 0.0f;
+  top = br_kv_max4(top);
+  float cf = 1.0f;
+  if (top > 8.0f * cmax) {
+    const unsigned e = min(max(__float_as_uint(top) >> 23, 20u), 252u) + 1;
+    cinv = __uint_as_float((254u - e) << 23);
+    cf = cmax * cinv;
+    cmax = __uint_as_float(e << 23);
+  }
+  const float wgt = vs * (256.0f * cinv);
+  // inside: every query of the tile sees all of its tokens, and all exist
+  const bool inside = t * BR_KV_TILE + BR_KV_TILE - 1 <= first_pos && (p.window == 0 || t * BR_KV_TILE > last_pos - p.window) && exist;
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    float f = q.qs[x] * ks;  // (not below zero: the sign of the caller's scale is in the queries)
+    float z[16], mx = BR_KV_NEG, wx = wgt;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) z[j] = s[x][j >> 2][j & 3];
+    if (!inside) {  // of the lane's tokens, those from `lo` on, `seen` of them
+      const int lo = p.window > 0 ? max(q.pos[x] - p.window + 1 - token, 0) : 0, seen = max(min(have, q.pos[x] + 1 - token) - lo, 0);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) z[j] = (unsigned)(j - lo) < (unsigned)seen ? z[j] * f : BR_KV_NEG;
+      f = 1.0f;
+      wx = seen > 0 ? wgt : 0.0f;  // (a block that is not seen has no weight, whatever its scale)
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) mx = fmaxf(mx, z[j]);
+    mx = br_kv_max4(mx * f);
+    const bool up = mx > m[x] + 4.0f;
+    if (__any(up || cf != 1.0f)) {
+      const float to = up ? mx : m[x];
+      const float al = m[x] == BR_KV_NEG ? (l[x] != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m[x] - to), ao = al * cf;
+      m[x] = to;
+      l[x] *= al;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[x][d][j] *= ao;
+    }
+    const float ref = m[x] == BR_KV_NEG ? 0.0f : m[x];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], f, -ref));
+      l[x] += e;
+      pf[x][j >> 3][j & 7] = (_Float16)(e * wx);
+    }
+  }
+}
+
+// HALF: blocks of 128 tokens, whose lines of values belong to two tiles.
 // Token tiles t .. stop - 1 of row r and key head h for the query rows from row0 on, whose positions lie in first_pos .. last_pos.
-template <int D, int NQ, bool FP8, bool ONCE>
+template <int D, int NQ, bool FP8, bool HALF>
 __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int r, int h, int row0, int first_pos, int last_pos, int t, int stop,
                                             BrKvSums<D, NQ> &sums) {
   constexpr int NI = D / 64, REST = D % 64 / 32, NK = 2 * NI + REST, ND = D / 16;
@@ -174,7 +293,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) kc[s][i] = br_kv_load16<ONCE>(at + 4 * s * D + 64 * i + 16 * g);
+      for (int i = 0; i < NI; ++i) kc[s][i] = br_kv_load16<true>(at + 4 * s * D + 64 * i + 16 * g);
       if (REST) kx[s] = *(const uint2 *)(at + 4 * s * D + 64 * NI + 8 * g);
     }
   };
@@ -198,60 +317,17 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     load_k(t, kid, true);
     load_scales(vid);
   };
-  // queries: channels 64 i + 16 g .. + 15 of its row for each lane, then 8 g .. + 7 of the last 32
-  br_h8 qf[NQ][NK];
-  float qs[NQ];
-  int pos[NQ];
-#pragma unroll
-  for (int x = 0; x < NQ; ++x) {
-    const int ri = row0 + 16 * x + n, i = br_kv_token(p, ri), t = w.start + i;
-    const bool in = i < w.n && t >= 0 && t < p.n_tokens;
-    pos[x] = in ? w.len - w.n + i : -1;
-    const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(h * p.group + ri - i * p.group) * p.q_head : 0);
-    uint4 e[NK];
-    auto channel = [&](int c) { return c < 2 * NI ? (c / 2) * 64 + g * 16 + (c & 1) * 8 : NI * 64 + g * 8; };
-    if (p.q_wide) {
-#pragma unroll
-      for (int c = 0; c < NK; ++c) e[c] = *(const uint4 *)(at + channel(c));
-    } else {
-#pragma unroll
-      for (int c = 0; c < NK; ++c) {
-        const unsigned short *y = at + channel(c);
-        e[c] = make_uint4(y[0] | (unsigned)y[1] << 16, y[2] | (unsigned)y[3] << 16, y[4] | (unsigned)y[5] << 16, y[6] | (unsigned)y[7] << 16);
-      }
-    }
-    if (x == 0 && t_any) load_first();  // (while the queries are on their way)
-    float f[NK * 8], top = 0.0f;
-    auto half = [&](int c) {
-      const uint4 y = e[c / 8];
-      const unsigned z = c % 8 < 2 ? y.x : c % 8 < 4 ? y.y : c % 8 < 6 ? y.z : y.w;
-      return (unsigned short)(c & 1 ? z >> 16 : z);
-    };
-    if (p.bf16) {
-#pragma unroll
-      for (int c = 0; c < 8 * NK; ++c) f[c] = br_kv_bf16(half(c));
-    } else {
-#pragma unroll
-      for (int c = 0; c < 8 * NK; ++c) f[c] = br_kv_f16(half(c));
-    }
-    // (a row of the tile that is none takes the first one's values: its results go nowhere)
-#pragma unroll
-    for (int c = 0; c < 8 * NK; ++c) top = fmaxf(top, fabsf(f[c]));
-    top = br_kv_max4(top);
-    // the power of two at or below `top`; not below 2^-100, where its inverse would leave the range
-    const int ex = max((int)(__float_as_uint(top) >> 23), 27);
-    const float inv = __builtin_copysignf(__uint_as_float((unsigned)(254 - min(ex, 253)) << 23), p.scale2);
-    qs[x] = top > 3.0e38f && top * 0.0f != 0.0f ? __builtin_nanf("") : __uint_as_float((unsigned)min(ex, 253) << 23) * fabsf(p.scale2);
-#pragma unroll
-    for (int c = 0; c < 8 * NK; ++c) qf[x][c / 8][c % 8] = (_Float16)(f[c] * inv);
-  }
+  BrKvQueries<D, NQ> q;
+  q.load(p, w, h, row0, [&] {
+    if (t_any) load_first();  // (while the queries are on their way)
+  });
 
   for (; t < stop; ++t) {
     const int token = t * BR_KV_TILE + 16 * g;  // of the lane's first weight
     {
       const unsigned char *at = p.v + ((((cache0 + (there(vid) ? vid : 0)) * p.kv_heads + h) * D + n) << p.shift) + (token & mask);
 #pragma unroll
-      for (int d = 0; d < ND; ++d) vc[d] = br_kv_load16<false>(at + ((16 * d) << p.shift));
+      for (int d = 0; d < ND; ++d) vc[d] = br_kv_load16<!HALF>(at + ((16 * d) << p.shift));
     }
     const float ks = there(vid) ? br_kv_sound(ks1) : 0.0f, vs = there(vid) ? br_kv_sound(vs1) : 0.0f;
     const int have = there(vid) ? min(max(w.len - token, 0), 16) : 0;  // of the lane's tokens, those that exist
@@ -269,7 +345,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
         if (c < 2 * NI) kf = c & 1 ? br_kv_decode8<FP8>(kc[y][c / 2].z, kc[y][c / 2].w) : br_kv_decode8<FP8>(kc[y][c / 2].x, kc[y][c / 2].y);
         else kf = br_kv_decode8<FP8>(kx[y].x, kx[y].y);
 #pragma unroll
-        for (int x = 0; x < NQ; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[x][c], s[x][y], 0, 0, 0);
+        for (int x = 0; x < NQ; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q.qf[x][c], s[x][y], 0, 0, 0);
       }
     }
     const int next = t + 1 < stop ? t + 1 : t, after = next + 1 < stop ? next + 1 : next;
@@ -279,55 +355,8 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     const int vid2 = id_of(after * BR_KV_TILE + 16 * g);
 
 
-    // (a block that no query of the tile sees has no say in c)
-    float top = have > 0 && token <= last_pos && (p.window == 0 || token + 15 > first_pos - p.window) ? vs : 0.0f;
-    top = br_kv_max4(top);
-    float cf = 1.0f;
-    if (top > 8.0f * cmax) {
-      const unsigned e = min(max(__float_as_uint(top) >> 23, 20u), 252u) + 1;
-      cinv = __uint_as_float((254u - e) << 23);
-      cf = cmax * cinv;
-      cmax = __uint_as_float(e << 23);
-    }
-    const float wgt = vs * (256.0f * cinv);
-    // inside: every query of the tile sees all of its tokens, and all exist
-    const bool inside = t * BR_KV_TILE + BR_KV_TILE - 1 <= first_pos && (p.window == 0 || t * BR_KV_TILE > last_pos - p.window) && !__any(!there(vid));
     br_h8 pf[NQ][2];
-#pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-      float f = qs[x] * ks;  // (not below zero: the sign of the caller's scale is in the queries)
-      float z[16], mx = BR_KV_NEG, wx = wgt;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) z[j] = s[x][j >> 2][j & 3];
-      if (!inside) {  // of the lane's tokens, those from `lo` on, `seen` of them
-        const int lo = p.window > 0 ? max(pos[x] - p.window + 1 - token, 0) : 0, seen = max(min(have, pos[x] + 1 - token) - lo, 0);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) z[j] = (unsigned)(j - lo) < (unsigned)seen ? z[j] * f : BR_KV_NEG;
-        f = 1.0f;
-        wx = seen > 0 ? wgt : 0.0f;  // (a block that is not seen has no weight, whatever its scale)
-      }
-#pragma unroll
-      for (int j = 0; j < 16; ++j) mx = fmaxf(mx, z[j]);
-      mx = br_kv_max4(mx * f);
-      const bool up = mx > m[x] + 4.0f;
-      if (__any(up || cf != 1.0f)) {
-        const float to = up ? mx : m[x];
-        const float al = m[x] == BR_KV_NEG ? (l[x] != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m[x] - to), ao = al * cf;
-        m[x] = to;
-        l[x] *= al;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[x][d][j] *= ao;
-      }
-      const float ref = m[x] == BR_KV_NEG ? 0.0f : m[x];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], f, -ref));
-        l[x] += e;
-        pf[x][j >> 3][j & 7] = (_Float16)(e * wx);
-      }
-    }
+    br_kv_weights<D, NQ>(p, q, s, ks, vs, have, t, first_pos, last_pos, !__any(!there(vid)), sums, cmax, cinv, pf);
     // bytes behind the row's end are whatever memory held: an 8-bit float may be a NaN there
     if (FP8 && __any(have < 16)) {
       const unsigned long long full = ~0ull;
@@ -586,7 +615,7 @@ struct BrKvShare {
 
 // Few query rows: a run for each wave, NW waves to a block.  A wave's pieces (of a query tile that it takes up in the middle, and of one that
 // goes on in the next wave) wait in LDS until the block's end, where all waves join them, each its share of the channels.
-template <int D, int NQ, bool FP8, int NW, int WAVES>
+template <int D, int NQ, bool FP8, bool HALF, int NW, int WAVES>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   constexpr int TQ = 16 * NQ, NT = 64 * NW, ND = D / 16;
   __shared__ typename BrKvRuns<TQ, NT>::Shared shared;
@@ -613,7 +642,7 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
     if (u < end && at.find(p, runs, u)) {
       for (;;) {
         const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg);
-        br_kv_tiles<D, NQ, FP8, true>(p, at.w, at.r, at.h, at.qi * TQ, at.pos_of(p, 0), at.pos_of(p, TQ - 1), at.t0 + a, min(at.t0 + b, at.t1), s);
+        br_kv_tiles<D, NQ, FP8, HALF>(p, at.w, at.r, at.h, at.qi * TQ, at.pos_of(p, 0), at.pos_of(p, TQ - 1), at.t0 + a, min(at.t0 + b, at.t1), s);
         if (a == 0 && b == at.size) {
           br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, 0, at.rows_q(p), s);
         } else {
@@ -707,15 +736,16 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   }
 }
 
-// Many query rows: the block's four waves have 16 NQ each and go over the same tokens.
+// Many query rows: the block's four waves have 16 NQ each and go over the same tokens.  Each wave brings a quarter of a tile's codes to f16 and
+// puts them into LDS as the matrix products take them (1 KB for each operand, 16 bytes a lane); two tiles there, one barrier a
+// tile.  Bound by the vector instructions between the products: 8 for a score, 4 of them the exponential.
 template <int D, int NQ, bool FP8, int WAVES>
 __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) {
-  constexpr int TQ = 64 * NQ, NT = 256;
+  constexpr int TQ = 64 * NQ, NT = 256, NI = D / 64, REST = D % 64 / 32, NK = D / 32, ND = D / 16, VG = (ND + 3) / 4;  // VG: groups of 16 channels of values that a wave brings
   __shared__ typename BrKvRuns<TQ, NT>::Shared shared;
-  __shared__ br_f4 sums[NT];
-  __shared__ float2 total[NT];
+  __shared__ br_h8 tile[2][(4 * NK + 2 * ND) * 64];
   __shared__ int arrived;
-  const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
   BrKvRuns<TQ, NT> runs(p, shared, gridDim.x);
   const int blocks = runs.workers, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
   if (wg >= blocks) return;
@@ -723,26 +753,142 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
   const long long end = runs.begin_of(wg + 1);
   BrKvPlace<TQ, NT> at;
   if (u >= end || !at.find(p, runs, u)) return;
+  const int kg = n >> 2, kr = n & 3, mask = (1 << p.shift) - 1;
+  auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  auto there = [&](int id) { return (unsigned)id < (unsigned)p.n_blocks; };
   for (;;) {
     const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg), rows_q = at.rows_q(p), row = 16 * NQ * wv;
     const bool whole = a == 0 && b == at.size;
+    const int first_pos = scalar(at.pos_of(p, row)), last_pos = scalar(at.pos_of(p, row + 16 * NQ - 1)), h = scalar(at.h), r = scalar(at.r), len = scalar(at.w.len);
+    const int first = scalar(at.t0 + a), stop = scalar(min(at.t0 + b, at.t1));
+    const bool busy = row < rows_q;
     BrKvSums<D, NQ> s;
-    const int last_pos = at.pos_of(p, row + 16 * NQ - 1);
-    // (tiles behind a wave's own last query have nothing for it)
-    const int stop = row < rows_q ? min(min(at.t0 + b, at.t1), last_pos / BR_KV_TILE + 1) : 0;
-    br_kv_tiles<D, NQ, FP8, false>(p, at.w, at.r, at.h, at.qi * TQ + row, at.pos_of(p, row), last_pos, at.t0 + a, stop, s);
+    float cmax = 0.0f, cinv = 0.0f;
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      s.m[x] = BR_KV_NEG, s.l[x] = 0.0f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) s.o[x][d] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const int *table = p.table + (long long)r * p.max_blocks;
+    const int last_block = max(0, (len - 1) >> p.shift);
+    const long long cache0 = (long long)(r / p.rows) * p.n_blocks;
+    auto id_of = [&](int token) { return table[min(token >> p.shift, last_block)]; };
+
+    // this wave's quarter of a tile: rows 4 wv + kr of each token group of K, channels 16 (wv + 4 i) + n of V
+    uint4 kc[NI + (NI == 0)], vc[VG];
+    uint2 kx;
+    float ks1 = 0.0f, vs1 = 0.0f;
+    auto fetch = [&](int t, int kid, int vid) {
+      const unsigned char *k = p.k + ((((cache0 + (there(kid) ? kid : 0)) * p.kv_heads + h) << p.shift) + ((t * BR_KV_TILE + 16 * kg) & mask) + 4 * wv + kr) * D;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) kc[i] = *(const uint4 *)(k + 64 * i + 16 * g);
+      if (REST) kx = *(const uint2 *)(k + 64 * NI + 8 * g);
+      const long long vb = (cache0 + (there(vid) ? vid : 0)) * p.kv_heads + h;
+      const unsigned char *v = p.v + (((vb * D + n) << p.shift) + ((t * BR_KV_TILE + 16 * g) & mask));
+#pragma unroll
+      for (int i = 0; i < VG; ++i)
+        if (wv + 4 * i < ND) vc[i] = *(const uint4 *)(v + ((16 * (wv + 4 * i)) << p.shift));
+      ks1 = p.ks[vb], vs1 = p.vs[vb];
+    };
+    auto bring = [&](int t, int vid, br_h8 *to) {
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        br_h8 y;
+        if (c < 2 * NI) y = c & 1 ? br_kv_decode8<FP8>(kc[c / 2].z, kc[c / 2].w) : br_kv_decode8<FP8>(kc[c / 2].x, kc[c / 2].y);
+        else y = br_kv_decode8<FP8>(kx.x, kx.y);
+        to[(wv * NK + c) * 64 + lane] = y;
+      }
+      // (bytes behind the row's end are whatever memory held: an 8-bit float may be a NaN there)
+      const int have = there(vid) ? min(max(len - t * BR_KV_TILE - 16 * g, 0), 16) : 0;
+      if (FP8 && __any(have < 16)) {
+        const unsigned long long full = ~0ull;
+        const unsigned long long m0 = have >= 8 ? full : ~(full << (8 * have)), m1 = have >= 16 ? full : have <= 8 ? 0ull : ~(full << (8 * (have - 8)));
+#pragma unroll
+        for (int i = 0; i < VG; ++i) vc[i].x &= (unsigned)m0, vc[i].y &= (unsigned)(m0 >> 32), vc[i].z &= (unsigned)m1, vc[i].w &= (unsigned)(m1 >> 32);
+      }
+#pragma unroll
+      for (int i = 0; i < VG; ++i) {
+        if (wv + 4 * i >= ND) continue;
+        to[(4 * NK + 2 * (wv + 4 * i)) * 64 + lane] = br_kv_decode8<FP8>(vc[i].x, vc[i].y);
+        to[(4 * NK + 2 * (wv + 4 * i) + 1) * 64 + lane] = br_kv_decode8<FP8>(vc[i].z, vc[i].w);
+      }
+    };
+    int kid1 = 0, vid = 0, vid1 = 0;  // of the next tile, of this one, of the next
+    float ks = 0.0f, vs = 0.0f;
+    if (first < stop) {
+      const int next = min(first + 1, stop - 1);
+      const int kid = id_of(first * BR_KV_TILE + 16 * kg);
+      vid = id_of(first * BR_KV_TILE + 16 * g);
+      kid1 = id_of(next * BR_KV_TILE + 16 * kg), vid1 = id_of(next * BR_KV_TILE + 16 * g);
+      fetch(first, kid, vid);
+    }
+    BrKvQueries<D, NQ> q;
+    q.load(p, at.w, h, at.qi * TQ + row, [] {});
+    if (first < stop) {
+      ks = ks1, vs = vs1;
+      bring(first, vid, tile[0]);
+      fetch(min(first + 1, stop - 1), kid1, vid1);
+    }
+    __syncthreads();
+    for (int t = first; t < stop; ++t) {
+      const br_h8 *now = tile[(t - first) & 1];
+      // the next tile to the other half, the one behind it on its way
+      const int after = min(t + 2, stop - 1);
+      const int kid2 = id_of(after * BR_KV_TILE + 16 * kg), vid2 = id_of(after * BR_KV_TILE + 16 * g);
+      const float ks_next = ks1, vs_next = vs1;
+      if (t + 1 < stop) bring(t + 1, vid1, tile[(t + 1 - first) & 1]);
+      fetch(after, kid2, vid2);
+      // (tiles behind a wave's last query, or before its first one's window, have nothing for it)
+      if (busy && t * BR_KV_TILE <= last_pos && (p.window == 0 || t * BR_KV_TILE + BR_KV_TILE - 1 > first_pos - p.window)) {
+        br_f4 z[NQ][4];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) z[x][y] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int c = 0; c < NK; ++c) {
+            const br_h8 kf = now[(y * NK + c) * 64 + lane];
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) z[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q.qf[x][c], z[x][y], 0, 0, 0);
+          }
+        const int have = there(vid) ? min(max(len - t * BR_KV_TILE - 16 * g, 0), 16) : 0;
+        br_h8 pf[NQ][2];
+        br_kv_weights<D, NQ>(p, q, z, there(vid) ? br_kv_sound(ks) : 0.0f, there(vid) ? br_kv_sound(vs) : 0.0f, have, t, first_pos, last_pos, !__any(!there(vid)), s, cmax, cinv, pf);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const br_h8 v0 = now[(4 * NK + 2 * d) * 64 + lane], v1 = now[(4 * NK + 2 * d + 1) * 64 + lane];
+#pragma unroll
+          for (int x = 0; x < NQ; ++x) {
+            s.o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[x][0], s.o[x][d], 0, 0, 0);
+            s.o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[x][1], s.o[x][d], 0, 0, 0);
+          }
+        }
+      }
+      ks = ks_next, vs = vs_next;
+      vid = vid1, vid1 = vid2;
+      __syncthreads();
+    }
+    s.c = cmax * (1.0f / 256.0f);
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      s.l[x] = br_kv_sum4(s.l[x]);
+      if (s.m[x] == BR_KV_NEG) s.m[x] = 0.0f;
+    }
     if (whole) {
       br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, row, rows_q, s);
     } else {
-      const int first = runs.owner_of(at.seg), parts = runs.owner_of(at.seg + at.size - 1) - first + 1;
+      const int from = runs.owner_of(at.seg), parts = runs.owner_of(at.seg + at.size - 1) - from + 1;
       br_kv_piece<D, NQ, TQ>(p, 2 * wg + (a == 0 ? 1 : 0), row, rows_q, s);
       br_kv_stores_done();
       __syncthreads();
-      if (tid == 0) arrived = __hip_atomic_fetch_add(&p.arrived[first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (tid == 0) arrived = __hip_atomic_fetch_add(&p.arrived[from], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       __syncthreads();
       if (arrived == parts - 1) {
-        br_kv_join<D, TQ, NT>(p, at.w, at.h, at.qi, rows_q, first, parts, sums, total);
-        if (tid == 0) p.arrived[first] = 0;  // (for the next launch)
+        br_kv_join<D, TQ, NT>(p, at.w, at.h, at.qi, rows_q, from, parts, (br_f4 *)tile[0], (float2 *)tile[1]);
+        if (tid == 0) p.arrived[from] = 0;  // (for the next launch)
       }
       __syncthreads();
     }
@@ -756,8 +902,8 @@ template <int D, int NQ, int NW, int WAVES>
 void br_kv_attend_few(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
   constexpr int PER = 4 * WAVES / NW;
   const int blocks = PER * cus < BR_KV_SPLIT_WGS ? PER * cus : BR_KV_SPLIT_WGS;
-  if (fp8) br_kv_k_attend<D, NQ, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
-  else br_kv_k_attend<D, NQ, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+  if (fp8) p.shift == 7 ? br_kv_k_attend<D, NQ, true, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p) : br_kv_k_attend<D, NQ, true, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+  else p.shift == 7 ? br_kv_k_attend<D, NQ, false, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p) : br_kv_k_attend<D, NQ, false, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
 }
 
 template <int D, int NQ, int WAVES>
