@@ -337,10 +337,11 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     for (int x = 0; x < NQ; ++x)
 #pragma unroll
       for (int y = 0; y < 4; ++y) s[x][y] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
+    // (products into one sum do not follow each other directly)
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
+    for (int c = 0; c < NK; ++c) {
 #pragma unroll
-      for (int c = 0; c < NK; ++c) {
+      for (int y = 0; y < 4; ++y) {
         br_h8 kf;
         if (c < 2 * NI) kf = c & 1 ? br_kv_decode8<FP8>(kc[y][c / 2].z, kc[y][c / 2].w) : br_kv_decode8<FP8>(kc[y][c / 2].x, kc[y][c / 2].y);
         else kf = br_kv_decode8<FP8>(kx[y].x, kx[y].y);
@@ -366,13 +367,15 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
       for (int d = 0; d < ND; ++d) vc[d].x &= (unsigned)m0, vc[d].y &= (unsigned)(m0 >> 32), vc[d].z &= (unsigned)m1, vc[d].w &= (unsigned)(m1 >> 32);
     }
 #pragma unroll
-    for (int d = 0; d < ND; ++d) {
-      const br_h8 v0 = br_kv_decode8<FP8>(vc[d].x, vc[d].y), v1 = br_kv_decode8<FP8>(vc[d].z, vc[d].w);
+    for (int d0 = 0; d0 < ND; d0 += 2) {
 #pragma unroll
-      for (int x = 0; x < NQ; ++x) {
-        o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[x][0], o[x][d], 0, 0, 0);
-        o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[x][1], o[x][d], 0, 0, 0);
-      }
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int d = d0; d < d0 + 2; ++d) {
+          const br_h8 v = k ? br_kv_decode8<FP8>(vc[d].z, vc[d].w) : br_kv_decode8<FP8>(vc[d].x, vc[d].y);
+#pragma unroll
+          for (int x = 0; x < NQ; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pf[x][k], o[x][d], 0, 0, 0);
+        }
     }
     vid = vid1, vid1 = vid2;
   }
@@ -389,27 +392,36 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 // well.  One way to memory and back: each thread weighs its pieces against the largest maximum among them.
 template <int D, int TQ, int NT>
 __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int rows_q, int first, int parts, br_f4 *sums, float2 *ml) {
-  constexpr int AT_ONCE = 8;
+  // few rows have many pieces (up to a block of the launch each), many rows few: places asked for at once are AT_ONCE pieces of ROWS rows
+  constexpr int ROWS = TQ > 32 ? 4 : 1, AT_ONCE = TQ > 32 ? 2 : 8, STEP = NT * ROWS;
   const int tid = threadIdx.x, items = rows_q * (D / 4), S = items < NT ? max(1, NT / items) : 1;
-  for (int at = tid; at < max(items, NT); at += NT) {
-    const int it = at % items, k0 = at / items, row = it / (D / 4), d = it % (D / 4) * 4;
-    br_f4 y = {0.0f, 0.0f, 0.0f, 0.0f};
-    float m = 0.0f, l = 0.0f;
-    if (k0 < S) {
-      for (int k = k0; k < parts; k += S * AT_ONCE) {
-        float2 x[AT_ONCE], v0[AT_ONCE], v1[AT_ONCE];
+  for (int at0 = tid; at0 < max(items, NT); at0 += STEP) {
+    br_f4 ys[ROWS];
+    float ms[ROWS], ls[ROWS];
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) ys[q] = br_f4{0.0f, 0.0f, 0.0f, 0.0f}, ms[q] = ls[q] = 0.0f;
+    const int k0 = at0 / items;
+    for (int k = k0; k < (k0 < S ? parts : 0); k += S * AT_ONCE) {
+      float2 x[ROWS][AT_ONCE], v0[ROWS][AT_ONCE], v1[ROWS][AT_ONCE];
+#pragma unroll
+      for (int q = 0; q < ROWS; ++q) {
+        const int it = S > 1 ? at0 % items : min(at0 + q * NT, items - 1), row = it / (D / 4), d = it % (D / 4) * 4;
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
           const int kk = min(k + j * S, parts - 1);
           const long long piece = (long long)(kk ? 2 * (first + kk) : 2 * first + 1) * TQ + row;
-          x[j] = br_kv_get2(p.ml + piece * 2);
-          v0[j] = br_kv_get2(p.part + piece * D + d), v1[j] = br_kv_get2(p.part + piece * D + d + 2);
+          x[q][j] = br_kv_get2(p.ml + piece * 2);
+          v0[q][j] = br_kv_get2(p.part + piece * D + d), v1[q][j] = br_kv_get2(p.part + piece * D + d + 2);
         }
-        float top = l != 0.0f ? m : BR_KV_NEG;
+      }
+#pragma unroll
+      for (int q = 0; q < ROWS; ++q) {
+        br_f4 &y = ys[q];
+        float &m = ms[q], &l = ls[q], top = l != 0.0f ? m : BR_KV_NEG;
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
-          if (k + j * S >= parts) x[j].y = 0.0f;
-          if (x[j].y != 0.0f) top = fmaxf(top, x[j].x);
+          if (k + j * S >= parts) x[q][j].y = 0.0f;
+          if (x[q][j].y != 0.0f) top = fmaxf(top, x[q][j].x);
         }
         const float e0 = l != 0.0f ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
         l *= e0;
@@ -417,14 +429,17 @@ __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w
         for (int c = 0; c < 4; ++c) y[c] *= e0;
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
-          if (x[j].y == 0.0f) continue;
-          const float e = __builtin_amdgcn_exp2f(x[j].x - top);
-          l += x[j].y * e;
-          y[0] = __builtin_fmaf(v0[j].x, e, y[0]), y[1] = __builtin_fmaf(v0[j].y, e, y[1]), y[2] = __builtin_fmaf(v1[j].x, e, y[2]), y[3] = __builtin_fmaf(v1[j].y, e, y[3]);
+          if (x[q][j].y == 0.0f) continue;
+          const float e = __builtin_amdgcn_exp2f(x[q][j].x - top);
+          l += x[q][j].y * e;
+          y[0] = __builtin_fmaf(v0[q][j].x, e, y[0]), y[1] = __builtin_fmaf(v0[q][j].y, e, y[1]);
+          y[2] = __builtin_fmaf(v1[q][j].x, e, y[2]), y[3] = __builtin_fmaf(v1[q][j].y, e, y[3]);
         }
         m = top == BR_KV_NEG ? 0.0f : top;
       }
     }
+    br_f4 y = ys[0];
+    float m = ms[0], l = ls[0];
     if (S > 1) {
       sums[tid] = y, ml[tid] = make_float2(m, l);
       __syncthreads();
@@ -446,11 +461,14 @@ __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w
         m = top;
       }
     }
-    if (k0 == 0) {
-      const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-      const br_f4 one[1] = {y};
-      br_kv_store<1>(p, w, h, qi * TQ + row, d, one, inv);
-      if (d == 0) br_kv_store_lse(p, w, h, qi * TQ + row, m, l);
+    ys[0] = y, ms[0] = m, ls[0] = l;
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) {
+      const int it = at0 + q * NT, row = it / (D / 4), d = it % (D / 4) * 4;
+      if (it >= items) continue;
+      const br_f4 one[1] = {ys[q]};
+      br_kv_store<1>(p, w, h, qi * TQ + row, d, one, ls[q] != 0.0f ? 1.0f / ls[q] : 0.0f);
+      if (d == 0) br_kv_store_lse(p, w, h, qi * TQ + row, ms[q], ls[q]);
     }
   }
 }
@@ -847,9 +865,9 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
 #pragma unroll
           for (int y = 0; y < 4; ++y) z[x][y] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
+        for (int c = 0; c < NK; ++c)
 #pragma unroll
-          for (int c = 0; c < NK; ++c) {
+          for (int y = 0; y < 4; ++y) {
             const br_h8 kf = now[(y * NK + c) * 64 + lane];
 #pragma unroll
             for (int x = 0; x < NQ; ++x) z[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q.qf[x][c], z[x][y], 0, 0, 0);
@@ -858,14 +876,13 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
         br_h8 pf[NQ][2];
         br_kv_weights<D, NQ>(p, q, z, there(vid) ? br_kv_sound(ks) : 0.0f, there(vid) ? br_kv_sound(vs) : 0.0f, have, t, first_pos, last_pos, !__any(!there(vid)), s, cmax, cinv, pf);
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          const br_h8 v0 = now[(4 * NK + 2 * d) * 64 + lane], v1 = now[(4 * NK + 2 * d + 1) * 64 + lane];
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int x = 0; x < NQ; ++x) {
-            s.o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[x][0], s.o[x][d], 0, 0, 0);
-            s.o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[x][1], s.o[x][d], 0, 0, 0);
+          for (int d = 0; d < ND; ++d) {
+            const br_h8 v = now[(4 * NK + 2 * d + k) * 64 + lane];
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) s.o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pf[x][k], s.o[x][d], 0, 0, 0);
           }
-        }
       }
       ks = ks_next, vs = vs_next;
       vid = vid1, vid1 = vid2;
