@@ -479,3 +479,16 @@ def test_offsets_beyond_32_bits():
         ref = torch.einsum("ht,thd->hd", w, v)
         assert ((out[r].double().cpu() - ref).abs().max() < 2e-3).item()
     cache.close()
+
+
+@pytest.mark.parametrize("fmt,policy", [("fp8", False), ("int8", True)])
+def test_routed_requests_on_their_workers(fmt, policy):
+    """The example: the router's loads are the workers' cached tokens in every step (it compares them itself)."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode_workers.py")
+    spec = importlib.util.spec_from_file_location("decode_workers", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    log = example.run(steps=40, fmt=fmt, policy=policy, block=16 if policy else 32)
+    assert len(log) == 40 and max(r["requests"] for r in log) > 20
