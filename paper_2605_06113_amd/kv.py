@@ -18,7 +18,7 @@ types, shapes, strides and devices, since the C ABI takes bare pointers.
 from __future__ import annotations
 
 import ctypes as C
-import math
+import struct
 from dataclasses import dataclass
 from typing import Dict, Optional
 
@@ -68,6 +68,8 @@ class _Layout(C.Structure):
     _fields_ = [("lens", C.c_uint64), ("table", C.c_uint64), ("total_bytes", C.c_uint64)]
 
 
+# The structs of the calls of a decode loop, packed in one go (a ctypes struct costs as much as the call): pointers, strides, numbers.
+_PACK_LENGTHS, _PACK_STEP, _PACK_TOKENS, _PACK_ATTENTION = (struct.Struct(f) for f in ("@2P", "@6P2i", "@3P4q2i", "@7P4q4ifi"))
 _lib = None
 
 
@@ -82,10 +84,8 @@ def load():
     lib.br_kv_workspace_bytes.restype = C.c_uint64
     lib.br_kv_workspace_bytes.argtypes = [C.POINTER(_Config)]
     lib.br_kv_init.argtypes = [C.POINTER(_Config), C.POINTER(_State), C.POINTER(_P)]
-    lib.br_kv_step.argtypes = [_P, C.POINTER(_Lengths), C.POINTER(_StepOut)]
-    lib.br_kv_append.argtypes = [_P, C.POINTER(_Layer), C.POINTER(_Tokens)]
-    lib.br_kv_read.argtypes = [_P, C.POINTER(_Layer), C.POINTER(_Tokens)]
-    lib.br_kv_attend.argtypes = [_P, C.POINTER(_Layer), C.POINTER(_Attention)]
+    for name in ("br_kv_step", "br_kv_append", "br_kv_read", "br_kv_attend"):
+        getattr(lib, name).argtypes = [_P, _P, _P]
     lib.br_kv_free.restype = None
     lib.br_kv_free.argtypes = [_P]
     lib.br_kv_last_hip_error.argtypes = [_P]
@@ -125,8 +125,9 @@ class KvLayer:
 
     def __init__(self, k, v, k_scale, v_scale):
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.sizes = (k.shape, k.get_device())  # a cache takes layers of its own sizes only
         self.struct = _Layer(k=k.data_ptr(), v=v.data_ptr(), k_scale=k_scale.data_ptr(), v_scale=v_scale.data_ptr())
-        self.ref = C.byref(self.struct)
+        self.ref, self.at = C.byref(self.struct), C.addressof(self.struct)
 
 
 class KvCache:
@@ -135,11 +136,10 @@ class KvCache:
     def __init__(self, cfg: KvConfig, lens=None, table=None, device="cuda:0", stream=None):
         """lens [n_workers, rows], table [n_workers, rows, max_blocks] (int32): requests held at the start."""
         import torch
-        self.torch, self.lib, self.cfg = torch, load(), cfg
-        self.device = torch.device(device)
-        if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
-        self._dtypes = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+        device = torch.device(device)
+        if device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        self._sizes(torch, load(), cfg, device)
         W, B = cfg.n_workers, cfg.rows
         nbytes = workspace_bytes(cfg)
         if nbytes == 0:
@@ -167,25 +167,42 @@ class KvCache:
         self.table = self.ws[lay.table // 4:lay.table // 4 + W * B * cfg.max_blocks].view(W, B, cfg.max_blocks)
 
     # -- checks ---------------------------------------------------------------
+    def _sizes(self, torch, lib, cfg: KvConfig, device) -> None:
+        """What the checks of every call go by, and room for the calls' structs."""
+        self.torch, self.lib, self.cfg, self.device = torch, lib, cfg, device
+        self._index = device.index if device.type == "cuda" else -1
+        self._dtypes = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+        self._i32, self._f32, self._i64 = torch.int32, torch.float32, torch.int64
+        W, B = cfg.n_workers, cfg.rows
+        self._rows, self._stats, self._tables = torch.Size((W, B)), torch.Size((W, NSTATS)), torch.Size((W, B, cfg.max_blocks))
+        self._scale = cfg.head_dim ** -0.5
+        self._layer = (torch.Size((W * cfg.n_blocks, cfg.n_kv_heads, cfg.block_tokens, cfg.head_dim)), self._index)
+        self._args = C.create_string_buffer(256)
+        self._at = C.addressof(self._args)
+
     def _done(self, rc: int, what: str) -> None:
         if rc != BR_OK:
             ctx = getattr(self, "ctx", None)
             raise BrError(f"{what} failed: rc={rc} hip_error={self.lib.br_kv_last_hip_error(ctx) if ctx else 0}")
 
-    def _check(self, x, name: str, shape, dtype) -> None:
-        """A contiguous tensor of that shape and type on this device."""
-        if tuple(x.shape) != tuple(shape) or x.dtype != dtype or x.device != self.device or not x.is_contiguous():
+    def _check(self, x, name: str, shape, dtype) -> int:
+        """The address of a contiguous tensor of that shape and type on this device."""
+        if x.shape != shape or x.dtype is not dtype or x.get_device() != self._index or not x.is_contiguous():
             raise BrError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}")
+        return x.data_ptr()
 
-    def _tokens(self, x, name: str, n, heads: int) -> int:
-        """The type code of keys, values, queries or outputs [n, heads, head_dim] with contiguous channels."""
-        shape = (x.shape[0] if n is None and x.dim() else n, heads, self.cfg.head_dim)
-        if tuple(x.shape) != shape or x.device != self.device or (x.stride(2) != 1 and x.numel()):
-            raise BrError(f"{name} must have shape {shape} with contiguous channels on {self.device}")
+    def _tokens(self, x, name: str, n, heads: int):
+        """(type code, strides of tokens and heads) of keys, values, queries or outputs [n, heads, head_dim] with contiguous channels."""
+        shape = x.shape
+        if len(shape) != 3 or (n is not None and shape[0] != n) or shape[1] != heads or shape[2] != self.cfg.head_dim or x.get_device() != self._index:
+            raise BrError(f"{name} must have shape {('tokens' if n is None else n, heads, self.cfg.head_dim)} on {self.device}")
+        token, head, channel = x.stride()
+        if channel != 1 and shape[0]:
+            raise BrError(f"{name} must have contiguous channels")
         dtype = self._dtypes.get(x.dtype)
         if dtype is None:
             raise BrError(f"{name} must be float16, bfloat16 or float32, not {x.dtype}")
-        return dtype
+        return dtype, token, head
 
     # -- memory ---------------------------------------------------------------
     def layer(self, k, v, k_scale, v_scale) -> KvLayer:
@@ -214,43 +231,43 @@ class KvCache:
     # -- calls ----------------------------------------------------------------
     def step_device(self, keep, add, out) -> None:
         """Tables of the next step (br_kv_step): keep, add [n_workers, rows] int32; out: alloc_step's arrays."""
-        i32, W, B = self.torch.int32, self.cfg.n_workers, self.cfg.rows
-        self._check(keep, "keep", (W, B), i32)
-        self._check(add, "add", (W, B), i32)
+        check, i32, rows = self._check, self._i32, self._rows
         slot = out["slot"]
-        if slot.dim() != 2:
+        if slot.dim() != 2 or slot.shape[0] != rows[0]:
             raise BrError("slot must have shape (n_workers, token_cap)")
-        cap = slot.shape[1]
-        self._check(slot, "slot", (W, cap), i32)
-        self._check(out["pos"], "pos", (W, cap), i32)
-        for name in ("start", "count", "status"):
-            self._check(out[name], name, (W, B), i32)
-        self._check(out["stats"], "stats", (W, NSTATS), self.torch.int64)
-        a = _Lengths(keep=keep.data_ptr(), add=add.data_ptr())
-        o = _StepOut(slot=slot.data_ptr(), pos=out["pos"].data_ptr(), start=out["start"].data_ptr(), count=out["count"].data_ptr(),
-                     status=out["status"].data_ptr(), stats=out["stats"].data_ptr(), token_cap=cap)
-        self._done(self.lib.br_kv_step(self.ctx, C.byref(a), C.byref(o)), "br_kv_step")
+        _PACK_LENGTHS.pack_into(self._args, 0, check(keep, "keep", rows, i32), check(add, "add", rows, i32))
+        _PACK_STEP.pack_into(self._args, 16, check(slot, "slot", slot.shape, i32), check(out["pos"], "pos", slot.shape, i32), check(out["start"], "start", rows, i32),
+                             check(out["count"], "count", rows, i32), check(out["status"], "status", rows, i32), check(out["stats"], "stats", self._stats, self._i64),
+                             slot.shape[1], 0)
+        rc = self.lib.br_kv_step(self.ctx, self._at, self._at + 16)
+        if rc:
+            self._done(rc, "br_kv_step")
 
-    def _token_struct(self, k, v, slot) -> _Tokens:
-        W = self.cfg.n_workers
-        n = slot.numel()
-        if n % W or slot.dtype != self.torch.int32 or slot.device != self.device or not slot.is_contiguous():
+    def _pack_tokens(self, layer, k, v, slot) -> None:
+        if layer.sizes != self._layer:
+            raise BrError("the layer is one of another cache's sizes")
+        W, n = self._rows[0], slot.numel()
+        if n % W or slot.dtype is not self._i32 or slot.get_device() != self._index or not slot.is_contiguous():
             raise BrError(f"slot must be a contiguous int32 tensor on {self.device} with the same number of tokens for each worker")
-        dtype = self._tokens(k, "k", n, self.cfg.n_kv_heads)
-        if self._tokens(v, "v", n, self.cfg.n_kv_heads) != dtype:
+        dtype, k_token, k_head = self._tokens(k, "k", n, self.cfg.n_kv_heads)
+        v_dtype, v_token, v_head = self._tokens(v, "v", n, self.cfg.n_kv_heads)
+        if v_dtype != dtype:
             raise BrError("k and v must have one type")
-        return _Tokens(k=k.data_ptr(), v=v.data_ptr(), slot=slot.data_ptr(), k_token=k.stride(0), k_head=k.stride(1), v_token=v.stride(0),
-                       v_head=v.stride(1), n_tokens=n // W, dtype=dtype)
+        _PACK_TOKENS.pack_into(self._args, 0, k.data_ptr(), v.data_ptr(), slot.data_ptr(), k_token, k_head, v_token, v_head, n // W, dtype)
 
     def append_device(self, layer: KvLayer, k, v, slot) -> None:
         """Tokens into the cache (br_kv_append): k, v [tokens, n_kv_heads, head_dim], slot [tokens] (step_device's, or alike)."""
-        a = self._token_struct(k, v, slot)
-        self._done(self.lib.br_kv_append(self.ctx, layer.ref, C.byref(a)), "br_kv_append")
+        self._pack_tokens(layer, k, v, slot)
+        rc = self.lib.br_kv_append(self.ctx, layer.at, self._at)
+        if rc:
+            self._done(rc, "br_kv_append")
 
     def read_device(self, layer: KvLayer, slot, k, v) -> None:
         """Tokens out of the cache into k, v [tokens, n_kv_heads, head_dim] (br_kv_read)."""
-        a = self._token_struct(k, v, slot)
-        self._done(self.lib.br_kv_read(self.ctx, layer.ref, C.byref(a)), "br_kv_read")
+        self._pack_tokens(layer, k, v, slot)
+        rc = self.lib.br_kv_read(self.ctx, layer.at, self._at)
+        if rc:
+            self._done(rc, "br_kv_read")
 
     def attend_device(self, layer: KvLayer, q, out, lse=None, start=None, count=None, max_count: int = 1, scale: Optional[float] = None, window: int = 0,
                       lens=None, table=None) -> None:
@@ -258,25 +275,30 @@ class KvCache:
 
         start, count [n_workers, rows] (step_device's): a row's query tokens; none: token r belongs to row r.  lse [tokens, n_q_heads] float32.
         scale: 1 / sqrt(head_dim) if not given.  lens, table: instead of the cache's own."""
-        c, t = self.cfg, self.torch
-        dtype = self._tokens(q, "q", None, c.n_q_heads)
+        if layer.sizes != self._layer:
+            raise BrError("the layer is one of another cache's sizes")
+        heads = self.cfg.n_q_heads
+        dtype, q_token, q_head = self._tokens(q, "q", None, heads)
         n = q.shape[0]
         if dtype == 2:
             raise BrError("q must be float16 or bfloat16")
-        if self._tokens(out, "out", n, c.n_q_heads) != dtype:
+        out_dtype, out_token, out_head = self._tokens(out, "out", n, heads)
+        if out_dtype != dtype:
             raise BrError("q and out must have one type")
-        rows = (c.n_workers, c.rows)
         if (start is None) != (count is None):
             raise BrError("start and count come together")
-        for x, name, shape, kind in ((lse, "lse", (n, c.n_q_heads), t.float32), (start, "start", rows, t.int32), (count, "count", rows, t.int32),
-                                     (lens, "lens", rows, t.int32), (table, "table", rows + (c.max_blocks,), t.int32)):
-            if x is not None and (x.numel() != math.prod(shape) or x.dtype != kind or x.device != self.device or not x.is_contiguous()):
-                raise BrError(f"{name} must be a contiguous {kind} tensor of shape {shape} on {self.device}")
-        p = lambda x: None if x is None else x.data_ptr()
-        a = _Attention(q=q.data_ptr(), out=out.data_ptr(), lse=p(lse), start=p(start), count=p(count), lens=p(lens), table=p(table), q_token=q.stride(0),
-                       q_head=q.stride(1), out_token=out.stride(0), out_head=out.stride(1), n_tokens=n, max_count=int(max_count), window=int(window),
-                       dtype=dtype, scale=c.head_dim ** -0.5 if scale is None else float(scale))
-        self._done(self.lib.br_kv_attend(self.ctx, layer.ref, C.byref(a)), "br_kv_attend")
+        check, i32, rows = self._check, self._i32, self._rows
+        at = (q.data_ptr(), out.data_ptr(), 0 if lse is None else check(lse, "lse", (n, heads), self._f32),
+              0 if start is None else check(start.view(rows) if start.shape != rows and start.numel() == rows.numel() else start, "start", rows, i32),
+              0 if count is None else check(count.view(rows) if count.shape != rows and count.numel() == rows.numel() else count, "count", rows, i32),
+              0 if lens is None else check(lens, "lens", rows, i32), 0 if table is None else check(table, "table", self._tables, i32), q_token, q_head, out_token, out_head, n)
+        try:
+            _PACK_ATTENTION.pack_into(self._args, 0, *at, max_count, window, dtype, self._scale if scale is None else scale, 0)
+        except (struct.error, OverflowError):
+            raise BrError("max_count and window must be whole numbers of 32 bits, scale a number of 32 bits") from None
+        rc = self.lib.br_kv_attend(self.ctx, layer.at, self._at)
+        if rc:
+            self._done(rc, "br_kv_attend")
 
     def close(self) -> None:
         if getattr(self, "ctx", None):

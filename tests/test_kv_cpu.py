@@ -29,6 +29,11 @@ def test_struct_sizes_match_header():
     assert C.sizeof(kv._StepOut) == 6 * 8 + 8
     assert C.sizeof(kv._Tokens) == 3 * 8 + 4 * 8 + 8
     assert C.sizeof(kv._Attention) == 7 * 8 + 4 * 8 + 6 * 4
+    for packed, struct in ((kv._PACK_LENGTHS, kv._Lengths), (kv._PACK_STEP, kv._StepOut), (kv._PACK_TOKENS, kv._Tokens), (kv._PACK_ATTENTION, kv._Attention)):
+        assert packed.size == C.sizeof(struct)
+    # the packed form of the longest one, field by field
+    a = kv._Attention.from_buffer_copy(kv._PACK_ATTENTION.pack(*range(1, 16), 0.5, 0))
+    assert [getattr(a, f) for f, _ in kv._Attention._fields_] == list(range(1, 16)) + [0.5, 0]
 
 
 @pytest.mark.parametrize("bad", [dict(rows=0), dict(rows=1025), dict(n_workers=0), dict(n_workers=1 << 20, rows=64), dict(block_tokens=8), dict(block_tokens=48),
@@ -64,8 +69,8 @@ def _cache(**kw):
     """A cache object without a context: what the checks look at."""
     import torch
     c = object.__new__(kv.KvCache)
-    c.torch, c.lib, c.cfg, c.device, c.ctx = torch, None, kv.KvConfig(**{**GOOD, **kw}), torch.device("cpu"), None
-    c._dtypes = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+    c._sizes(torch, None, kv.KvConfig(**{**GOOD, **kw}), torch.device("cpu"))
+    c.ctx = None
     return c
 
 
@@ -85,24 +90,33 @@ def test_binding_refuses_what_does_not_fit():
     with pytest.raises(kv.BrError):
         c.step_device(i32(1, 96), i32(1, 96), dict(out, stats=i32(1, 8)))
     k = f16(7, 8, 128)
+    u8 = lambda *s: torch.zeros(s, dtype=torch.uint8)
+    layer = c.layer(u8(512, 8, 16, 128), u8(512, 8, 128, 16), torch.zeros(512, 8), torch.zeros(512, 8))
     for bad in (dict(k=f16(6, 8, 128)), dict(k=f16(7, 8, 64)), dict(k=f16(7, 128, 8).transpose(1, 2)), dict(v=k.float()), dict(k=k.double(), v=k.double()),
                 dict(slot=i32(7).long()), dict(slot=i32(14)[::2])):
         a = {**dict(k=k, v=k, slot=i32(7)), **bad}
         with pytest.raises(kv.BrError):
-            c.append_device(None, a["k"], a["v"], a["slot"])
+            c.append_device(layer, a["k"], a["v"], a["slot"])
         with pytest.raises(kv.BrError):
-            c.read_device(None, a["slot"], a["k"], a["v"])
+            c.read_device(layer, a["slot"], a["k"], a["v"])
     q = f16(5, 32, 128)
     for bad in (dict(q=f16(5, 31, 128)), dict(q=q.float(), out=q.float()), dict(out=q.bfloat16()), dict(out=f16(4, 32, 128)), dict(lse=f16(5, 32)),
                 dict(lse=torch.zeros(5, 31)), dict(start=i32(1, 96)), dict(start=i32(1, 95), count=i32(1, 96)), dict(lens=i32(1, 97)), dict(table=i32(1, 96, 63))):
         a = {**dict(q=q, out=q), **bad}
         with pytest.raises(kv.BrError):
-            c.attend_device(None, a.pop("q"), a.pop("out"), **a)
+            c.attend_device(layer, a.pop("q"), a.pop("out"), **a)
     with pytest.raises(kv.BrError):
         c.layer(*[torch.zeros(512, 8, 16, 128, dtype=torch.uint8)] * 2, torch.zeros(512, 8), torch.zeros(512, 8))
     two = _cache(n_workers=2)
+    wide = two.layer(u8(1024, 8, 16, 128), u8(1024, 8, 128, 16), torch.zeros(1024, 8), torch.zeros(1024, 8))
     with pytest.raises(kv.BrError):
-        two.append_device(None, k, k, i32(7))
+        two.append_device(wide, k, k, i32(7))
+    for call in (lambda: c.append_device(wide, k, k, i32(7)), lambda: c.read_device(wide, i32(7), k, k), lambda: c.attend_device(wide, q, q)):  # another cache's layer
+        with pytest.raises(kv.BrError):
+            call()
+    for bad in (dict(window=2 ** 31), dict(max_count=1.5), dict(scale="1")):
+        with pytest.raises(kv.BrError):
+            c.attend_device(layer, q, q, **bad)
 
 
 def test_e4m3_of_the_oracle():
