@@ -101,8 +101,9 @@ __device__ __forceinline__ void br_kv_list4(const BrKvTables &t, const BrKvStep 
     }
   }
   if (s.wide) {
-    if (s.slot) *(int4 *)(s.slot + list + j0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
-    if (s.pos) *(int4 *)(s.pos + list + j0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+    typedef int i4 __attribute__((ext_vector_type(4)));
+    if (s.slot) __builtin_nontemporal_store(i4{slot[0], slot[1], slot[2], slot[3]}, (i4 *)(s.slot + list + j0));
+    if (s.pos) __builtin_nontemporal_store(i4{pos[0], pos[1], pos[2], pos[3]}, (i4 *)(s.pos + list + j0));
   } else {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
