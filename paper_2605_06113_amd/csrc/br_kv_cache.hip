@@ -189,13 +189,13 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
   const long long k0 = u.t * a.k_token + (long long)u.h * a.k_head + kd, v0 = u.t * a.v_token + (long long)u.h * a.v_head;
   // values: channels vd and vd + 1 of the block's tokens 16 vg .. 16 vg + 15
-  const int vg0 = u.off >> 4, vitems = (((u.off + u.n - 1) >> 4) - vg0 + 1) * pairs;
+  const int vg0 = u.off >> 4, vgs = ((u.off + u.n - 1) >> 4) - vg0 + 1, vitems = vgs * pairs;
   float top_k = 0.0f, top_v = 0.0f;
   int bad = 0;
   BrKvRaw<DT, 8> rk[AT_ONCE];
   BrKvRaw<DT, 2> rv[16];
   auto fetch_v = [&](int i) {
-    const int g = vg0 + i / pairs, d = (i % pairs) * 2, lo = u.off - 16 * g, hi = u.off + u.n - 16 * g;
+    const int pair = i / vgs, g = vg0 + i - pair * vgs, d = 2 * pair, lo = u.off - 16 * g, hi = u.off + u.n - 16 * g;
     const long long at = v0 + (16 * g - u.off) * a.v_token + d;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
@@ -288,7 +288,7 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   const bool again = vitems > NT;
   for (int i = tid; i < (few ? 0 : vitems); i += NT) {
     if (again) fetch_v(i);
-    const int g = vg0 + i / pairs, d = (i % pairs) * 2, lo = max(u.off - 16 * g, 0), hi = min(u.off + u.n - 16 * g, 16);  // new ones: lo .. hi - 1
+    const int pair = i / vgs, g = vg0 + i - pair * vgs, d = 2 * pair, lo = max(u.off - 16 * g, 0), hi = min(u.off + u.n - 16 * g, 16);  // new ones: lo .. hi - 1
     unsigned char *at = vc + ((long long)d << c.shift) + 16 * g;
     br_u4 y[2];
 #pragma unroll
@@ -317,10 +317,10 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
   const float ks = br_kv_sound(c.ks[u.block]), vs = br_kv_sound(c.vs[u.block]);
   const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
   const long long k0 = u.t * a.k_token + (long long)u.h * a.k_head + kd, v0 = u.t * a.v_token + (long long)u.h * a.v_head;
-  const int vg0 = u.off >> 4, vitems = (((u.off + u.n - 1) >> 4) - vg0 + 1) * pairs;
+  const int vg0 = u.off >> 4, vgs = ((u.off + u.n - 1) >> 4) - vg0 + 1, vitems = vgs * pairs;
   br_u4 x0, x1;
   auto fetch_v = [&](int i) {
-    const int g = vg0 + i / pairs, d = (i % pairs) * 2;
+    const int pair = i / vgs, g = vg0 + i - pair * vgs, d = 2 * pair;
     const unsigned char *at = vc + ((long long)d << c.shift) + 16 * g;
     x0 = *(const br_u4 *)at, x1 = *(const br_u4 *)(at + b);
   };
@@ -345,7 +345,7 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
   }
   for (int i = tid; i < (few ? 0 : vitems); i += NT) {
     if (i != tid) fetch_v(i);
-    const int g = vg0 + i / pairs, d = (i % pairs) * 2, lo = u.off - 16 * g, hi = u.off + u.n - 16 * g;
+    const int pair = i / vgs, g = vg0 + i - pair * vgs, d = 2 * pair, lo = u.off - 16 * g, hi = u.off + u.n - 16 * g;
     const long long at = v0 + (16 * g - u.off) * a.v_token + d;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
