@@ -41,6 +41,7 @@ extern "C" {
 #define BR_KV_MAX_BLOCKS 262144      /* blocks of a worker */
 #define BR_KV_MAX_LEN 1048576        /* tokens that a row's table may span */
 #define BR_KV_MAX_HEADS 1024         /* query heads */
+#define BR_KV_MAX_STRIDE 8388608     /* elements between a token's keys (values) and the next one's */
 #define BR_KV_NSTATS 8
 
 enum { BR_KV_INT8 = 0, BR_KV_E4M3 = 1 };             /* fmt: codes of the cache */
@@ -142,7 +143,7 @@ typedef struct {
   void *k;
   void *v;
   const int32_t *slot;
-  int64_t k_token, k_head, v_token, v_head;
+  int64_t k_token, k_head, v_token, v_head; /* k_token and v_token in 0 .. BR_KV_MAX_STRIDE - 1 */
   int32_t n_tokens; /* >= 0 */
   int32_t dtype;    /* BR_KV_F16, BR_KV_BF16 or BR_KV_F32 */
 } br_kv_tokens;

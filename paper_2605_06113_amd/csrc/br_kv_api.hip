@@ -96,6 +96,7 @@ bool tokens_ok(const br_kv_ctx *ctx, const br_kv_tokens *x) {
   if ((int64_t)ctx->cfg.n_workers * x->n_tokens > INT32_MAX) return false;
   if (x->n_tokens == 0) return true;
   if (!x->k || !x->v || !x->slot) return false;
+  if (x->k_token < 0 || x->k_token >= BR_KV_MAX_STRIDE || x->v_token < 0 || x->v_token >= BR_KV_MAX_STRIDE) return false;  // (32-bit offsets within a block)
   const uintptr_t size = x->dtype == BR_KV_F32 ? 4 : 2;
   return (((uintptr_t)x->k | (uintptr_t)x->v) & (size - 1)) == 0 && ((uintptr_t)x->slot & 3u) == 0;
 }

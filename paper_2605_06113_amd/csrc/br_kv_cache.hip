@@ -61,14 +61,14 @@ __device__ __forceinline__ float br_kv_to_float(unsigned short u) {
   return DT == BR_KV_BF16 ? br_kv_bf16(u) : br_kv_f16(u);
 }
 
-// N = 8 or 2 neighbours of the caller's array as they lie there, and as floats; wide: they are aligned to their size
-template <int DT, int N>
+// N = 8 or 2 neighbours of the caller's array as they lie there, and as floats; WIDE: they are aligned to their size
+template <int DT, int N, bool WIDE>
 struct BrKvRaw {
   static constexpr int WORDS = DT == BR_KV_F32 ? N : N / 2;
   unsigned u[WORDS];
 
-  __device__ __forceinline__ void fetch(const void *x, long long at, int wide) {
-    if (wide) {
+  __device__ __forceinline__ void fetch(const void *x, unsigned at) {
+    if constexpr (WIDE) {
       const unsigned *p = DT == BR_KV_F32 ? (const unsigned *)x + at : (const unsigned *)((const unsigned short *)x + at);
       if constexpr (WORDS >= 4) {
 #pragma unroll
@@ -90,13 +90,14 @@ struct BrKvRaw {
       for (int k = 0; k < WORDS; ++k) u[k] = ((const unsigned short *)x)[at + 2 * k] | (unsigned)((const unsigned short *)x)[at + 2 * k + 1] << 16;
     }
   }
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int k = 0; k < WORDS; ++k) u[k] = 0;
-  }
   __device__ __forceinline__ float get(int j) const {
     if constexpr (DT == BR_KV_F32) return __uint_as_float(u[j]);
     else return br_kv_to_float<DT>((unsigned short)(j & 1 ? u[j / 2] >> 16 : u[j / 2]));
+  }
+  // (keeps the compiler from keeping the floats of the first look at them, twice the registers, for the second)
+  __device__ __forceinline__ void keep_raw() {
+#pragma unroll
+    for (int k = 0; k < WORDS; ++k) __asm__ volatile("" : "+v"(u[k]));
   }
   __device__ __forceinline__ void look(float &top, int &bad, int bit) const {
 #pragma unroll
@@ -108,11 +109,11 @@ struct BrKvRaw {
   }
 };
 
-template <int DT, int N>
-__device__ __forceinline__ void br_kv_store_out(void *x, long long at, int wide, const float (&y)[N]) {
+template <int DT, int N, bool WIDE>
+__device__ __forceinline__ void br_kv_store_out(void *x, unsigned at, const float (&y)[N]) {
   if constexpr (DT == BR_KV_F32) {
     float *p = (float *)x + at;
-    if (wide) {
+    if constexpr (WIDE) {
       if constexpr (N == 8) {
         *(float4 *)p = *(const float4 *)y;
         *(float4 *)(p + 4) = *(const float4 *)(y + 4);
@@ -128,7 +129,7 @@ __device__ __forceinline__ void br_kv_store_out(void *x, long long at, int wide,
     unsigned u[N / 2];
 #pragma unroll
     for (int j = 0; j < N / 2; ++j) u[j] = DT == BR_KV_BF16 ? br_kv_pair<__bf16>(y[2 * j], y[2 * j + 1]) : br_kv_pair<_Float16>(y[2 * j], y[2 * j + 1]);
-    if (wide) {
+    if constexpr (WIDE) {
       if constexpr (N == 8) *(uint4 *)p = *(const uint4 *)u;
       else *(unsigned *)p = u[0];
     } else {
@@ -179,41 +180,37 @@ __device__ __forceinline__ BrKvScale br_kv_scale(float top, bool bad, int off, f
 
 // NT threads (a wave, or a block that is all here) write a run.  red: 16 floats of LDS.  The first AT_ONCE rows of keys and 16 x 2 values
 // of a thread (all, up to 64 tokens of 128 channels for a block) stay in registers between the maximum and the codes.
-template <bool FP8, int DT, int NT>
+template <bool FP8, int DT, bool WIDE, int NT>
 __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, int tid, float *red) {
-  constexpr int AT_ONCE = 4;
+  constexpr int AT_ONCE = 4, SIZE = DT == BR_KV_F32 ? 4 : 2;
   const int D = c.dim, b = 1 << c.shift, chunks = D >> 3, pairs = D >> 1;
   unsigned char *kc = c.k + ((u.block * D) << c.shift), *vc = c.v + ((u.block * D) << c.shift);
   const float old_k = u.off ? c.ks[u.block] : 0.0f, old_v = u.off ? c.vs[u.block] : 0.0f;
   // keys: 8 channels from kd on of tokens kj, kj + kstep, ...
   const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
-  const long long k0 = u.t * a.k_token + (long long)u.h * a.k_head + kd, v0 = u.t * a.v_token + (long long)u.h * a.v_head;
+  const char *xk = (const char *)a.k + (u.t * a.k_token + (long long)u.h * a.k_head) * SIZE, *xv = (const char *)a.v + (u.t * a.v_token + (long long)u.h * a.v_head) * SIZE;
+  const int k_token = (int)a.k_token, v_token = (int)a.v_token;
   // values: channels vd and vd + 1 of the block's tokens 16 vg .. 16 vg + 15
   const int vg0 = u.off >> 4, vgs = ((u.off + u.n - 1) >> 4) - vg0 + 1, vitems = vgs * pairs;
   float top_k = 0.0f, top_v = 0.0f;
   int bad = 0;
-  BrKvRaw<DT, 8> rk[AT_ONCE];
-  BrKvRaw<DT, 2> rv[16];
+  BrKvRaw<DT, 8, WIDE> rk[AT_ONCE];
+  BrKvRaw<DT, 2, WIDE> rv[16];
   auto fetch_v = [&](int i) {
     const int pair = i / vgs, g = vg0 + i - pair * vgs, d = 2 * pair, lo = u.off - 16 * g, hi = u.off + u.n - 16 * g;
-    const long long at = v0 + (16 * g - u.off) * a.v_token + d;
+    const int at = (16 * g - u.off) * v_token + d;
+    // (places that get no new token take a neighbour's: no branches between the loads, nothing for the maximum)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      rv[j].zero();
-      if (j >= lo && j < hi) rv[j].fetch(a.v, at + j * a.v_token, a.wide);
-    }
+    for (int j = 0; j < 16; ++j) rv[j].fetch(xv, at + min(max(j, lo), hi - 1) * v_token);
   };
 #pragma unroll
-  for (int m = 0; m < AT_ONCE; ++m) {
-    rk[m].zero();
-    if (kj + m * kstep < kn) rk[m].fetch(a.k, k0 + (kj + m * kstep) * a.k_token, a.wide);
-  }
+  for (int m = 0; m < AT_ONCE; ++m) rk[m].fetch(xk, min(kj + m * kstep, u.n - 1) * k_token + kd);
   // a decode step's few tokens: two channels of one token at a time
   const bool few = NT == 64 && u.n <= BR_KV_FEW;
   if (few) {
     for (int i = tid; i < u.n * pairs; i += NT) {
       const int j = i / pairs;
-      rv[0].fetch(a.v, v0 + j * a.v_token + (i - j * pairs) * 2, a.wide);
+      rv[0].fetch(xv, j * v_token + (i - j * pairs) * 2);
       rv[0].look(top_v, bad, 2);
     }
   } else {
@@ -226,10 +223,14 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
 #pragma unroll
   for (int m = 0; m < AT_ONCE; ++m) rk[m].look(top_k, bad, 1);
   for (int j = kj + AT_ONCE * kstep; j < kn; j += kstep) {
-    BrKvRaw<DT, 8> x;
-    x.fetch(a.k, k0 + j * a.k_token, a.wide);
+    BrKvRaw<DT, 8, WIDE> x;
+    x.fetch(xk, j * k_token + kd);
     x.look(top_k, bad, 1);
   }
+#pragma unroll
+  for (int m = 0; m < AT_ONCE; ++m) rk[m].keep_raw();
+#pragma unroll
+  for (int j = 0; j < 16; ++j) rv[j].keep_raw();
   top_k = br_kv_max64(top_k), top_v = br_kv_max64(top_v);
   bad = (__any(bad & 1) ? 1 : 0) | (__any(bad & 2) ? 2 : 0);
   if constexpr (NT > 64) {
@@ -248,7 +249,7 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
       *at = make_uint2(br_kv_recode4<FP8>(at->x, zk.r), br_kv_recode4<FP8>(at->y, zk.r));
     }
   }
-  auto put_k = [&](int j, const BrKvRaw<DT, 8> &x) {
+  auto put_k = [&](int j, const BrKvRaw<DT, 8, WIDE> &x) {
     auto q = [&](int m) { return zk.bad ? 0.0f : x.get(m) * zk.inv; };
     *(uint2 *)(kc + (long long)(u.off + j) * D + kd) = make_uint2(br_kv_code4<FP8>(q(0), q(1), q(2), q(3)), br_kv_code4<FP8>(q(4), q(5), q(6), q(7)));
   };
@@ -256,8 +257,8 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   for (int m = 0; m < AT_ONCE; ++m)
     if (kj + m * kstep < kn) put_k(kj + m * kstep, rk[m]);
   for (int j = kj + AT_ONCE * kstep; j < kn; j += kstep) {
-    BrKvRaw<DT, 8> x;
-    x.fetch(a.k, k0 + j * a.k_token, a.wide);
+    BrKvRaw<DT, 8, WIDE> x;
+    x.fetch(xk, j * k_token + kd);
     put_k(j, x);
   }
 
@@ -279,7 +280,7 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   if (few) {
     for (int i = tid; i < u.n * pairs; i += NT) {
       const int j = i / pairs, d = (i - j * pairs) * 2;
-      if (u.n * pairs > NT) rv[0].fetch(a.v, v0 + j * a.v_token + d, a.wide);
+      if (u.n * pairs > NT) rv[0].fetch(xv, j * v_token + d);
       const unsigned q = br_kv_code4<FP8>(zv.bad ? 0.0f : rv[0].get(0) * zv.inv, zv.bad ? 0.0f : rv[0].get(1) * zv.inv, 0.0f, 0.0f);
       unsigned char *at = vc + ((long long)d << c.shift) + u.off + j;
       at[0] = (unsigned char)q, at[b] = (unsigned char)(q >> 8);
@@ -310,13 +311,15 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   if (tid == 0) c.ks[u.block] = zk.s, c.vs[u.block] = zv.s;
 }
 
-template <bool FP8, int DT, int NT>
+template <bool FP8, int DT, bool WIDE, int NT>
 __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, bool in, int tid) {
+  constexpr int SIZE = DT == BR_KV_F32 ? 4 : 2;
   const int D = c.dim, b = 1 << c.shift, chunks = D >> 3, pairs = D >> 1;
   const unsigned char *kc = c.k + ((u.block * D) << c.shift), *vc = c.v + ((u.block * D) << c.shift);
   const float ks = br_kv_sound(c.ks[u.block]), vs = br_kv_sound(c.vs[u.block]);
   const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
-  const long long k0 = u.t * a.k_token + (long long)u.h * a.k_head + kd, v0 = u.t * a.v_token + (long long)u.h * a.v_head;
+  char *xk = (char *)a.k + (u.t * a.k_token + (long long)u.h * a.k_head) * SIZE, *xv = (char *)a.v + (u.t * a.v_token + (long long)u.h * a.v_head) * SIZE;
+  const int k_token = (int)a.k_token, v_token = (int)a.v_token;
   const int vg0 = u.off >> 4, vgs = ((u.off + u.n - 1) >> 4) - vg0 + 1, vitems = vgs * pairs;
   br_u4 x0, x1;
   auto fetch_v = [&](int i) {
@@ -330,7 +333,7 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
       const int j = i / pairs, d = (i - j * pairs) * 2;
       const unsigned char *at = vc + ((long long)d << c.shift) + u.off + j;
       const float y[2] = {in ? br_kv_value<FP8>(at[0]) * vs : 0.0f, in ? br_kv_value<FP8>(at[b]) * vs : 0.0f};
-      br_kv_store_out<DT, 2>(a.v, v0 + j * a.v_token + d, a.wide, y);
+      br_kv_store_out<DT, 2, WIDE>(xv, j * v_token + d, y);
     }
   } else if (tid < vitems) {
     fetch_v(tid);
@@ -341,17 +344,17 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
     float y[8];
 #pragma unroll
     for (int m = 0; m < 8; ++m) y[m] = in ? br_kv_value<FP8>((m < 4 ? x.x : x.y) >> (8 * (m & 3))) * ks : 0.0f;
-    br_kv_store_out<DT, 8>(a.k, k0 + j * a.k_token, a.wide, y);
+    br_kv_store_out<DT, 8, WIDE>(xk, j * k_token + kd, y);
   }
   for (int i = tid; i < (few ? 0 : vitems); i += NT) {
     if (i != tid) fetch_v(i);
     const int pair = i / vgs, g = vg0 + i - pair * vgs, d = 2 * pair, lo = u.off - 16 * g, hi = u.off + u.n - 16 * g;
-    const long long at = v0 + (16 * g - u.off) * a.v_token + d;
+    const int at = (16 * g - u.off) * v_token + d;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       if (j < lo || j >= hi) continue;
       const float y[2] = {in ? br_kv_value<FP8>(x0[j / 4] >> (8 * (j & 3))) * vs : 0.0f, in ? br_kv_value<FP8>(x1[j / 4] >> (8 * (j & 3))) * vs : 0.0f};
-      br_kv_store_out<DT, 2>(a.v, at + j * a.v_token, a.wide, y);
+      br_kv_store_out<DT, 2, WIDE>(xv, at + j * v_token, y);
     }
   }
 }
@@ -368,7 +371,7 @@ __device__ __forceinline__ unsigned long long br_kv_heads(const int *slot, int t
 }
 
 // `span` tokens of a list (at most 64) and a key head for a block, or one for a wave (WAVE).
-template <bool FP8, int DT, bool READ, bool WAVE>
+template <bool FP8, int DT, bool READ, bool WIDE, bool WAVE>
 __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a, int span) {
   __shared__ float red[16];
   if (WAVE) span = 1;
@@ -401,25 +404,30 @@ __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a,
       u.off = in ? s & b1 : 0;
       u.block = ((long long)w * c.n_blocks + (in ? s >> c.shift : 0)) * c.heads + u.h;
       if constexpr (READ) {
-        if (WAVE || apart) br_kv_read_run<FP8, DT, 64>(c, a, u, in, lane);
-        else br_kv_read_run<FP8, DT, 256>(c, a, u, in, threadIdx.x);
+        if (WAVE || apart) br_kv_read_run<FP8, DT, WIDE, 64>(c, a, u, in, lane);
+        else br_kv_read_run<FP8, DT, WIDE, 256>(c, a, u, in, threadIdx.x);
       } else {
-        if (WAVE || apart) br_kv_append_run<FP8, DT, 64>(c, a, u, lane, red);
-        else br_kv_append_run<FP8, DT, 256>(c, a, u, threadIdx.x, red);
+        if (WAVE || apart) br_kv_append_run<FP8, DT, WIDE, 64>(c, a, u, lane, red);
+        else br_kv_append_run<FP8, DT, WIDE, 256>(c, a, u, threadIdx.x, red);
       }
     }
   }
 }
 
-template <bool FP8, int DT, bool READ>
-static void launch(const BrKvCache &c, const BrKvTokens &t, int rows, hipStream_t st) {
+template <bool FP8, int DT, bool READ, bool WIDE>
+static void launch_wide(const BrKvCache &c, const BrKvTokens &t, int rows, hipStream_t st) {
   const long long tokens = (long long)t.W * t.n * c.heads;
   auto grid = [](long long n) { return (unsigned)(n < 1 ? 1 : n > 1 << 20 ? 1 << 20 : n); };
   // a wave for each token and head while they fit the chip about once; most waves of a longer list would begin no run.  A list of
   // more than a few tokens a row has runs of whole blocks: 64 tokens are four runs of 16, one for each wave, or at most two longer ones
   const int span = t.n > 4 * rows ? (c.shift == 5 ? 32 : 64) : 16;
-  if (tokens <= 16384) br_kv_k_tokens<FP8, DT, READ, true><<<grid((tokens + 3) / 4), 256, 0, st>>>(c, t, 1);
-  else br_kv_k_tokens<FP8, DT, READ, false><<<grid((long long)t.W * ((t.n + span - 1) / span) * c.heads), 256, 0, st>>>(c, t, span);
+  if (tokens <= 16384) br_kv_k_tokens<FP8, DT, READ, WIDE, true><<<grid((tokens + 3) / 4), 256, 0, st>>>(c, t, 1);
+  else br_kv_k_tokens<FP8, DT, READ, WIDE, false><<<grid((long long)t.W * ((t.n + span - 1) / span) * c.heads), 256, 0, st>>>(c, t, span);
+}
+
+template <bool FP8, int DT, bool READ>
+static void launch(const BrKvCache &c, const BrKvTokens &t, int rows, hipStream_t st) {
+  t.wide ? launch_wide<FP8, DT, READ, true>(c, t, rows, st) : launch_wide<FP8, DT, READ, false>(c, t, rows, st);
 }
 
 template <bool READ>
