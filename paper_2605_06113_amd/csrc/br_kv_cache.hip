@@ -3,8 +3,8 @@
 // Bound by memory: values are read once (append: twice, the second time from a cache) and written once.  The unit of work is a run, tokens
 // that stand together in the call's list and in one block, with a key head: nobody else writes that block's codes or scales, so there
 // are no atomics.  Lists of single tokens (decode steps) take a wave per token and head, long ones a block per 16 to 64 tokens and
-// head, whose four waves share a run or take runs of their own.  Values lie with their tokens side by side: a thread has two channels
-// of 16 tokens, reads them token by token (lanes side by side) and moves 16 bytes of each channel.
+// head, whose four waves share a run or take runs of their own.  Values lie with their tokens side by side: a thread turns 8 channels
+// of 4 tokens, 16 bytes of a token on one side and 4 of a channel on the other, its neighbours the tokens beside.
 #include "br_kv_device.h"
 
 #define BR_KV_LEAST 27u  // biased exponent of 2^-100, the smallest scale
@@ -178,7 +178,7 @@ __device__ __forceinline__ BrKvScale br_kv_scale(float top, bool bad, int off, f
   return z;
 }
 
-// NT threads (a wave, or a block that is all here) write a run.  red: 16 floats of LDS.  The first AT_ONCE rows of keys and 16 x 2 values
+// NT threads (a wave, or a block that is all here) write a run.  red: 16 floats of LDS.  The first AT_ONCE rows of keys and 4 x 8 values
 // of a thread (all, up to 64 tokens of 128 channels for a block) stay in registers between the maximum and the codes.
 template <bool FP8, int DT, bool WIDE, int NT>
 __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, int tid, float *red) {
@@ -190,18 +190,19 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
   const char *xk = (const char *)a.k + (u.t * a.k_token + (long long)u.h * a.k_head) * SIZE, *xv = (const char *)a.v + (u.t * a.v_token + (long long)u.h * a.v_head) * SIZE;
   const int k_token = (int)a.k_token, v_token = (int)a.v_token;
-  // values: channels vd and vd + 1 of the block's tokens 16 vg .. 16 vg + 15
-  const int vg0 = u.off >> 4, vgs = ((u.off + u.n - 1) >> 4) - vg0 + 1, vitems = vgs * pairs;
+  // values: 8 channels of the block's tokens 4 q .. 4 q + 3
+  const int vq0 = u.off >> 2, vqs = ((u.off + u.n - 1) >> 2) - vq0 + 1, vitems = vqs * chunks;
   float top_k = 0.0f, top_v = 0.0f;
   int bad = 0;
   BrKvRaw<DT, 8, WIDE> rk[AT_ONCE];
-  BrKvRaw<DT, 2, WIDE> rv[16];
+  BrKvRaw<DT, 8, WIDE> rv[4];
+  BrKvRaw<DT, 2, WIDE> rf;
   auto fetch_v = [&](int i) {
-    const int pair = i / vgs, g = vg0 + i - pair * vgs, d = 2 * pair, lo = u.off - 16 * g, hi = u.off + u.n - 16 * g;
-    const int at = (16 * g - u.off) * v_token + d;
+    const int oct = i / vqs, q = vq0 + i - oct * vqs, lo = u.off - 4 * q, hi = u.off + u.n - 4 * q;
+    const int at = (4 * q - u.off) * v_token + 8 * oct;
     // (places that get no new token take a neighbour's: no branches between the loads, nothing for the maximum)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) rv[j].fetch(xv, at + min(max(j, lo), hi - 1) * v_token);
+    for (int j = 0; j < 4; ++j) rv[j].fetch(xv, at + min(max(j, lo), hi - 1) * v_token);
   };
 #pragma unroll
   for (int m = 0; m < AT_ONCE; ++m) rk[m].fetch(xk, min(kj + m * kstep, u.n - 1) * k_token + kd);
@@ -210,14 +211,14 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   if (few) {
     for (int i = tid; i < u.n * pairs; i += NT) {
       const int j = i / pairs;
-      rv[0].fetch(xv, j * v_token + (i - j * pairs) * 2);
-      rv[0].look(top_v, bad, 2);
+      rf.fetch(xv, j * v_token + (i - j * pairs) * 2);
+      rf.look(top_v, bad, 2);
     }
   } else {
     for (int i = tid; i < vitems; i += NT) {
       fetch_v(i);
 #pragma unroll
-      for (int j = 0; j < 16; ++j) rv[j].look(top_v, bad, 2);
+      for (int j = 0; j < 4; ++j) rv[j].look(top_v, bad, 2);
     }
   }
 #pragma unroll
@@ -230,7 +231,7 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
 #pragma unroll
   for (int m = 0; m < AT_ONCE; ++m) rk[m].keep_raw();
 #pragma unroll
-  for (int j = 0; j < 16; ++j) rv[j].keep_raw();
+  for (int j = 0; j < 4; ++j) rv[j].keep_raw();
   top_k = br_kv_max64(top_k), top_v = br_kv_max64(top_v);
   bad = (__any(bad & 1) ? 1 : 0) | (__any(bad & 2) ? 2 : 0);
   if constexpr (NT > 64) {
@@ -262,8 +263,8 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
     put_k(j, x);
   }
 
-  if (zv.r != 1.0f) {  // earlier values: those in the first new group's 16 tokens too
-    for (int i = tid; i < (vg0 + 1) * D; i += NT) {
+  if (zv.r != 1.0f) {  // earlier values
+    for (int i = tid; i < ((u.off + 15) >> 4) * D; i += NT) {
       const int g = i / D, n = min(u.off - 16 * g, 16);
       br_u4 *at = (br_u4 *)(vc + ((long long)(i - g * D) << c.shift) + 16 * g);
       br_u4 x = *at;
@@ -280,8 +281,8 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   if (few) {
     for (int i = tid; i < u.n * pairs; i += NT) {
       const int j = i / pairs, d = (i - j * pairs) * 2;
-      if (u.n * pairs > NT) rv[0].fetch(xv, j * v_token + d);
-      const unsigned q = br_kv_code4<FP8>(zv.bad ? 0.0f : rv[0].get(0) * zv.inv, zv.bad ? 0.0f : rv[0].get(1) * zv.inv, 0.0f, 0.0f);
+      if (u.n * pairs > NT) rf.fetch(xv, j * v_token + d);
+      const unsigned q = br_kv_code4<FP8>(zv.bad ? 0.0f : rf.get(0) * zv.inv, zv.bad ? 0.0f : rf.get(1) * zv.inv, 0.0f, 0.0f);
       unsigned char *at = vc + ((long long)d << c.shift) + u.off + j;
       at[0] = (unsigned char)q, at[b] = (unsigned char)(q >> 8);
     }
@@ -289,23 +290,17 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   const bool again = vitems > NT;
   for (int i = tid; i < (few ? 0 : vitems); i += NT) {
     if (again) fetch_v(i);
-    const int pair = i / vgs, g = vg0 + i - pair * vgs, d = 2 * pair, lo = max(u.off - 16 * g, 0), hi = min(u.off + u.n - 16 * g, 16);  // new ones: lo .. hi - 1
-    unsigned char *at = vc + ((long long)d << c.shift) + 16 * g;
-    br_u4 y[2];
+    const int oct = i / vqs, q = vq0 + i - oct * vqs, lo = max(u.off - 4 * q, 0), hi = min(u.off + u.n - 4 * q, 4);  // new ones: lo .. hi - 1
+    unsigned char *at = vc + ((long long)(8 * oct) << c.shift) + 4 * q;
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        auto q = [&](int j) { return zv.bad ? 0.0f : rv[4 * m + j].get(k) * zv.inv; };
-        y[k][m] = br_kv_code4<FP8>(q(0), q(1), q(2), q(3));
+    for (int k = 0; k < 8; ++k) {
+      auto x = [&](int j) { return zv.bad ? 0.0f : rv[j].get(k) * zv.inv; };
+      const unsigned y = br_kv_code4<FP8>(x(0), x(1), x(2), x(3));
+      if (hi - lo == 4) {
+        *(unsigned *)(at + k * b) = y;
+      } else {
+        for (int j = lo; j < hi; ++j) at[k * b + j] = (unsigned char)(y >> (8 * j));
       }
-    if (hi - lo == 16) {
-      *(br_u4 *)at = y[0];
-      *(br_u4 *)(at + b) = y[1];
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (j >= lo && j < hi) at[j] = (unsigned char)(y[0][j / 4] >> (8 * (j & 3))), at[b + j] = (unsigned char)(y[1][j / 4] >> (8 * (j & 3)));
     }
   }
   if (tid == 0) c.ks[u.block] = zk.s, c.vs[u.block] = zv.s;
@@ -320,12 +315,13 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
   const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
   char *xk = (char *)a.k + (u.t * a.k_token + (long long)u.h * a.k_head) * SIZE, *xv = (char *)a.v + (u.t * a.v_token + (long long)u.h * a.v_head) * SIZE;
   const int k_token = (int)a.k_token, v_token = (int)a.v_token;
-  const int vg0 = u.off >> 4, vgs = ((u.off + u.n - 1) >> 4) - vg0 + 1, vitems = vgs * pairs;
-  br_u4 x0, x1;
+  // values: 8 channels of the block's tokens 4 q .. 4 q + 3
+  const int vq0 = u.off >> 2, vqs = ((u.off + u.n - 1) >> 2) - vq0 + 1, vitems = vqs * chunks;
+  unsigned x[8];
   auto fetch_v = [&](int i) {
-    const int pair = i / vgs, g = vg0 + i - pair * vgs, d = 2 * pair;
-    const unsigned char *at = vc + ((long long)d << c.shift) + 16 * g;
-    x0 = *(const br_u4 *)at, x1 = *(const br_u4 *)(at + b);
+    const int oct = i / vqs, q = vq0 + i - oct * vqs;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = *(const unsigned *)(vc + ((long long)(8 * oct + k) << c.shift) + 4 * q);
   };
   const bool few = NT == 64 && u.n <= BR_KV_FEW;
   if (few) {
@@ -348,13 +344,14 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
   }
   for (int i = tid; i < (few ? 0 : vitems); i += NT) {
     if (i != tid) fetch_v(i);
-    const int pair = i / vgs, g = vg0 + i - pair * vgs, d = 2 * pair, lo = u.off - 16 * g, hi = u.off + u.n - 16 * g;
-    const int at = (16 * g - u.off) * v_token + d;
+    const int oct = i / vqs, q = vq0 + i - oct * vqs, lo = u.off - 4 * q, hi = u.off + u.n - 4 * q, at = (4 * q - u.off) * v_token + 8 * oct;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
+    for (int j = 0; j < 4; ++j) {
       if (j < lo || j >= hi) continue;
-      const float y[2] = {in ? br_kv_value<FP8>(x0[j / 4] >> (8 * (j & 3))) * vs : 0.0f, in ? br_kv_value<FP8>(x1[j / 4] >> (8 * (j & 3))) * vs : 0.0f};
-      br_kv_store_out<DT, 2, WIDE>(xv, at + j * v_token, y);
+      float y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = in ? br_kv_value<FP8>(x[k] >> (8 * j)) * vs : 0.0f;
+      br_kv_store_out<DT, 8, WIDE>(xv, at + j * v_token, y);
     }
   }
 }
