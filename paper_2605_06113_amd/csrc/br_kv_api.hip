@@ -226,7 +226,7 @@ int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_atten
   p.least = 1, p.most = both ? few : INT32_MAX;
   if (!both || few > 0) {
     const int64_t most = both ? 16 : rows;
-    const int32_t rc = enqueue(ctx, [&] { launch(most <= 16 || c.head_dim > 128 ? BR_KV_TILE_16 : BR_KV_TILE_32); });
+    const int32_t rc = enqueue(ctx, [&] { launch(most <= 16 ? BR_KV_TILE_16 : most <= 32 ? BR_KV_TILE_32 : BR_KV_TILE_64); });
     if (rc != BR_OK || !both) return rc;
   }
   p.least = few + 1, p.most = INT32_MAX;

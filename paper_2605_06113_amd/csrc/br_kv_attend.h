@@ -23,6 +23,7 @@
 #include "br_kv_device.h"
 
 #define BR_KV_NEG (-__builtin_inff())
+#define BR_KV_LEAST_TILES 8  // of a block with many query rows: its pieces are large
 
 struct BrKvRow {
   int n, len, start;  // query tokens, cached tokens, first token
@@ -251,9 +252,9 @@ __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQue
   }
 }
 
-// HALF: blocks of 128 tokens, whose lines of values belong to two tiles.
+// ONCE: nobody else reads these codes; ONCE_V: nor these values' lines (blocks of 128 tokens have two tiles' in one).
 // Token tiles t .. stop - 1 of row r and key head h for the query rows from row0 on, whose positions lie in first_pos .. last_pos.
-template <int D, int NQ, bool FP8, bool HALF>
+template <int D, int NQ, bool FP8, bool ONCE_V, bool ONCE>
 __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int r, int h, int row0, int first_pos, int last_pos, int t, int stop,
                                             BrKvSums<D, NQ> &sums) {
   constexpr int NI = D / 64, REST = D % 64 / 32, NK = 2 * NI + REST, ND = D / 16;
@@ -293,7 +294,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) kc[s][i] = br_kv_load16<true>(at + 4 * s * D + 64 * i + 16 * g);
+      for (int i = 0; i < NI; ++i) kc[s][i] = br_kv_load16<ONCE>(at + 4 * s * D + 64 * i + 16 * g);
       if (REST) kx[s] = *(const uint2 *)(at + 4 * s * D + 64 * NI + 8 * g);
     }
   };
@@ -327,7 +328,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     {
       const unsigned char *at = p.v + ((((cache0 + (there(vid) ? vid : 0)) * p.kv_heads + h) * D + n) << p.shift) + (token & mask);
 #pragma unroll
-      for (int d = 0; d < ND; ++d) vc[d] = br_kv_load16<!HALF>(at + ((16 * d) << p.shift));
+      for (int d = 0; d < ND; ++d) vc[d] = br_kv_load16<ONCE_V>(at + ((16 * d) << p.shift));
     }
     const float ks = there(vid) ? br_kv_sound(ks1) : 0.0f, vs = there(vid) ? br_kv_sound(vs1) : 0.0f;
     const int have = there(vid) ? min(max(w.len - token, 0), 16) : 0;  // of the lane's tokens, those that exist
@@ -485,7 +486,8 @@ struct BrKvRuns {
   unsigned share, more;
   int per, workers;
 
-  __device__ __forceinline__ BrKvRuns(const BrKvAttend &p, Shared &sh, int most) : s(sh) {
+  // (a worker gets at least `least` tiles, if there are as many)
+  __device__ __forceinline__ BrKvRuns(const BrKvAttend &p, Shared &sh, int most, int least) : s(sh) {
     const int tid = threadIdx.x, lane = tid & 63;
     per = (p.n_rows + NT - 1) / NT;
     long long mine = 0;
@@ -506,15 +508,12 @@ struct BrKvRuns {
     if (tid == 0) s.before[0] = 0;
     __syncthreads();
     all = s.before[NT];
-    // all / most where there is a tile for each, by the reciprocal (exact behind the step up or down); else a tile each
-    workers = (int)max(1ll, min((long long)most, all));
-    share = 1, more = 0;
-    if (all >= most) {
-      long long q = (long long)((double)all * (1.0 / most)), left = all - q * most;
-      if (left < 0) --q, left += most;
-      if (left >= most) ++q, left -= most;
-      share = (unsigned)q, more = (unsigned)left;  // the first `more` have one tile more
-    }
+    // all / workers by the reciprocal (exact behind the step up or down)
+    workers = all >= (long long)most * least ? most : max(1, (int)all / least);
+    long long q = (long long)((double)all * (1.0 / workers)), left = all - q * workers;
+    if (left < 0) --q, left += workers;
+    if (left >= workers) ++q, left -= workers;
+    share = (unsigned)q, more = (unsigned)left;  // the first `more` have one tile more
   }
   __device__ __forceinline__ long long begin_of(int k) const {
     k = min(k, workers);
@@ -631,56 +630,56 @@ struct BrKvShare {
   int on, first, parts, r, h, qi;
 };
 
-// Few query rows: a run for each wave, NW waves to a block.  A wave's pieces (of a query tile that it takes up in the middle, and of one that
-// goes on in the next wave) wait in LDS until the block's end, where all waves join them, each its share of the channels.
-template <int D, int NQ, bool FP8, bool HALF, int NW, int WAVES>
+// Few query rows: a run for each SHARE waves, which have 16 query rows each, NW waves to a block.  Pieces of a run (of a query tile that it
+// takes up in the middle, and of one that goes on in the next run) wait in LDS until the block's end, where all waves join them,
+// each its share of the channels.  Bound by memory: each code comes once from there (waves of one run find it in the caches).
+template <int D, int SHARE, bool FP8, bool HALF, int NW, int WAVES>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
-  constexpr int TQ = 16 * NQ, NT = 64 * NW, ND = D / 16;
+  constexpr int TQ = 16 * SHARE, NT = 64 * NW, ND = D / 16, NR = NW / SHARE;  // NR: runs of a block
   __shared__ typename BrKvRuns<TQ, NT>::Shared shared;
-  __shared__ br_f4 kept[2 * NW * NQ * ND * 64];  // piece 2 k: taken up by wave k, 2 k + 1: begun by it
-  __shared__ float2 kept_ml[2 * NW * NQ * 16];
-  __shared__ int goes_on[NW], arrived[2];
-  __shared__ BrKvShare chains[NW + 1];  // of the query tile that wave k has begun; the last: of one that an earlier block has
+  __shared__ br_f4 kept[2 * NW * ND * 64];  // piece 2 k: taken up by run k, 2 k + 1: begun by it
+  __shared__ float2 kept_ml[2 * NW * 16];
+  __shared__ int goes_on[NR], arrived[2];
+  __shared__ BrKvShare chains[NR + 1];  // of the query tile that run k has begun; the last: of one that an earlier block has
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
-  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  BrKvRuns<TQ, NT> runs(p, shared, gridDim.x * NW);
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), rn = wv / SHARE, row = 16 * (wv % SHARE);  // the wave's run, its first query row of the tile
+  BrKvRuns<TQ, NT> runs(p, shared, gridDim.x * NR, 1);
   // runs that follow each other go to one XCD (blocks go round them), which has what they share in its L2
-  const int blocks = (runs.workers + NW - 1) / NW, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
+  const int blocks = (runs.workers + NR - 1) / NR, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
   if (wg >= blocks) return;
-  if (tid <= NW) chains[tid].on = 0;
+  if (tid <= NR) chains[tid].on = 0;
   __syncthreads();
-  const int me = wg * NW + wv;
+  const int me = wg * NR + rn;
   long long u = runs.begin_of(me);
   const long long end = runs.begin_of(me + 1);
 
   bool open = false;  // the query tile that was taken up goes on in the next wave
   {
     BrKvPlace<TQ, NT> at;
-    BrKvSums<D, NQ> s;
+    BrKvSums<D, 1> s;
     if (u < end && at.find(p, runs, u)) {
       for (;;) {
         const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg);
-        br_kv_tiles<D, NQ, FP8, HALF>(p, at.w, at.r, at.h, at.qi * TQ, at.pos_of(p, 0), at.pos_of(p, TQ - 1), at.t0 + a, min(at.t0 + b, at.t1), s);
+        const int rows_q = at.rows_q(p);
+        br_kv_tiles<D, 1, FP8, SHARE == 1 && !HALF, SHARE == 1>(p, at.w, at.r, at.h, at.qi * TQ + row, at.pos_of(p, row), at.pos_of(p, row + 15), at.t0 + a,
+                                                               row < rows_q ? min(at.t0 + b, at.t1) : 0, s);
         if (a == 0 && b == at.size) {
-          br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, 0, at.rows_q(p), s);
+          br_kv_result<D, 1, TQ>(p, at.w, at.h, at.qi, row, rows_q, s);
         } else {
-          const int piece = 2 * wv + (a == 0);
+          const int piece = (2 * rn + (a == 0)) * SHARE + wv % SHARE;
 #pragma unroll
-          for (int x = 0; x < NQ; ++x) {
+          for (int d = 0; d < ND; ++d) {
+            br_f4 y = s.o[0][d];
 #pragma unroll
-            for (int d = 0; d < ND; ++d) {
-              br_f4 y = s.o[x][d];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) y[j] *= s.c;
-              kept[((piece * NQ + x) * ND + d) * 64 + lane] = y;
-            }
-            if (g == 0) kept_ml[(piece * NQ + x) * 16 + n] = make_float2(s.m[x], s.l[x]);
+            for (int j = 0; j < 4; ++j) y[j] *= s.c;
+            kept[(piece * ND + d) * 64 + lane] = y;
           }
+          if (g == 0) kept_ml[piece * 16 + n] = make_float2(s.m[0], s.l[0]);
           open = a > 0 && b < at.size;
-          if (a == 0 || (wv == 0 && at.seg < u)) {
+          if (row == 0 && (a == 0 || rn == 0)) {
             BrKvShare c = {1, wg, 1, at.r, at.h, at.qi};
-            if (a > 0 || at.seg + at.size > runs.begin_of((wg + 1) * NW)) c.first = runs.owner_of(at.seg) / NW, c.parts = runs.owner_of(at.seg + at.size - 1) / NW - c.first + 1;
-            if (lane == 0) chains[a == 0 ? wv : NW] = c;
+            if (a > 0 || at.seg + at.size > runs.begin_of((wg + 1) * NR)) c.first = runs.owner_of(at.seg) / NR, c.parts = runs.owner_of(at.seg + at.size - 1) / NR - c.first + 1;
+            if (lane == 0) chains[a == 0 ? rn : NR] = c;
           }
         }
         u = at.seg + b;
@@ -688,33 +687,33 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
       }
     }
   }
-  if (lane == 0) goes_on[wv] = open;
+  if (lane == 0 && row == 0) goes_on[rn] = open;
   __syncthreads();
 
-  const unsigned on = (unsigned)__ballot(lane <= NW && chains[min(lane, NW)].on), going_on = (unsigned)__ballot(lane < NW && goes_on[min(lane, NW - 1)]);
+  const unsigned on = (unsigned)__ballot(lane <= NR && chains[min(lane, NR)].on), going_on = (unsigned)__ballot(lane < NR && goes_on[min(lane, NR - 1)]);
 #pragma unroll 1
   for (unsigned left = on; left; left &= left - 1) {
     const int c = __ffs(left) - 1;
     const BrKvShare chain = chains[c];
-    const int k0 = c < NW ? c + 1 : 0;  // the chain: piece 2 c + 1 (c < NW), then the pieces taken up by waves k0 .. k1
-    const int k1 = min(k0 + __ffs(~(going_on >> k0)) - 1, NW - 1);
+    const int k0 = c < NR ? c + 1 : 0;  // the chain: piece 2 c + 1 (c < NR), then the pieces taken up by runs k0 .. k1
+    const int k1 = min(k0 + __ffs(~(going_on >> k0)) - 1, NR - 1);
     auto member = [&](int k) { return k < k0 ? 2 * c + 1 : 2 * k; };
-    const int begin = c < NW ? k0 - 1 : k0;
+    const int begin = c < NR ? k0 - 1 : k0;
     const BrKvRow w = runs.row_of(p, chain.r);
     const int rows_q = (int)min((long long)TQ, (long long)w.n * p.group - (long long)chain.qi * TQ);
-    for (int it = wv; it < NQ * ND; it += NW) {
+    for (int it = wv; it < SHARE * ND; it += NW) {
       const int x = it / ND, d = it - x * ND, row = 16 * x + n;
       float top = BR_KV_NEG, l = 0.0f;
 #pragma unroll 4
       for (int k = begin; k <= k1; ++k) {
-        const float2 ml = kept_ml[(member(k) * NQ + x) * 16 + n];
+        const float2 ml = kept_ml[(member(k) * SHARE + x) * 16 + n];
         if (ml.y != 0.0f) top = fmaxf(top, ml.x);
       }
       br_f4 y[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll 4
       for (int k = begin; k <= k1; ++k) {
-        const float2 ml = kept_ml[(member(k) * NQ + x) * 16 + n];
-        const br_f4 v = kept[((member(k) * NQ + x) * ND + d) * 64 + lane];
+        const float2 ml = kept_ml[(member(k) * SHARE + x) * 16 + n];
+        const br_f4 v = kept[((member(k) * SHARE + x) * ND + d) * 64 + lane];
         const float e = ml.y != 0.0f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
         l += ml.y * e;
 #pragma unroll
@@ -726,7 +725,7 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
         br_kv_store<1>(p, w, chain.h, chain.qi * TQ + row, 16 * d + 4 * g, y, l != 0.0f ? 1.0f / l : 0.0f);
         if (d == 0 && g == 0) br_kv_store_lse(p, w, chain.h, chain.qi * TQ + row, top, l);
       } else {
-        const long long piece = (long long)(2 * wg + (c < NW)) * TQ + row;
+        const long long piece = (long long)(2 * wg + (c < NR)) * TQ + row;
         br_kv_put2(p.part + piece * D + 16 * d + 4 * g, y[0][0], y[0][1]);
         br_kv_put2(p.part + piece * D + 16 * d + 4 * g + 2, y[0][2], y[0][3]);
         if (d == 0 && g == 0) br_kv_put2(p.ml + piece * 2, top, l);
@@ -736,16 +735,16 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   br_kv_stores_done();
   __syncthreads();
   // the query tiles that other blocks have pieces of: at most one of an earlier block, and one that goes on in a later one
-  const unsigned going = (unsigned)__ballot(lane < NW && chains[min(lane, NW - 1)].on && chains[min(lane, NW - 1)].parts > 1);
-  const bool goes = going != 0, came = on >> NW & 1;
+  const unsigned going = (unsigned)__ballot(lane < NR && chains[min(lane, NR - 1)].on && chains[min(lane, NR - 1)].parts > 1);
+  const bool goes = going != 0, came = on >> NR & 1;
   const int which = goes ? __ffs(going) - 1 : 0;
   if (!goes && !came) return;
-  if (tid == 0 && came) arrived[0] = __hip_atomic_fetch_add(&p.arrived[chains[NW].first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (tid == 0 && came) arrived[0] = __hip_atomic_fetch_add(&p.arrived[chains[NR].first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   if (tid == 1 && goes) arrived[1] = __hip_atomic_fetch_add(&p.arrived[chains[which].first], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
 #pragma unroll 1
   for (int k = 0; k < 2; ++k) {
-    const BrKvShare c = chains[k ? which : NW];
+    const BrKvShare c = chains[k ? which : NR];
     if ((k ? !goes : !came) || arrived[k] != c.parts - 1) continue;
     const BrKvRow w = runs.row_of(p, c.r);
     br_kv_join<D, TQ, NT>(p, w, c.h, c.qi, (int)min((long long)TQ, (long long)w.n * p.group - (long long)c.qi * TQ), c.first, c.parts, kept, (float2 *)(kept + NT));
@@ -764,7 +763,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
   __shared__ br_h8 tile[2][(4 * NK + 2 * ND) * 64];
   __shared__ int arrived;
   const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
-  BrKvRuns<TQ, NT> runs(p, shared, gridDim.x);
+  BrKvRuns<TQ, NT> runs(p, shared, gridDim.x, BR_KV_LEAST_TILES);
   const int blocks = runs.workers, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
   if (wg >= blocks) return;
   long long u = runs.begin_of(wg);
@@ -915,12 +914,20 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
 }
 
 // WAVES on a SIMD, by the registers that the tile needs; PER blocks of NW waves on a compute unit
-template <int D, int NQ, int NW, int WAVES>
+template <int D, int SHARE, int NW, int WAVES>
 void br_kv_attend_few(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
   constexpr int PER = 4 * WAVES / NW;
   const int blocks = PER * cus < BR_KV_SPLIT_WGS ? PER * cus : BR_KV_SPLIT_WGS;
-  if (fp8) p.shift == 7 ? br_kv_k_attend<D, NQ, true, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p) : br_kv_k_attend<D, NQ, true, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
-  else p.shift == 7 ? br_kv_k_attend<D, NQ, false, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p) : br_kv_k_attend<D, NQ, false, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+  const bool half = SHARE == 1 && p.shift == 7;
+  if constexpr (SHARE == 1) {
+    if (half) {
+      if (fp8) br_kv_k_attend<D, SHARE, true, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+      else br_kv_k_attend<D, SHARE, false, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+      return;
+    }
+  }
+  if (fp8) br_kv_k_attend<D, SHARE, true, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+  else br_kv_k_attend<D, SHARE, false, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
 }
 
 template <int D, int NQ, int WAVES>
@@ -932,12 +939,11 @@ void br_kv_attend_rows(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
 
 template <int D>
 void br_kv_attend_dim(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st) {
-  // (a tile's launch skips the rows of the other: least, most)
-  if constexpr (D <= 128) {
-    if (tile == BR_KV_TILE_32) return br_kv_attend_few<D, 2, D <= 64 ? 8 : 4, D <= 64 ? 2 : 1>(p, fp8, cus, st);
-  }
-  if (tile == BR_KV_TILE_128) br_kv_attend_rows<D, 2, D <= 128 ? 2 : 1>(p, fp8, cus, st);
-  else br_kv_attend_few<D, 1, D <= 64 ? 12 : D <= 128 ? 8 : 4, D <= 64 ? 3 : D <= 128 ? 2 : 1>(p, fp8, cus, st);
+  constexpr int NW = D <= 64 ? 12 : D <= 128 ? 8 : 4, WAVES = D <= 64 ? 3 : D <= 128 ? 2 : 1;
+  if (tile == BR_KV_TILE_16) br_kv_attend_few<D, 1, NW, WAVES>(p, fp8, cus, st);
+  else if (tile == BR_KV_TILE_32) br_kv_attend_few<D, 2, NW, WAVES>(p, fp8, cus, st);
+  else if (tile == BR_KV_TILE_64) br_kv_attend_few<D, 4, NW, WAVES>(p, fp8, cus, st);
+  else br_kv_attend_rows<D, 2, D <= 128 ? 2 : 1>(p, fp8, cus, st);
 }
 
 #endif

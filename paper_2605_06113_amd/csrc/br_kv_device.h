@@ -67,7 +67,7 @@ void br_kv_launch_append(const BrKvCache &c, const BrKvTokens &t, int rows, bool
 void br_kv_launch_read(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st);
 
 // br_kv_attend_*.hip, one per head width
-enum { BR_KV_TILE_16 = 0, BR_KV_TILE_32 = 1, BR_KV_TILE_128 = 2 };  // rows of queries of a block's tile
+enum { BR_KV_TILE_16 = 0, BR_KV_TILE_32 = 1, BR_KV_TILE_64 = 2, BR_KV_TILE_128 = 3 };  // rows of queries of a block's tile
 void br_kv_launch_attend_64(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
 void br_kv_launch_attend_96(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
 void br_kv_launch_attend_128(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
