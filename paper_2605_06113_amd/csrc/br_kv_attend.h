@@ -53,16 +53,17 @@ __device__ __forceinline__ int br_kv_span(const BrKvAttend &p, const BrKvRow &w,
   return max(1, t1 - t0);
 }
 
-// Tiles of one row and key head.
+// Query tiles of one row and key head, their token tiles, and the most that one of them has.
 template <int TQ>
-__device__ __forceinline__ long long br_kv_row_tiles(const BrKvAttend &p, const BrKvRow &w) {
+__device__ __forceinline__ int br_kv_row_tiles(const BrKvAttend &p, const BrKvRow &w, long long &tiles, int &most) {
   const int nq = (int)(((long long)w.n * p.group + TQ - 1) / TQ);
-  long long s = 0;
+  tiles = 0, most = 0;
   for (int qi = 0; qi < nq; ++qi) {
     int t0, t1;
-    s += br_kv_span<TQ>(p, w, qi, t0, t1);
+    const int size = br_kv_span<TQ>(p, w, qi, t0, t1);
+    tiles += size, most = max(most, size);
   }
-  return s;
+  return nq;
 }
 
 // 16 codes; ONCE: that nobody else of the launch reads
@@ -474,47 +475,81 @@ __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w
   }
 }
 
-// The division of a call's tiles: `workers` of them (waves or blocks) get runs that differ by one tile at most.
-template <int TQ, int NT>
+// The division of a call's tiles among `workers` (waves, groups of waves, or blocks: NR to a block).  Where there are few query tiles and
+// none is much longer than an equal share, each goes to a block, in NR parts: nothing is left to be joined through memory, which
+// takes about as long as SLACK tiles.  Else the workers get runs of tiles that differ by one at most.  What is dealt are units: tiles, or a
+// query tile's NR parts.
+template <int TQ, int NT, int NR, int SLACK>
 struct BrKvRuns {
   struct Shared {
     long long before[NT + 1], wave_sum[NT / 64];
+    int wave_parts[NT / 64], wave_most[NT / 64];
     int4 row[NT];
   };
   Shared &s;
   long long all;
   unsigned share, more;
   int per, workers;
+  bool parts;  // the units are parts of query tiles
 
   // (a worker gets at least `least` tiles, if there are as many)
-  __device__ __forceinline__ BrKvRuns(const BrKvAttend &p, Shared &sh, int most, int least) : s(sh) {
+  __device__ __forceinline__ BrKvRuns(const BrKvAttend &p, Shared &sh, int blocks, int least) : s(sh) {
     const int tid = threadIdx.x, lane = tid & 63;
     per = (p.n_rows + NT - 1) / NT;
     long long mine = 0;
+    int mine_q = 0, most = 0;
     for (int r = tid * per; r < min(p.n_rows, (tid + 1) * per); ++r) {
       const BrKvRow w = br_kv_row(p, r);
-      if (w.n > 0) mine += br_kv_row_tiles<TQ>(p, w) * p.kv_heads;
       s.row[tid] = make_int4(w.n, w.len, w.start, 0);
+      if (w.n <= 0) continue;
+      long long tiles;
+      int longest;
+      mine_q += br_kv_row_tiles<TQ>(p, w, tiles, longest);
+      mine += tiles, most = max(most, longest);
     }
+    mine *= p.kv_heads;
+    // (query tiles as far as they could go to a block each)
+    mine_q = min(mine_q, 4096) * p.kv_heads * NR;
     long long sum = mine;
+    int sum_q = mine_q;
     for (int d = 1; d < 64; d <<= 1) {
       const long long o = __shfl_up(sum, d, 64);
-      if (lane >= d) sum += o;
+      const int q = __shfl_up(sum_q, d, 64);
+      if (lane >= d) sum += o, sum_q = min(sum_q + q, 1 << 28);
+      most = max(most, __shfl_xor(most, d, 64));
     }
-    if (lane == 63) s.wave_sum[tid >> 6] = sum;
+    if (lane == 63) s.wave_sum[tid >> 6] = sum, s.wave_parts[tid >> 6] = sum_q, s.wave_most[tid >> 6] = most;
     __syncthreads();
-    for (int k = 0; k < (tid >> 6); ++k) sum += s.wave_sum[k];
-    s.before[tid + 1] = sum;
-    if (tid == 0) s.before[0] = 0;
-    __syncthreads();
-    all = s.before[NT];
-    // all / workers by the reciprocal (exact behind the step up or down)
-    workers = all >= (long long)most * least ? most : max(1, (int)all / least);
-    long long q = (long long)((double)all * (1.0 / workers)), left = all - q * workers;
+    long long total = 0;
+    int total_q = 0;
+#pragma unroll
+    for (int k = 0; k < NT / 64; ++k) {
+      if (k < (tid >> 6)) sum += s.wave_sum[k], sum_q += s.wave_parts[k];
+      total += s.wave_sum[k], total_q = min(total_q + s.wave_parts[k], 1 << 28), most = max(most, s.wave_most[k]);
+    }
+    const int workers_most = blocks * NR;
+    workers = total >= (long long)workers_most * least ? workers_most : max(1, (int)total / least);
+    long long q = (long long)((double)total * (1.0 / workers)), left = total - q * workers;  // (exact behind the step up or down)
     if (left < 0) --q, left += workers;
     if (left >= workers) ++q, left -= workers;
     share = (unsigned)q, more = (unsigned)left;  // the first `more` have one tile more
+    all = total;
+    parts = total_q <= workers_most && (most + NR - 1) / NR <= (int)min(q, 1ll << 20) + SLACK;
+    if (parts) workers = total_q, all = total_q, share = 1, more = 0, sum = sum_q;
+    s.before[tid + 1] = sum;
+    if (tid == 0) s.before[0] = 0;
+    __syncthreads();
   }
+  // units of one row and key head, and of one query tile of `size` tiles
+  __device__ __forceinline__ long long units_of(const BrKvAttend &p, const BrKvRow &w) const {
+    if (w.n <= 0) return 0;
+    long long tiles;
+    int most;
+    if (parts) return (int)(((long long)w.n * p.group + TQ - 1) / TQ) * NR;
+    br_kv_row_tiles<TQ>(p, w, tiles, most);
+    return tiles;
+  }
+  __device__ __forceinline__ int units_of(int size) const { return parts ? NR : size; }
   __device__ __forceinline__ long long begin_of(int k) const {
     k = min(k, workers);
     return min((unsigned long long)all, (unsigned long long)(unsigned)k * share + min((unsigned)k, more));
@@ -543,19 +578,19 @@ struct BrKvRuns {
 };
 
 // Where a run stands: query tile qi of row r and key head h, tiles t0 .. t1 - 1 of its tokens, the first of which is tile `seg` of the call.
-template <int TQ, int NT>
+template <int TQ, int NT, class Runs>
 struct BrKvPlace {
   BrKvRow w;
   long long base, seg, tiles;
-  int r, h, qi, size, t0, t1;
+  int r, h, qi, size, t0, t1;  // size: units of the query tile
 
-  __device__ __forceinline__ bool find(const BrKvAttend &p, const BrKvRuns<TQ, NT> &runs, long long u) {
+  __device__ __forceinline__ bool find(const BrKvAttend &p, const Runs &runs, long long u) {
     const int lo = runs.find(u);
     r = lo * runs.per;
     base = runs.s.before[lo];
     for (; r < p.n_rows; ++r) {
       w = runs.row_of(p, r);
-      tiles = w.n > 0 ? br_kv_row_tiles<TQ>(p, w) : 0;
+      tiles = runs.units_of(p, w);
       if (u < base + tiles * p.kv_heads) break;
       base += tiles * p.kv_heads;
     }
@@ -565,11 +600,11 @@ struct BrKvPlace {
     while (u - base >= (h + 1) * tiles) ++h;
     qi = 0;
     seg = base + h * tiles;
-    size = br_kv_span<TQ>(p, w, 0, t0, t1);
-    while (u >= seg + size) seg += size, size = br_kv_span<TQ>(p, w, ++qi, t0, t1);
+    size = runs.units_of(br_kv_span<TQ>(p, w, 0, t0, t1));
+    while (u >= seg + size) seg += size, size = runs.units_of(br_kv_span<TQ>(p, w, ++qi, t0, t1));
     return true;
   }
-  __device__ __forceinline__ bool next(const BrKvAttend &p, const BrKvRuns<TQ, NT> &runs) {
+  __device__ __forceinline__ bool next(const BrKvAttend &p, const Runs &runs) {
     seg += size;
     if (seg < base + (h + 1) * tiles) {
       ++qi;
@@ -580,15 +615,17 @@ struct BrKvPlace {
         base += tiles * p.kv_heads;
         while (++r < p.n_rows) {
           w = runs.row_of(p, r);
-          tiles = w.n > 0 ? br_kv_row_tiles<TQ>(p, w) : 0;
+          tiles = runs.units_of(p, w);
           if (tiles > 0) break;
         }
         if (r >= p.n_rows) return false;
       }
     }
-    size = br_kv_span<TQ>(p, w, qi, t0, t1);
+    size = runs.units_of(br_kv_span<TQ>(p, w, qi, t0, t1));
     return true;
   }
+  // the first tile of its unit k (one past the last, for k = size)
+  __device__ __forceinline__ int tile_of(const Runs &runs, int k) const { return runs.parts ? t0 + (int)((long long)(t1 - t0) * k / size) : min(t0 + k, t1); }
   __device__ __forceinline__ int rows_q(const BrKvAttend &p) const { return (int)min((long long)TQ, (long long)w.n * p.group - (long long)qi * TQ); }
   // positions of the first and the last query of rows a .. b of the tile
   __device__ __forceinline__ int pos_of(const BrKvAttend &p, int row) const { return w.len - w.n + min(w.n - 1, br_kv_token(p, qi * TQ + row)); }
@@ -636,14 +673,15 @@ struct BrKvShare {
 template <int D, int SHARE, bool FP8, bool HALF, int NW, int WAVES>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   constexpr int TQ = 16 * SHARE, NT = 64 * NW, ND = D / 16, NR = NW / SHARE;  // NR: runs of a block
-  __shared__ typename BrKvRuns<TQ, NT>::Shared shared;
+  using Runs = BrKvRuns<TQ, NT, NR, 6>;
+  __shared__ typename Runs::Shared shared;
   __shared__ br_f4 kept[2 * NW * ND * 64];  // piece 2 k: taken up by run k, 2 k + 1: begun by it
   __shared__ float2 kept_ml[2 * NW * 16];
   __shared__ int goes_on[NR], arrived[2];
   __shared__ BrKvShare chains[NR + 1];  // of the query tile that run k has begun; the last: of one that an earlier block has
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), rn = wv / SHARE, row = 16 * (wv % SHARE);  // the wave's run, its first query row of the tile
-  BrKvRuns<TQ, NT> runs(p, shared, gridDim.x * NR, 1);
+  Runs runs(p, shared, gridDim.x, 1);
   // runs that follow each other go to one XCD (blocks go round them), which has what they share in its L2
   const int blocks = (runs.workers + NR - 1) / NR, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
   if (wg >= blocks) return;
@@ -655,14 +693,14 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
 
   bool open = false;  // the query tile that was taken up goes on in the next wave
   {
-    BrKvPlace<TQ, NT> at;
+    BrKvPlace<TQ, NT, Runs> at;
     BrKvSums<D, 1> s;
     if (u < end && at.find(p, runs, u)) {
       for (;;) {
         const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg);
         const int rows_q = at.rows_q(p);
-        br_kv_tiles<D, 1, FP8, SHARE == 1 && !HALF, SHARE == 1>(p, at.w, at.r, at.h, at.qi * TQ + row, at.pos_of(p, row), at.pos_of(p, row + 15), at.t0 + a,
-                                                               row < rows_q ? min(at.t0 + b, at.t1) : 0, s);
+        br_kv_tiles<D, 1, FP8, SHARE == 1 && !HALF, SHARE == 1>(p, at.w, at.r, at.h, at.qi * TQ + row, at.pos_of(p, row), at.pos_of(p, row + 15), at.tile_of(runs, a),
+                                                               row < rows_q ? at.tile_of(runs, b) : 0, s);
         if (a == 0 && b == at.size) {
           br_kv_result<D, 1, TQ>(p, at.w, at.h, at.qi, row, rows_q, s);
         } else {
@@ -759,16 +797,17 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
 template <int D, int NQ, bool FP8, int WAVES>
 __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) {
   constexpr int TQ = 64 * NQ, NT = 256, NI = D / 64, REST = D % 64 / 32, NK = D / 32, ND = D / 16, VG = (ND + 3) / 4;  // VG: groups of 16 channels of values that a wave brings
-  __shared__ typename BrKvRuns<TQ, NT>::Shared shared;
+  using Runs = BrKvRuns<TQ, NT, 1, 8>;
+  __shared__ typename Runs::Shared shared;
   __shared__ br_h8 tile[2][(4 * NK + 2 * ND) * 64];
   __shared__ int arrived;
   const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
-  BrKvRuns<TQ, NT> runs(p, shared, gridDim.x, BR_KV_LEAST_TILES);
+  Runs runs(p, shared, gridDim.x, BR_KV_LEAST_TILES);
   const int blocks = runs.workers, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
   if (wg >= blocks) return;
   long long u = runs.begin_of(wg);
   const long long end = runs.begin_of(wg + 1);
-  BrKvPlace<TQ, NT> at;
+  BrKvPlace<TQ, NT, Runs> at;
   if (u >= end || !at.find(p, runs, u)) return;
   const int kg = n >> 2, kr = n & 3, mask = (1 << p.shift) - 1;
   auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
@@ -777,7 +816,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
     const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg), rows_q = at.rows_q(p), row = 16 * NQ * wv;
     const bool whole = a == 0 && b == at.size;
     const int first_pos = scalar(at.pos_of(p, row)), last_pos = scalar(at.pos_of(p, row + 16 * NQ - 1)), h = scalar(at.h), r = scalar(at.r), len = scalar(at.w.len);
-    const int first = scalar(at.t0 + a), stop = scalar(min(at.t0 + b, at.t1));
+    const int first = scalar(at.tile_of(runs, a)), stop = scalar(at.tile_of(runs, b));
     const bool busy = row < rows_q;
     BrKvSums<D, NQ> s;
     float cmax = 0.0f, cinv = 0.0f;
