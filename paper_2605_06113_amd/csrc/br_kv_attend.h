@@ -504,20 +504,25 @@ struct BrKvRuns {
       if (w.n <= 0) continue;
       long long tiles;
       int longest;
-      mine_q += br_kv_row_tiles<TQ>(p, w, tiles, longest);
+      mine_q = min(mine_q + br_kv_row_tiles<TQ>(p, w, tiles, longest), 4096);
       mine += tiles, most = max(most, longest);
     }
     mine *= p.kv_heads;
     // (query tiles as far as they could go to a block each)
-    mine_q = min(mine_q, 4096) * p.kv_heads * NR;
+    mine_q *= p.kv_heads * NR;
     long long sum = mine;
-    int sum_q = mine_q;
-    for (int d = 1; d < 64; d <<= 1) {
-      const long long o = __shfl_up(sum, d, 64);
-      const int q = __shfl_up(sum_q, d, 64);
-      if (lane >= d) sum += o, sum_q = min(sum_q + q, 1 << 28);
-      most = max(most, __shfl_xor(most, d, 64));
+    mine_q = min(mine_q, 1 << 20);
+    const int sum_lane = br_kv_wave_scan(mine_q);
+    most = (int)br_kv_max64((float)most);
+    if (!__any(mine >> 24 != 0)) {
+      sum = br_kv_wave_scan((int)mine);
+    } else {  // (sums beyond 32 bits)
+      for (int d = 1; d < 64; d <<= 1) {
+        const long long o = __shfl_up(sum, d, 64);
+        if (lane >= d) sum += o;
+      }
     }
+    int sum_q = sum_lane;
     if (lane == 63) s.wave_sum[tid >> 6] = sum, s.wave_parts[tid >> 6] = sum_q, s.wave_most[tid >> 6] = most;
     __syncthreads();
     long long total = 0;
@@ -525,7 +530,7 @@ struct BrKvRuns {
 #pragma unroll
     for (int k = 0; k < NT / 64; ++k) {
       if (k < (tid >> 6)) sum += s.wave_sum[k], sum_q += s.wave_parts[k];
-      total += s.wave_sum[k], total_q = min(total_q + s.wave_parts[k], 1 << 28), most = max(most, s.wave_most[k]);
+      total += s.wave_sum[k], total_q += s.wave_parts[k], most = max(most, s.wave_most[k]);
     }
     const int workers_most = blocks * NR;
     workers = total >= (long long)workers_most * least ? workers_most : max(1, (int)total / least);

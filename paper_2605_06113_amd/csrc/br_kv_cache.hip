@@ -145,17 +145,6 @@ struct BrKvRun {
   int h, off, n;
 };
 
-// Over the wave: within rows of 16 lanes by their neighbours and mirrors, between rows by exchanges
-__device__ __forceinline__ float br_kv_max64(float x) {
-#define BR_KV_STEP(CTRL) x = fmaxf(x, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), CTRL, 0xf, 0xf, true)))
-  BR_KV_STEP(0xB1);   // lane ^ 1
-  BR_KV_STEP(0x4E);   // lane ^ 2
-  BR_KV_STEP(0x141);  // mirrored in 8
-  BR_KV_STEP(0x140);  // mirrored in 16
-#undef BR_KV_STEP
-  return br_kv_max4(x);
-}
-
 // The scale of the new tokens' block: `top` of them, `bad`: one is not finite.  r: what earlier codes are multiplied by.
 struct BrKvScale {
   float inv, s, r;

@@ -114,6 +114,30 @@ __device__ __forceinline__ float br_kv_max4(float x) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// Over the wave: within rows of 16 lanes by their neighbours and mirrors, between rows by exchanges
+__device__ __forceinline__ float br_kv_max64(float x) {
+#define BR_KV_STEP(CTRL) x = fmaxf(x, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), CTRL, 0xf, 0xf, true)))
+  BR_KV_STEP(0xB1);   // lane ^ 1
+  BR_KV_STEP(0x4E);   // lane ^ 2
+  BR_KV_STEP(0x141);  // mirrored in 8
+  BR_KV_STEP(0x140);  // mirrored in 16
+#undef BR_KV_STEP
+  return br_kv_max4(x);
+}
+
+// Inclusive sum over the wave, in the vector registers: within rows of 16 lanes, then the rows' last ones handed on
+__device__ __forceinline__ int br_kv_wave_scan(int x) {
+#define BR_KV_STEP(CTRL, ROWS) x += __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false)
+  BR_KV_STEP(0x111, 0xf);  // from 1 lane below
+  BR_KV_STEP(0x112, 0xf);
+  BR_KV_STEP(0x114, 0xf);
+  BR_KV_STEP(0x118, 0xf);
+  BR_KV_STEP(0x142, 0xa);  // rows 1 and 3: the last of the row below
+  BR_KV_STEP(0x143, 0xc);  // rows 2 and 3: the last of row 1
+#undef BR_KV_STEP
+  return x;
+}
+
 // A block's scale; one that is none (below zero or not finite) makes NaN of what is read with it.
 __device__ __forceinline__ float br_kv_sound(float s) { return s >= 0.0f && s < __builtin_inff() ? s : __builtin_nanf(""); }
 

@@ -30,19 +30,6 @@ __global__ __launch_bounds__(256) void br_kv_k_load(BrKvTables t, const int *len
   }
 }
 
-// Inclusive sum over the wave, in the vector registers: within rows of 16 lanes, then the rows' last ones handed on
-__device__ __forceinline__ int br_kv_wave_scan(int x) {
-#define BR_KV_STEP(CTRL, ROWS) x += __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false)
-  BR_KV_STEP(0x111, 0xf);  // from 1 lane below
-  BR_KV_STEP(0x112, 0xf);
-  BR_KV_STEP(0x114, 0xf);
-  BR_KV_STEP(0x118, 0xf);
-  BR_KV_STEP(0x142, 0xa);  // rows 1 and 3: the last of the row below
-  BR_KV_STEP(0x143, 0xc);  // rows 2 and 3: the last of row 1
-#undef BR_KV_STEP
-  return x;
-}
-
 // Inclusive sums of K values each over the block's threads; total: all of them.  One barrier (part: 2 x K x NT / 64 words, used in turn).
 template <int NT, int K>
 __device__ __forceinline__ void br_kv_scan(int (&x)[K], int (&total)[K], int *part, int &turn) {
