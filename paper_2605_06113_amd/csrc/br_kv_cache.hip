@@ -2,8 +2,8 @@
 //
 // Bound by memory: values are read once (append: twice, the second time from a cache) and written once.  The unit of work is a run, tokens
 // that stand together in the call's list and in one block, with a key head: nobody else writes that block's codes or scales, so there
-// are no atomics.  Lists of single tokens (decode steps) take a wave per token and head, long ones a block per 16 to 64 tokens and
-// head, whose four waves share a run or take runs of their own.  Values lie with their tokens side by side: a thread turns 8 channels
+// are no atomics.  A block has 4 to 64 tokens of the list and a head; its four
+// waves share a run or take runs of their own.  Values lie with their tokens side by side: a thread turns 8 channels
 // of 4 tokens, 16 bytes of a token on one side and 4 of a channel on the other, its neighbours the tokens beside.
 #include "br_kv_device.h"
 
@@ -356,26 +356,25 @@ __device__ __forceinline__ unsigned long long br_kv_heads(const int *slot, int t
   return __ballot(head);
 }
 
-// `span` tokens of a list (at most 64) and a key head for a block, or one for a wave (WAVE).
-template <bool FP8, int DT, bool READ, bool WIDE, bool WAVE>
-__global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a, int span) {
+// `span` tokens of a list (at most 64) and a key head for a block.  `grain`: tokens that a run may have, less one (append: a block's).
+template <bool FP8, int DT, bool READ, bool WIDE>
+__global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a, int span, int grain) {
   __shared__ float red[16];
-  if (WAVE) span = 1;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, b1 = (1 << c.shift) - 1, slots = c.n_blocks << c.shift;
   const int spans = (a.n + span - 1) / span;
-  const long long units = (long long)a.W * spans * c.heads, step = WAVE ? (long long)gridDim.x * 4 : gridDim.x;
-  for (long long id = WAVE ? (long long)blockIdx.x * 4 + wv : blockIdx.x; id < units; id += step) {
+  const long long units = (long long)a.W * spans * c.heads;
+  for (long long id = blockIdx.x; id < units; id += gridDim.x) {
     const long long part = id / c.heads;
     BrKvRun u;
     u.h = (int)(id - part * c.heads);
     const int w = (int)(part / spans), t0 = (int)(part - (long long)w * spans) * span;
     const int *slot = a.slot + (long long)w * a.n;
-    // heads of the span's tokens, and of those that its last run may reach (a block's more)
-    unsigned long long heads[3] = {br_kv_heads(slot, t0, a.n, slots, b1), ~0ull, ~0ull};
-    if (span + b1 + 1 > 64) heads[1] = br_kv_heads(slot, t0 + 64, a.n, slots, b1);
-    if (span + b1 + 1 > 128) heads[2] = br_kv_heads(slot, t0 + 128, a.n, slots, b1);
+    // heads of the span's tokens, and of those that its last run may reach (a grain more)
+    unsigned long long heads[3] = {br_kv_heads(slot, t0, a.n, slots, grain), ~0ull, ~0ull};
+    if (span + grain + 1 > 64) heads[1] = br_kv_heads(slot, t0 + 64, a.n, slots, grain);
+    if (span + grain + 1 > 128) heads[2] = br_kv_heads(slot, t0 + 128, a.n, slots, grain);
     unsigned long long left = heads[0] & (~0ull >> (64 - min(span, a.n - t0)));
-    const bool apart = !WAVE && __popcll(left) > 2;  // several short runs: one for each wave
+    const bool apart = __popcll(left) > 2;  // several short runs: one for each wave
     int turn = 0;
     for (; left; left &= left - 1, ++turn) {
       if (apart && (turn & 3) != wv) continue;
@@ -386,14 +385,14 @@ __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a,
       const bool in = s >= 0 && s < slots;
       if (!READ && !in) continue;
       u.t = (long long)w * a.n + t0 + k;
-      u.n = in ? min(end - k, b1 + 1) : 1;
+      u.n = in ? min(end - k, grain + 1) : 1;
       u.off = in ? s & b1 : 0;
       u.block = ((long long)w * c.n_blocks + (in ? s >> c.shift : 0)) * c.heads + u.h;
       if constexpr (READ) {
-        if (WAVE || apart) br_kv_read_run<FP8, DT, WIDE, 64>(c, a, u, in, lane);
+        if (apart) br_kv_read_run<FP8, DT, WIDE, 64>(c, a, u, in, lane);
         else br_kv_read_run<FP8, DT, WIDE, 256>(c, a, u, in, threadIdx.x);
       } else {
-        if (WAVE || apart) br_kv_append_run<FP8, DT, WIDE, 64>(c, a, u, lane, red);
+        if (apart) br_kv_append_run<FP8, DT, WIDE, 64>(c, a, u, lane, red);
         else br_kv_append_run<FP8, DT, WIDE, 256>(c, a, u, threadIdx.x, red);
       }
     }
@@ -402,13 +401,13 @@ __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a,
 
 template <bool FP8, int DT, bool READ, bool WIDE>
 static void launch_wide(const BrKvCache &c, const BrKvTokens &t, int rows, hipStream_t st) {
-  const long long tokens = (long long)t.W * t.n * c.heads;
-  auto grid = [](long long n) { return (unsigned)(n < 1 ? 1 : n > 1 << 20 ? 1 << 20 : n); };
-  // a wave for each token and head while they fit the chip about once; most waves of a longer list would begin no run.  A list of
-  // more than a few tokens a row has runs of whole blocks: 64 tokens are four runs of 16, one for each wave, or at most two longer ones
-  const int span = t.n > 4 * rows ? (c.shift == 5 ? 32 : 64) : 16;
-  if (tokens <= 16384) br_kv_k_tokens<FP8, DT, READ, WIDE, true><<<grid((tokens + 3) / 4), 256, 0, st>>>(c, t, 1);
-  else br_kv_k_tokens<FP8, DT, READ, WIDE, false><<<grid((long long)t.W * ((t.n + span - 1) / span) * c.heads), 256, 0, st>>>(c, t, span);
+  // Short lists: four tokens to a block, so that a decode step's have a wave each and a prompt's runs a block each, read in pieces of 16.
+  // Long ones would have too many blocks that find nothing: of more than a few tokens a row, which are runs of whole blocks, 64 are
+  // four runs of 16, one for each wave, or at most two longer ones.
+  const bool few = (long long)t.W * t.n * c.heads <= 16384;
+  const int span = few ? 4 : t.n > 4 * rows ? (c.shift == 5 ? 32 : 64) : 16, block = 1 << c.shift, grain = READ && few ? 15 : block - 1;
+  const long long blocks = (long long)t.W * ((t.n + span - 1) / span) * c.heads;
+  br_kv_k_tokens<FP8, DT, READ, WIDE><<<(unsigned)(blocks > 1 << 20 ? 1 << 20 : blocks), 256, 0, st>>>(c, t, span, grain);
 }
 
 template <bool FP8, int DT, bool READ>
