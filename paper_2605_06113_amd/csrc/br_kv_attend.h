@@ -104,9 +104,34 @@ __device__ __forceinline__ void br_kv_store_lse(const BrKvAttend &p, const BrKvR
   p.lse[(long long)t * p.kv_heads * p.group + h * p.group + ri - i * p.group] = l == 0.0f ? BR_KV_NEG : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
 
-// Pieces go from block to block past the L2s that the XCDs do not share, 8 bytes at a time; the writer waits for its stores before it
-// says that it has delivered.  (Plain stores between fences of the device cost more than the attention: the fences empty
-// whole L2s, 144 rows 390 us.)
+// Pieces go from block to block past the L2s that the XCDs do not share; the writer waits for its stores before it says that it has
+// delivered.  (Plain stores between fences of the device cost more than the attention: the fences empty whole L2s, 144 rows 390 us.)
+// Sums go 16 bytes a lane, in the order in which the lanes have them: piece after piece of TQ rows, 16 rows' channels 16 d + 4 g
+// .. + 3 side by side; of a query tile of fewer rows, so many.  (8 bytes at a time, row after row, every store is half of each of
+// 16 lines: 48 rows of 80 queries and 7 key heads of 256 channels 112 us.)
+template <int D, int TQ>
+struct BrKvPieces {
+  typedef unsigned u4 __attribute__((ext_vector_type(4)));
+  static constexpr int PAST_L2 = 16;  // (sc1)
+  __amdgpu_buffer_rsrc_t all;
+  int rows, n16;  // rows side by side
+  __device__ __forceinline__ BrKvPieces(const BrKvAttend &p, int rows_q)
+      : all(__builtin_amdgcn_make_buffer_rsrc(p.part, 0, 2 * BR_KV_SPLIT_WGS * TQ * D * 4, 0x00020000)), rows(min(rows_q, 16)), n16((rows_q + 15) / 16) {}
+  __device__ __forceinline__ int items() const { return n16 * (D / 4) * rows; }
+  __device__ __forceinline__ int item(int x, int d, int g, int n) const { return ((x * (D / 16) + d) * 4 + g) * rows + n; }
+  // row and first channel of an item
+  __device__ __forceinline__ void place(int item, int &row, int &channel) const {
+    const int c = rows == 16 ? item >> 4 : (int)((unsigned)item / (unsigned)rows), x = c / (D / 4);
+    row = 16 * x + item - c * rows, channel = 4 * (c - x * (D / 4));
+  }
+  __device__ __forceinline__ void put(int piece, int item, br_f4 y) const {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, y), all, (piece * (TQ * D / 4) + item) * 16, 0, PAST_L2);
+  }
+  __device__ __forceinline__ br_f4 get(int piece, int item) const {
+    return __builtin_bit_cast(br_f4, __builtin_amdgcn_raw_buffer_load_b128(all, (piece * (TQ * D / 4) + item) * 16, 0, PAST_L2));
+  }
+};
+
 __device__ __forceinline__ void br_kv_put2(float *at, float x, float y) {
   __hip_atomic_store((unsigned long long *)at, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -396,7 +421,8 @@ template <int D, int TQ, int NT>
 __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int rows_q, int first, int parts, br_f4 *sums, float2 *ml) {
   // few rows have many pieces (up to a block of the launch each), many rows few: places asked for at once are AT_ONCE pieces of ROWS rows
   constexpr int ROWS = TQ > 32 ? 4 : 1, AT_ONCE = TQ > 32 ? 2 : 8, STEP = NT * ROWS;
-  const int tid = threadIdx.x, items = rows_q * (D / 4), S = items < NT ? max(1, NT / items) : 1;
+  const BrKvPieces<D, TQ> pieces(p, rows_q);
+  const int tid = threadIdx.x, items = pieces.items(), S = items < NT ? max(1, NT / items) : 1;
   for (int at0 = tid; at0 < max(items, NT); at0 += STEP) {
     br_f4 ys[ROWS];
     float ms[ROWS], ls[ROWS];
@@ -404,16 +430,19 @@ __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w
     for (int q = 0; q < ROWS; ++q) ys[q] = br_f4{0.0f, 0.0f, 0.0f, 0.0f}, ms[q] = ls[q] = 0.0f;
     const int k0 = at0 / items;
     for (int k = k0; k < (k0 < S ? parts : 0); k += S * AT_ONCE) {
-      float2 x[ROWS][AT_ONCE], v0[ROWS][AT_ONCE], v1[ROWS][AT_ONCE];
+      float2 x[ROWS][AT_ONCE];
+      br_f4 v[ROWS][AT_ONCE];
 #pragma unroll
       for (int q = 0; q < ROWS; ++q) {
-        const int it = S > 1 ? at0 % items : min(at0 + q * NT, items - 1), row = it / (D / 4), d = it % (D / 4) * 4;
+        const int it = S > 1 ? at0 % items : min(at0 + q * NT, items - 1);
+        int row, d;
+        pieces.place(it, row, d);
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
           const int kk = min(k + j * S, parts - 1);
-          const long long piece = (long long)(kk ? 2 * (first + kk) : 2 * first + 1) * TQ + row;
-          x[q][j] = br_kv_get2(p.ml + piece * 2);
-          v0[q][j] = br_kv_get2(p.part + piece * D + d), v1[q][j] = br_kv_get2(p.part + piece * D + d + 2);
+          const int piece = kk ? 2 * (first + kk) : 2 * first + 1;
+          x[q][j] = br_kv_get2(p.ml + (piece * TQ + row) * 2);
+          v[q][j] = pieces.get(piece, it);
         }
       }
 #pragma unroll
@@ -434,8 +463,8 @@ __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w
           if (x[q][j].y == 0.0f) continue;
           const float e = __builtin_amdgcn_exp2f(x[q][j].x - top);
           l += x[q][j].y * e;
-          y[0] = __builtin_fmaf(v0[q][j].x, e, y[0]), y[1] = __builtin_fmaf(v0[q][j].y, e, y[1]);
-          y[2] = __builtin_fmaf(v1[q][j].x, e, y[2]), y[3] = __builtin_fmaf(v1[q][j].y, e, y[3]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) y[c] = __builtin_fmaf(v[q][j][c], e, y[c]);
         }
         m = top == BR_KV_NEG ? 0.0f : top;
       }
@@ -466,8 +495,11 @@ __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w
     ys[0] = y, ms[0] = m, ls[0] = l;
 #pragma unroll
     for (int q = 0; q < ROWS; ++q) {
-      const int it = at0 + q * NT, row = it / (D / 4), d = it % (D / 4) * 4;
+      const int it = at0 + q * NT;
       if (it >= items) continue;
+      int row, d;
+      pieces.place(it, row, d);
+      if (row >= rows_q) continue;
       const br_f4 one[1] = {ys[q]};
       br_kv_store<1>(p, w, h, qi * TQ + row, d, one, ls[q] != 0.0f ? 1.0f / ls[q] : 0.0f);
       if (d == 0) br_kv_store_lse(p, w, h, qi * TQ + row, ms[q], ls[q]);
@@ -653,17 +685,19 @@ __device__ __forceinline__ void br_kv_result(const BrKvAttend &p, const BrKvRow 
 template <int D, int NQ, int TQ>
 __device__ __forceinline__ void br_kv_piece(const BrKvAttend &p, int piece, int row, int rows_q, const BrKvSums<D, NQ> &s) {
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const BrKvPieces<D, TQ> pieces(p, rows_q);
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
     const int at = row + 16 * x + n;
     if (at >= rows_q) continue;
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) {
-      float *to = p.part + ((long long)piece * TQ + at) * D + 16 * d + 4 * g;
-      br_kv_put2(to, s.o[x][d][0] * s.c, s.o[x][d][1] * s.c);
-      br_kv_put2(to + 2, s.o[x][d][2] * s.c, s.o[x][d][3] * s.c);
+      br_f4 y = s.o[x][d];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] *= s.c;
+      pieces.put(piece, pieces.item(row / 16 + x, d, g, n), y);
     }
-    if (g == 0) br_kv_put2(p.ml + ((long long)piece * TQ + at) * 2, s.m[x], s.l[x]);
+    if (g == 0) br_kv_put2(p.ml + (piece * TQ + at) * 2, s.m[x], s.l[x]);
   }
 }
 
@@ -768,10 +802,10 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
         br_kv_store<1>(p, w, chain.h, chain.qi * TQ + row, 16 * d + 4 * g, y, l != 0.0f ? 1.0f / l : 0.0f);
         if (d == 0 && g == 0) br_kv_store_lse(p, w, chain.h, chain.qi * TQ + row, top, l);
       } else {
-        const long long piece = (long long)(2 * wg + (c < NR)) * TQ + row;
-        br_kv_put2(p.part + piece * D + 16 * d + 4 * g, y[0][0], y[0][1]);
-        br_kv_put2(p.part + piece * D + 16 * d + 4 * g + 2, y[0][2], y[0][3]);
-        if (d == 0 && g == 0) br_kv_put2(p.ml + piece * 2, top, l);
+        const int piece = 2 * wg + (c < NR);
+        const BrKvPieces<D, TQ> pieces(p, rows_q);
+        pieces.put(piece, pieces.item(x, d, g, n), y[0]);
+        if (d == 0 && g == 0) br_kv_put2(p.ml + (piece * TQ + row) * 2, top, l);
       }
     }
   }
