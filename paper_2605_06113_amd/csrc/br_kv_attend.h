@@ -830,12 +830,27 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   }
 }
 
+// Steps 0 .. N - 1 with four operands from LDS each, asked for AHEAD steps before.
+template <int N, int AHEAD, class Get, class Use>
+__device__ __forceinline__ void br_kv_ahead(Get &&get, Use &&use) {
+  br_h8 f[AHEAD + 1][4];
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) get(k, f[k]);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    if (k + AHEAD < N) get(k + AHEAD, f[(k + AHEAD) % (AHEAD + 1)]);
+    __builtin_amdgcn_sched_barrier(0);
+    use(k, f[k % (AHEAD + 1)]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 // Many query rows: the block's four waves have 16 NQ each and go over the same tokens.  Each wave brings a quarter of a tile's codes to f16 and
 // puts them into LDS as the matrix products take them (1 KB for each operand, 16 bytes a lane); two tiles there, one barrier a
 // tile.  Bound by the vector instructions between the products: 8 for a score, 4 of them the exponential.
 template <int D, int NQ, bool FP8, int WAVES>
 __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) {
-  constexpr int TQ = 64 * NQ, NT = 256, NI = D / 64, REST = D % 64 / 32, NK = D / 32, ND = D / 16, VG = (ND + 3) / 4;  // VG: groups of 16 channels of values that a wave brings
+  constexpr int TQ = 64 * NQ, NT = 256, NI = D / 64, REST = D % 64 / 32, NK = D / 32, ND = D / 16, VG = (ND + 3) / 4, AHEAD = WAVES == 1 ? 2 : 1;  // VG: groups of 16 channels of values that a wave brings
   using Runs = BrKvRuns<TQ, NT, 1, 8>;
   __shared__ typename Runs::Shared shared;
   __shared__ br_h8 tile[2][(4 * NK + 2 * ND) * 64];
@@ -909,13 +924,15 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
         to[(4 * NK + 2 * (wv + 4 * i) + 1) * 64 + lane] = br_kv_decode8<FP8>(vc[i].z, vc[i].w);
       }
     };
-    int kid1 = 0, vid = 0, vid1 = 0;  // of the next tile, of this one, of the next
+    int kid2 = 0, vid = 0, vid1 = 0, vid2 = 0;  // of this tile, of the next, of the one behind it
     float ks = 0.0f, vs = 0.0f;
+    int kid1 = 0;
     if (first < stop) {
-      const int next = min(first + 1, stop - 1);
+      const int next = min(first + 1, stop - 1), after = min(first + 2, stop - 1);
       const int kid = id_of(first * BR_KV_TILE + 16 * kg);
       vid = id_of(first * BR_KV_TILE + 16 * g);
       kid1 = id_of(next * BR_KV_TILE + 16 * kg), vid1 = id_of(next * BR_KV_TILE + 16 * g);
+      kid2 = id_of(after * BR_KV_TILE + 16 * kg), vid2 = id_of(after * BR_KV_TILE + 16 * g);
       fetch(first, kid, vid);
     }
     BrKvQueries<D, NQ> q;
@@ -928,9 +945,9 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
     __syncthreads();
     for (int t = first; t < stop; ++t) {
       const br_h8 *now = tile[(t - first) & 1];
-      // the next tile to the other half, the one behind it on its way
-      const int after = min(t + 2, stop - 1);
-      const int kid2 = id_of(after * BR_KV_TILE + 16 * kg), vid2 = id_of(after * BR_KV_TILE + 16 * g);
+      // the next tile to the other half, the one behind it on its way, the ids of the third
+      const int after = min(t + 2, stop - 1), third = min(t + 3, stop - 1);
+      const int kid3 = id_of(third * BR_KV_TILE + 16 * kg), vid3 = id_of(third * BR_KV_TILE + 16 * g);
       const float ks_next = ks1, vs_next = vs1;
       if (t + 1 < stop) bring(t + 1, vid1, tile[(t + 1 - first) & 1]);
       fetch(after, kid2, vid2);
@@ -941,28 +958,37 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
         for (int x = 0; x < NQ; ++x)
 #pragma unroll
           for (int y = 0; y < 4; ++y) z[x][y] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
+        br_kv_ahead<NK, AHEAD>(
+            [&](int c, br_h8 (&f)[4]) {
 #pragma unroll
-        for (int c = 0; c < NK; ++c)
+              for (int y = 0; y < 4; ++y) f[y] = now[(y * NK + c) * 64 + lane];
+            },
+            [&](int c, const br_h8 (&f)[4]) {
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const br_h8 kf = now[(y * NK + c) * 64 + lane];
+              for (int y = 0; y < 4; ++y)
 #pragma unroll
-            for (int x = 0; x < NQ; ++x) z[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q.qf[x][c], z[x][y], 0, 0, 0);
-          }
+                for (int x = 0; x < NQ; ++x) z[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[y], q.qf[x][c], z[x][y], 0, 0, 0);
+            });
         const int have = there(vid) ? min(max(len - t * BR_KV_TILE - 16 * g, 0), 16) : 0;
         br_h8 pf[NQ][2];
         br_kv_weights<D, NQ>(p, q, z, there(vid) ? br_kv_sound(ks) : 0.0f, there(vid) ? br_kv_sound(vs) : 0.0f, have, t, first_pos, last_pos, !__any(!there(vid)), s, cmax, cinv, pf);
+        br_kv_ahead<ND / 2, AHEAD>(
+            [&](int d, br_h8 (&f)[4]) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+              for (int y = 0; y < 4; ++y) f[y] = now[(4 * NK + 4 * d + y) * 64 + lane];
+            },
+            [&](int d, const br_h8 (&f)[4]) {
 #pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            const br_h8 v = now[(4 * NK + 2 * d + k) * 64 + lane];
+              for (int y = 0; y < 4; ++y)  // (products into one sum do not follow each other directly)
 #pragma unroll
-            for (int x = 0; x < NQ; ++x) s.o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pf[x][k], s.o[x][d], 0, 0, 0);
-          }
+                for (int x = 0; x < NQ; ++x) {
+                  const int v = y % 2 * 2 + y / 2, ch = 2 * d + v / 2;
+                  s.o[x][ch] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[v], pf[x][v % 2], s.o[x][ch], 0, 0, 0);
+                }
+            });
       }
       ks = ks_next, vs = vs_next;
-      vid = vid1, vid1 = vid2;
+      vid = vid1, vid1 = vid2, vid2 = vid3, kid2 = kid3;
       __syncthreads();
     }
     s.c = cmax * (1.0f / 256.0f);
