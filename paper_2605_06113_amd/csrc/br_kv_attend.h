@@ -864,6 +864,8 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
   BrKvPlace<TQ, NT, Runs> at;
   if (u >= end || !at.find(p, runs, u)) return;
   const int kg = n >> 2, kr = n & 3, mask = (1 << p.shift) - 1;
+  // Of two blocks on a compute unit the one that came first would have its way, and be done long before the other: they go first in turns.
+  const int turn = 2 * blockIdx.x >= gridDim.x;
   auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
   auto there = [&](int id) { return (unsigned)id < (unsigned)p.n_blocks; };
   for (;;) {
@@ -882,24 +884,30 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
     }
     const int *table = p.table + (long long)r * p.max_blocks;
     const int last_block = max(0, (len - 1) >> p.shift);
-    const long long cache0 = (long long)(r / p.rows) * p.n_blocks;
     auto id_of = [&](int token) { return table[min(token >> p.shift, last_block)]; };
 
-    // this wave's quarter of a tile: rows 4 wv + kr of each token group of K, channels 16 (wv + 4 i) + n of V
+    // this wave's quarter of a tile: rows 4 wv + kr of each token group of K, channels 16 (wv + 4 i) + n of V; from a lane's place in the
+    // worker's block 0 to that in block id: one multiplication
+    const long long block0 = (long long)(r / p.rows) * p.n_blocks * p.kv_heads + h;
+    const unsigned char *k0 = p.k + ((block0 << p.shift) + ((16 * kg) & mask) + 4 * wv + kr) * D + 16 * g;
+    const unsigned char *v0 = p.v + ((block0 * D + 16 * wv + n) << p.shift) + ((16 * g) & mask);
+    const float *ks0 = p.ks + block0, *vs0 = p.vs + block0;
+    const unsigned step = (unsigned)(p.kv_heads * D) << p.shift;
     uint4 kc[NI + (NI == 0)], vc[VG];
     uint2 kx;
     float ks1 = 0.0f, vs1 = 0.0f;
     auto fetch = [&](int t, int kid, int vid) {
-      const unsigned char *k = p.k + ((((cache0 + (there(kid) ? kid : 0)) * p.kv_heads + h) << p.shift) + ((t * BR_KV_TILE + 16 * kg) & mask) + 4 * wv + kr) * D;
+      const int in = (t * BR_KV_TILE) & mask;
+      const unsigned char *k = k0 + (unsigned long long)(there(kid) ? (unsigned)kid : 0u) * step + in * D;
 #pragma unroll
-      for (int i = 0; i < NI; ++i) kc[i] = *(const uint4 *)(k + 64 * i + 16 * g);
-      if (REST) kx = *(const uint2 *)(k + 64 * NI + 8 * g);
-      const long long vb = (cache0 + (there(vid) ? vid : 0)) * p.kv_heads + h;
-      const unsigned char *v = p.v + (((vb * D + n) << p.shift) + ((t * BR_KV_TILE + 16 * g) & mask));
+      for (int i = 0; i < NI; ++i) kc[i] = *(const uint4 *)(k + 64 * i);
+      if (REST) kx = *(const uint2 *)(k + 64 * NI - 8 * g);
+      const unsigned vb = there(vid) ? (unsigned)vid : 0u;
+      const unsigned char *v = v0 + (unsigned long long)vb * step + in;
 #pragma unroll
       for (int i = 0; i < VG; ++i)
-        if (wv + 4 * i < ND) vc[i] = *(const uint4 *)(v + ((16 * (wv + 4 * i)) << p.shift));
-      ks1 = p.ks[vb], vs1 = p.vs[vb];
+        if (ND % 4 == 0 || wv + 4 * i < ND) vc[i] = *(const uint4 *)(v + ((64 * i) << p.shift));
+      ks1 = ks0[(unsigned long long)vb * (unsigned)p.kv_heads], vs1 = vs0[(unsigned long long)vb * (unsigned)p.kv_heads];
     };
     auto bring = [&](int t, int vid, br_h8 *to) {
 #pragma unroll
@@ -910,8 +918,9 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
         to[(wv * NK + c) * 64 + lane] = y;
       }
       // (bytes behind the row's end are whatever memory held: an 8-bit float may be a NaN there)
-      const int have = there(vid) ? min(max(len - t * BR_KV_TILE - 16 * g, 0), 16) : 0;
-      if (FP8 && __any(have < 16)) {
+      if (FP8 && (t * BR_KV_TILE + BR_KV_TILE > len || __any(!there(vid)))) {
+        const int have = there(vid) ? min(max(len - t * BR_KV_TILE - 16 * g, 0), 16) : 0;
+        __asm__ volatile("");  // (a branch: taken at a row's end)
         const unsigned long long full = ~0ull;
         const unsigned long long m0 = have >= 8 ? full : ~(full << (8 * have)), m1 = have >= 16 ? full : have <= 8 ? 0ull : ~(full << (8 * (have - 8)));
 #pragma unroll
@@ -919,7 +928,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
       }
 #pragma unroll
       for (int i = 0; i < VG; ++i) {
-        if (wv + 4 * i >= ND) continue;
+        if (ND % 4 != 0 && wv + 4 * i >= ND) continue;
         to[(4 * NK + 2 * (wv + 4 * i)) * 64 + lane] = br_kv_decode8<FP8>(vc[i].x, vc[i].y);
         to[(4 * NK + 2 * (wv + 4 * i) + 1) * 64 + lane] = br_kv_decode8<FP8>(vc[i].z, vc[i].w);
       }
@@ -945,6 +954,8 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
     __syncthreads();
     for (int t = first; t < stop; ++t) {
       const br_h8 *now = tile[(t - first) & 1];
+      if (turn ^ (t & 1)) __builtin_amdgcn_s_setprio(1);
+      else __builtin_amdgcn_s_setprio(0);
       // the next tile to the other half, the one behind it on its way, the ids of the third
       const int after = min(t + 2, stop - 1), third = min(t + 3, stop - 1);
       const int kid3 = id_of(third * BR_KV_TILE + 16 * kg), vid3 = id_of(third * BR_KV_TILE + 16 * g);
