@@ -53,12 +53,12 @@ __device__ __forceinline__ int br_kv_span(const BrKvAttend &p, const BrKvRow &w,
   return max(1, t1 - t0);
 }
 
-// Query tiles of one row and key head, their token tiles, and the most that one of them has.
+// Query tiles of one row and key head; the token tiles of every `step`-th from `first` on, and the most that one of them has.
 template <int TQ>
-__device__ __forceinline__ int br_kv_row_tiles(const BrKvAttend &p, const BrKvRow &w, long long &tiles, int &most) {
+__device__ __forceinline__ int br_kv_row_tiles(const BrKvAttend &p, const BrKvRow &w, long long &tiles, int &most, int first = 0, int step = 1) {
   const int nq = (int)(((long long)w.n * p.group + TQ - 1) / TQ);
   tiles = 0, most = 0;
-  for (int qi = 0; qi < nq; ++qi) {
+  for (int qi = first; qi < nq; qi += step) {
     int t0, t1;
     const int size = br_kv_span<TQ>(p, w, qi, t0, t1);
     tiles += size, most = max(most, size);
@@ -420,7 +420,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 template <int D, int TQ, int NT>
 __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int rows_q, int first, int parts, br_f4 *sums, float2 *ml) {
   // few rows have many pieces (up to a block of the launch each), many rows few: places asked for at once are AT_ONCE pieces of ROWS rows
-  constexpr int ROWS = TQ > 32 ? 4 : 1, AT_ONCE = TQ > 32 ? 2 : 8, STEP = NT * ROWS;
+  constexpr int ROWS = TQ > 64 ? 8 : TQ > 32 ? 4 : 1, AT_ONCE = TQ > 32 ? 2 : 8, STEP = NT * ROWS;
   const BrKvPieces<D, TQ> pieces(p, rows_q);
   const int tid = threadIdx.x, items = pieces.items(), S = items < NT ? max(1, NT / items) : 1;
   for (int at0 = tid; at0 < max(items, NT); at0 += STEP) {
@@ -513,6 +513,7 @@ __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w
 // query tile's NR parts.
 template <int TQ, int NT, int NR, int SLACK>
 struct BrKvRuns {
+  static constexpr bool MANY = TQ > 64;  // a row may well have more than one query tile
   struct Shared {
     long long before[NT + 1], wave_sum[NT / 64];
     int wave_parts[NT / 64], wave_most[NT / 64];
@@ -523,21 +524,28 @@ struct BrKvRuns {
   unsigned share, more;
   int per, workers;
   bool parts;  // the units are parts of query tiles
+  int log_per_row;  // 2^.. threads count a row's tiles (chunks of thousands of query rows have many: one thread 5 us); the first has the sum
 
   // (a worker gets at least `least` tiles, if there are as many)
   __device__ __forceinline__ BrKvRuns(const BrKvAttend &p, Shared &sh, int blocks, int least) : s(sh) {
     const int tid = threadIdx.x, lane = tid & 63;
     per = (p.n_rows + NT - 1) / NT;
+    log_per_row = MANY && per == 1 ? min(__builtin_ctz(NT) - (p.n_rows > 1 ? 32 - __builtin_clz(p.n_rows - 1) : 0), 6) : 0;
+    const int at = tid >> log_per_row, one = tid & ((1 << log_per_row) - 1);
     long long mine = 0;
     int mine_q = 0, most = 0;
-    for (int r = tid * per; r < min(p.n_rows, (tid + 1) * per); ++r) {
+    for (int r = at * per; r < min(p.n_rows, (at + 1) * per); ++r) {
       const BrKvRow w = br_kv_row(p, r);
-      s.row[tid] = make_int4(w.n, w.len, w.start, 0);
+      s.row[at] = make_int4(w.n, w.len, w.start, 0);
       if (w.n <= 0) continue;
       long long tiles;
       int longest;
-      mine_q = min(mine_q + br_kv_row_tiles<TQ>(p, w, tiles, longest), 4096);
+      mine_q = min(mine_q + br_kv_row_tiles<TQ>(p, w, tiles, longest, one, 1 << log_per_row), 4096);
       mine += tiles, most = max(most, longest);
+    }
+    if (MANY) {
+      for (int d = 1; d < 1 << log_per_row; d <<= 1) mine += __shfl_xor(mine, d, 64);
+      if (one) mine = 0, mine_q = 0;
     }
     mine *= p.kv_heads;
     // (query tiles as far as they could go to a block each)
@@ -583,7 +591,12 @@ struct BrKvRuns {
     long long tiles;
     int most;
     if (parts) return (int)(((long long)w.n * p.group + TQ - 1) / TQ) * NR;
-    br_kv_row_tiles<TQ>(p, w, tiles, most);
+    if (MANY) {
+      br_kv_row_tiles<TQ>(p, w, tiles, most, threadIdx.x & 63, 64);
+      for (int d = 1; d < 64; d <<= 1) tiles += __shfl_xor(tiles, d, 64);
+    } else {
+      br_kv_row_tiles<TQ>(p, w, tiles, most);
+    }
     return tiles;
   }
   __device__ __forceinline__ int units_of(int size) const { return parts ? NR : size; }
@@ -623,7 +636,7 @@ struct BrKvPlace {
 
   __device__ __forceinline__ bool find(const BrKvAttend &p, const Runs &runs, long long u) {
     const int lo = runs.find(u);
-    r = lo * runs.per;
+    r = (lo >> runs.log_per_row) * runs.per;
     base = runs.s.before[lo];
     for (; r < p.n_rows; ++r) {
       w = runs.row_of(p, r);
@@ -637,6 +650,16 @@ struct BrKvPlace {
     while (u - base >= (h + 1) * tiles) ++h;
     qi = 0;
     seg = base + h * tiles;
+    if (Runs::MANY) {  // 64 query tiles at a time
+      const int last = (int)(((long long)w.n * p.group + TQ - 1) / TQ) - 1;
+      for (int k = 64; k == 64; qi += k) {
+        const int sum = br_kv_wave_scan(runs.units_of(br_kv_span<TQ>(p, w, min(qi + (int)(threadIdx.x & 63), last), t0, t1)));
+        k = __popcll(__ballot(seg + sum <= u));
+        if (k > 0) seg += __shfl(sum, k - 1, 64);
+      }
+      size = runs.units_of(br_kv_span<TQ>(p, w, qi, t0, t1));
+      return true;
+    }
     size = runs.units_of(br_kv_span<TQ>(p, w, 0, t0, t1));
     while (u >= seg + size) seg += size, size = runs.units_of(br_kv_span<TQ>(p, w, ++qi, t0, t1));
     return true;
