@@ -356,14 +356,15 @@ __device__ __forceinline__ unsigned long long br_kv_heads(const int *slot, int t
   return __ballot(head);
 }
 
-// `span` tokens of a list (at most 64) and a key head for a block.  `grain`: tokens that a run may have, less one (append: a block's).
-template <bool FP8, int DT, bool READ, bool WIDE>
+// `span` tokens of a list (at most 64) and a key head for a block, or one for a wave (WAVE).  `grain`: tokens that a run may have, less one (append: a block's).
+template <bool FP8, int DT, bool READ, bool WIDE, bool WAVE>
 __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a, int span, int grain) {
   __shared__ float red[16];
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, b1 = (1 << c.shift) - 1, slots = c.n_blocks << c.shift;
+  if (WAVE) span = 1;
   const int spans = (a.n + span - 1) / span;
-  const long long units = (long long)a.W * spans * c.heads;
-  for (long long id = blockIdx.x; id < units; id += gridDim.x) {
+  const long long units = (long long)a.W * spans * c.heads, step = WAVE ? (long long)gridDim.x * 4 : gridDim.x;
+  for (long long id = WAVE ? (long long)blockIdx.x * 4 + wv : blockIdx.x; id < units; id += step) {
     const long long part = id / c.heads;
     BrKvRun u;
     u.h = (int)(id - part * c.heads);
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a,
     if (span + grain + 1 > 64) heads[1] = br_kv_heads(slot, t0 + 64, a.n, slots, grain);
     if (span + grain + 1 > 128) heads[2] = br_kv_heads(slot, t0 + 128, a.n, slots, grain);
     unsigned long long left = heads[0] & (~0ull >> (64 - min(span, a.n - t0)));
-    const bool apart = __popcll(left) > 2;  // several short runs: one for each wave
+    const bool apart = !WAVE && __popcll(left) > 2;  // several short runs: one for each wave
     int turn = 0;
     for (; left; left &= left - 1, ++turn) {
       if (apart && (turn & 3) != wv) continue;
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a,
       u.off = in ? s & b1 : 0;
       u.block = ((long long)w * c.n_blocks + (in ? s >> c.shift : 0)) * c.heads + u.h;
       if constexpr (READ) {
-        if (apart) br_kv_read_run<FP8, DT, WIDE, 64>(c, a, u, in, lane);
+        if (WAVE || apart) br_kv_read_run<FP8, DT, WIDE, 64>(c, a, u, in, lane);
         else br_kv_read_run<FP8, DT, WIDE, 256>(c, a, u, in, threadIdx.x);
       } else {
         if (apart) br_kv_append_run<FP8, DT, WIDE, 64>(c, a, u, lane, red);
@@ -401,13 +402,23 @@ __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a,
 
 template <bool FP8, int DT, bool READ, bool WIDE>
 static void launch_wide(const BrKvCache &c, const BrKvTokens &t, int rows, hipStream_t st) {
-  // Short lists: four tokens to a block, so that a decode step's have a wave each and a prompt's runs a block each, read in pieces of 16.
-  // Long ones would have too many blocks that find nothing: of more than a few tokens a row, which are runs of whole blocks, 64 are
-  // four runs of 16, one for each wave, or at most two longer ones.
-  const bool few = (long long)t.W * t.n * c.heads <= 16384;
-  const int span = few ? 4 : t.n > 4 * rows ? (c.shift == 5 ? 32 : 64) : 16, block = 1 << c.shift, grain = READ && few ? 15 : block - 1;
-  const long long blocks = (long long)t.W * ((t.n + span - 1) / span) * c.heads;
-  br_kv_k_tokens<FP8, DT, READ, WIDE><<<(unsigned)(blocks > 1 << 20 ? 1 << 20 : blocks), 256, 0, st>>>(c, t, span, grain);
+  // Short lists: four tokens go to a block, so that a decode step's have a wave each and a prompt's runs a block each, reads cut every
+  // 16 tokens; those of fewer tokens a row have a wave for each piece (144 rows of 9 tokens, 8 heads of 128 channels: 9.9 us, by blocks
+  // 11.7; 5 rows of 600 tokens, 4 heads of 256 channels: 29 us, by blocks 15.5).  Long ones would have too many that
+  // find nothing: of more than a few tokens a row, which are runs of whole blocks, 64 are four runs of 16, one for each wave, or
+  // at most two longer ones.
+  const long long tokens = (long long)t.W * t.n * c.heads;
+  const int block = 1 << c.shift;
+  auto grid = [](long long blocks) { return (unsigned)(blocks > 1 << 20 ? 1 << 20 : blocks); };
+  const bool few = tokens <= 16384;
+  if constexpr (READ) {
+    if (few && t.n <= 16 * rows) {
+      br_kv_k_tokens<FP8, DT, READ, WIDE, true><<<grid((tokens + 3) / 4), 256, 0, st>>>(c, t, 1, 15);
+      return;
+    }
+  }
+  const int span = few ? 4 : t.n > 4 * rows ? (c.shift == 5 ? 32 : 64) : 16;
+  br_kv_k_tokens<FP8, DT, READ, WIDE, false><<<grid((long long)t.W * ((t.n + span - 1) / span) * c.heads), 256, 0, st>>>(c, t, span, READ && few ? 15 : block - 1);
 }
 
 template <bool FP8, int DT, bool READ>
