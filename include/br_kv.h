@@ -15,6 +15,8 @@
  * buffers stay alive until it ran; BR_OK or a negative code of br.h comes back, nothing is printed, nothing aborts.  No
  * call but br_kv_init allocates host memory; all of them may be captured into a graph.  Calls on one context
  * share its workspace: from several threads they are serialised by the caller.
+ * The context's GPU has to be the current device of the calling thread, as for br.h's calls.  Memory that other streams have written or
+ * will read is ordered against the context's stream by the caller (events); the library adds no waits.
  *
  * What is read on the device is checked there and never leads outside a buffer: lengths, block ids, slots, starts and
  * counts out of range are clamped or skipped as each call says.
@@ -207,10 +209,19 @@ int32_t br_kv_step(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out
  */
 int32_t br_kv_append(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_tokens *in);
 
-/* Reads tokens out of the cache: code * scale, rounded to dtype.  Slots in any order. */
+/*
+ * Reads tokens out of the cache: code * scale, rounded to dtype.  Slots in any order.  A block's scale that is none (below
+ * zero or not finite) reads as NaN.
+ */
 int32_t br_kv_read(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_tokens *out);
 
-/* out = softmax(scale * q k^T) v over the visible cached tokens.  Equal inputs give equal outputs, bit for bit. */
+/*
+ * out = softmax(scale * q k^T) v over the visible cached tokens.  Equal inputs give equal outputs, bit for bit.  Tokens that a
+ * query does not see have no part in its result, whatever their codes and scales; the scale of a block that it does see
+ * makes its result NaN if it is none (below zero or not finite), and so do queries that are not finite.
+ * Arithmetic: scores and sums in 32 bits; the queries' channels, each row scaled by a power of two to a largest of 1..2, and the weights
+ * e^(s - m) v_scale go to the matrix units in f16 (the codes are exact there).
+ */
 int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *args);
 
 /* Destroy the context (host memory only). NULL is allowed. */

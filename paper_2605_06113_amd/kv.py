@@ -3,7 +3,8 @@ values, attention over it.
 
 As in `binding`: argument marshalling only, every step runs in the library's kernels, PyTorch supplies device memory and
 the stream, and nothing falls back to the CPU.  All `*_device` calls enqueue on the cache's stream and return; they check
-types, shapes, strides and devices, since the C ABI takes bare pointers.
+types, shapes, strides and devices, since the C ABI takes bare pointers.  Tensors made or used on another stream are the
+caller's to order against the cache's stream (`stream.wait_stream`, `Tensor.record_stream`).
 
     cfg = kv.KvConfig(rows=96, n_blocks=4096, max_blocks=512, n_kv_heads=8, n_q_heads=32, head_dim=128, fmt="fp8")
     cache = kv.KvCache(cfg)
