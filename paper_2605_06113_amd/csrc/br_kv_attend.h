@@ -806,21 +806,25 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
     const int rows_q = (int)min((long long)TQ, (long long)w.n * p.group - (long long)chain.qi * TQ);
     for (int it = wv; it < SHARE * ND; it += NW) {
       const int x = it / ND, d = it - x * ND, row = 16 * x + n;
-      float top = BR_KV_NEG, l = 0.0f;
-#pragma unroll 4
-      for (int k = begin; k <= k1; ++k) {
-        const float2 ml = kept_ml[(member(k) * SHARE + x) * 16 + n];
-        if (ml.y != 0.0f) top = fmaxf(top, ml.x);
-      }
-      br_f4 y[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
-#pragma unroll 4
-      for (int k = begin; k <= k1; ++k) {
-        const float2 ml = kept_ml[(member(k) * SHARE + x) * 16 + n];
-        const br_f4 v = kept[((member(k) * SHARE + x) * ND + d) * 64 + lane];
-        const float e = ml.y != 0.0f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.0f;
-        l += ml.y * e;
+      // (all asked for at once, the last one again for those that a chain may have and this one has not)
+      float2 mls[NR + 1];
+      br_f4 vs[NR + 1];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[0][j] = __builtin_fmaf(v[j], e, y[0][j]);
+      for (int i = 0; i <= NR; ++i) {
+        const int at = member(min(begin + i, k1)) * SHARE + x;
+        mls[i] = kept_ml[at * 16 + n], vs[i] = kept[(at * ND + d) * 64 + lane];
+      }
+      float top = BR_KV_NEG, l = 0.0f;
+#pragma unroll
+      for (int i = 0; i <= NR; ++i)
+        if (mls[i].y != 0.0f) top = fmaxf(top, mls[i].x);
+      br_f4 y[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+      for (int i = 0; i <= NR; ++i) {
+        const float e = mls[i].y != 0.0f && begin + i <= k1 ? __builtin_amdgcn_exp2f(mls[i].x - top) : 0.0f;
+        l += mls[i].y * e;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[0][j] = __builtin_fmaf(vs[i][j], e, y[0][j]);
       }
       if (row >= rows_q) continue;
       if (top == BR_KV_NEG) top = 0.0f;
