@@ -507,6 +507,13 @@ __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w
   }
 }
 
+// What is the same for the wave, in scalar registers
+template <class T>
+__device__ __forceinline__ T br_kv_scalar(T x) {
+  if constexpr (sizeof(T) == 8) return (T)((unsigned long long)br_kv_scalar((unsigned)((unsigned long long)x >> 32)) << 32 | br_kv_scalar((unsigned)x));
+  else return (T)__builtin_amdgcn_readfirstlane((int)x);
+}
+
 // The division of a call's tiles among `workers` (waves, groups of waves, or blocks: NR to a block).  Where there are few query tiles and
 // none is much longer than an equal share, each goes to a block, in NR parts: nothing is left to be joined through memory, which
 // takes about as long as SLACK tiles.  Else the workers get runs of tiles that differ by one at most.  What is dealt are units: tiles, or a
@@ -521,7 +528,7 @@ struct BrKvRuns {
   };
   Shared &s;
   long long all;
-  unsigned share, more;
+  unsigned share, extra;  // a worker has `share` units, and extra / 2^32 of one more
   int per, workers;
   bool parts;  // the units are parts of query tiles
   int log_per_row;  // 2^.. threads count a row's tiles (chunks of thousands of query rows have many: one thread 5 us); the first has the sum
@@ -577,10 +584,13 @@ struct BrKvRuns {
     long long q = (long long)((double)total * (1.0 / workers)), left = total - q * workers;  // (exact behind the step up or down)
     if (left < 0) --q, left += workers;
     if (left >= workers) ++q, left -= workers;
-    share = (unsigned)q, more = (unsigned)left;  // the first `more` have one tile more
+    // (those with one more are spread evenly: one row of 40960 tokens, the first half of the blocks 24 tiles and the others 16, not 20
+    // each: 34 us)
+    share = (unsigned)q, extra = (unsigned)((double)left * 4294967296.0 * (1.0 / workers) + 0.5);
     all = total;
     parts = total_q <= workers_most && (most + NR - 1) / NR <= (int)min(q, 1ll << 20) + SLACK;
-    if (parts) workers = total_q, all = total_q, share = 1, more = 0, sum = sum_q;
+    if (parts) workers = total_q, all = total_q, share = 1, extra = 0, sum = sum_q;
+    share = br_kv_scalar(share), extra = br_kv_scalar(extra), workers = br_kv_scalar(workers), all = br_kv_scalar(all);
     s.before[tid + 1] = sum;
     if (tid == 0) s.before[0] = 0;
     __syncthreads();
@@ -601,8 +611,8 @@ struct BrKvRuns {
   }
   __device__ __forceinline__ int units_of(int size) const { return parts ? NR : size; }
   __device__ __forceinline__ long long begin_of(int k) const {
-    k = min(k, workers);
-    return min((unsigned long long)all, (unsigned long long)(unsigned)k * share + min((unsigned)k, more));
+    const long long at = (long long)((unsigned long long)(unsigned)k * share + __umulhi((unsigned)k, extra));
+    return k < workers ? at : all;
   }
   // The thread in whose rows tile u is: every lane looks at NT / 64 threads' ends, then at one of them.
   __device__ __forceinline__ int find(long long u) const {
@@ -611,14 +621,12 @@ struct BrKvRuns {
     const int chunk = __popcll(__ballot(s.before[(lane + 1) * PER_LANE] <= u)) * PER_LANE;
     return chunk + __popcll(__ballot(lane < PER_LANE && s.before[min(chunk + lane + 1, NT)] <= u));
   }
-  __device__ __forceinline__ int owner_of(long long x) const {  // (a search: 64-bit divisions are long code, and cold when they run)
-    int lo = 0, hi = workers - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (begin_of(mid) <= x) lo = mid;
-      else hi = mid - 1;
-    }
-    return lo;
+  // The last worker that begins at x or before (within one of what 24 bits say)
+  __device__ __forceinline__ int owner_of(long long x) const {
+    int k = min(max((int)((float)x * ((float)workers * __builtin_amdgcn_rcpf((float)all))), 0), workers - 1);
+    while (k > 0 && begin_of(k) > x) --k;
+    while (k + 1 < workers && begin_of(k + 1) <= x) ++k;
+    return k;
   }
   __device__ __forceinline__ BrKvRow row_of(const BrKvAttend &p, int r) const {
     if (per > 1) return br_kv_row(p, r);
@@ -658,10 +666,10 @@ struct BrKvPlace {
         if (k > 0) seg += __shfl(sum, k - 1, 64);
       }
       size = runs.units_of(br_kv_span<TQ>(p, w, qi, t0, t1));
-      return true;
+    } else {
+      size = runs.units_of(br_kv_span<TQ>(p, w, 0, t0, t1));
+      while (u >= seg + size) seg += size, size = runs.units_of(br_kv_span<TQ>(p, w, ++qi, t0, t1));
     }
-    size = runs.units_of(br_kv_span<TQ>(p, w, 0, t0, t1));
-    while (u >= seg + size) seg += size, size = runs.units_of(br_kv_span<TQ>(p, w, ++qi, t0, t1));
     return true;
   }
   __device__ __forceinline__ bool next(const BrKvAttend &p, const Runs &runs) {
@@ -986,7 +994,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
     __syncthreads();
     for (int t = first; t < stop; ++t) {
       const br_h8 *now = tile[(t - first) & 1];
-      if (turn ^ (t & 1)) __builtin_amdgcn_s_setprio(1);
+      if (turn ^ ((t - first) & 1)) __builtin_amdgcn_s_setprio(1);
       else __builtin_amdgcn_s_setprio(0);
       // the next tile to the other half, the one behind it on its way, the ids of the third
       const int after = min(t + 2, stop - 1), third = min(t + 3, stop - 1);
