@@ -346,12 +346,14 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
   }
 }
 
-// Which tokens of t .. t + 63 of a list of n begin a run (also those behind the list's end; bit k: token t + k).
-__device__ __forceinline__ unsigned long long br_kv_heads(const int *slot, int t, int n, int slots, int b1) {
+// Which tokens of t .. t + 63 of a list of n begin a run (also those behind the list's end; bit k: token t + k).  s: the lane's token's slot.
+__device__ __forceinline__ unsigned long long br_kv_heads(const int *slot, int t, int n, int slots, int b1, int &s) {
   const int at = t + (threadIdx.x & 63);
   bool head = true;
+  s = -1;
   if (at < n) {
-    const int s = slot[at], before = at > 0 ? slot[at - 1] : -1;
+    s = slot[at];
+    const int before = at > 0 ? slot[at - 1] : -1;
     head = s < 0 || s >= slots || (s & b1) == 0 || before != s - 1;
   }
   return __ballot(head);
@@ -372,9 +374,10 @@ __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a,
     const int w = (int)(part / spans), t0 = (int)(part - (long long)w * spans) * span;
     const int *slot = a.slot + (long long)w * a.n;
     // heads of the span's tokens, and of those that its last run may reach (a grain more)
-    unsigned long long heads[3] = {br_kv_heads(slot, t0, a.n, slots, grain), ~0ull, ~0ull};
-    if (span + grain + 1 > 64) heads[1] = br_kv_heads(slot, t0 + 64, a.n, slots, grain);
-    if (span + grain + 1 > 128) heads[2] = br_kv_heads(slot, t0 + 128, a.n, slots, grain);
+    int own, other;
+    unsigned long long heads[3] = {br_kv_heads(slot, t0, a.n, slots, grain, own), ~0ull, ~0ull};
+    if (span + grain + 1 > 64) heads[1] = br_kv_heads(slot, t0 + 64, a.n, slots, grain, other);
+    if (span + grain + 1 > 128) heads[2] = br_kv_heads(slot, t0 + 128, a.n, slots, grain, other);
     unsigned long long left = heads[0] & (~0ull >> (64 - min(span, a.n - t0)));
     const bool apart = !WAVE && __popcll(left) > 2;  // several short runs: one for each wave
     int turn = 0;
@@ -383,7 +386,7 @@ __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a,
       const int k = __ffsll(left) - 1;
       const unsigned long long rest = k < 63 ? heads[0] >> (k + 1) << (k + 1) : 0;
       const int end = rest ? __ffsll(rest) - 1 : heads[1] ? 63 + __ffsll(heads[1]) : heads[2] ? 127 + __ffsll(heads[2]) : 192;
-      const int s = slot[t0 + k];
+      const int s = __builtin_amdgcn_readlane(own, k);
       const bool in = s >= 0 && s < slots;
       if (!READ && !in) continue;
       u.t = (long long)w * a.n + t0 + k;
