@@ -62,6 +62,23 @@ __device__ __forceinline__ float br_kv_to_float(unsigned short u) {
   return DT == BR_KV_BF16 ? br_kv_bf16(u) : br_kv_f16(u);
 }
 
+// The largest magnitude so far.  Without their signs the types' bits are ordered as whole numbers, what is not finite above the rest: two
+// instructions a word, two values where they have 16 bits.
+template <int DT>
+struct BrKvTop {
+  typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+  unsigned top = 0;
+  __device__ __forceinline__ void add(unsigned u) {
+    if constexpr (DT == BR_KV_F32) top = max(top, u & 0x7fffffffu);
+    else top = __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(us2, top), __builtin_bit_cast(us2, u & 0x7fff7fffu)));
+  }
+  // (infinite if one was not finite)
+  __device__ __forceinline__ float get() const {
+    if constexpr (DT == BR_KV_F32) return __uint_as_float(min(top, 0x7f800000u));
+    else return br_kv_to_float<DT>((unsigned short)min(max(top & 0xffffu, top >> 16), DT == BR_KV_BF16 ? 0x7f80u : 0x7c00u));
+  }
+};
+
 // N = 8 or 2 neighbours of the caller's array as they lie there, and as floats; WIDE: they are aligned to their size
 template <int DT, int N, bool WIDE>
 struct BrKvRaw {
@@ -100,13 +117,9 @@ struct BrKvRaw {
 #pragma unroll
     for (int k = 0; k < WORDS; ++k) __asm__ volatile("" : "+v"(u[k]));
   }
-  __device__ __forceinline__ void look(float &top, int &bad, int bit) const {
+  __device__ __forceinline__ void look(BrKvTop<DT> &top) const {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float y = fabsf(get(j));
-      top = fmaxf(top, y);
-      bad |= y < __builtin_inff() ? 0 : bit;
-    }
+    for (int j = 0; j < WORDS; ++j) top.add(u[j]);
   }
 };
 
@@ -146,14 +159,15 @@ struct BrKvRun {
   int h, off, n;
 };
 
-// The scale of the new tokens' block: `top` of them, `bad`: one is not finite.  r: what earlier codes are multiplied by.
+// The scale of the new tokens' block: `top` of them, infinite if one is not finite.  r: what earlier codes are multiplied by.
 struct BrKvScale {
   float inv, s, r;
   bool bad;
 };
 
 template <bool FP8>
-__device__ __forceinline__ BrKvScale br_kv_scale(float top, bool bad, int off, float old) {
+__device__ __forceinline__ BrKvScale br_kv_scale(float top, int off, float old) {
+  const bool bad = !(top < __builtin_inff());
   unsigned e = br_kv_scale_exp<FP8>(bad ? 0.0f : top);
   BrKvScale z = {0.0f, 0.0f, 1.0f, bad};
   if (off > 0) {
@@ -168,7 +182,7 @@ __device__ __forceinline__ BrKvScale br_kv_scale(float top, bool bad, int off, f
   return z;
 }
 
-// NT threads (a wave, or a block that is all here) write a run.  red: 16 floats of LDS.  The first AT_ONCE rows of keys and 4 x 8 values
+// NT threads (a wave, or a block that is all here) write a run.  red: 8 floats of LDS.  The first AT_ONCE rows of keys and 4 x 8 values
 // of a thread (all, up to 64 tokens of 128 channels for a block) stay in registers between the maximum and the codes.
 template <bool FP8, int DT, bool WIDE, int NT>
 __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, int tid, float *red) {
@@ -182,8 +196,7 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   const int k_token = (int)a.k_token, v_token = (int)a.v_token;
   // values: 8 channels of the block's tokens 4 q .. 4 q + 3
   const int vq0 = u.off >> 2, vqs = ((u.off + u.n - 1) >> 2) - vq0 + 1, vitems = vqs * chunks;
-  float top_k = 0.0f, top_v = 0.0f;
-  int bad = 0;
+  BrKvTop<DT> most_k, most_v;
   BrKvRaw<DT, 8, WIDE> rk[AT_ONCE];
   BrKvRaw<DT, 8, WIDE> rv[4];
   BrKvRaw<DT, 2, WIDE> rf;
@@ -202,37 +215,35 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
     for (int i = tid; i < u.n * pairs; i += NT) {
       const int j = i / pairs;
       rf.fetch(xv, j * v_token + (i - j * pairs) * 2);
-      rf.look(top_v, bad, 2);
+      rf.look(most_v);
     }
   } else {
     for (int i = tid; i < vitems; i += NT) {
       fetch_v(i);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) rv[j].look(top_v, bad, 2);
+      for (int j = 0; j < 4; ++j) rv[j].look(most_v);
     }
   }
 #pragma unroll
-  for (int m = 0; m < AT_ONCE; ++m) rk[m].look(top_k, bad, 1);
+  for (int m = 0; m < AT_ONCE; ++m) rk[m].look(most_k);
   for (int j = kj + AT_ONCE * kstep; j < kn; j += kstep) {
     BrKvRaw<DT, 8, WIDE> x;
     x.fetch(xk, j * k_token + kd);
-    x.look(top_k, bad, 1);
+    x.look(most_k);
   }
 #pragma unroll
   for (int m = 0; m < AT_ONCE; ++m) rk[m].keep_raw();
 #pragma unroll
   for (int j = 0; j < 4; ++j) rv[j].keep_raw();
-  top_k = br_kv_max64(top_k), top_v = br_kv_max64(top_v);
-  bad = (__any(bad & 1) ? 1 : 0) | (__any(bad & 2) ? 2 : 0);
+  float top_k = br_kv_max64(most_k.get()), top_v = br_kv_max64(most_v.get());
   if constexpr (NT > 64) {
     __syncthreads();
-    if ((tid & 63) == 0) red[tid >> 6] = top_k, red[4 + (tid >> 6)] = top_v, red[8 + (tid >> 6)] = __uint_as_float((unsigned)bad);
+    if ((tid & 63) == 0) red[tid >> 6] = top_k, red[4 + (tid >> 6)] = top_v;
     __syncthreads();
-    bad = 0;
 #pragma unroll
-    for (int k = 0; k < NT / 64; ++k) top_k = fmaxf(top_k, red[k]), top_v = fmaxf(top_v, red[4 + k]), bad |= (int)__float_as_uint(red[8 + k]);
+    for (int k = 0; k < NT / 64; ++k) top_k = fmaxf(top_k, red[k]), top_v = fmaxf(top_v, red[4 + k]);
   }
-  const BrKvScale zk = br_kv_scale<FP8>(top_k, bad & 1, u.off, old_k), zv = br_kv_scale<FP8>(top_v, bad & 2, u.off, old_v);
+  const BrKvScale zk = br_kv_scale<FP8>(top_k, u.off, old_k), zv = br_kv_scale<FP8>(top_v, u.off, old_v);
 
   if (zk.r != 1.0f) {  // earlier keys
     for (int j = kj; j < (kj < kstep ? u.off : 0); j += kstep) {
@@ -241,8 +252,9 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
     }
   }
   auto put_k = [&](int j, const BrKvRaw<DT, 8, WIDE> &x) {
-    auto q = [&](int m) { return zk.bad ? 0.0f : x.get(m) * zk.inv; };
-    *(uint2 *)(kc + (long long)(u.off + j) * D + kd) = make_uint2(br_kv_code4<FP8>(q(0), q(1), q(2), q(3)), br_kv_code4<FP8>(q(4), q(5), q(6), q(7)));
+    auto q = [&](int m) { return x.get(m) * zk.inv; };
+    const unsigned lo = br_kv_code4<FP8>(q(0), q(1), q(2), q(3)), hi = br_kv_code4<FP8>(q(4), q(5), q(6), q(7));
+    *(uint2 *)(kc + (long long)(u.off + j) * D + kd) = make_uint2(zk.bad ? 0u : lo, zk.bad ? 0u : hi);
   };
 #pragma unroll
   for (int m = 0; m < AT_ONCE; ++m)
@@ -284,8 +296,8 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
     unsigned char *at = vc + ((long long)(8 * oct) << c.shift) + 4 * q;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      auto x = [&](int j) { return zv.bad ? 0.0f : rv[j].get(k) * zv.inv; };
-      const unsigned y = br_kv_code4<FP8>(x(0), x(1), x(2), x(3));
+      auto x = [&](int j) { return rv[j].get(k) * zv.inv; };
+      const unsigned code = br_kv_code4<FP8>(x(0), x(1), x(2), x(3)), y = zv.bad ? 0u : code;
       if (hi - lo == 4) {
         *(unsigned *)(at + k * b) = y;
       } else {
@@ -301,7 +313,9 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
   constexpr int SIZE = DT == BR_KV_F32 ? 4 : 2;
   const int D = c.dim, b = 1 << c.shift, chunks = D >> 3, pairs = D >> 1;
   const unsigned char *kc = c.k + ((u.block * D) << c.shift), *vc = c.v + ((u.block * D) << c.shift);
-  const float ks = br_kv_sound(c.ks[u.block]), vs = br_kv_sound(c.vs[u.block]);
+  // (a slot that is none reads as codes of zero)
+  const float ks = in ? br_kv_sound(c.ks[u.block]) : 0.0f, vs = in ? br_kv_sound(c.vs[u.block]) : 0.0f;
+  const unsigned there = in ? ~0u : 0u;
   const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
   char *xk = (char *)a.k + (u.t * a.k_token + (long long)u.h * a.k_head) * SIZE, *xv = (char *)a.v + (u.t * a.v_token + (long long)u.h * a.v_head) * SIZE;
   const int k_token = (int)a.k_token, v_token = (int)a.v_token;
@@ -311,7 +325,7 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
   auto fetch_v = [&](int i) {
     const int oct = i / vqs, q = vq0 + i - oct * vqs;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = *(const unsigned *)(vc + ((long long)(8 * oct + k) << c.shift) + 4 * q);
+    for (int k = 0; k < 8; ++k) x[k] = *(const unsigned *)(vc + ((long long)(8 * oct + k) << c.shift) + 4 * q) & there;
   };
   const bool few = NT == 64 && u.n <= BR_KV_FEW;
   if (few) {
@@ -329,7 +343,7 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
     const uint2 x = *(const uint2 *)(kc + (long long)(u.off + j) * D + kd);
     float y[8];
 #pragma unroll
-    for (int m = 0; m < 8; ++m) y[m] = in ? br_kv_value<FP8>((m < 4 ? x.x : x.y) >> (8 * (m & 3))) * ks : 0.0f;
+    for (int m = 0; m < 8; ++m) y[m] = br_kv_value<FP8>((m < 4 ? x.x & there : x.y & there) >> (8 * (m & 3))) * ks;
     br_kv_store_out<DT, 8, WIDE>(xk, j * k_token + kd, y);
   }
   for (int i = tid; i < (few ? 0 : vitems); i += NT) {
@@ -340,7 +354,7 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
       if (j < lo || j >= hi) continue;
       float y[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = in ? br_kv_value<FP8>(x[k] >> (8 * j)) * vs : 0.0f;
+      for (int k = 0; k < 8; ++k) y[k] = br_kv_value<FP8>(x[k] >> (8 * j)) * vs;
       br_kv_store_out<DT, 8, WIDE>(xv, at + j * v_token, y);
     }
   }
@@ -362,7 +376,7 @@ __device__ __forceinline__ unsigned long long br_kv_heads(const int *slot, int t
 // `span` tokens of a list (at most 64) and a key head for a block, or one for a wave (WAVE).  `grain`: tokens that a run may have, less one (append: a block's).
 template <bool FP8, int DT, bool READ, bool WIDE, bool WAVE>
 __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a, int span, int grain) {
-  __shared__ float red[16];
+  __shared__ float red[8];
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, b1 = (1 << c.shift) - 1, slots = c.n_blocks << c.shift;
   if (WAVE) span = 1;
   const int spans = (a.n + span - 1) / span;
