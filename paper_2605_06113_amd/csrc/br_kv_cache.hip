@@ -226,10 +226,12 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   }
 #pragma unroll
   for (int m = 0; m < AT_ONCE; ++m) rk[m].look(most_k);
-  for (int j = kj + AT_ONCE * kstep; j < kn; j += kstep) {
-    BrKvRaw<DT, 8, WIDE> x;
-    x.fetch(xk, j * k_token + kd);
-    x.look(most_k);
+  for (int j = kj + AT_ONCE * kstep; j < kn; j += AT_ONCE * kstep) {
+    BrKvRaw<DT, 8, WIDE> x[AT_ONCE];
+#pragma unroll
+    for (int m = 0; m < AT_ONCE; ++m) x[m].fetch(xk, min(j + m * kstep, u.n - 1) * k_token + kd);
+#pragma unroll
+    for (int m = 0; m < AT_ONCE; ++m) x[m].look(most_k);
   }
 #pragma unroll
   for (int m = 0; m < AT_ONCE; ++m) rk[m].keep_raw();
@@ -259,10 +261,13 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
 #pragma unroll
   for (int m = 0; m < AT_ONCE; ++m)
     if (kj + m * kstep < kn) put_k(kj + m * kstep, rk[m]);
-  for (int j = kj + AT_ONCE * kstep; j < kn; j += kstep) {
-    BrKvRaw<DT, 8, WIDE> x;
-    x.fetch(xk, j * k_token + kd);
-    put_k(j, x);
+  for (int j = kj + AT_ONCE * kstep; j < kn; j += AT_ONCE * kstep) {
+    BrKvRaw<DT, 8, WIDE> x[AT_ONCE];
+#pragma unroll
+    for (int m = 0; m < AT_ONCE; ++m) x[m].fetch(xk, min(j + m * kstep, u.n - 1) * k_token + kd);
+#pragma unroll
+    for (int m = 0; m < AT_ONCE; ++m)
+      if (j + m * kstep < kn) put_k(j + m * kstep, x[m]);
   }
 
   if (zv.r != 1.0f) {  // earlier values

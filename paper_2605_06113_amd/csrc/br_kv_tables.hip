@@ -316,7 +316,9 @@ void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, h
 template <bool LIST>
 static void launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st) {
   const size_t lds = (size_t)t.words * 4;
+  // (as few rows to a thread as will do: its arrays in LDS go by it, and with them the blocks on a compute unit)
   if (t.B <= 256) br_kv_k_step<256, 1, LIST><<<t.W, 256, lds, st>>>(t, s);
+  else if (t.B <= 512) br_kv_k_step<256, 2, LIST><<<t.W, 256, lds, st>>>(t, s);
   else br_kv_k_step<256, 4, LIST><<<t.W, 256, lds, st>>>(t, s);
 }
 
