@@ -155,14 +155,14 @@ int32_t br_kv_init(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx *
 
 int32_t br_kv_step(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out *out) {
   if (!ctx || !in || !in->keep || !in->add || !out || out->token_cap < 0) return BR_EINVAL;
-  if ((int64_t)ctx->cfg.n_workers * out->token_cap > INT32_MAX) return BR_EINVAL;
+  if ((int64_t)ctx->cfg.n_workers * out->token_cap > INT32_MAX - 2 * BR_KV_LIST) return BR_EINVAL;
   BrKvStep s;
   s.keep = in->keep, s.add = in->add;
   s.slot = out->slot, s.pos = out->pos, s.start = out->start, s.count = out->count, s.status = out->status;
   s.stats = (long long *)out->stats;
   s.runs = (int2 *)((char *)ctx->cfg.workspace + ctx->at.runs);
   s.cap = out->token_cap;
-  s.wide = ((((uintptr_t)s.slot | (uintptr_t)s.pos) & 15u) | (s.cap & 3)) == 0;
+  s.wide = (((uintptr_t)s.slot | (uintptr_t)s.pos) & 15u) == 0;
   return enqueue(ctx, [&] { br_kv_launch_step(ctx->t, s, ctx->st); });
 }
 

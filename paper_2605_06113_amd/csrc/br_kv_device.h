@@ -25,7 +25,7 @@ struct BrKvStep {
   int *slot, *pos, *start, *count, *status;
   long long *stats;
   int2 *runs;     // [W][B] workspace: each row's first place in the token list and first position there
-  int cap, wide;  // wide: four places of the lists can be written at once
+  int cap, wide;  // wide: the lists begin at 16 bytes
 };
 
 // One layer's cache and what indexes it.

@@ -72,24 +72,30 @@ __device__ __forceinline__ int br_kv_find(const int *before, int n, int k) {
   return lo;
 }
 
-// Places j0 .. j0 + 3 of a worker's token list: rows' tokens from before[r] on, at positions from kp[r] on.  tail: the block of the last
+// Fours of places begin where 16 bytes of the workers' lists side by side do, as many places before a worker's first one (by its own
+// places, four stores of 4 bytes where the lists' length is odd: 1350 lists of 5159 places 38 us).
+__device__ __forceinline__ int br_kv_lead(int w, int cap) { return (int)((unsigned)w * (unsigned)cap & 3u); }
+__host__ __device__ __forceinline__ int br_kv_list_parts(int cap) { return (cap + 3 + BR_KV_LIST - 1) / BR_KV_LIST; }
+
+// Places j0 .. j0 + 3 of a worker's token list, those that it has (j0 may be below 0): rows' tokens from before[r] on, at positions from kp[r] on.  tail: the block of the last
 // position before those (a decode step then reads no table: a line for each row would be more than all the rest, 16384 workers
 // of 144 rows 99 us), or null.
 __device__ __forceinline__ void br_kv_list4(const BrKvTables &t, const BrKvStep &s, long long list, const int *table, const int *before, const int *kp, const int *tail, int rows,
                                             int total, int j0, int cap) {
   int slot[4] = {-1, -1, -1, -1}, pos[4] = {-1, -1, -1, -1};
   if (j0 < total) {
-    int r = br_kv_find(before, rows, j0);
+    int r = br_kv_find(before, rows, max(j0, 0));
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if (j0 + k >= total) break;
+      if (j0 + k < 0) continue;
       while (r + 1 < rows && before[r + 1] <= j0 + k) ++r;
       pos[k] = kp[r] + j0 + k - before[r];
       const int id = tail && pos[k] >> t.shift == (kp[r] - 1) >> t.shift ? tail[r] : table[(long long)r * t.max_blocks + (pos[k] >> t.shift)];
       slot[k] = id < 0 ? -1 : (id << t.shift) + (pos[k] & ((1 << t.shift) - 1));
     }
   }
-  if (s.wide) {
+  if (s.wide && j0 >= 0 && j0 + 4 <= cap) {
     typedef int i4 __attribute__((ext_vector_type(4)));
     if (s.slot) __builtin_nontemporal_store(i4{slot[0], slot[1], slot[2], slot[3]}, (i4 *)(s.slot + list + j0));
     if (s.pos) __builtin_nontemporal_store(i4{pos[0], pos[1], pos[2], pos[3]}, (i4 *)(s.pos + list + j0));
@@ -97,6 +103,7 @@ __device__ __forceinline__ void br_kv_list4(const BrKvTables &t, const BrKvStep 
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if (j0 + k >= cap) break;
+      if (j0 + k < 0) continue;
       if (s.slot) s.slot[list + j0 + k] = slot[k];
       if (s.pos) s.pos[list + j0 + k] = pos[k];
     }
@@ -285,14 +292,14 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
   __syncthreads();
   for (int i = tid; i < t.words; i += NT) gused[i] = used[i];
   if (LIST && (s.slot || s.pos))
-    for (int j = 4 * tid; j < s.cap; j += 4 * NT) br_kv_list4(t, s, (long long)w * s.cap, table, tok_before, row_kp, row_tail, ROWS, total, j, s.cap);
+    for (int j = 4 * tid - br_kv_lead(w, s.cap); j < s.cap; j += 4 * NT) br_kv_list4(t, s, (long long)w * s.cap, table, tok_before, row_kp, row_tail, ROWS, total, j, s.cap);
 }
 
 // The token lists of a step, BR_KV_LIST places of a worker's for each block (behind br_kv_k_step).  Bound by the search for each place's
 // row and the trip to its table: 37 workers, 7 M places, 16 us, 61 MB = 3.9 TB/s.
 __global__ __launch_bounds__(256) void br_kv_k_list(BrKvTables t, BrKvStep s) {
   __shared__ int before[BR_KV_MAX_ROWS], kp[BR_KV_MAX_ROWS], total;
-  const int parts = (s.cap + BR_KV_LIST - 1) / BR_KV_LIST, w = blockIdx.x / parts, j0 = (blockIdx.x - w * parts) * BR_KV_LIST, B = t.B;
+  const int parts = br_kv_list_parts(s.cap), w = blockIdx.x / parts, j0 = (blockIdx.x - w * parts) * BR_KV_LIST - br_kv_lead(w, s.cap), B = t.B;
   for (int r = threadIdx.x; r < B; r += 256) {
     const int2 x = s.runs[(long long)w * B + r];
     before[r] = x.x, kp[r] = x.y;
@@ -326,5 +333,5 @@ void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st) {
   const bool list = s.slot || s.pos;
   if (!list || s.cap <= BR_KV_LIST) return launch_step<true>(t, s, st);
   launch_step<false>(t, s, st);
-  br_kv_k_list<<<t.W * ((s.cap + BR_KV_LIST - 1) / BR_KV_LIST), 256, 0, st>>>(t, s);
+  br_kv_k_list<<<t.W * br_kv_list_parts(s.cap), 256, 0, st>>>(t, s);
 }

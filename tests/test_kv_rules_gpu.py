@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from paper_2605_06113_amd import kv
-from tests import kv_oracle as ko
+from tests import kv_oracle as ko, test_kv_gpu
 from tests.test_kv_gpu import _attend_case, _cache_of, _dev, _say, _torch
 
 pytestmark = pytest.mark.gpu
@@ -147,3 +147,10 @@ def test_tokens_too_far_apart_are_refused():
             cache.read_device(layer, slot, k, v)
     cache.append_device(layer, near, near, slot)
     cache.close()
+
+
+@pytest.mark.parametrize("case", [(5, 40, 16, 900, 60, 4099, 900), (3, 300, 32, 600, 40, 4097, 600), (4, 512, 16, 3000, 100, 8190, 700), (2, 513, 64, 1100, 30, 9001, 900),
+                                  (7, 9, 16, 2100, 300, 4095, 4000), (3, 257, 128, 700, 9, 3, 500)], ids=str)
+def test_token_lists_of_odd_lengths(case):
+    """Several workers' lists side by side, none but the first at 16 bytes; both sides of the step's own lists and of rows to a thread."""
+    test_kv_gpu.test_tables(case)
