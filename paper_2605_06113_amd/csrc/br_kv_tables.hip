@@ -113,8 +113,8 @@ __device__ __forceinline__ void br_kv_list4(const BrKvTables &t, const BrKvStep 
 // One block of NT threads per worker; a thread has the RPT rows from tid * RPT on.  The used bits are in LDS.  LIST: writes the
 // token list as well; else leaves each row's first place in it and first position to br_kv_k_list.
 // A chain of dependent steps (rows, blocks given back, sums, free ids, lists), so its time is their latencies: barriers are few (the
-// sums of a step in which nothing is refused take one), scans stay in registers.  One worker of 144 rows 5.0 us (a launch that does
-// nothing: 4); 16384 workers of 144 rows, a token each, 62 us, 259 MB = 4.2 TB/s, most of them stores of the outputs.
+// sums of a step in which nothing is refused take one), scans stay in registers.  One worker of 96 rows 4.8 us (a launch that does
+// nothing: 4); 16384 workers of 144 rows, a token each, 62 us, 259 MB = 4.1 TB/s, most of them stores of the outputs.
 template <int NT, int RPT, bool LIST>
 __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
   constexpr int ROWS = NT * RPT, IDS = NT * 8, AT_ONCE = 8;
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
 }
 
 // The token lists of a step, BR_KV_LIST places of a worker's for each block (behind br_kv_k_step).  Bound by the search for each place's
-// row and the trip to its table: 37 workers, 7 M places, 16 us, 61 MB = 3.9 TB/s.
+// row and the trip to its table: 37 workers, 7 M places, 16 us, 61 MB = 3.7 TB/s.
 __global__ __launch_bounds__(256) void br_kv_k_list(BrKvTables t, BrKvStep s) {
   __shared__ int before[BR_KV_MAX_ROWS], kp[BR_KV_MAX_ROWS], total;
   const int parts = br_kv_list_parts(s.cap), w = blockIdx.x / parts, j0 = (blockIdx.x - w * parts) * BR_KV_LIST - br_kv_lead(w, s.cap), B = t.B;
