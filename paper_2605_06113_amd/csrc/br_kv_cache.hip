@@ -20,6 +20,21 @@ __device__ __forceinline__ float br_kv_value(unsigned c) {  // of the lowest byt
   else return (float)(signed char)c;
 }
 
+// ... of byte m (the 8-bit float's conversion takes any byte, by a constant)
+template <bool FP8>
+__device__ __forceinline__ float br_kv_value_at(unsigned c, int m) {
+  if constexpr (FP8) {
+    switch (m) {
+      case 0: return __builtin_amdgcn_cvt_f32_fp8((int)c, 0);
+      case 1: return __builtin_amdgcn_cvt_f32_fp8((int)c, 1);
+      case 2: return __builtin_amdgcn_cvt_f32_fp8((int)c, 2);
+      default: return __builtin_amdgcn_cvt_f32_fp8((int)c, 3);
+    }
+  } else {
+    return br_kv_value<FP8>(c >> (8 * m));
+  }
+}
+
 // Codes of four values of magnitude at most the format's top
 template <bool FP8>
 __device__ __forceinline__ unsigned br_kv_code4(float a, float b, float c, float d) {
@@ -348,7 +363,7 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
     const uint2 x = *(const uint2 *)(kc + (long long)(u.off + j) * D + kd);
     float y[8];
 #pragma unroll
-    for (int m = 0; m < 8; ++m) y[m] = br_kv_value<FP8>((m < 4 ? x.x & there : x.y & there) >> (8 * (m & 3))) * ks;
+    for (int m = 0; m < 8; ++m) y[m] = br_kv_value_at<FP8>(m < 4 ? x.x & there : x.y & there, m & 3) * ks;
     br_kv_store_out<DT, 8, WIDE>(xk, j * k_token + kd, y);
   }
   for (int i = tid; i < (few ? 0 : vitems); i += NT) {
@@ -359,7 +374,7 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
       if (j < lo || j >= hi) continue;
       float y[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = br_kv_value<FP8>(x[k] >> (8 * j)) * vs;
+      for (int k = 0; k < 8; ++k) y[k] = br_kv_value_at<FP8>(x[k], j) * vs;
       br_kv_store_out<DT, 8, WIDE>(xv, at + j * v_token, y);
     }
   }
