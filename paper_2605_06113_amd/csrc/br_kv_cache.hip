@@ -197,16 +197,16 @@ __device__ __forceinline__ BrKvScale br_kv_scale(float top, int off, float old) 
   return z;
 }
 
-// NT threads (a wave, or a block that is all here) write a run.  red: 8 floats of LDS.  The first AT_ONCE rows of keys and 4 x 8 values
+// nt threads (64, a wave, or 256, a block that is all here) write a run.  red: 8 floats of LDS.  The first AT_ONCE rows of keys and 4 x 8 values
 // of a thread (all, up to 64 tokens of 128 channels for a block) stay in registers between the maximum and the codes.
-template <bool FP8, int DT, bool WIDE, int NT>
-__device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, int tid, float *red) {
+template <bool FP8, int DT, bool WIDE>
+__device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, int nt, int tid, float *red) {
   constexpr int AT_ONCE = 4, SIZE = DT == BR_KV_F32 ? 4 : 2;
   const int D = c.dim, b = 1 << c.shift, chunks = D >> 3, pairs = D >> 1;
   unsigned char *kc = c.k + ((u.block * D) << c.shift), *vc = c.v + ((u.block * D) << c.shift);
   const float old_k = u.off ? c.ks[u.block] : 0.0f, old_v = u.off ? c.vs[u.block] : 0.0f;
   // keys: 8 channels from kd on of tokens kj, kj + kstep, ...
-  const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
+  const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = nt / chunks, kn = kj < kstep ? u.n : 0;
   const char *xk = (const char *)a.k + (u.t * a.k_token + (long long)u.h * a.k_head) * SIZE, *xv = (const char *)a.v + (u.t * a.v_token + (long long)u.h * a.v_head) * SIZE;
   const int k_token = (int)a.k_token, v_token = (int)a.v_token;
   // values: 8 channels of the block's tokens 4 q .. 4 q + 3
@@ -225,15 +225,15 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
 #pragma unroll
   for (int m = 0; m < AT_ONCE; ++m) rk[m].fetch(xk, min(kj + m * kstep, u.n - 1) * k_token + kd);
   // a decode step's few tokens: two channels of one token at a time
-  const bool few = NT == 64 && u.n <= BR_KV_FEW;
+  const bool few = nt == 64 && u.n <= BR_KV_FEW;
   if (few) {
-    for (int i = tid; i < u.n * pairs; i += NT) {
+    for (int i = tid; i < u.n * pairs; i += nt) {
       const int j = i / pairs;
       rf.fetch(xv, j * v_token + (i - j * pairs) * 2);
       rf.look(most_v);
     }
   } else {
-    for (int i = tid; i < vitems; i += NT) {
+    for (int i = tid; i < vitems; i += nt) {
       fetch_v(i);
 #pragma unroll
       for (int j = 0; j < 4; ++j) rv[j].look(most_v);
@@ -253,12 +253,12 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
 #pragma unroll
   for (int j = 0; j < 4; ++j) rv[j].keep_raw();
   float top_k = br_kv_max64(most_k.get()), top_v = br_kv_max64(most_v.get());
-  if constexpr (NT > 64) {
+  if (nt > 64) {
     __syncthreads();
     if ((tid & 63) == 0) red[tid >> 6] = top_k, red[4 + (tid >> 6)] = top_v;
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < NT / 64; ++k) top_k = fmaxf(top_k, red[k]), top_v = fmaxf(top_v, red[4 + k]);
+    for (int k = 0; k < 4; ++k) top_k = fmaxf(top_k, red[k]), top_v = fmaxf(top_v, red[4 + k]);
   }
   const BrKvScale zk = br_kv_scale<FP8>(top_k, u.off, old_k), zv = br_kv_scale<FP8>(top_v, u.off, old_v);
 
@@ -286,7 +286,7 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   }
 
   if (zv.r != 1.0f) {  // earlier values
-    for (int i = tid; i < ((u.off + 15) >> 4) * D; i += NT) {
+    for (int i = tid; i < ((u.off + 15) >> 4) * D; i += nt) {
       const int g = i / D, n = min(u.off - 16 * g, 16);
       br_u4 *at = (br_u4 *)(vc + ((long long)(i - g * D) << c.shift) + 16 * g);
       br_u4 x = *at;
@@ -297,20 +297,20 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
       }
       if (n > 0) *at = x;
     }
-    if constexpr (NT > 64) __syncthreads();  // (other threads put new values beside them)
+    if (nt > 64) __syncthreads();  // (other threads put new values beside them)
     else __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   }
   if (few) {
-    for (int i = tid; i < u.n * pairs; i += NT) {
+    for (int i = tid; i < u.n * pairs; i += nt) {
       const int j = i / pairs, d = (i - j * pairs) * 2;
-      if (u.n * pairs > NT) rf.fetch(xv, j * v_token + d);
+      if (u.n * pairs > nt) rf.fetch(xv, j * v_token + d);
       const unsigned q = br_kv_code4<FP8>(zv.bad ? 0.0f : rf.get(0) * zv.inv, zv.bad ? 0.0f : rf.get(1) * zv.inv, 0.0f, 0.0f);
       unsigned char *at = vc + ((long long)d << c.shift) + u.off + j;
       at[0] = (unsigned char)q, at[b] = (unsigned char)(q >> 8);
     }
   }
-  const bool again = vitems > NT;
-  for (int i = tid; i < (few ? 0 : vitems); i += NT) {
+  const bool again = vitems > nt;
+  for (int i = tid; i < (few ? 0 : vitems); i += nt) {
     if (again) fetch_v(i);
     const int oct = i / vqs, q = vq0 + i - oct * vqs, lo = max(u.off - 4 * q, 0), hi = min(u.off + u.n - 4 * q, 4);  // new ones: lo .. hi - 1
     unsigned char *at = vc + ((long long)(8 * oct) << c.shift) + 4 * q;
@@ -328,15 +328,15 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   if (tid == 0) c.ks[u.block] = zk.s, c.vs[u.block] = zv.s;
 }
 
-template <bool FP8, int DT, bool WIDE, int NT>
-__device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, bool in, int tid) {
+template <bool FP8, int DT, bool WIDE>
+__device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, bool in, int nt, int tid) {
   constexpr int SIZE = DT == BR_KV_F32 ? 4 : 2;
   const int D = c.dim, b = 1 << c.shift, chunks = D >> 3, pairs = D >> 1;
   const unsigned char *kc = c.k + ((u.block * D) << c.shift), *vc = c.v + ((u.block * D) << c.shift);
   // (a slot that is none reads as codes of zero)
   const float ks = in ? br_kv_sound(c.ks[u.block]) : 0.0f, vs = in ? br_kv_sound(c.vs[u.block]) : 0.0f;
   const unsigned there = in ? ~0u : 0u;
-  const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = NT / chunks, kn = kj < kstep ? u.n : 0;
+  const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = nt / chunks, kn = kj < kstep ? u.n : 0;
   char *xk = (char *)a.k + (u.t * a.k_token + (long long)u.h * a.k_head) * SIZE, *xv = (char *)a.v + (u.t * a.v_token + (long long)u.h * a.v_head) * SIZE;
   const int k_token = (int)a.k_token, v_token = (int)a.v_token;
   // values: 8 channels of the block's tokens 4 q .. 4 q + 3
@@ -347,9 +347,9 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] = *(const unsigned *)(vc + ((long long)(8 * oct + k) << c.shift) + 4 * q) & there;
   };
-  const bool few = NT == 64 && u.n <= BR_KV_FEW;
+  const bool few = nt == 64 && u.n <= BR_KV_FEW;
   if (few) {
-    for (int i = tid; i < u.n * pairs; i += NT) {
+    for (int i = tid; i < u.n * pairs; i += nt) {
       const int j = i / pairs, d = (i - j * pairs) * 2;
       const unsigned char *at = vc + ((long long)d << c.shift) + u.off + j;
       const float y[2] = {in ? br_kv_value<FP8>(at[0]) * vs : 0.0f, in ? br_kv_value<FP8>(at[b]) * vs : 0.0f};
@@ -366,7 +366,7 @@ __device__ __forceinline__ void br_kv_read_run(const BrKvCache &c, const BrKvTok
     for (int m = 0; m < 8; ++m) y[m] = br_kv_value_at<FP8>(m < 4 ? x.x & there : x.y & there, m & 3) * ks;
     br_kv_store_out<DT, 8, WIDE>(xk, j * k_token + kd, y);
   }
-  for (int i = tid; i < (few ? 0 : vitems); i += NT) {
+  for (int i = tid; i < (few ? 0 : vitems); i += nt) {
     if (i != tid) fetch_v(i);
     const int oct = i / vqs, q = vq0 + i - oct * vqs, lo = u.off - 4 * q, hi = u.off + u.n - 4 * q, at = (4 * q - u.off) * v_token + 8 * oct;
 #pragma unroll
@@ -427,13 +427,9 @@ __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a,
       u.n = in ? min(end - k, grain + 1) : 1;
       u.off = in ? s & b1 : 0;
       u.block = ((long long)w * c.n_blocks + (in ? s >> c.shift : 0)) * c.heads + u.h;
-      if constexpr (READ) {
-        if (WAVE || apart) br_kv_read_run<FP8, DT, WIDE, 64>(c, a, u, in, lane);
-        else br_kv_read_run<FP8, DT, WIDE, 256>(c, a, u, in, threadIdx.x);
-      } else {
-        if (apart) br_kv_append_run<FP8, DT, WIDE, 64>(c, a, u, lane, red);
-        else br_kv_append_run<FP8, DT, WIDE, 256>(c, a, u, threadIdx.x, red);
-      }
+      const int nt = WAVE || apart ? 64 : 256, tid = WAVE || apart ? lane : threadIdx.x;
+      if constexpr (READ) br_kv_read_run<FP8, DT, WIDE>(c, a, u, in, nt, tid);
+      else br_kv_append_run<FP8, DT, WIDE>(c, a, u, nt, tid, red);
     }
   }
 }
