@@ -436,23 +436,25 @@ __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a,
 
 template <bool FP8, int DT, bool READ, bool WIDE>
 static void launch_wide(const BrKvCache &c, const BrKvTokens &t, int rows, hipStream_t st) {
-  // Short lists: four tokens go to a block, so that a decode step's have a wave each and a prompt's runs a block each, reads cut every
-  // 16 tokens; those of fewer tokens a row have a wave for each piece (144 rows of 9 tokens, 8 heads of 128 channels: 9.9 us, by blocks
-  // 11.7; 5 rows of 600 tokens, 4 heads of 256 channels: 29 us, by blocks 15.5).  Long ones would have too many that
-  // find nothing: of more than a few tokens a row, which are runs of whole blocks, 64 are four runs of 16, one for each wave, or
-  // at most two longer ones.
+  // A block's span: at least four tokens, so that a decode step's have a wave each and a prompt's runs a block each, and as many as leave
+  // some blocks for each compute unit (7250 tokens, 2 heads of 64 channels in blocks of 16, four tokens each: 22.6 us), up to 16
+  // where there are at most a few tokens to a row, and 64 of longer runs, which are four runs of 16, one for each wave, or at
+  // most two longer ones.  Reads with short spans are cut every 16 tokens; short lists of fewer tokens a row have a wave for each such
+  // piece (144 rows of 9 tokens, 8 heads of 128 channels: 9.9 us, by blocks 11.7; 5 rows of 600 tokens, 4 heads of 256
+  // channels: 29 us, by blocks 15.5).
   const long long tokens = (long long)t.W * t.n * c.heads;
   const int block = 1 << c.shift;
   auto grid = [](long long blocks) { return (unsigned)(blocks > 1 << 20 ? 1 << 20 : blocks); };
-  const bool few = tokens <= 16384;
   if constexpr (READ) {
-    if (few && t.n <= 16 * rows) {
+    if (tokens <= 16384 && t.n <= 16 * rows) {
       br_kv_k_tokens<FP8, DT, READ, WIDE, true><<<grid((tokens + 3) / 4), 256, 0, st>>>(c, t, 1, 15);
       return;
     }
   }
-  const int span = few ? 4 : t.n > 4 * rows ? (c.shift == 5 ? 32 : 64) : 16;
-  br_kv_k_tokens<FP8, DT, READ, WIDE, false><<<grid((long long)t.W * ((t.n + span - 1) / span) * c.heads), 256, 0, st>>>(c, t, span, READ && few ? 15 : block - 1);
+  const int most = t.n > 4 * rows ? (c.shift == 5 ? 32 : 64) : 16;
+  int span = 4;
+  while (span < most && tokens > 1024ll * span) span *= 2;
+  br_kv_k_tokens<FP8, DT, READ, WIDE, false><<<grid((long long)t.W * ((t.n + span - 1) / span) * c.heads), 256, 0, st>>>(c, t, span, READ && span <= 16 ? 15 : block - 1);
 }
 
 template <bool FP8, int DT, bool READ>
