@@ -4,8 +4,8 @@
 // that stand together in the call's list and in one block, with a key head: nobody else writes that block's codes or scales, so there
 // are no atomics.  A block has 4 to 64 tokens of the list and a head; its four waves share a run or take runs of their own.  Values
 // lie with their tokens side by side: a thread turns 8 channels of 4 tokens, 16 bytes of a token on one side and 4 of a channel on
-// the other, its neighbours the tokens beside.  Prompts of 57 thousand tokens, 8 heads of 128 channels in f16: append 93 us, 351 MB =
-// 3.8 TB/s, read 80 us, 354 MB = 4.4 TB/s; a decode step of 144 rows 7 us, a launch and the chain slot, scale, codes.
+// the other, its neighbours the tokens beside.  Prompts of 57 thousand tokens, 8 heads of 128 channels in f16: append 94 us, 351 MB =
+// 3.7 TB/s, read 79 us, 354 MB = 4.5 TB/s; a decode step of 144 rows 7 us, a launch and the chain slot, scale, codes.
 #include "br_kv_device.h"
 
 #define BR_KV_LEAST 27u  // biased exponent of 2^-100, the smallest scale
