@@ -220,7 +220,8 @@ int32_t br_kv_read(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_tokens 
  * query does not see have no part in its result, whatever their codes and scales; the scale of a block that it does see
  * makes its result NaN if it is none (below zero or not finite), and so do queries that are not finite.
  * Arithmetic: scores and sums in 32 bits; the queries' channels, each row scaled by a power of two to a largest of 1..2, and the weights
- * e^(s - m) v_scale go to the matrix units in f16 (the codes are exact there).
+ * e^(s - m) v_scale go to the matrix units in f16 (the codes are exact there), each off by 2^-11 of itself at most and by 2^-33 of the largest that
+ * its query sees.  Tokens of which e^(s - m) is below 2^-126, m the query's largest score, may count as none.
  */
 int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *args);
 

@@ -14,9 +14,10 @@
 //     holds tokens 16 g .. 16 g + 15 of the tile, which one block covers: one ks and one vs per lane;
 //   O^T [channel][query] += V^T P^T: the weights of lane (n, g) are this product's operand as they stand, and the values come as
 //     16 bytes of 16 consecutive tokens of a channel (the cache keeps them that way round).
-// Nothing passes between lanes but the maxima.  Weights go to f16 as 256 e^(s - m) vs / c, c a power of two above the largest vs so
-// far, so that they use f16's range whatever the scales are: 11 bits, where the codes have 4 or 8; sums stay in 32 bits.
-// m and c only move when a weight would pass 2^4 and a ratio 2^3: the sums are rescaled a few times a row.
+// Nothing passes between lanes but the maxima.  Weights go to f16 as 512 e^(s - m) vs / c, where c is a power of two about the largest product
+// e^(s - m) vs that the query has seen so far: 11 bits, where the codes have 4 or 8, of every weight down to 2^-22 of the largest, and none is
+// off by more than 2^-33 of it, whatever the scales are; sums stay in 32 bits.  m and c are the query's own (what another query of
+// the tile sees has no say in them) and only move when e^(s - m) would pass 2^4 or a product 2^5 c: the sums are rescaled a few times a row.
 #ifndef BR_KV_ATTEND_H
 #define BR_KV_ATTEND_H
 
@@ -149,8 +150,22 @@ __device__ __forceinline__ void br_kv_stores_done() {
 // weights, both of e^(s - m), m in powers of two (0 where nothing was seen).
 template <int D, int NQ>
 struct BrKvSums {
+  // m is kept ROOM below the largest score, so that weights of 2^-126 and a scale of 2^126 meet in range; UNIT: a weight of 1 there is 1 / UNIT
+  static constexpr float ROOM = 13.0f, UNIT = 0x1p-13f;
+  static constexpr float ONE = 512.0f;  // what a product of c is in f16; products of 2^6 c are below its end
   br_f4 o[NQ][D / 16];
-  float m[NQ], l[NQ], c;
+  float m[NQ], l[NQ], c[NQ];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      m[x] = BR_KV_NEG, l[x] = 0.0f, c[x] = 0x1p-106f;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) o[x][d] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  }
+  // behind the last tile: l of all the row's lanes, in weights of m; what o is to be multiplied by
+  __device__ __forceinline__ void close();
 };
 
 __device__ __forceinline__ float br_kv_sum4(float x) {
@@ -158,6 +173,16 @@ __device__ __forceinline__ float br_kv_sum4(float x) {
   x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
   auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+template <int D, int NQ>
+__device__ __forceinline__ void BrKvSums<D, NQ>::close() {
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    l[x] = br_kv_sum4(l[x]) * UNIT;
+    c[x] *= 1.0f / ONE;
+    m[x] = m[x] == BR_KV_NEG ? 0.0f : m[x] + ROOM;
+  }
 }
 
 // The queries of 16 NQ rows from row0 on in f16, one row's to four lanes: channels 64 i + 16 g .. + 15 of its row for each lane, then
@@ -222,29 +247,21 @@ struct BrKvQueries {
 // `have` of them; exist: all of the tile's blocks do.  Moves m and c, and the sums with them.
 template <int D, int NQ>
 __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQueries<D, NQ> &q, const br_f4 (&s)[NQ][4], float ks, float vs, int have, int t, int first_pos,
-                                              int last_pos, bool exist, BrKvSums<D, NQ> &sums, float &cmax, float &cinv, br_h8 (&pf)[NQ][2]) {
+                                              int last_pos, bool exist, BrKvSums<D, NQ> &sums, br_h8 (&pf)[NQ][2]) {
   constexpr int ND = D / 16;
+  constexpr float ROOM = BrKvSums<D, NQ>::ROOM, UNIT = BrKvSums<D, NQ>::UNIT;
   const int token = t * BR_KV_TILE + 16 * ((threadIdx.x & 63) >> 4);
   auto &o = sums.o;
   auto &m = sums.m;
   auto &l = sums.l;
-  // (a block that no query of the tile sees has no say in c)
-  float top = have > 0 && token <= last_pos && (p.window == 0 || token + 15 > first_pos - p.window) ? vs : 0.0f;
-  top = br_kv_max4(top);
-  float cf = 1.0f;
-  if (top > 8.0f * cmax) {
-    const unsigned e = min(max(__float_as_uint(top) >> 23, 20u), 252u) + 1;
-    cinv = __uint_as_float((254u - e) << 23);
-    cf = cmax * cinv;
-    cmax = __uint_as_float(e << 23);
-  }
-  const float wgt = vs * (256.0f * cinv);
+  auto &c = sums.c;
+  const float vmax = br_kv_max4(have > 0 ? vs : 0.0f);  // (of who sees what is asked below, where it matters)
   // inside: every query of the tile sees all of its tokens, and all exist
   const bool inside = t * BR_KV_TILE + BR_KV_TILE - 1 <= first_pos && (p.window == 0 || t * BR_KV_TILE > last_pos - p.window) && exist;
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
     float f = q.qs[x] * ks;  // (not below zero: the sign of the caller's scale is in the queries)
-    float z[16], mx = BR_KV_NEG, wx = wgt;
+    float z[16], mx = BR_KV_NEG, vx = vs;
 #pragma unroll
     for (int j = 0; j < 16; ++j) z[j] = s[x][j >> 2][j & 3];
     if (!inside) {  // of the lane's tokens, those from `lo` on, `seen` of them
@@ -252,15 +269,20 @@ __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQue
 #pragma unroll
       for (int j = 0; j < 16; ++j) z[j] = (unsigned)(j - lo) < (unsigned)seen ? z[j] * f : BR_KV_NEG;
       f = 1.0f;
-      wx = seen > 0 ? wgt : 0.0f;  // (a block that is not seen has no weight, whatever its scale)
+      vx = seen > 0 ? vs : 0.0f;  // (a block that is not seen has no weight, whatever its scale)
     }
 #pragma unroll
     for (int j = 0; j < 16; ++j) mx = fmaxf(mx, z[j]);
-    mx = br_kv_max4(mx * f);
-    const bool up = mx > m[x] + 4.0f;
-    if (__any(up || cf != 1.0f)) {
-      const float to = up ? mx : m[x];
-      const float al = m[x] == BR_KV_NEG ? (l[x] != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m[x] - to), ao = al * cf;
+    const float all = br_kv_max4(mx * f);
+    const bool up = all > m[x] + (ROOM + 4.0f);
+    // (without any of these no product passes 2^6 c, whatever the tile's scores; rounded sums beyond 2^22 may be off by more than the 4 allow for)
+    if (__any(up | (vmax > 4.0f * c[x]) | (fabsf(all) > 0x1p22f))) {
+      const float to = up ? all - ROOM : m[x], al = m[x] == BR_KV_NEG ? (l[x] != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m[x] - to), was = c[x] * al;
+      const float top = br_kv_max4(__builtin_amdgcn_exp2f(__builtin_fmaf(mx, f, to == BR_KV_NEG ? 0.0f : -to)) * UNIT * vx);  // the tile's largest product
+      // c falls as the sums do (to a power of two below: what is larger than c already is in 32 bits), so that it is the largest product's still
+      const unsigned e = min(max(max(__float_as_uint(was) >> 23 & 255u, (__float_as_uint(top) >> 23 & 255u) + 1), 21u), 253u);
+      c[x] = __uint_as_float(up | top > 32.0f * c[x] ? e << 23 : __float_as_uint(c[x]));
+      const float ao = was * __uint_as_float(0x7f000000u - __float_as_uint(c[x]));
       m[x] = to;
       l[x] *= al;
 #pragma unroll
@@ -268,7 +290,11 @@ __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQue
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[x][d][j] *= ao;
     }
+    __asm__("" : "+v"(m[x]), "+v"(c[x]));  // (or what follows is partly done on both ways here, and all sums are moved for the shorter one)
     const float ref = m[x] == BR_KV_NEG ? 0.0f : m[x];
+    // (a scale far above c has weights that are next to nothing: their product stays in range, and a scale of NaN one)
+    float wx = vx * (BrKvSums<D, NQ>::ONE * UNIT * __uint_as_float(0x7f000000u - __float_as_uint(c[x])));
+    wx = wx > 3.0e38f ? 3.0e38f : wx;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], f, -ref));
@@ -291,15 +317,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   r = scalar(r), h = scalar(h), row0 = scalar(row0), first_pos = scalar(first_pos), last_pos = scalar(last_pos), t = scalar(t), stop = scalar(stop);
   const BrKvRow &w = w0;
   auto &o = sums.o;
-  auto &m = sums.m;
-  auto &l = sums.l;
-  float cmax = 0.0f, cinv = 0.0f;  // c and its inverse
-#pragma unroll
-  for (int x = 0; x < NQ; ++x) {
-    m[x] = BR_KV_NEG, l[x] = 0.0f;
-#pragma unroll
-    for (int d = 0; d < ND; ++d) o[x][d] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  sums.clear();
 
   const int worker = r / p.rows;
   const int *table = p.table + (long long)r * p.max_blocks;
@@ -384,7 +402,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 
 
     br_h8 pf[NQ][2];
-    br_kv_weights<D, NQ>(p, q, s, ks, vs, have, t, first_pos, last_pos, !__any(!there(vid)), sums, cmax, cinv, pf);
+    br_kv_weights<D, NQ>(p, q, s, ks, vs, have, t, first_pos, last_pos, !__any(!there(vid)), sums, pf);
     // bytes behind the row's end are whatever memory held: an 8-bit float may be a NaN there
     if (FP8 && __any(have < 16)) {
       const unsigned long long full = ~0ull;
@@ -406,12 +424,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     }
     vid = vid1, vid1 = vid2;
   }
-  sums.c = cmax * (1.0f / 256.0f);
-#pragma unroll
-  for (int x = 0; x < NQ; ++x) {
-    l[x] = br_kv_sum4(l[x]);
-    if (m[x] == BR_KV_NEG) m[x] = 0.0f;
-  }
+  sums.close();
 }
 
 // Joins the pieces of a query tile, of blocks first .. first + parts - 1, into its result (all of the block's threads; sums and ml: NT of
@@ -707,7 +720,7 @@ __device__ __forceinline__ void br_kv_result(const BrKvAttend &p, const BrKvRow 
   for (int x = 0; x < NQ; ++x) {
     const int at = row + 16 * x + n;
     if (at >= rows_q) continue;
-    const float inv = s.l[x] != 0.0f ? s.c / s.l[x] : 0.0f;
+    const float inv = s.l[x] != 0.0f ? s.c[x] / s.l[x] : 0.0f;
     br_kv_store<D / 16>(p, w, h, qi * TQ + at, 4 * g, s.o[x], inv);
     if (g == 0) br_kv_store_lse(p, w, h, qi * TQ + at, s.m[x], s.l[x]);
   }
@@ -725,7 +738,7 @@ __device__ __forceinline__ void br_kv_piece(const BrKvAttend &p, int piece, int 
     for (int d = 0; d < D / 16; ++d) {
       br_f4 y = s.o[x][d];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] *= s.c;
+      for (int j = 0; j < 4; ++j) y[j] *= s.c[x];
       pieces.put(piece, pieces.item(row / 16 + x, d, g, n), y);
     }
     if (g == 0) br_kv_put2(p.ml + (piece * TQ + at) * 2, s.m[x], s.l[x]);
@@ -782,7 +795,7 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
           for (int d = 0; d < ND; ++d) {
             br_f4 y = s.o[0][d];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] *= s.c;
+            for (int j = 0; j < 4; ++j) y[j] *= s.c[0];
             kept[(piece * ND + d) * 64 + lane] = y;
           }
           if (g == 0) kept_ml[piece * 16 + n] = make_float2(s.m[0], s.l[0]);
@@ -915,13 +928,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
     const int first = scalar(at.tile_of(runs, a)), stop = scalar(at.tile_of(runs, b));
     const bool busy = row < rows_q;
     BrKvSums<D, NQ> s;
-    float cmax = 0.0f, cinv = 0.0f;
-#pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-      s.m[x] = BR_KV_NEG, s.l[x] = 0.0f;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) s.o[x][d] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
+    s.clear();
     const int *table = p.table + (long long)r * p.max_blocks;
     const int last_block = max(0, (len - 1) >> p.shift);
     auto id_of = [&](int token) { return table[min(token >> p.shift, last_block)]; };
@@ -1022,7 +1029,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
             });
         const int have = there(vid) ? min(max(len - t * BR_KV_TILE - 16 * g, 0), 16) : 0;
         br_h8 pf[NQ][2];
-        br_kv_weights<D, NQ>(p, q, z, there(vid) ? br_kv_sound(ks) : 0.0f, there(vid) ? br_kv_sound(vs) : 0.0f, have, t, first_pos, last_pos, !__any(!there(vid)), s, cmax, cinv, pf);
+        br_kv_weights<D, NQ>(p, q, z, there(vid) ? br_kv_sound(ks) : 0.0f, there(vid) ? br_kv_sound(vs) : 0.0f, have, t, first_pos, last_pos, !__any(!there(vid)), s, pf);
         br_kv_ahead<ND / 2, AHEAD>(
             [&](int d, br_h8 (&f)[4]) {
 #pragma unroll
@@ -1042,12 +1049,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
       vid = vid1, vid1 = vid2, vid2 = vid3, kid2 = kid3;
       __syncthreads();
     }
-    s.c = cmax * (1.0f / 256.0f);
-#pragma unroll
-    for (int x = 0; x < NQ; ++x) {
-      s.l[x] = br_kv_sum4(s.l[x]);
-      if (s.m[x] == BR_KV_NEG) s.m[x] = 0.0f;
-    }
+    s.close();
     if (whole) {
       br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, row, rows_q, s);
     } else {
