@@ -275,8 +275,15 @@ __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQue
     for (int j = 0; j < 16; ++j) mx = fmaxf(mx, z[j]);
     const float all = br_kv_max4(mx * f);
     const bool up = all > m[x] + (ROOM + 4.0f);
-    // (without any of these no product passes 2^6 c, whatever the tile's scores; rounded sums beyond 2^22 may be off by more than the 4 allow for)
-    if (__any(up | (vmax > 4.0f * c[x]) | (fabsf(all) > 0x1p22f))) {
+    const bool large = fabsf(all) > 0x1p22f;
+    // (without any of these no product passes 2^6 c, whatever the tile's scores)
+    if (__any(up | (vmax > 4.0f * c[x]) | large)) {
+      // (where rounding moves a score by more than those 4, the rounded ones go against m, which is one of them)
+      const float g = large ? f : 1.0f;
+      f = large ? 1.0f : f;
+      mx *= g;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) z[j] *= g;
       const float to = up ? all - ROOM : m[x], al = m[x] == BR_KV_NEG ? (l[x] != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m[x] - to), was = c[x] * al;
       const float top = br_kv_max4(__builtin_amdgcn_exp2f(__builtin_fmaf(mx, f, to == BR_KV_NEG ? 0.0f : -to)) * UNIT * vx);  // the tile's largest product
       // c falls as the sums do (to a power of two below: what is larger than c already is in 32 bits), so that it is the largest product's still

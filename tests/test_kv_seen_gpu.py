@@ -125,3 +125,29 @@ def test_scales_of_tokens_that_hardly_count(fmt, n, group, D):
         out, lse = _run(h, cache, layer, q, lens, start, count, scale=1.0)
         _check((fmt, n, group, D, score.tolist(), e.tolist()), h, q, out, lse, lens, start, count, group, b, fmt, scale=1.0)
     cache.close()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("n,group,D", [(1, 1, 64), (2, 7, 128), (70, 2, 128)])
+def test_scores_beyond_what_32_bits_tell_apart(fmt, n, group, D):
+    """Scores of 2^24 to 2^40, thousands apart, at scales that are no powers of two: the token with the largest has all of the weight."""
+    torch = _torch()
+    rng = np.random.default_rng(D + n)
+    b, L = 16, 333
+    lens, count, start = np.array([L]), np.array([n]), np.array([0])
+    cache, layer, h = _cache_of(rng, fmt, 1, 1, b, D, 1, group, lens[None])
+    ids = h["table"][0, 0, :-(-L // b)]
+    h["ks"][ids], h["vs"][ids] = 1.0 / 3.0, (1.0 / 3.0 * np.exp(rng.normal(size=len(ids)) * 0.5))[:, None]
+    for e in (18, 26, 34):
+        q = torch.zeros(n, group, D, dtype=torch.bfloat16, device="cuda:0")
+        q[:, :, 0] = 2.0 ** e
+        for best in (3, 100, L - n):  # (seen by all)
+            code = rng.integers(-100, 80, (len(ids), 1, b)).astype(np.float64)
+            code[best // b, 0, best % b] = 96
+            h["k"][ids, :, :, 0] = ko.encode(code, fmt)
+            out, lse = _run(h, cache, layer, q, lens, start, count, scale=1.0)
+            want = ko.decode(h["v"][ids[best // b], 0, :, best % b], fmt) * float(h["vs"][ids[best // b], 0])
+            err = np.abs(out.double().cpu().numpy() - want)
+            assert (err <= np.abs(want) * (2.0 ** -8 + 2.0 ** -10)).all(), (fmt, n, e, best)
+            assert (np.abs(lse.double().cpu().numpy() / (2.0 ** e * 32) - 1) < 2.0 ** -20).all()
+    cache.close()
