@@ -200,7 +200,8 @@ int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_atten
   p.ml = (float *)(base + ctx->at.ml);
   p.arrived = (int *)(base + ctx->at.arrived);
   p.q_token = a->q_token, p.q_head = a->q_head, p.out_token = a->out_token, p.out_head = a->out_head;
-  p.n_rows = c.n_workers * c.rows, p.rows = c.rows, p.n_tokens = a->n_tokens, p.window = a->window;
+  p.n_rows = c.n_workers * c.rows, p.rows = c.rows, p.n_tokens = a->n_tokens;
+  p.window = a->window < c.max_blocks << ctx->t.shift ? a->window : 0;  // (a longer one hides nothing)
   p.group = group, p.kv_heads = c.n_kv_heads, p.shift = ctx->t.shift, p.n_blocks = c.n_blocks, p.max_blocks = c.max_blocks;
   p.group_shift = (unsigned)log2_of(group);
   p.group_mul = (unsigned)((((uint64_t)1 << 32) * (((uint64_t)1 << p.group_shift) - group)) / group + 1);

@@ -48,7 +48,7 @@ __device__ __forceinline__ int br_kv_token(const BrKvAttend &p, int row) { retur
 template <int TQ>
 __device__ __forceinline__ int br_kv_span(const BrKvAttend &p, const BrKvRow &w, int qi, int &t0, int &t1) {
   const int i0 = br_kv_token(p, qi * TQ), i1 = min(w.n - 1, br_kv_token(p, qi * TQ + TQ - 1)), at = w.len - w.n;
-  const int hi = max(0, at + i1 + 1), lo = p.window > 0 ? max(0, at + i0 - p.window + 1) : 0;
+  const int hi = max(0, at + i1 + 1), lo = p.window > 0 ? max(0, max(at + i0, 0) - p.window + 1) : 0;
   t0 = lo / BR_KV_TILE;
   t1 = max(t0, (hi + BR_KV_TILE - 1) / BR_KV_TILE);
   return max(1, t1 - t0);
@@ -201,7 +201,7 @@ struct BrKvQueries {
     for (int x = 0; x < NQ; ++x) {
       const int ri = row0 + 16 * x + n, i = br_kv_token(p, ri), t = w.start + i;
       const bool in = i < w.n && t >= 0 && t < p.n_tokens;
-      pos[x] = in ? w.len - w.n + i : -1;
+      pos[x] = in ? max(w.len - w.n + i, -1) : -1;
       const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(h * p.group + ri - i * p.group) * p.q_head : 0);
       uint4 e[NK];
       auto channel = [&](int c) { return c < 2 * NI ? (c / 2) * 64 + g * 16 + (c & 1) * 8 : NI * 64 + g * 8; };
@@ -715,8 +715,8 @@ struct BrKvPlace {
   // the first tile of its unit k (one past the last, for k = size)
   __device__ __forceinline__ int tile_of(const Runs &runs, int k) const { return runs.parts ? t0 + (int)((long long)(t1 - t0) * k / size) : min(t0 + k, t1); }
   __device__ __forceinline__ int rows_q(const BrKvAttend &p) const { return (int)min((long long)TQ, (long long)w.n * p.group - (long long)qi * TQ); }
-  // positions of the first and the last query of rows a .. b of the tile
-  __device__ __forceinline__ int pos_of(const BrKvAttend &p, int row) const { return w.len - w.n + min(w.n - 1, br_kv_token(p, qi * TQ + row)); }
+  // position of the query of that row of the tile, or of the last one; -1 of any before the row's first token
+  __device__ __forceinline__ int pos_of(const BrKvAttend &p, int row) const { return max(w.len - w.n + min(w.n - 1, br_kv_token(p, qi * TQ + row)), -1); }
 };
 
 // A wave's result of query rows row.. of the tile, to its place, or as piece `piece` to memory
