@@ -204,8 +204,8 @@ int32_t br_kv_step(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out
  * power of two, if the cache was written elsewhere).  Codes are value / s rounded to nearest, ties to even; codes of the earlier tokens
  * are rescaled to the new s the same way.  A value that is not finite makes the scale NaN (the new tokens' codes 0) until the block is
  * begun again at offset 0: every value read there is NaN.  An earlier scale that is none (below 0, not finite, 2^126 or more) does the same.
- * Tokens of one block stand together in the list, offsets ascending by one, as br_kv_step lists them.  A block that
- * occurs in two places of one call's list holds what one or the other of them has left.
+ * Tokens of one block stand together in the list, offsets ascending by one, as br_kv_step lists them.  What a block holds
+ * that occurs in two places of one call's list is not said; other blocks hold what they would without it.
  */
 int32_t br_kv_append(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_tokens *in);
 

@@ -197,14 +197,15 @@ __device__ __forceinline__ BrKvScale br_kv_scale(float top, int off, float old) 
   return z;
 }
 
-// nt threads (64, a wave, or 256, a block that is all here) write a run.  red: 8 floats of LDS.  The first AT_ONCE rows of keys and 4 x 8 values
+// nt threads (64, a wave, or 256, a block that is all here) write a run.  red: 10 floats of LDS.  Earlier scales are read once for all threads: where a
+// list has the run's block in another place too they may be changed beside this, and what threads do behind them has to agree.  The first AT_ONCE rows of keys and 4 x 8 values
 // of a thread (all, up to 64 tokens of 128 channels for a block) stay in registers between the maximum and the codes.
 template <bool FP8, int DT, bool WIDE>
 __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvTokens &a, const BrKvRun &u, int nt, int tid, float *red) {
   constexpr int AT_ONCE = 4, SIZE = DT == BR_KV_F32 ? 4 : 2;
   const int D = c.dim, b = 1 << c.shift, chunks = D >> 3, pairs = D >> 1;
   unsigned char *kc = c.k + ((u.block * D) << c.shift), *vc = c.v + ((u.block * D) << c.shift);
-  const float old_k = u.off ? c.ks[u.block] : 0.0f, old_v = u.off ? c.vs[u.block] : 0.0f;
+  float old_k = u.off ? c.ks[u.block] : 0.0f, old_v = u.off ? c.vs[u.block] : 0.0f;
   // keys: 8 channels from kd on of tokens kj, kj + kstep, ...
   const int kj = tid / chunks, kd = (tid - kj * chunks) * 8, kstep = nt / chunks, kn = kj < kstep ? u.n : 0;
   const char *xk = (const char *)a.k + (u.t * a.k_token + (long long)u.h * a.k_head) * SIZE, *xv = (const char *)a.v + (u.t * a.v_token + (long long)u.h * a.v_head) * SIZE;
@@ -256,9 +257,11 @@ __device__ __forceinline__ void br_kv_append_run(const BrKvCache &c, const BrKvT
   if (nt > 64) {
     __syncthreads();
     if ((tid & 63) == 0) red[tid >> 6] = top_k, red[4 + (tid >> 6)] = top_v;
+    if (tid == 0) red[8] = old_k, red[9] = old_v;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 4; ++k) top_k = fmaxf(top_k, red[k]), top_v = fmaxf(top_v, red[4 + k]);
+    old_k = red[8], old_v = red[9];
   }
   const BrKvScale zk = br_kv_scale<FP8>(top_k, u.off, old_k), zv = br_kv_scale<FP8>(top_v, u.off, old_v);
 
@@ -396,7 +399,7 @@ __device__ __forceinline__ unsigned long long br_kv_heads(const int *slot, int t
 // `span` tokens of a list (at most 64) and a key head for a block, or one for a wave (WAVE).  `grain`: tokens that a run may have, less one (append: a block's).
 template <bool FP8, int DT, bool READ, bool WIDE, bool WAVE>
 __global__ __launch_bounds__(256) void br_kv_k_tokens(BrKvCache c, BrKvTokens a, int span, int grain) {
-  __shared__ float red[8];
+  __shared__ float red[10];
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, b1 = (1 << c.shift) - 1, slots = c.n_blocks << c.shift;
   if (WAVE) span = 1;
   const int spans = (a.n + span - 1) / span;

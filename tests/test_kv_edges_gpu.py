@@ -20,3 +20,32 @@ def test_windows_that_hide_nothing(window, group):
     lens, counts = [[20, 3, 40, 0, 100]], [[30, 9, 2, 3, 4]]  # (tables of 8 blocks of 16 tokens)
     _attend_case("window", "int8", "float16", 64, 2, group, 16, lens, counts, window=window)
     _attend_case("window", "fp8", "bfloat16", 128, 1, group, 16, lens, counts, window=window)
+
+
+@pytest.mark.parametrize("fmt,D,b,H", [("int8", 128, 64, 3), ("fp8", 256, 128, 2), ("int8", 64, 16, 1), ("fp8", 96, 32, 4)])
+def test_lists_that_name_a_block_twice(fmt, D, b, H):
+    """What such a block then holds is not said; all others hold what they would without it."""
+    torch = _torch()
+    _say("twice", fmt, D, b, H)
+    rng = np.random.default_rng(D)
+    N = 60
+    cache = kv.KvCache(kv.KvConfig(rows=2, block_tokens=b, n_blocks=N, max_blocks=N, n_kv_heads=H, n_q_heads=H, head_dim=D, fmt=fmt))
+    layer = cache.new_layer()
+    k = ko.encode(rng.integers(-110, 111, (N, H, b, D)).astype(np.float64), fmt)
+    s = np.exp2(rng.integers(-12, 3, (N, H))).astype(np.float32)
+    layer.k.copy_(_dev(k)), layer.v.copy_(layer.k.transpose(2, 3)), layer.k_scale.copy_(_dev(s)), layer.v_scale.copy_(_dev(s))
+    slot = []
+    for i in rng.permutation(N - 2):  # blocks N - 2 and N - 1: again and again, from offsets inside them, between all others
+        off = int(rng.integers(0, b - 3))
+        slot += list(i * b + np.arange(off, b if rng.random() < 0.5 else off + 3))
+        off = int(rng.integers(1, b - 3))
+        slot += list((N - 1 - int(rng.integers(0, 2))) * b + np.arange(off, b))
+    slot = np.array(slot, np.int32)
+    T = len(slot)
+    x = (rng.normal(size=(T, H, D)) * np.exp(rng.normal(size=(T, 1, 1)) * 3)).astype(np.float32)
+    cache.append_device(layer, _dev(x), _dev(x), _dev(slot))
+    ok = slot // b < N - 2
+    ko.append(k, s, x[ok], slot[ok], b, fmt)
+    for scale, codes in ((layer.k_scale, layer.k), (layer.v_scale, layer.v.transpose(2, 3))):
+        assert np.array_equal(scale[:N - 2].cpu().numpy(), s[:N - 2]) and np.array_equal(codes[:N - 2].cpu().numpy(), k[:N - 2])
+    cache.close()
