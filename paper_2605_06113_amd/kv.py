@@ -4,7 +4,8 @@ values, attention over it.
 As in `binding`: argument marshalling only, every step runs in the library's kernels, PyTorch supplies device memory and
 the stream, and nothing falls back to the CPU.  All `*_device` calls enqueue on the cache's stream and return; they check
 types, shapes, strides and devices, since the C ABI takes bare pointers.  Tensors made or used on another stream are the
-caller's to order against the cache's stream (`stream.wait_stream`, `Tensor.record_stream`).
+caller's to order against the cache's stream (`stream.wait_stream`, `Tensor.record_stream`).  Memory that a cache makes itself
+(workspace, `new_layer`, `alloc_step`) is the cache's stream's, whatever stream is current; `lens` and `table` at the start may be the current one's.
 
     cfg = kv.KvConfig(rows=96, n_blocks=4096, max_blocks=512, n_kv_heads=8, n_q_heads=32, head_dim=128, fmt="fp8")
     cache = kv.KvCache(cfg)
@@ -18,6 +19,7 @@ caller's to order against the cache's stream (`stream.wait_stream`, `Tensor.reco
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import struct
 from dataclasses import dataclass
@@ -152,9 +154,13 @@ class KvCache:
             self._check(lens, "lens", (W, B), torch.int32)
             self._check(table, "table", (W, B, cfg.max_blocks), torch.int32)
             state = C.byref(_State(lens=lens.data_ptr(), table=table.data_ptr()))
-        self.ws = torch.empty(nbytes // 4 + 64, dtype=torch.int32, device=self.device)
+        current = torch.cuda.current_stream(self.device)
+        self.stream = stream if stream is not None else current
+        if lens is not None and self.stream != current:  # what is on its way there comes first
+            self.stream.wait_stream(current)
+        with self._own():
+            self.ws = torch.empty(nbytes // 4 + 64, dtype=torch.int32, device=self.device)
         assert self.ws.data_ptr() % 256 == 0
-        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         c = _config(cfg, stream=self.stream.cuda_stream, workspace=self.ws.data_ptr(), workspace_bytes=self.ws.numel() * 4)
         ctx = _P()
         with torch.cuda.device(self.device):
@@ -206,6 +212,10 @@ class KvCache:
         return dtype, token, head
 
     # -- memory ---------------------------------------------------------------
+    def _own(self):
+        """Memory made in here belongs to the cache's stream: the allocator hands it out again behind that stream's work."""
+        return self.torch.cuda.stream(self.stream) if self._index >= 0 else contextlib.nullcontext()
+
     def layer(self, k, v, k_scale, v_scale) -> KvLayer:
         """A layer over memory that is there (16-byte aligned)."""
         t, c = self.torch, self.cfg
@@ -220,14 +230,16 @@ class KvCache:
         t, c = self.torch, self.cfg
         n, H, b, D = c.n_workers * c.n_blocks, c.n_kv_heads, c.block_tokens, c.head_dim
         e = lambda shape, dtype: t.empty(shape, dtype=dtype, device=self.device)
-        return self.layer(e((n, H, b, D), t.uint8), e((n, H, D, b), t.uint8), e((n, H), t.float32), e((n, H), t.float32))
+        with self._own():
+            return self.layer(e((n, H, b, D), t.uint8), e((n, H, D, b), t.uint8), e((n, H), t.float32), e((n, H), t.float32))
 
     def alloc_step(self, token_cap: int) -> Dict[str, object]:
         """Output arrays of step_device, with room for token_cap new tokens per worker."""
         t, W, B = self.torch, self.cfg.n_workers, self.cfg.rows
         e = lambda *shape: t.empty(shape, dtype=t.int32, device=self.device)
-        return dict(slot=e(W, token_cap), pos=e(W, token_cap), start=e(W, B), count=e(W, B), status=e(W, B),
-                    stats=t.empty((W, NSTATS), dtype=t.int64, device=self.device))
+        with self._own():
+            return dict(slot=e(W, token_cap), pos=e(W, token_cap), start=e(W, B), count=e(W, B), status=e(W, B),
+                        stats=t.empty((W, NSTATS), dtype=t.int64, device=self.device))
 
     # -- calls ----------------------------------------------------------------
     def step_device(self, keep, add, out) -> None:

@@ -49,3 +49,60 @@ def test_lists_that_name_a_block_twice(fmt, D, b, H):
     for scale, codes in ((layer.k_scale, layer.k), (layer.v_scale, layer.v.transpose(2, 3))):
         assert np.array_equal(scale[:N - 2].cpu().numpy(), s[:N - 2]) and np.array_equal(codes[:N - 2].cpu().numpy(), k[:N - 2])
     cache.close()
+
+
+def _in_use(shape, dtype):
+    """Memory of the current stream that is free again while zeros are still on their way there."""
+    torch = _torch()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    x = torch.empty(shape, dtype=dtype, device="cuda:0")
+    torch.cuda._sleep(20_000_000)
+    x.zero_()
+
+
+def test_a_cache_on_a_stream_of_its_own():
+    """Workspace, layers and step arrays made while another stream is current: what that stream still does in memory that it has given back does not
+    reach them, and what they give back is not handed out there while the cache's stream works in it.  Requests at the start may be that stream's."""
+    torch = _torch()
+    stream = torch.cuda.Stream()
+    rng = np.random.default_rng(3)
+    W, B, b, N, M = 1, 40, 16, 4096, 60
+    lens = rng.integers(1, 900, (W, B))
+    table = _scattered(rng, lens, b, N, M)
+    cfg = kv.KvConfig(n_workers=W, rows=B, block_tokens=b, n_blocks=N, max_blocks=M, n_kv_heads=1, head_dim=128)
+    dl, dt = _dev(lens, torch.int32), _dev(table)
+    _in_use(kv.workspace_bytes(cfg) // 4 + 64, torch.int32)
+    cache = kv.KvCache(cfg, lens=dl, table=dt, stream=stream)
+    torch.cuda.synchronize()
+    assert np.array_equal(cache.lens.cpu().numpy(), lens) and np.array_equal(cache.table.cpu().numpy(), table)
+    shape = (N, 1, b, 128)
+    _in_use(shape, torch.uint8)
+    layer = cache.new_layer()
+    with torch.cuda.stream(stream):
+        layer.k.fill_(7)
+    torch.cuda.synchronize()
+    assert bool((layer.k == 7).all())
+    _in_use((W, 1 << 21), torch.int32)
+    step = cache.alloc_step(1 << 21)
+    with torch.cuda.stream(stream):
+        step["slot"].fill_(7)
+    torch.cuda.synchronize()
+    assert bool((step["slot"] == 7).all())
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(20_000_000)
+        layer.k.fill_(9)
+    del layer
+    mine = torch.empty(shape, dtype=torch.uint8, device="cuda:0").fill_(3)
+    torch.cuda.synchronize()
+    assert bool((mine == 3).all())
+    cache.close()
+    # lengths and blocks that the current stream has yet to write
+    late, at = torch.zeros_like(dl), torch.full_like(dt, -1)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    late.copy_(dl), at.copy_(dt)
+    cache = kv.KvCache(cfg, lens=late, table=at, stream=stream)
+    torch.cuda.synchronize()
+    assert np.array_equal(cache.lens.cpu().numpy(), lens) and np.array_equal(cache.table.cpu().numpy(), table)
+    cache.close()
