@@ -166,7 +166,8 @@ class KvCache:
         with torch.cuda.device(self.device):
             self._done(self.lib.br_kv_init(C.byref(c), state, C.byref(ctx)), "br_kv_init")
         self.ctx = ctx
-        self._init = (lens, table)  # alive until they have been copied
+        if lens is not None and self.stream != current:  # (their memory is not handed out again before they have been copied)
+            lens.record_stream(self.stream), table.record_stream(self.stream)
         lay = _Layout()
         self._done(self.lib.br_kv_get_layout(ctx, C.byref(lay)), "br_kv_get_layout")
         #: cached tokens of every row and the block tables, as they are on the device: [n_workers, rows] and [n_workers, rows, max_blocks]

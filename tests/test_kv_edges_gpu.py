@@ -1,6 +1,4 @@
 """Calls at the limits of what include/br_kv.h allows, on the GPU: windows, strides, scales, lists that name a block twice, streams."""
-import ctypes as C
-import math
 import weakref
 
 import numpy as np
@@ -105,4 +103,18 @@ def test_a_cache_on_a_stream_of_its_own():
     cache = kv.KvCache(cfg, lens=late, table=at, stream=stream)
     torch.cuda.synchronize()
     assert np.array_equal(cache.lens.cpu().numpy(), lens) and np.array_equal(cache.table.cpu().numpy(), table)
+    cache.close()
+
+
+def test_requests_of_the_start_are_not_kept():
+    """The tensors that a cache begins with are the caller's alone once it has them."""
+    torch = _torch()
+    cfg = kv.KvConfig(rows=4, n_blocks=8, max_blocks=2)
+    lens, table = torch.ones((1, 4), dtype=torch.int32, device="cuda:0"), torch.arange(8, dtype=torch.int32, device="cuda:0").view(1, 4, 2)
+    cache = kv.KvCache(cfg, lens=lens, table=table, stream=torch.cuda.Stream())
+    refs = weakref.ref(lens), weakref.ref(table)
+    del lens, table
+    assert refs[0]() is None and refs[1]() is None
+    torch.cuda.synchronize()
+    assert cache.lens.tolist() == [[1] * 4] and cache.table[0, :, 0].tolist() == [0, 2, 4, 6]
     cache.close()
