@@ -203,7 +203,7 @@ int32_t br_kv_step(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out
  * a <= top * s, or that of the block's earlier tokens (the first new token is not at its offset 0) if that is larger (rounded up to a
  * power of two, if the cache was written elsewhere).  Codes are value / s rounded to nearest, ties to even; codes of the earlier tokens
  * are rescaled to the new s the same way.  A value that is not finite makes the scale NaN (the new tokens' codes 0) until the block is
- * begun again at offset 0: every value read there is NaN.  An earlier scale that is none (below 0, not finite, 2^126 or more) does the same.
+ * begun again at offset 0: every value read there is NaN.  An earlier scale that is none (below 0, not finite, above 2^126) does the same.
  * Tokens of one block stand together in the list, offsets ascending by one, as br_kv_step lists them.  What a block holds
  * that occurs in two places of one call's list is not said; other blocks hold what they would without it.
  */

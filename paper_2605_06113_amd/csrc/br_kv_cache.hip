@@ -186,8 +186,8 @@ __device__ __forceinline__ BrKvScale br_kv_scale(float top, int off, float old) 
   unsigned e = br_kv_scale_exp<FP8>(bad ? 0.0f : top);
   BrKvScale z = {0.0f, 0.0f, 1.0f, bad};
   if (off > 0) {
-    // (a scale that is no power of two, in a cache that was written elsewhere, moves up to one)
-    z.bad = z.bad || !(old >= 0.0f && old < 8.5e37f);
+    // (a scale that is no power of two, in a cache that was written elsewhere, moves up to one: 2^126 at most, whose inverse is the least normal number)
+    z.bad = z.bad || !(old >= 0.0f && old <= 0x1p126f);
     const unsigned u = z.bad ? 0u : __float_as_uint(old);
     e = max(e, (u >> 23) + ((u & 0x7fffffu) != 0));
     z.r = z.bad ? 1.0f : old * br_kv_inverse(e);

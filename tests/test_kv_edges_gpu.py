@@ -118,3 +118,31 @@ def test_requests_of_the_start_are_not_kept():
     torch.cuda.synchronize()
     assert cache.lens.tolist() == [[1] * 4] and cache.table[0, :, 0].tolist() == [0, 2, 4, 6]
     cache.close()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_scales_up_to_the_largest(fmt):
+    """Earlier scales up to 2^126 are scales, whatever their bits, and stay what an append has made of them; those above are none."""
+    torch = _torch()
+    D, b = 64, 16
+    good = [2.0 ** 124, 2.0 ** 125, 1.5 * 2.0 ** 125, 8.5e37, 8.505e37, float(np.nextafter(np.float32(2.0 ** 126), np.float32(0))), 2.0 ** 126]
+    none = [float(np.nextafter(np.float32(2.0 ** 126), np.float32(np.inf))), 1.5 * 2.0 ** 126, 2.0 ** 127, 3.4e38]
+    s = np.array(good + none, np.float32)[:, None]
+    N = len(s)
+    cache = kv.KvCache(kv.KvConfig(rows=2, block_tokens=b, n_blocks=N, max_blocks=4, head_dim=D, fmt=fmt))
+    layer = cache.new_layer()
+    rng = np.random.default_rng(1)
+    k = ko.encode(rng.integers(-110, 111, (N, 1, b, D)).astype(np.float64), fmt)
+    layer.k.copy_(_dev(k)), layer.v.copy_(layer.k.transpose(2, 3))
+    layer.k_scale.copy_(_dev(s)), layer.v_scale.copy_(_dev(s))
+    ks, n = s[:len(good)].copy(), len(good)
+    k = k[:n]
+    for off in (5, 6, 7):
+        x = rng.normal(size=(N, 1, D)).astype(np.float32) * (1.0 if off < 7 else 1e37)
+        slot = np.arange(N) * b + off
+        cache.append_device(layer, _dev(x), _dev(x), _dev(slot, torch.int32))
+        ko.append(k, ks, x[:n], slot[:n], b, fmt)
+        for scale, codes in ((layer.k_scale, layer.k), (layer.v_scale, layer.v.transpose(2, 3))):
+            assert np.array_equal(scale[:n].cpu().numpy(), ks) and np.array_equal(codes[:n].cpu().numpy(), k), off
+            assert bool(torch.isnan(scale[n:]).all()), off
+    cache.close()
