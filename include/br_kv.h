@@ -39,6 +39,7 @@
 extern "C" {
 #endif
 
+#define BR_KV_MAX_WORKERS 16777215
 #define BR_KV_MAX_ROWS 1024
 #define BR_KV_MAX_BLOCKS 262144      /* blocks of a worker */
 #define BR_KV_MAX_LEN 1048576        /* tokens that a row's table may span */
@@ -72,7 +73,7 @@ enum {
 typedef struct br_kv_ctx br_kv_ctx; /* opaque; host object owned by the library */
 
 typedef struct {
-  int32_t n_workers;    /* >= 1; n_workers * rows < 2^26 */
+  int32_t n_workers;    /* 1..2^24 - 1; n_workers * rows < 2^26 */
   int32_t rows;         /* requests a worker may hold (its slot limit), 1..1024 */
   int32_t block_tokens; /* 16, 32, 64 or 128 */
   int32_t n_blocks;     /* blocks of each worker, 1..262144 */

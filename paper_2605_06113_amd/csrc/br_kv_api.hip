@@ -20,7 +20,8 @@ int log2_of(int32_t x) {
 
 bool config_ok(const br_kv_config *c) {
   if (!c) return false;
-  if (c->n_workers < 1 || c->rows < 1 || c->rows > BR_KV_MAX_ROWS || (int64_t)c->n_workers * c->rows >= 1 << 26) return false;
+  if (c->n_workers < 1 || c->n_workers > BR_KV_MAX_WORKERS) return false;  // (a block of 256 threads each: a launch has fewer than 2^32)
+  if (c->rows < 1 || c->rows > BR_KV_MAX_ROWS || (int64_t)c->n_workers * c->rows >= 1 << 26) return false;
   if (c->block_tokens != 16 && c->block_tokens != 32 && c->block_tokens != 64 && c->block_tokens != 128) return false;
   if (c->n_blocks < 1 || c->n_blocks > BR_KV_MAX_BLOCKS) return false;
   if (c->max_blocks < 1 || c->max_blocks > BR_KV_MAX_LEN / c->block_tokens) return false;
