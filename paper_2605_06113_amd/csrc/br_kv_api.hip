@@ -94,7 +94,7 @@ BrKvCache cache_of(const br_kv_ctx *ctx, const br_kv_layer *l) {
 
 bool tokens_ok(const br_kv_ctx *ctx, const br_kv_tokens *x) {
   if (!x || x->n_tokens < 0 || x->dtype < BR_KV_F16 || x->dtype > BR_KV_F32) return false;
-  if ((int64_t)ctx->cfg.n_workers * x->n_tokens > INT32_MAX) return false;
+  if ((int64_t)ctx->cfg.n_workers * x->n_tokens > INT32_MAX - 256) return false;  // (the kernels look up to 192 places ahead)
   if (x->n_tokens == 0) return true;
   if (!x->k || !x->v || !x->slot) return false;
   if (x->k_token < 0 || x->k_token >= BR_KV_MAX_STRIDE || x->v_token < 0 || x->v_token >= BR_KV_MAX_STRIDE) return false;  // (32-bit offsets within a block)

@@ -37,6 +37,7 @@ const char *stand_in_log() { static std::string out; out = log_; log_.clear(); r
 }
 """
 THREADS = 2 ** 32  # of a launch: fewer
+INT_MAX = 2 ** 31 - 1
 
 
 class Library:
@@ -45,6 +46,7 @@ class Library:
         self.fake.stand_in_log.restype = C.c_char_p
         from paper_2605_06113_amd import kv
         self.kv, self.lib = kv, kv.load()
+        self.layer = kv._Layer(k=1 << 30, v=1 << 30, k_scale=1 << 30, v_scale=1 << 30)
 
     def context(self, **cfg):
         c = self.kv._config(self.kv.KvConfig(**cfg), workspace=1 << 20, workspace_bytes=1 << 62)
@@ -53,6 +55,10 @@ class Library:
 
     def launches(self):
         return [(name, int(n)) for name, n in re.findall(r"(br_kv_k_[a-z]+)\S* (\d+)", self.fake.stand_in_log().decode())]
+
+    def tokens(self, call, **kw):
+        a = self.kv._Tokens(**{**dict(k=1 << 30, v=1 << 30, slot=1 << 30, k_token=64, k_head=64, v_token=64, v_head=64, n_tokens=1, dtype=0), **kw})
+        return getattr(self.lib, call)(self.ctx, C.byref(self.layer), C.byref(a))
 
 
 def as_many_workers_as_a_launch_has_blocks_for(lib):
@@ -68,7 +74,21 @@ def as_many_workers_as_a_launch_has_blocks_for(lib):
         assert lib.context(n_workers=W, rows=rows, n_blocks=1, max_blocks=1) == -1 and not lib.ctx.value
 
 
-SCENARIOS = [as_many_workers_as_a_launch_has_blocks_for]
+def lists_as_long_as_their_places_can_be_counted(lib):
+    for W in (1, 3, 1024):
+        assert lib.context(n_workers=W, rows=2, n_blocks=1, max_blocks=1) == 0
+        lib.launches()
+        most = (INT_MAX - 256) // W
+        for call in ("br_kv_append", "br_kv_read"):
+            assert lib.tokens(call, n_tokens=most) == 0
+            done = lib.launches()
+            assert [n for n, _ in done] == ["br_kv_k_tokens"] and all(n < THREADS for _, n in done)
+            for n in {most + 1, most + 100 // W + 1, INT_MAX // W, INT_MAX}:
+                assert lib.tokens(call, n_tokens=n) == -1 and lib.launches() == []
+        lib.lib.br_kv_free(lib.ctx)
+
+
+SCENARIOS = [as_many_workers_as_a_launch_has_blocks_for, lists_as_long_as_their_places_can_be_counted]
 
 
 @pytest.fixture(scope="module")
