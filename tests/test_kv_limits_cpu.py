@@ -83,7 +83,7 @@ def lists_as_long_as_their_places_can_be_counted(lib):
             assert lib.tokens(call, n_tokens=most) == 0
             done = lib.launches()
             assert [n for n, _ in done] == ["br_kv_k_tokens"] and all(n < THREADS for _, n in done)
-            for n in {most + 1, most + 100 // W + 1, INT_MAX // W, INT_MAX}:
+            for n in {most + 1, most + 100 // W + 1, max(most + 1, INT_MAX // W), INT_MAX}:
                 assert lib.tokens(call, n_tokens=n) == -1 and lib.launches() == []
         lib.lib.br_kv_free(lib.ctx)
 
