@@ -146,7 +146,7 @@ typedef struct {
   void *k;
   void *v;
   const int32_t *slot;
-  int64_t k_token, k_head, v_token, v_head; /* k_token and v_token in 0 .. BR_KV_MAX_STRIDE - 1 */
+  int64_t k_token, k_head, v_token, v_head; /* k_token and v_token in 0 .. BR_KV_MAX_STRIDE - 1 (of one token: anything) */
   int32_t n_tokens; /* >= 0; n_workers * n_tokens at most 2^31 - 257 */
   int32_t dtype;    /* BR_KV_F16, BR_KV_BF16 or BR_KV_F32 */
 } br_kv_tokens;

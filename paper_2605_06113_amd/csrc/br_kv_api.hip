@@ -92,12 +92,16 @@ BrKvCache cache_of(const br_kv_ctx *ctx, const br_kv_layer *l) {
   return c;
 }
 
+// (no token stride is looked at)
+bool one_token(const br_kv_ctx *ctx, const br_kv_tokens *x) { return ctx->cfg.n_workers == 1 && x->n_tokens == 1; }
+
 bool tokens_ok(const br_kv_ctx *ctx, const br_kv_tokens *x) {
   if (!x || x->n_tokens < 0 || x->dtype < BR_KV_F16 || x->dtype > BR_KV_F32) return false;
   if ((int64_t)ctx->cfg.n_workers * x->n_tokens > INT32_MAX - 256) return false;  // (the kernels look up to 192 places ahead)
   if (x->n_tokens == 0) return true;
   if (!x->k || !x->v || !x->slot) return false;
-  if (x->k_token < 0 || x->k_token >= BR_KV_MAX_STRIDE || x->v_token < 0 || x->v_token >= BR_KV_MAX_STRIDE) return false;  // (32-bit offsets within a block)
+  if (!one_token(ctx, x) && (x->k_token < 0 || x->k_token >= BR_KV_MAX_STRIDE || x->v_token < 0 || x->v_token >= BR_KV_MAX_STRIDE))
+    return false;  // (32-bit offsets within a block)
   const uintptr_t size = x->dtype == BR_KV_F32 ? 4 : 2;
   return (((uintptr_t)x->k | (uintptr_t)x->v) & (size - 1)) == 0 && ((uintptr_t)x->slot & 3u) == 0;
 }
@@ -106,8 +110,9 @@ BrKvTokens tokens_of(const br_kv_ctx *ctx, const br_kv_tokens *x) {
   BrKvTokens t;
   t.k = x->k, t.v = x->v, t.slot = x->slot;
   t.k_token = x->k_token, t.k_head = x->k_head, t.v_token = x->v_token, t.v_head = x->v_head;
+  if (one_token(ctx, x)) t.k_token = t.v_token = 0;
   t.n = x->n_tokens, t.W = ctx->cfg.n_workers, t.dtype = x->dtype;
-  const int64_t strides = x->k_token | x->k_head | x->v_token | x->v_head;
+  const int64_t strides = t.k_token | t.k_head | t.v_token | t.v_head;
   t.wide = (((uintptr_t)x->k | (uintptr_t)x->v) & 15u) == 0 && (strides & (x->dtype == BR_KV_F32 ? 3 : 7)) == 0;
   return t;
 }

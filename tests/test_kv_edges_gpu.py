@@ -146,3 +146,23 @@ def test_scales_up_to_the_largest(fmt):
             assert np.array_equal(scale[:n].cpu().numpy(), ks) and np.array_equal(codes[:n].cpu().numpy(), k), off
             assert bool(torch.isnan(scale[n:]).all()), off
     cache.close()
+
+
+def test_one_token_of_any_stride():
+    """Where there is one token, what lies between it and a next one is nobody's."""
+    torch = _torch()
+    H, D = 2, 64
+    cache = kv.KvCache(kv.KvConfig(rows=2, n_blocks=4, max_blocks=2, n_kv_heads=H, n_q_heads=H, head_dim=D))
+    layer = cache.new_layer()
+    x = torch.randn(2, H, D, dtype=torch.float16, device="cuda:0")
+    far = [torch.as_strided(x[i], (1, H, D), (2 ** 40 + 1, D, 1)) for i in range(2)]
+    slot = torch.full((1,), 16, dtype=torch.int32, device="cuda:0")
+    cache.append_device(layer, far[0], far[1], slot)
+    y = torch.zeros(2, H, D, dtype=torch.float16, device="cuda:0")
+    back = [torch.as_strided(y[i], (1, H, D), (2 ** 40 + 1, D, 1)) for i in range(2)]
+    cache.read_device(layer, slot, back[0], back[1])
+    near = torch.zeros_like(y)
+    cache.append_device(layer, x[:1].clone(), x[1:].clone(), slot)
+    cache.read_device(layer, slot, near[:1], near[1:])
+    assert torch.equal(y, near) and bool((y - x).abs().max() < 0.05)
+    cache.close()
