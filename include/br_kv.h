@@ -18,6 +18,9 @@
  * The context's GPU has to be the current device of the calling thread, as for br.h's calls.  Memory that other streams have written or
  * will read is ordered against the context's stream by the caller (events); the library adds no waits.
  *
+ * What a call reads on the device stays as it is until the call has run.  An attention whose lengths or counts are changed under it leaves outputs
+ * that are not said, and so may those behind it up to the next br_kv_step.
+ *
  * What is read on the device is checked there and never leads outside a buffer: lengths, block ids, slots, starts and
  * counts out of range are clamped or skipped as each call says.
  *

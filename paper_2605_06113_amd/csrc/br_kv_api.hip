@@ -149,7 +149,8 @@ int32_t br_kv_init(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx *
   t.table = (int *)(base + at.table);
   t.tail = (int *)(base + at.tail);
   t.used = (unsigned *)(base + at.used);
-  int32_t rc = enqueue(ctx, [&] { br_kv_launch_clear(t, (int *)(base + at.arrived), ctx->st); });
+  t.arrived = (int *)(base + at.arrived);
+  int32_t rc = enqueue(ctx, [&] { br_kv_launch_clear(t, ctx->st); });
   if (rc == BR_OK && init) rc = enqueue(ctx, [&] { br_kv_launch_load(t, init->lens, init->table, ctx->st); });
   if (rc != BR_OK) {
     delete ctx;
@@ -204,7 +205,7 @@ int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_atten
   p.k = layer->k, p.v = layer->v, p.ks = layer->k_scale, p.vs = layer->v_scale;
   p.part = (float *)(base + ctx->at.part);
   p.ml = (float *)(base + ctx->at.ml);
-  p.arrived = (int *)(base + ctx->at.arrived);
+  p.arrived = ctx->t.arrived;
   p.q_token = a->q_token, p.q_head = a->q_head, p.out_token = a->out_token, p.out_head = a->out_head;
   p.n_rows = c.n_workers * c.rows, p.rows = c.rows, p.n_tokens = a->n_tokens;
   p.window = a->window < c.max_blocks << ctx->t.shift ? a->window : 0;  // (a longer one hides nothing)

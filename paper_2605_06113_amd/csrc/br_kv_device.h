@@ -18,6 +18,7 @@ struct BrKvTables {
   int *table;                                    // [W][B][max_blocks]
   int *tail;                                     // [W][B] each row's last block
   unsigned *used;                                // [W][words]
+  int *arrived;                                  // BrKvAttend's
 };
 
 struct BrKvStep {
@@ -51,7 +52,8 @@ struct BrKvAttend {
   const float *ks, *vs;
   float *part;  // sums of the pieces of split rows, see br_kv_attend.h
   float *ml;    // their maxima and sums of weights
-  int *arrived; // per block: blocks that have delivered a piece of the query tile that is split and begins in it; 0 between launches
+  int *arrived; // per block: blocks that have delivered a piece of the query tile that is split and begins in it; 0 between launches (a
+                // call whose lengths are changed under it may leave others, until the next step)
   long long q_token, q_head, out_token, out_head;
   int least, most;  // query tokens of the rows that this launch takes
   int n_rows, rows, n_tokens, window, group, kv_heads, shift, n_blocks, max_blocks;
@@ -60,7 +62,7 @@ struct BrKvAttend {
   float scale2;                // scale * log2(e)
 };
 
-void br_kv_launch_clear(const BrKvTables &t, int *arrived, hipStream_t st);
+void br_kv_launch_clear(const BrKvTables &t, hipStream_t st);
 void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, hipStream_t st);
 void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st);
 void br_kv_launch_append(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st);

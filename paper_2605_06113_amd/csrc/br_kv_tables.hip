@@ -4,7 +4,7 @@
 #include "br_kv_device.h"
 
 // Every row empty, every block free; nothing begun.
-__global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t, int *arrived) {
+__global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t) {
   const long long n = (long long)t.W * t.B * t.max_blocks, rows = (long long)t.W * t.B, words = (long long)t.W * t.words;
   const long long step = (long long)gridDim.x * 256;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
@@ -12,7 +12,7 @@ __global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t, int *arrived)
     if (i < rows) t.lens[i] = 0, t.tail[i] = -1;
   }
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < words; i += step) t.used[i] = 0;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < BR_KV_SPLIT_WGS; i += step) arrived[i] = 0;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < BR_KV_SPLIT_WGS; i += step) t.arrived[i] = 0;
 }
 
 // The rows held at the start (behind br_kv_k_clear).
@@ -127,6 +127,8 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
   int *tails = t.tail + (long long)w * B;
   unsigned *gused = t.used + (long long)w * t.words;
   if (tid == 0) give_n = 0;
+  if (w == 0)  // (nothing of an attention that went wrong outlives the step behind it)
+    for (int i = tid; i < BR_KV_SPLIT_WGS; i += NT) t.arrived[i] = 0;
   int kp[RPT], have[RPT], why[RPT], held[RPT], want[RPT], tail[RPT];
 #pragma unroll
   for (int i = 0; i < RPT; ++i) {
@@ -312,8 +314,8 @@ __global__ __launch_bounds__(256) void br_kv_k_list(BrKvTables t, BrKvStep s) {
 
 static int grid_for(long long n) { return (int)(n < 1 ? 1 : n > 4096ll * 256 ? 4096 : (n + 255) / 256); }
 
-void br_kv_launch_clear(const BrKvTables &t, int *arrived, hipStream_t st) {
-  br_kv_k_clear<<<grid_for((long long)t.W * t.B * t.max_blocks), 256, 0, st>>>(t, arrived);
+void br_kv_launch_clear(const BrKvTables &t, hipStream_t st) {
+  br_kv_k_clear<<<grid_for((long long)t.W * t.B * t.max_blocks), 256, 0, st>>>(t);
 }
 
 void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, hipStream_t st) {

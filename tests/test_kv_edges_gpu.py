@@ -166,3 +166,30 @@ def test_one_token_of_any_stride():
     cache.read_device(layer, slot, near[:1], near[1:])
     assert torch.equal(y, near) and bool((y - x).abs().max() < 0.05)
     cache.close()
+
+
+def test_a_step_clears_what_a_broken_call_has_left():
+    """Counters of delivered pieces that are not zero, as a call leaves them whose lengths were changed under it: after a step the next call is
+    right again."""
+    torch = _torch()
+    rng = np.random.default_rng(7)
+    D, b, L = 64, 16, 40000
+    N = L // b
+    cfg = kv.KvConfig(rows=2, block_tokens=b, n_blocks=N, max_blocks=N, head_dim=D)
+    lens, table = _dev([[L, 0]], torch.int32), _dev(_scattered(rng, np.array([[L, 0]]), b, N, N))
+    cache = kv.KvCache(cfg, lens=lens, table=table)
+    layer = cache.new_layer()
+    layer.k.random_(0, 256), layer.v.random_(0, 256), layer.k_scale.fill_(0.01), layer.v_scale.fill_(0.01)
+    q = torch.randn(2, 1, D, dtype=torch.float16, device="cuda:0")
+    want, out = torch.empty_like(q), torch.zeros_like(q)
+    cache.attend_device(layer, q, want)
+    zero, step = torch.zeros((1, 2), dtype=torch.int32, device="cuda:0"), cache.alloc_step(4)
+    total = kv.workspace_bytes(cfg) // 4
+    for left in (1, -1, 1000):
+        cache.ws[total - 768:total].fill_(left)  # (the last of the workspace, the counters among them)
+        cache.step_device(zero - 1, zero, step)
+        for _ in range(2):
+            out.zero_()
+            cache.attend_device(layer, q, out)
+            assert torch.equal(out, want), left
+    cache.close()
