@@ -49,7 +49,7 @@ Places make_layout(const br_kv_config &c) {
   l.used = take((uint64_t)c.n_workers * ((c.n_blocks + 31) / 32));
   l.runs = take(2 * rows);
   // two pieces of a query tile's rows for each block of the attention's largest launch
-  const uint64_t pieces = 2ull * BR_KV_SPLIT_WGS * 128;
+  const uint64_t pieces = 2ull * BR_KV_SPLIT_WGS_OF(c.head_dim) * 128;
   l.part = take(pieces * c.head_dim);
   l.ml = take(pieces * 2);
   l.arrived = take(BR_KV_SPLIT_WGS);

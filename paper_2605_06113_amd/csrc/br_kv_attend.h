@@ -117,7 +117,7 @@ struct BrKvPieces {
   __amdgpu_buffer_rsrc_t all;
   int rows, n16;  // rows side by side
   __device__ __forceinline__ BrKvPieces(const BrKvAttend &p, int rows_q)
-      : all(__builtin_amdgcn_make_buffer_rsrc(p.part, 0, 2 * BR_KV_SPLIT_WGS * TQ * D * 4, 0x00020000)), rows(min(rows_q, 16)), n16((rows_q + 15) / 16) {}
+      : all(__builtin_amdgcn_make_buffer_rsrc(p.part, 0, 2 * BR_KV_SPLIT_WGS_OF(D) * TQ * D * 4, 0x00020000)), rows(min(rows_q, 16)), n16((rows_q + 15) / 16) {}
   __device__ __forceinline__ int items() const { return n16 * (D / 4) * rows; }
   __device__ __forceinline__ int item(int x, int d, int g, int n) const { return ((x * (D / 16) + d) * 4 + g) * rows + n; }
   // row and first channel of an item
@@ -1081,7 +1081,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
 template <int D, int SHARE, int NW, int WAVES>
 void br_kv_attend_few(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
   constexpr int PER = 4 * WAVES / NW;
-  const int blocks = PER * cus < BR_KV_SPLIT_WGS ? PER * cus : BR_KV_SPLIT_WGS;
+  const int blocks = PER * cus < BR_KV_SPLIT_WGS_OF(D) ? PER * cus : BR_KV_SPLIT_WGS_OF(D);
   const bool half = SHARE == 1 && p.shift == 7;
   if constexpr (SHARE == 1) {
     if (half) {
@@ -1096,7 +1096,7 @@ void br_kv_attend_few(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
 
 template <int D, int NQ, int WAVES>
 void br_kv_attend_rows(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
-  const int blocks = WAVES * cus < BR_KV_SPLIT_WGS ? WAVES * cus : BR_KV_SPLIT_WGS;
+  const int blocks = WAVES * cus < BR_KV_SPLIT_WGS_OF(D) ? WAVES * cus : BR_KV_SPLIT_WGS_OF(D);
   if (fp8) br_kv_k_attend_rows<D, NQ, true, WAVES><<<blocks, 256, 0, st>>>(p);
   else br_kv_k_attend_rows<D, NQ, false, WAVES><<<blocks, 256, 0, st>>>(p);
 }

@@ -7,7 +7,9 @@
 
 #include "br_kv.h"
 
-#define BR_KV_SPLIT_WGS 768  // most blocks of an attention launch that split rows' tokens among them
+// Most blocks of an attention launch that split rows' tokens among them: two for each of 256 compute units where two waves fit on a SIMD
+#define BR_KV_SPLIT_WGS 512
+#define BR_KV_SPLIT_WGS_OF(dim) ((dim) <= 128 ? BR_KV_SPLIT_WGS : BR_KV_SPLIT_WGS / 2)
 #define BR_KV_LIST 4096      // places of a token list that are written with the tables; longer lists have a launch of their own
 #define BR_KV_TILE 64        // cached tokens of an attention tile
 

@@ -27,7 +27,7 @@ void __hipRegisterVar(void **, void *, char *, char *, int, size_t, int, int) {}
 int __hipPushCallConfiguration(D3 gg, D3 bb, size_t s, void *st) { g = gg, b = bb, shm = s, str = st; return 0; }
 int __hipPopCallConfiguration(D3 *gg, D3 *bb, size_t *s, void **st) { *gg = g, *bb = b, *s = shm, *st = str; return 0; }
 int hipLaunchKernel(const void *f, D3 gg, D3 bb, void **, size_t, void *) {
-  log_ += names[f] + " " + std::to_string((uint64_t)gg.x * bb.x) + "\n";
+  log_ += names[f] + " " + std::to_string((uint64_t)gg.x * bb.x) + " " + std::to_string(gg.x) + "\n";
   return 0;
 }
 int hipGetLastError() { return 0; }
@@ -54,7 +54,9 @@ class Library:
         return self.lib.br_kv_init(C.byref(c), None, C.byref(self.ctx))
 
     def launches(self):
-        return [(name, int(n)) for name, n in re.findall(r"(br_kv_k_[a-z]+)\S* (\d+)", self.fake.stand_in_log().decode())]
+        found = re.findall(r"(br_kv_k_[a-z]+(?:_rows)?)\S* (\d+) (\d+)", self.fake.stand_in_log().decode())
+        self.blocks = [int(n) for _, _, n in found]
+        return [(name, int(n)) for name, n, _ in found]
 
     def tokens(self, call, **kw):
         a = self.kv._Tokens(**{**dict(k=1 << 30, v=1 << 30, slot=1 << 30, k_token=64, k_head=64, v_token=64, v_head=64, n_tokens=1, dtype=0), **kw})
@@ -88,7 +90,25 @@ def lists_as_long_as_their_places_can_be_counted(lib):
         lib.lib.br_kv_free(lib.ctx)
 
 
-SCENARIOS = [as_many_workers_as_a_launch_has_blocks_for, lists_as_long_as_their_places_can_be_counted]
+def a_workspace_holds_the_pieces_of_what_is_launched(lib):
+    """Two pieces of 128 query rows for each block of the largest launch on 256 compute units, their maxima and sums, a counter a block, and
+    the tables: no more than that and the places' alignment."""
+    for dim in (64, 96, 128, 192, 256):
+        cfg = dict(rows=3, n_blocks=4, max_blocks=5, head_dim=dim)
+        assert lib.context(**cfg) == 0
+        lib.launches()
+        most = 0
+        for queries in (1, 20, 40, 100):
+            a = lib.kv._Attention(q=1 << 30, out=1 << 30, q_token=dim, q_head=dim, out_token=dim, out_head=dim, n_tokens=300, max_count=queries, dtype=0, scale=1.0)
+            assert lib.lib.br_kv_attend(lib.ctx, C.byref(lib.layer), C.byref(a)) == 0
+            assert [n for n, _ in lib.launches()] in (["br_kv_k_attend"], ["br_kv_k_attend_rows"])
+            most = max([most] + lib.blocks)
+        need = most * (2 * 128 * 4 * (dim + 2) + 4)
+        assert need <= lib.kv.workspace_bytes(lib.kv.KvConfig(**cfg)) <= need + 4 * 512 + 9 * 256, (dim, most)
+        lib.lib.br_kv_free(lib.ctx)
+
+
+SCENARIOS = [a_workspace_holds_the_pieces_of_what_is_launched, as_many_workers_as_a_launch_has_blocks_for, lists_as_long_as_their_places_can_be_counted]
 
 
 @pytest.fixture(scope="module")
