@@ -760,8 +760,8 @@ struct BrKvShare {
 // Few query rows: a run for each SHARE waves, which have 16 query rows each, NW waves to a block.  Pieces of a run (of a query tile that it
 // takes up in the middle, and of one that goes on in the next run) wait in LDS until the block's end, where all waves join them,
 // each its share of the channels.  Bound by memory: each code comes once from there (waves of one run find it in the caches).  144 rows
-// of 256 to 8192 tokens, 8 key heads of 128 channels, groups of 8: 128 us, 695 MB = 5.4 TB/s (a large copy: 5.1).  One row of 40 thousand
-// tokens: 27 us, 87 MB, of them some 6 us for the pieces' way through LDS and memory; one of 500 13 us, a launch and a chain
+// of 256 to 8192 tokens, 8 key heads of 128 channels, groups of 8: 128 us, 691 MB = 5.4 TB/s (a large copy: 5.1).  One row of 40 thousand
+// tokens: 26 us, 87 MB, of them some 6 us for the pieces' way through LDS and memory; one of 500 13 us, a launch and a chain
 // of loads (lengths, ids, codes, the join).
 template <int D, int SHARE, bool FP8, bool HALF, int NW, int WAVES>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
@@ -906,7 +906,7 @@ __device__ __forceinline__ void br_kv_ahead(Get &&get, Use &&use) {
 // Many query rows: the block's four waves have 16 NQ each and go over the same tokens.  Each wave brings a quarter of a tile's codes to f16 and
 // puts them into LDS as the matrix products take them (1 KB for each operand, 16 bytes a lane); two tiles there, one barrier a
 // tile.  Bound by the issue of vector instructions between the products (310 a tile and wave, 32 of them exponentials, to 64 products): chunks
-// of 512 tokens of two rows, groups of 4, 8 key heads of 128 channels behind up to 8192 tokens 200 us, 0.63 PFLOP/s; a wave issues in 44 %
+// of 512 tokens of two rows, groups of 4, 8 key heads of 128 channels behind up to 8192 tokens 207 us, 0.61 PFLOP/s; a wave issues in 44 %
 // of its time and waits for its turn, beside the other wave of its SIMD, in 30 %; the matrix units are busy a third.
 template <int D, int NQ, bool FP8, int WAVES>
 __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) {

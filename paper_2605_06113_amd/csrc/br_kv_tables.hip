@@ -113,8 +113,9 @@ __device__ __forceinline__ void br_kv_list4(const BrKvTables &t, const BrKvStep 
 // One block of NT threads per worker; a thread has the RPT rows from tid * RPT on.  The used bits are in LDS.  LIST: writes the
 // token list as well; else leaves each row's first place in it and first position to br_kv_k_list.
 // A chain of dependent steps (rows, blocks given back, sums, free ids, lists), so its time is their latencies: barriers are few (the
-// sums of a step in which nothing is refused take one), scans stay in registers.  One worker of 96 rows 4.7 us (a launch that does
-// nothing: 4); 16384 workers of 144 rows, a token each, 62 us, 259 MB = 4.1 TB/s, most of them stores of the outputs.
+// sums of a step in which nothing is refused take one), scans stay in registers.  One worker of 96 rows 4.8 us (a launch that does
+// nothing: 4); 16384 workers of 144 rows, a token each, 259 MB, most of them stores of the outputs: 58 us = 4.5 TB/s where the 256 MB cache has part
+// of them from the call before, 76 us = 3.4 TB/s where three such states take turns.
 template <int NT, int RPT, bool LIST>
 __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
   constexpr int ROWS = NT * RPT, IDS = NT * 8, AT_ONCE = 8;
