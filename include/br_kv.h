@@ -7,6 +7,11 @@
  *   br_kv_append  keys and values of the new tokens into the cache: 8 bits, a scale for each block of tokens and head
  *   br_kv_attend  attention of the new tokens over their requests' cached tokens
  *   br_kv_read    keys and values of cached tokens back out (hand-over of a request to another worker)
+ * Requests that begin alike may hold the same blocks (a context of br_kv_init_shared):
+ *   br_kv_fork         rows take over other rows' tokens by holding their blocks
+ *   br_kv_step_shared  br_kv_step, in which a row that writes into a block that others hold too gets one of its own
+ *   br_kv_compact      the blocks in use move to the lowest ids
+ *   br_kv_copy         keys and values of blocks, for those two and from worker to worker
  * A context serves n_workers workers side by side (several DP ranks of a replay on one GPU, or one).  The tables are one
  * per worker for all layers of a model; the cache of each layer is memory of the caller's (br_kv_layer).
  *
@@ -228,6 +233,72 @@ int32_t br_kv_read(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_tokens 
  * its query sees.  Tokens of which e^(s - m) is below 2^-126, m the query's largest score, may count as none.
  */
 int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *args);
+
+/*
+ * Blocks that several rows hold.
+ *
+ * A context of br_kv_init_shared counts for each block the entries of its worker's tables that name it (its holders); a block without any is free.  All
+ * calls take such a context but br_kv_step, in whose place br_kv_step_shared comes; br_kv_fork and br_kv_compact take no other one.  Its
+ * workspace holds the tables twice.  A state at the start may name a block in several rows.
+ */
+uint64_t br_kv_shared_workspace_bytes(const br_kv_config *cfg); /* 0 if the configuration is invalid */
+int32_t br_kv_init_shared(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx **out);
+
+/* Where the counts live inside the workspace (byte offset, int32): holders [n_workers][n_blocks]. */
+typedef struct {
+  uint64_t holders, total_bytes;
+} br_kv_shared_layout;
+
+int32_t br_kv_get_shared_layout(const br_kv_ctx *ctx, br_kv_shared_layout *out);
+
+/*
+ * Both [n_workers][rows].  from: the row of the same worker whose tokens the row takes over; outside [0, rows): it stays as it is.  len: how many of
+ * them, from the first on (clamped to what from holds; < 0, or NULL: all).
+ */
+typedef struct {
+  const int32_t *from;
+  const int32_t *len;
+} br_kv_forks;
+
+/*
+ * Every row r with from[r] in range becomes the first len[r] tokens of row from[r], all as they were before the call: rows may be forked many times,
+ * trade places, be cut (from[r] = r) or emptied (len[r] = 0).  Their entries name the same blocks, no key or value moves; the blocks that the row held are given
+ * back, those without holders are free.
+ */
+int32_t br_kv_fork(br_kv_ctx *ctx, const br_kv_forks *in);
+
+/* Blocks to copy: src and dst [n_workers][n], block ids of worker w at w * n.  A pair with an id outside the worker's blocks (-1) is none. */
+typedef struct {
+  int32_t *src;
+  int32_t *dst;
+  const int32_t *src_worker; /* read by br_kv_copy: [n_workers][n], the worker whose block src is; NULL: w itself */
+  int32_t n;                 /* >= 0; n_workers * n at most 2^31 - 257 */
+  int32_t pad;
+} br_kv_moves;
+
+/*
+ * br_kv_step of a context of br_kv_init_shared.  In its order, with what is different:
+ *  1. a block that is given back is free once no row holds it;
+ *  2. a row with add > 0 whose kp tokens end inside a block that other rows hold too, after 1, needs one block more: it comes to stand in that
+ *     one's place in the row's table.  Each such row gets one, also if all holders of the block do; it is counted by the refusals and the stats as any other;
+ *  3. the block taken in another's place is the row's first.  A block that lost its last holder in this way is free after the step.
+ * copies (src, dst [n_workers][rows], n = rows): what row r needs copied, src the block that it held, dst the one that it holds now; -1, -1 if nothing.  br_kv_copy
+ * with this list comes before the step's tokens are appended, for every layer.
+ */
+int32_t br_kv_step_shared(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out *out, const br_kv_moves *copies);
+
+/*
+ * The blocks in use become, as far as the list reaches, those of the lowest ids.  With u = blocks in use of the worker: the k-th highest id in use not below u
+ * becomes the k-th lowest free id below u, for k < n; tables and holders change accordingly, and list k says so (src, dst; -1 behind the last).  br_kv_copy with
+ * this list, for every layer, comes before anything else is done with the layer.  Sources and destinations are different blocks.
+ */
+int32_t br_kv_compact(br_kv_ctx *ctx, const br_kv_moves *out);
+
+/*
+ * Codes and scales of blocks src to blocks dst, as they are.  A block that is dst of two pairs, or src of one and dst of another, of the same call: what it and
+ * the latter's dst get is not said.  Takes every context.
+ */
+int32_t br_kv_copy(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_moves *in);
 
 /* Destroy the context (host memory only). NULL is allowed. */
 void br_kv_free(br_kv_ctx *ctx);

@@ -31,10 +31,10 @@ bool config_ok(const br_kv_config *c) {
 }
 
 struct Places {
-  uint64_t lens, table, tail, used, runs, part, ml, arrived, total;
+  uint64_t lens, table, tail, used, runs, part, ml, arrived, holders, next_lens, next_table, moved, least, total;
 };
 
-Places make_layout(const br_kv_config &c) {
+Places make_layout(const br_kv_config &c, bool shared) {
   const uint64_t rows = (uint64_t)c.n_workers * c.rows;
   uint64_t off = 0;
   auto take = [&](uint64_t words) {
@@ -42,7 +42,7 @@ Places make_layout(const br_kv_config &c) {
     off = align_up(off + words * 4u);
     return at;
   };
-  Places l;
+  Places l = {};
   l.lens = take(rows);
   l.table = take(rows * c.max_blocks);
   l.tail = take(rows);
@@ -53,6 +53,14 @@ Places make_layout(const br_kv_config &c) {
   l.part = take(pieces * c.head_dim);
   l.ml = take(pieces * 2);
   l.arrived = take(BR_KV_SPLIT_WGS);
+  if (shared) {
+    const uint64_t blocks = (uint64_t)c.n_workers * c.n_blocks;
+    l.holders = take(blocks);
+    l.next_lens = take(2 * rows);
+    l.next_table = take(rows * c.max_blocks);
+    l.moved = take(blocks);
+    l.least = take((uint64_t)c.n_workers);
+  }
   l.total = off;
   return l;
 }
@@ -66,6 +74,7 @@ struct br_kv_ctx {
   hipStream_t st;
   int32_t last_hip;
   int cus;
+  bool shared;
 };
 
 namespace {
@@ -78,6 +87,21 @@ int32_t enqueue(br_kv_ctx *ctx, Fn &&fn) {
   if (e == hipSuccess) return BR_OK;
   ctx->last_hip = (int32_t)e;
   return BR_EHIP;
+}
+
+BrKvNext next_of(const br_kv_ctx *ctx) {
+  char *base = (char *)ctx->cfg.workspace;
+  BrKvNext x;
+  x.lens = (int2 *)(base + ctx->at.next_lens);
+  x.table = (int *)(base + ctx->at.next_table);
+  x.moved = (int *)(base + ctx->at.moved);
+  x.least = (int *)(base + ctx->at.least);
+  return x;
+}
+
+bool moves_ok(const br_kv_ctx *ctx, const br_kv_moves *m) {
+  if (!m || m->n < 0 || (int64_t)ctx->cfg.n_workers * m->n > INT32_MAX - 256) return false;
+  return m->n == 0 || (m->src && m->dst);
 }
 
 bool layer_ok(const br_kv_layer *l) {
@@ -121,12 +145,10 @@ BrKvTokens tokens_of(const br_kv_ctx *ctx, const br_kv_tokens *x) {
 
 extern "C" {
 
-uint64_t br_kv_workspace_bytes(const br_kv_config *cfg) { return config_ok(cfg) ? make_layout(*cfg).total : 0; }
-
-int32_t br_kv_init(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx **out) {
+static int32_t init_context(const br_kv_config *cfg, const br_kv_state *init, bool shared, br_kv_ctx **out) {
   if (!out || !config_ok(cfg) || !cfg->workspace || ((uintptr_t)cfg->workspace & 255u) != 0) return BR_EINVAL;
   if (init && (!init->lens || !init->table)) return BR_EINVAL;
-  const Places at = make_layout(*cfg);
+  const Places at = make_layout(*cfg, shared);
   if (cfg->workspace_bytes < at.total) return BR_ENOMEM;
   br_kv_ctx *ctx = new (std::nothrow) br_kv_ctx();
   if (!ctx) return BR_ENOMEM;
@@ -134,6 +156,7 @@ int32_t br_kv_init(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx *
   ctx->at = at;
   ctx->st = (hipStream_t)cfg->stream;
   ctx->last_hip = 0;
+  ctx->shared = shared;
   int device = 0;
   hipError_t e = hipGetDevice(&device);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&ctx->cus, hipDeviceAttributeMultiprocessorCount, device);
@@ -150,6 +173,7 @@ int32_t br_kv_init(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx *
   t.tail = (int *)(base + at.tail);
   t.used = (unsigned *)(base + at.used);
   t.arrived = (int *)(base + at.arrived);
+  t.holders = shared ? (int *)(base + at.holders) : nullptr;
   int32_t rc = enqueue(ctx, [&] { br_kv_launch_clear(t, ctx->st); });
   if (rc == BR_OK && init) rc = enqueue(ctx, [&] { br_kv_launch_load(t, init->lens, init->table, ctx->st); });
   if (rc != BR_OK) {
@@ -160,7 +184,15 @@ int32_t br_kv_init(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx *
   return BR_OK;
 }
 
-int32_t br_kv_step(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out *out) {
+uint64_t br_kv_workspace_bytes(const br_kv_config *cfg) { return config_ok(cfg) ? make_layout(*cfg, false).total : 0; }
+
+uint64_t br_kv_shared_workspace_bytes(const br_kv_config *cfg) { return config_ok(cfg) ? make_layout(*cfg, true).total : 0; }
+
+int32_t br_kv_init(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx **out) { return init_context(cfg, init, false, out); }
+
+int32_t br_kv_init_shared(const br_kv_config *cfg, const br_kv_state *init, br_kv_ctx **out) { return init_context(cfg, init, true, out); }
+
+static int32_t step_tables(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out *out, const br_kv_moves *copies) {
   if (!ctx || !in || !in->keep || !in->add || !out || out->token_cap < 0) return BR_EINVAL;
   if ((int64_t)ctx->cfg.n_workers * out->token_cap > INT32_MAX - 2 * BR_KV_LIST) return BR_EINVAL;
   BrKvStep s;
@@ -168,9 +200,39 @@ int32_t br_kv_step(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out
   s.slot = out->slot, s.pos = out->pos, s.start = out->start, s.count = out->count, s.status = out->status;
   s.stats = (long long *)out->stats;
   s.runs = (int2 *)((char *)ctx->cfg.workspace + ctx->at.runs);
+  s.copy_src = copies ? copies->src : nullptr, s.copy_dst = copies ? copies->dst : nullptr;
   s.cap = out->token_cap;
   s.wide = (((uintptr_t)s.slot | (uintptr_t)s.pos) & 15u) == 0;
   return enqueue(ctx, [&] { br_kv_launch_step(ctx->t, s, ctx->st); });
+}
+
+int32_t br_kv_step(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out *out) {
+  if (!ctx || ctx->shared) return BR_EINVAL;  // (blocks with several holders need the list of what is to be copied)
+  return step_tables(ctx, in, out, nullptr);
+}
+
+int32_t br_kv_step_shared(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_step_out *out, const br_kv_moves *copies) {
+  if (!ctx || !ctx->shared || !copies || copies->n != ctx->cfg.rows || !copies->src || !copies->dst) return BR_EINVAL;
+  return step_tables(ctx, in, out, copies);
+}
+
+int32_t br_kv_fork(br_kv_ctx *ctx, const br_kv_forks *in) {
+  if (!ctx || !ctx->shared || !in || !in->from) return BR_EINVAL;
+  return enqueue(ctx, [&] { br_kv_launch_fork(ctx->t, next_of(ctx), in->from, in->len, ctx->st); });
+}
+
+int32_t br_kv_compact(br_kv_ctx *ctx, const br_kv_moves *out) {
+  if (!ctx || !ctx->shared || !moves_ok(ctx, out)) return BR_EINVAL;
+  if (out->n == 0) return BR_OK;
+  const BrKvMoves m = {out->src, out->dst, nullptr, out->n};
+  return enqueue(ctx, [&] { br_kv_launch_compact(ctx->t, next_of(ctx), m, ctx->st); });
+}
+
+int32_t br_kv_copy(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_moves *in) {
+  if (!ctx || !layer_ok(layer) || !moves_ok(ctx, in)) return BR_EINVAL;
+  if (in->n == 0) return BR_OK;
+  const BrKvMoves m = {in->src, in->dst, in->src_worker, in->n};
+  return enqueue(ctx, [&] { br_kv_launch_copy(cache_of(ctx, layer), m, ctx->cfg.n_workers, ctx->st); });
 }
 
 int32_t br_kv_append(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_tokens *in) {
@@ -252,6 +314,13 @@ int32_t br_kv_get_layout(const br_kv_ctx *ctx, br_kv_layout *out) {
   if (!ctx || !out) return BR_EINVAL;
   out->lens = ctx->at.lens;
   out->table = ctx->at.table;
+  out->total_bytes = ctx->at.total;
+  return BR_OK;
+}
+
+int32_t br_kv_get_shared_layout(const br_kv_ctx *ctx, br_kv_shared_layout *out) {
+  if (!ctx || !ctx->shared || !out) return BR_EINVAL;
+  out->holders = ctx->at.holders;
   out->total_bytes = ctx->at.total;
   return BR_OK;
 }

@@ -21,6 +21,21 @@ struct BrKvTables {
   int *tail;                                     // [W][B] each row's last block
   unsigned *used;                                // [W][words]
   int *arrived;                                  // BrKvAttend's
+  int *holders;                                  // [W][n_blocks] entries that name a block; null: a block has one holder at most
+};
+
+// What rows become (br_kv_fork) and where blocks go (br_kv_compact), from one launch to the next.
+struct BrKvNext {
+  int2 *lens;     // [W][B] tokens before and after; after < 0: the row stays as it is
+  int *table;     // [W][B][max_blocks]
+  int *moved;     // [W][n_blocks]
+  int *least;     // [W] blocks from this id on have moved, if they are in use
+};
+
+struct BrKvMoves {
+  int *src, *dst;
+  const int *src_worker;
+  int n;
 };
 
 struct BrKvStep {
@@ -28,6 +43,7 @@ struct BrKvStep {
   int *slot, *pos, *start, *count, *status;
   long long *stats;
   int2 *runs;     // [W][B] workspace: each row's first place in the token list and first position there
+  int *copy_src, *copy_dst;  // [W][B] of blocks with several holders
   int cap, wide;  // wide: the lists begin at 16 bytes
 };
 
@@ -67,6 +83,9 @@ struct BrKvAttend {
 void br_kv_launch_clear(const BrKvTables &t, hipStream_t st);
 void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, hipStream_t st);
 void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st);
+void br_kv_launch_fork(const BrKvTables &t, const BrKvNext &x, const int *from, const int *len, hipStream_t st);
+void br_kv_launch_compact(const BrKvTables &t, const BrKvNext &x, const BrKvMoves &m, hipStream_t st);
+void br_kv_launch_copy(const BrKvCache &c, const BrKvMoves &m, int W, hipStream_t st);
 void br_kv_launch_append(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st);
 void br_kv_launch_read(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st);
 
@@ -140,6 +159,35 @@ __device__ __forceinline__ int br_kv_wave_scan(int x) {
   BR_KV_STEP(0x143, 0xc);  // rows 2 and 3: the last of row 1
 #undef BR_KV_STEP
   return x;
+}
+
+// Inclusive sums of K values each over the block's threads; total: all of them.  One barrier (part: 2 x K x NT / 64 words, used in turn).
+template <int NT, int K>
+__device__ __forceinline__ void br_kv_scan(int (&x)[K], int (&total)[K], int *part, int &turn) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+#pragma unroll
+  for (int k = 0; k < K; ++k) x[k] = br_kv_wave_scan(x[k]);
+  if constexpr (NT == 64) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) total[k] = __builtin_amdgcn_readlane(x[k], 63);
+  } else {
+    int *at = part + (turn & 1) * 8 * (NT / 64);
+    ++turn;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (lane == 63) at[k * (NT / 64) + wv] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      total[k] = 0;
+#pragma unroll
+      for (int v = 0; v < NT / 64; ++v) {
+        const int y = at[k * (NT / 64) + v];
+        if (v < wv) x[k] += y;
+        total[k] += y;
+      }
+    }
+  }
 }
 
 // A block's scale; one that is none (below zero or not finite) makes NaN of what is read with it.

@@ -13,6 +13,8 @@ __global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t) {
   }
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < words; i += step) t.used[i] = 0;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < BR_KV_SPLIT_WGS; i += step) t.arrived[i] = 0;
+  if (t.holders)
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)t.W * t.n_blocks; i += step) t.holders[i] = 0;
 }
 
 // The rows held at the start (behind br_kv_k_clear).
@@ -29,35 +31,7 @@ __global__ __launch_bounds__(256) void br_kv_k_load(BrKvTables t, const int *len
     t.table[i] = id;
     if (j == (len - 1) >> t.shift) t.tail[row] = id;
     atomicOr(&t.used[row / t.B * t.words + (id >> 5)], 1u << (id & 31));
-  }
-}
-
-// Inclusive sums of K values each over the block's threads; total: all of them.  One barrier (part: 2 x K x NT / 64 words, used in turn).
-template <int NT, int K>
-__device__ __forceinline__ void br_kv_scan(int (&x)[K], int (&total)[K], int *part, int &turn) {
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-#pragma unroll
-  for (int k = 0; k < K; ++k) x[k] = br_kv_wave_scan(x[k]);
-  if constexpr (NT == 64) {
-#pragma unroll
-    for (int k = 0; k < K; ++k) total[k] = __builtin_amdgcn_readlane(x[k], 63);
-  } else {
-    int *at = part + (turn & 1) * 8 * (NT / 64);
-    ++turn;
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-      if (lane == 63) at[k * (NT / 64) + wv] = x[k];
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      total[k] = 0;
-#pragma unroll
-      for (int v = 0; v < NT / 64; ++v) {
-        const int y = at[k * (NT / 64) + v];
-        if (v < wv) x[k] += y;
-        total[k] += y;
-      }
-    }
+    if (t.holders) atomicAdd(&t.holders[row / t.B * t.n_blocks + id], 1);
   }
 }
 
@@ -116,18 +90,27 @@ __device__ __forceinline__ void br_kv_list4(const BrKvTables &t, const BrKvStep 
 // sums of a step in which nothing is refused take one), scans stay in registers.  One worker of 96 rows 4.8 us (a launch that does
 // nothing: 4); 16384 workers of 144 rows, a token each, 259 MB, most of them stores of the outputs: 58 us = 4.5 TB/s where the 256 MB cache has part
 // of them from the call before, 76 us = 3.4 TB/s where three such states take turns.
-template <int NT, int RPT, bool LIST>
+// SHARED: blocks may have several holders, whose counts are in global memory (a worker's may be 1 MB): a block that is given back is free when
+// the last one gives it, and a row that would write into one that others hold gets another in its place.
+template <int NT, int RPT, bool LIST, bool SHARED>
 __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
   constexpr int ROWS = NT * RPT, IDS = NT * 8, AT_ONCE = 8;
   extern __shared__ unsigned used[];
   __shared__ int part[16 * (NT / 64)], give_n, need_before[ROWS], tok_before[ROWS], row_kp[ROWS], give[ROWS], row_tail[ROWS], ids[IDS];
+  __shared__ int row_in[SHARED ? ROWS : 1], dropped;  // 1: the row's first block comes in the place of its last one
   const int w = blockIdx.x, tid = threadIdx.x, B = t.B, b1 = (1 << t.shift) - 1;
   int turn = 0;
   int *lens = t.lens + (long long)w * B;
   int *table = t.table + (long long)w * B * t.max_blocks;
   int *tails = t.tail + (long long)w * B;
   unsigned *gused = t.used + (long long)w * t.words;
+  int *holders = SHARED ? t.holders + (long long)w * t.n_blocks : nullptr;
+  // (the count's change comes back: whoever takes it to 0 is the last)
+  auto give_back = [&](int id) {
+    if (!SHARED || atomicSub(&holders[id], 1) == 1) atomicAnd(&used[id >> 5], ~(1u << (id & 31)));
+  };
   if (tid == 0) give_n = 0;
+  if (SHARED && tid == 0) dropped = 0;
   if (w == 0)  // (nothing of an attention that went wrong outlives the step behind it)
     for (int i = tid; i < BR_KV_SPLIT_WGS; i += NT) t.arrived[i] = 0;
   int kp[RPT], have[RPT], why[RPT], held[RPT], want[RPT], tail[RPT];
@@ -154,7 +137,7 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
     if (held[i] == have[i] + 1) {
       int *at = table + (long long)r * t.max_blocks + have[i];
       const int id = *at;
-      if (id >= 0) atomicAnd(&used[id >> 5], ~(1u << (id & 31)));
+      if (id >= 0) give_back(id);
       *at = -1;
     } else if (held[i] > have[i]) {
       give[atomicAdd(&give_n, 1)] = r, need_before[r] = have[i], tok_before[r] = held[i];
@@ -176,13 +159,18 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
 #pragma unroll
         for (int m = 0; m < AT_ONCE; ++m) {
           if (j + 16 * m >= to) continue;
-          if (id[m] >= 0) atomicAnd(&used[id[m] >> 5], ~(1u << (id[m] & 31)));
+          if (id[m] >= 0) give_back(id[m]);
           row[j + 16 * m] = -1;
         }
       }
     }
     __syncthreads();
   }
+
+  int in[RPT];
+#pragma unroll
+  for (int i = 0; i < RPT; ++i)
+    in[i] = SHARED && want[i] > 0 && (kp[i] & b1) && tail[i] >= 0 && __hip_atomic_load(&holders[max(tail[i], 0)], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 1;
 
   // sums, as if nothing were refused: tokens, blocks, and what is counted of them
   int need[RPT], sum[6], all[6], nfree = 0;
@@ -192,6 +180,7 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
       need[i] = ((kp[i] + want[i] + b1) >> t.shift) - have[i];
+      if (SHARED && want[i] > 0) need[i] += in[i];
       sum[0] += want[i], sum[1] += need[i], sum[2] += kp[i] + want[i];
       sum[3] += kp[i] + want[i] > 0, sum[5] += (why[i] > 0) + (why[i] == BR_KV_NO_BLOCKS ? 1 << 16 : 0);
     }
@@ -238,15 +227,19 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
       if (s.count) s.count[at] = want[i];
       if (s.status) s.status[at] = why[i];
       if (!LIST) s.runs[at] = make_int2(y, kp[i]);
+      if (SHARED) s.copy_src[at] = want[i] > 0 && in[i] ? tail[i] : -1;
+      if (SHARED && !(want[i] > 0 && in[i])) s.copy_dst[at] = -1;
     }
+    if (SHARED) row_in[r] = want[i] > 0 ? in[i] : 0;
     x += need[i], y += want[i];
   }
-  if (tid == 0 && s.stats) {
+  auto say = [&](int free_again) {
     long long *o = s.stats + (long long)w * BR_KV_NSTATS;
-    const int n_used = t.n_blocks - free_blocks + need_all;
+    const int n_used = t.n_blocks - free_blocks + need_all - free_again;
     o[BR_KV_ST_TOKENS] = all[2], o[BR_KV_ST_USED] = n_used, o[BR_KV_ST_FREE] = t.n_blocks - n_used, o[BR_KV_ST_ROWS] = all[3];
     o[BR_KV_ST_ADDED] = total, o[BR_KV_ST_REFUSED] = all[5] & 0xffff, o[BR_KV_ST_NO_BLOCKS] = all[5] >> 16, o[BR_KV_ST_TAKEN] = need_all;
-  }
+  };
+  if (!SHARED && tid == 0 && s.stats) say(0);
   // ids of blocks first .. first + n - 1 of those taken, to their rows
   auto hand_out = [&](auto many, int first, int n) {
     constexpr int MINE = decltype(many)::value;
@@ -261,7 +254,13 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
     for (int m = 0; m < MINE; ++m) {
       const int j = tid + m * NT, q = first + j;
       if (j >= n) continue;
-      table[(long long)r[m] * t.max_blocks + ((row_kp[r[m]] + b1) >> t.shift) + q - need_before[r[m]]] = ids[j];
+      int entry = ((row_kp[r[m]] + b1) >> t.shift) + q - need_before[r[m]];
+      if (SHARED) {
+        holders[ids[j]] = 1;
+        entry -= row_in[r[m]];
+        if (row_in[r[m]] && q == need_before[r[m]]) row_tail[r[m]] = ids[j], s.copy_dst[(long long)w * B + r[m]] = ids[j];
+      }
+      table[(long long)r[m] * t.max_blocks + entry] = ids[j];
       if (q + 1 == (r[m] + 1 < ROWS ? need_before[r[m] + 1] : need_all)) tails[r[m]] = ids[j];
     }
   };
@@ -293,6 +292,14 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
     taken += n;
   }
   __syncthreads();
+  if (SHARED) {
+    // (those in whose place others came: none of them was free for this step)
+#pragma unroll
+    for (int i = 0; i < RPT; ++i)
+      if (want[i] > 0 && in[i] && atomicSub(&holders[tail[i]], 1) == 1) atomicAnd(&used[tail[i] >> 5], ~(1u << (tail[i] & 31))), atomicAdd(&dropped, 1);
+    __syncthreads();
+    if (tid == 0 && s.stats) say(dropped);
+  }
   for (int i = tid; i < t.words; i += NT) gused[i] = used[i];
   if (LIST && (s.slot || s.pos))
     for (int j = 4 * tid - br_kv_lead(w, s.cap); j < s.cap; j += 4 * NT) br_kv_list4(t, s, (long long)w * s.cap, table, tok_before, row_kp, row_tail, ROWS, total, j, s.cap);
@@ -323,18 +330,19 @@ void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, h
   br_kv_k_load<<<grid_for((long long)t.W * t.B * t.max_blocks), 256, 0, st>>>(t, lens, table);
 }
 
-template <bool LIST>
+template <bool LIST, bool SHARED>
 static void launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st) {
   const size_t lds = (size_t)t.words * 4;
   // (as few rows to a thread as will do: its arrays in LDS go by it, and with them the blocks on a compute unit)
-  if (t.B <= 256) br_kv_k_step<256, 1, LIST><<<t.W, 256, lds, st>>>(t, s);
-  else if (t.B <= 512) br_kv_k_step<256, 2, LIST><<<t.W, 256, lds, st>>>(t, s);
-  else br_kv_k_step<256, 4, LIST><<<t.W, 256, lds, st>>>(t, s);
+  if (t.B <= 256) br_kv_k_step<256, 1, LIST, SHARED><<<t.W, 256, lds, st>>>(t, s);
+  else if (t.B <= 512) br_kv_k_step<256, 2, LIST, SHARED><<<t.W, 256, lds, st>>>(t, s);
+  else br_kv_k_step<256, 4, LIST, SHARED><<<t.W, 256, lds, st>>>(t, s);
 }
 
 void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st) {
   const bool list = s.slot || s.pos;
-  if (!list || s.cap <= BR_KV_LIST) return launch_step<true>(t, s, st);
-  launch_step<false>(t, s, st);
+  if (!list || s.cap <= BR_KV_LIST) return t.holders ? launch_step<true, true>(t, s, st) : launch_step<true, false>(t, s, st);
+  if (t.holders) launch_step<false, true>(t, s, st);
+  else launch_step<false, false>(t, s, st);
   br_kv_k_list<<<t.W * br_kv_list_parts(s.cap), 256, 0, st>>>(t, s);
 }

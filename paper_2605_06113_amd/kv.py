@@ -16,6 +16,14 @@ caller's to order against the cache's stream (`stream.wait_stream`, `Tensor.reco
     for layer in layers:
         cache.append_device(layer, k, v, step["slot"])        # k, v [token_cap, n_kv_heads, head_dim]
         cache.attend_device(layer, q, out, start=step["start"], count=step["count"], max_count=longest)
+
+Of a cache with `shared=True` several rows may hold the same blocks (samples of one prompt, beams):
+
+    cache.fork_device(rows, length)                           # row r goes on from the first length[r] tokens of row rows[r]
+    cache.step_device(keep, add, step)                        # rows that write into a block that others hold get one of their own
+    for layer in layers:
+        cache.copy_device(layer, step["copy_src"], step["copy_dst"])   # ... with what it held, before anything is appended
+        cache.append_device(layer, k, v, step["slot"])
 """
 from __future__ import annotations
 
@@ -32,7 +40,8 @@ NSTATS = 8
 ST = dict(tokens=0, used=1, free=2, rows=3, added=4, refused=5, no_blocks=6, taken=7)
 STATUS = dict(taken=0, no_blocks=1, too_long=2, no_room=3)
 EXPORTS = ("br_kv_workspace_bytes", "br_kv_init", "br_kv_step", "br_kv_append", "br_kv_read", "br_kv_attend", "br_kv_free",
-           "br_kv_last_hip_error", "br_kv_get_layout")
+           "br_kv_last_hip_error", "br_kv_get_layout", "br_kv_shared_workspace_bytes", "br_kv_init_shared", "br_kv_get_shared_layout", "br_kv_fork", "br_kv_step_shared",
+           "br_kv_compact", "br_kv_copy")
 
 _P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
 
@@ -71,8 +80,21 @@ class _Layout(C.Structure):
     _fields_ = [("lens", C.c_uint64), ("table", C.c_uint64), ("total_bytes", C.c_uint64)]
 
 
+class _SharedLayout(C.Structure):
+    _fields_ = [("holders", C.c_uint64), ("total_bytes", C.c_uint64)]
+
+
+class _Forks(C.Structure):
+    _fields_ = [("from_", _P), ("len", _P)]
+
+
+class _Moves(C.Structure):
+    _fields_ = [(k, _P) for k in ("src", "dst", "src_worker")] + [("n", _I), ("pad", _I)]
+
+
 # The structs of the calls of a decode loop, packed in one go (a ctypes struct costs as much as the call): pointers, strides, numbers.
 _PACK_LENGTHS, _PACK_STEP, _PACK_TOKENS, _PACK_ATTENTION = (struct.Struct(f) for f in ("@2P", "@6P2i", "@3P4q2i", "@7P4q4ifi"))
+_PACK_FORKS, _PACK_MOVES = (struct.Struct(f) for f in ("@2P", "@3P2i"))
 _lib = None
 
 
@@ -84,11 +106,17 @@ def load():
     lib = _load()
     for name in EXPORTS:
         getattr(lib, name).restype = C.c_int32
-    lib.br_kv_workspace_bytes.restype = C.c_uint64
-    lib.br_kv_workspace_bytes.argtypes = [C.POINTER(_Config)]
-    lib.br_kv_init.argtypes = [C.POINTER(_Config), C.POINTER(_State), C.POINTER(_P)]
-    for name in ("br_kv_step", "br_kv_append", "br_kv_read", "br_kv_attend"):
+    for name in ("br_kv_workspace_bytes", "br_kv_shared_workspace_bytes"):
+        getattr(lib, name).restype = C.c_uint64
+        getattr(lib, name).argtypes = [C.POINTER(_Config)]
+    for name in ("br_kv_init", "br_kv_init_shared"):
+        getattr(lib, name).argtypes = [C.POINTER(_Config), C.POINTER(_State), C.POINTER(_P)]
+    for name in ("br_kv_step", "br_kv_append", "br_kv_read", "br_kv_attend", "br_kv_copy"):
         getattr(lib, name).argtypes = [_P, _P, _P]
+    lib.br_kv_step_shared.argtypes = [_P, _P, _P, _P]
+    for name in ("br_kv_fork", "br_kv_compact"):
+        getattr(lib, name).argtypes = [_P, _P]
+    lib.br_kv_get_shared_layout.argtypes = [_P, C.POINTER(_SharedLayout)]
     lib.br_kv_free.restype = None
     lib.br_kv_free.argtypes = [_P]
     lib.br_kv_last_hip_error.argtypes = [_P]
@@ -110,6 +138,7 @@ class KvConfig:
     n_q_heads: int = 1
     head_dim: int = 64
     fmt: str = "int8"         # "int8" or "fp8" (e4m3)
+    shared: bool = False      # several rows may hold a block (br_kv_init_shared)
 
 
 def _config(cfg: KvConfig, stream=0, workspace=0, workspace_bytes=0) -> _Config:
@@ -119,7 +148,8 @@ def _config(cfg: KvConfig, stream=0, workspace=0, workspace_bytes=0) -> _Config:
 
 
 def workspace_bytes(cfg: KvConfig) -> int:
-    return int(load().br_kv_workspace_bytes(C.byref(_config(cfg))))
+    lib = load()
+    return int((lib.br_kv_shared_workspace_bytes if cfg.shared else lib.br_kv_workspace_bytes)(C.byref(_config(cfg))))
 
 
 class KvLayer:
@@ -164,7 +194,8 @@ class KvCache:
         c = _config(cfg, stream=self.stream.cuda_stream, workspace=self.ws.data_ptr(), workspace_bytes=self.ws.numel() * 4)
         ctx = _P()
         with torch.cuda.device(self.device):
-            self._done(self.lib.br_kv_init(C.byref(c), state, C.byref(ctx)), "br_kv_init")
+            init = "br_kv_init_shared" if cfg.shared else "br_kv_init"
+            self._done(getattr(self.lib, init)(C.byref(c), state, C.byref(ctx)), init)
         self.ctx = ctx
         if lens is not None and self.stream != current:  # (their memory is not handed out again before they have been copied)
             lens.record_stream(self.stream), table.record_stream(self.stream)
@@ -173,6 +204,11 @@ class KvCache:
         #: cached tokens of every row and the block tables, as they are on the device: [n_workers, rows] and [n_workers, rows, max_blocks]
         self.lens = self.ws[lay.lens // 4:lay.lens // 4 + W * B].view(W, B)
         self.table = self.ws[lay.table // 4:lay.table // 4 + W * B * cfg.max_blocks].view(W, B, cfg.max_blocks)
+        if cfg.shared:
+            own = _SharedLayout()
+            self._done(self.lib.br_kv_get_shared_layout(ctx, C.byref(own)), "br_kv_get_shared_layout")
+            #: how many entries of its worker's tables name each block: [n_workers, n_blocks]
+            self.holders = self.ws[own.holders // 4:own.holders // 4 + W * cfg.n_blocks].view(W, cfg.n_blocks)
 
     # -- checks ---------------------------------------------------------------
     def _sizes(self, torch, lib, cfg: KvConfig, device) -> None:
@@ -235,16 +271,25 @@ class KvCache:
             return self.layer(e((n, H, b, D), t.uint8), e((n, H, D, b), t.uint8), e((n, H), t.float32), e((n, H), t.float32))
 
     def alloc_step(self, token_cap: int) -> Dict[str, object]:
-        """Output arrays of step_device, with room for token_cap new tokens per worker."""
+        """Output arrays of step_device, with room for token_cap new tokens per worker (of a shared cache copy_src and copy_dst among them)."""
         t, W, B = self.torch, self.cfg.n_workers, self.cfg.rows
         e = lambda *shape: t.empty(shape, dtype=t.int32, device=self.device)
         with self._own():
-            return dict(slot=e(W, token_cap), pos=e(W, token_cap), start=e(W, B), count=e(W, B), status=e(W, B),
-                        stats=t.empty((W, NSTATS), dtype=t.int64, device=self.device))
+            out = dict(slot=e(W, token_cap), pos=e(W, token_cap), start=e(W, B), count=e(W, B), status=e(W, B),
+                       stats=t.empty((W, NSTATS), dtype=t.int64, device=self.device))
+            if self.cfg.shared:
+                out.update(copy_src=e(W, B), copy_dst=e(W, B))
+            return out
+
+    def alloc_moves(self, n: int) -> Dict[str, object]:
+        """Output arrays of compact_device: at most n blocks of a worker move in a call."""
+        t, W = self.torch, self.cfg.n_workers
+        with self._own():
+            return {k: t.empty((W, n), dtype=t.int32, device=self.device) for k in ("src", "dst")}
 
     # -- calls ----------------------------------------------------------------
     def step_device(self, keep, add, out) -> None:
-        """Tables of the next step (br_kv_step): keep, add [n_workers, rows] int32; out: alloc_step's arrays."""
+        """Tables of the next step (br_kv_step, br_kv_step_shared): keep, add [n_workers, rows] int32; out: alloc_step's arrays."""
         check, i32, rows = self._check, self._i32, self._rows
         slot = out["slot"]
         if slot.dim() != 2 or slot.shape[0] != rows[0]:
@@ -253,9 +298,52 @@ class KvCache:
         _PACK_STEP.pack_into(self._args, 16, check(slot, "slot", slot.shape, i32), check(out["pos"], "pos", slot.shape, i32), check(out["start"], "start", rows, i32),
                              check(out["count"], "count", rows, i32), check(out["status"], "status", rows, i32), check(out["stats"], "stats", self._stats, self._i64),
                              slot.shape[1], 0)
-        rc = self.lib.br_kv_step(self.ctx, self._at, self._at + 16)
+        if self.cfg.shared:
+            _PACK_MOVES.pack_into(self._args, 96, check(out["copy_src"], "copy_src", rows, i32), check(out["copy_dst"], "copy_dst", rows, i32), 0, rows[1], 0)
+            rc = self.lib.br_kv_step_shared(self.ctx, self._at, self._at + 16, self._at + 96)
+        else:
+            rc = self.lib.br_kv_step(self.ctx, self._at, self._at + 16)
         if rc:
-            self._done(rc, "br_kv_step")
+            self._done(rc, "br_kv_step_shared" if self.cfg.shared else "br_kv_step")
+
+    def _is_shared(self) -> None:
+        if not self.cfg.shared:
+            raise BrError("the cache's blocks have one holder each (shared=False)")
+
+    def fork_device(self, rows, length=None) -> None:
+        """Row r becomes the first length[r] tokens (below 0, or no length: all) of row rows[r] of its worker, by holding the same blocks (br_kv_fork).
+
+        rows, length [n_workers, rows] int32, both as they are before the call; rows outside the worker's (-1): row r stays as it is."""
+        self._is_shared()
+        check, i32, shape = self._check, self._i32, self._rows
+        _PACK_FORKS.pack_into(self._args, 0, check(rows, "rows", shape, i32), 0 if length is None else check(length, "length", shape, i32))
+        rc = self.lib.br_kv_fork(self.ctx, self._at)
+        if rc:
+            self._done(rc, "br_kv_fork")
+
+    def _pack_moves(self, src, dst, src_worker) -> None:
+        if src.dim() != 2 or src.shape[0] != self._rows[0]:
+            raise BrError("src must have shape (n_workers, n)")
+        check, i32, shape = self._check, self._i32, src.shape
+        _PACK_MOVES.pack_into(self._args, 0, check(src, "src", shape, i32), check(dst, "dst", shape, i32), 0 if src_worker is None else check(src_worker, "src_worker", shape, i32),
+                              shape[1], 0)
+
+    def compact_device(self, out) -> None:
+        """The blocks in use move to the lowest ids, as many as out (alloc_moves) has room for (br_kv_compact); copy_device with out moves what they hold."""
+        self._is_shared()
+        self._pack_moves(out["src"], out["dst"], None)
+        rc = self.lib.br_kv_compact(self.ctx, self._at)
+        if rc:
+            self._done(rc, "br_kv_compact")
+
+    def copy_device(self, layer: KvLayer, src, dst, src_worker=None) -> None:
+        """What blocks src hold to blocks dst (br_kv_copy): [n_workers, n] block ids of each worker, -1: none; src_worker: whose block src is, if another worker's."""
+        if layer.sizes != self._layer:
+            raise BrError("the layer is one of another cache's sizes")
+        self._pack_moves(src, dst, src_worker)
+        rc = self.lib.br_kv_copy(self.ctx, layer.at, self._at)
+        if rc:
+            self._done(rc, "br_kv_copy")
 
     def _pack_tokens(self, layer, k, v, slot) -> None:
         if layer.sizes != self._layer:
