@@ -12,6 +12,8 @@
  *   br_kv_step_shared  br_kv_step, in which a row that writes into a block that others hold too gets one of its own
  *   br_kv_compact      the blocks in use move to the lowest ids
  *   br_kv_copy         keys and values of blocks, for those two and from worker to worker
+ *   br_kv_plan, br_kv_attend_shared  attention of single tokens that reads what rows hold together once for all of them
+ *   br_kv_attend_diff  differential attention: the difference of two maps
  * A context serves n_workers workers side by side (several DP ranks of a replay on one GPU, or one).  The tables are one
  * per worker for all layers of a model; the cache of each layer is memory of the caller's (br_kv_layer).
  *
@@ -299,6 +301,46 @@ int32_t br_kv_compact(br_kv_ctx *ctx, const br_kv_moves *out);
  * the latter's dst get is not said.  Takes every context.
  */
 int32_t br_kv_copy(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_moves *in);
+
+/*
+ * Rows whose single tokens are read together.  lead [n_workers][rows]: the row of the same worker that leads row r (itself, outside [0, rows), or NULL: it is
+ * alone).  Rows of one leader are a family; what they hold together with it is found in the tables: whatever lead says, each row's result is
+ * that of its own tokens.  start, count: as br_kv_attention's, or both NULL; rows whose count is not 1 have no part in it.  members: a family's rows are
+ * taken together, so many at most (and 64 query rows, where they have more heads than that allows).
+ */
+typedef struct {
+  const int32_t *lead;
+  const int32_t *start;
+  const int32_t *count;
+  int32_t members; /* >= 1 */
+  int32_t pad;
+} br_kv_families;
+
+/*
+ * Plans the attentions of a step, for all layers: of a context of br_kv_init_shared, behind the step and whatever else changes its tables or lengths.
+ */
+int32_t br_kv_plan(br_kv_ctx *ctx, const br_kv_families *in);
+
+/*
+ * br_kv_attend of the planned rows' tokens (start, count, lens and table are NULL, max_count 1 or more): whole tiles of 64 tokens that the rows read together hold in
+ * the same blocks are read once for all of them.  Results are br_kv_attend's but for the order of the sums, which the families have a say in; equal plans and inputs give
+ * equal outputs.  Before the first plan: BR_EINVAL.
+ */
+int32_t br_kv_attend_shared(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *args);
+
+/*
+ * Differential attention.  A head's keys and queries are two halves of head_dim / 2 channels side by side, k = (k1, k2), q = (q1, q2); its values have head_dim.
+ *   out = softmax(scale * q1 k1^T) v - lambda softmax(scale * q2 k2^T) v
+ * over the tokens that br_kv_attend would see.  lambda of token t and query head h is lambda[t * lambda_token + h] (lambda_token 0: one set of n_q_heads for
+ * all tokens).  lse [n_tokens][n_q_heads][2]: of both maps.  A query that sees nothing gets zeros, whatever lambda is, and lse -infinity.
+ * Each map is br_kv_attend's; their difference is formed in 32 bits and rounded once.  n_tokens * 2 n_q_heads / n_kv_heads at most 2^31 - 257.
+ */
+typedef struct {
+  const float *lambda;
+  int64_t lambda_token;
+} br_kv_diff;
+
+int32_t br_kv_attend_diff(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *args, const br_kv_diff *diff);
 
 /* Destroy the context (host memory only). NULL is allowed. */
 void br_kv_free(br_kv_ctx *ctx);

@@ -31,7 +31,7 @@ bool config_ok(const br_kv_config *c) {
 }
 
 struct Places {
-  uint64_t lens, table, tail, used, runs, part, ml, arrived, holders, next_lens, next_table, moved, least, total;
+  uint64_t lens, table, tail, used, runs, part, ml, arrived, holders, next_lens, next_table, moved, least, common, companies, members, total;
 };
 
 Places make_layout(const br_kv_config &c, bool shared) {
@@ -60,6 +60,9 @@ Places make_layout(const br_kv_config &c, bool shared) {
     l.next_table = take(rows * c.max_blocks);
     l.moved = take(blocks);
     l.least = take((uint64_t)c.n_workers);
+    l.common = take(rows);
+    l.companies = take(4 * rows);
+    l.members = take(4 * rows);
   }
   l.total = off;
   return l;
@@ -75,6 +78,7 @@ struct br_kv_ctx {
   int32_t last_hip;
   int cus;
   bool shared;
+  int plan_tile;  // BR_KV_TILE_* of the companies of the last plan, -1: none
 };
 
 namespace {
@@ -141,6 +145,76 @@ BrKvTokens tokens_of(const br_kv_ctx *ctx, const br_kv_tokens *x) {
   return t;
 }
 
+// What an attention of any kind reads and writes; maps: query rows of a head.
+bool attention_of(const br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *a, int maps, BrKvAttend &p) {
+  const br_kv_config &c = ctx->cfg;
+  const int group = c.n_q_heads / c.n_kv_heads * maps;
+  if ((int64_t)a->n_tokens * group > INT32_MAX - 256) return false;
+  char *base = (char *)c.workspace;
+  p = {};
+  p.q = (const unsigned short *)a->q;
+  p.out = (unsigned short *)a->out;
+  p.lse = a->lse;
+  p.start = a->start, p.count = a->count;
+  p.lens = a->lens ? a->lens : ctx->t.lens;
+  p.table = a->table ? a->table : ctx->t.table;
+  p.k = layer->k, p.v = layer->v, p.ks = layer->k_scale, p.vs = layer->v_scale;
+  p.part = (float *)(base + ctx->at.part);
+  p.ml = (float *)(base + ctx->at.ml);
+  p.arrived = ctx->t.arrived;
+  p.q_token = a->q_token, p.q_head = a->q_head, p.out_token = a->out_token, p.out_head = a->out_head;
+  p.n_rows = c.n_workers * c.rows, p.rows = c.rows, p.n_tokens = a->n_tokens;
+  p.window = a->window < c.max_blocks << ctx->t.shift ? a->window : 0;  // (a longer one hides nothing)
+  p.group = group, p.kv_heads = c.n_kv_heads, p.shift = ctx->t.shift, p.n_blocks = c.n_blocks, p.max_blocks = c.max_blocks;
+  p.group_shift = (unsigned)log2_of(group);
+  p.group_mul = (unsigned)((((uint64_t)1 << 32) * (((uint64_t)1 << p.group_shift) - group)) / group + 1);
+  p.bf16 = a->dtype == BR_KV_BF16;
+  p.q_wide = ((uintptr_t)a->q & 15u) == 0 && ((a->q_token | a->q_head) & 7) == 0;
+  p.out_wide = ((uintptr_t)a->out & 7u) == 0 && ((a->out_token | a->out_head) & 3) == 0;
+  p.scale2 = a->scale * 1.4426950408889634f;
+  p.least = 1, p.most = INT32_MAX;
+  return true;
+}
+
+bool attention_ok(const br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *a) {
+  if (!ctx || !layer_ok(layer) || !a || a->n_tokens < 0 || a->max_count < 1 || a->window < 0 || !std::isfinite(a->scale)) return false;
+  if (a->dtype != BR_KV_F16 && a->dtype != BR_KV_BF16) return false;
+  if ((a->start == nullptr) != (a->count == nullptr)) return false;
+  return a->n_tokens == 0 || (a->q && a->out && (((uintptr_t)a->q | (uintptr_t)a->out) & 1u) == 0 && ((uintptr_t)a->lse & 3u) == 0);
+}
+
+#define BR_KV_BY_DIM(CALL)             \
+  switch (ctx->cfg.head_dim) {         \
+    case 64: CALL##_64 BR_KV_ARGS; break;   \
+    case 96: CALL##_96 BR_KV_ARGS; break;   \
+    case 128: CALL##_128 BR_KV_ARGS; break; \
+    case 192: CALL##_192 BR_KV_ARGS; break; \
+    default: CALL##_256 BR_KV_ARGS; break;  \
+  }
+#define BR_KV_ARGS (p, tile, ctx->cfg.fmt == BR_KV_E4M3, ctx->cus, ctx->st)
+
+// Rows of many queries share their block's token tiles, those of few have waves of their own: two launches where a call may have
+// both (two chunks of 512 tokens beside 46 single ones: 375 us in one launch).
+template <class Fn>
+int32_t attend_by_rows(br_kv_ctx *ctx, BrKvAttend &p, int max_count, Fn &&launch) {
+  const br_kv_config &c = ctx->cfg;
+  const int group = p.group;
+  const int64_t rows = (int64_t)max_count * group;
+  // One does where the tables span few tiles: 10 rows of up to 110 tokens and 6 key heads 13.4 us, in two launches 24; 30 rows of 470 and
+  // 8 key heads, near the line, 27 to 33 us and 38.
+  const int64_t tiles = (int64_t)p.n_rows * c.n_kv_heads * ((((int64_t)c.max_blocks << ctx->t.shift) + BR_KV_TILE - 1) / BR_KV_TILE);
+  const bool both = rows > 64 && tiles > 8 * ctx->cus;
+  const int few = both ? 16 / group : 0;  // query tokens up to which a row of a mixed call goes with the few
+  p.least = 1, p.most = both ? few : INT32_MAX;
+  if (rows <= 64 || few > 0) {
+    const int64_t most = both ? 16 : rows;
+    const int32_t rc = enqueue(ctx, [&] { launch(p, most <= 16 ? BR_KV_TILE_16 : most <= 32 ? BR_KV_TILE_32 : BR_KV_TILE_64); });
+    if (rc != BR_OK || rows <= 64) return rc;
+  }
+  p.least = few + 1, p.most = INT32_MAX;
+  return enqueue(ctx, [&] { launch(p, BR_KV_TILE_128); });
+}
+
 }  // namespace
 
 extern "C" {
@@ -156,7 +230,7 @@ static int32_t init_context(const br_kv_config *cfg, const br_kv_state *init, bo
   ctx->at = at;
   ctx->st = (hipStream_t)cfg->stream;
   ctx->last_hip = 0;
-  ctx->shared = shared;
+  ctx->shared = shared, ctx->plan_tile = -1;
   int device = 0;
   hipError_t e = hipGetDevice(&device);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&ctx->cus, hipDeviceAttributeMultiprocessorCount, device);
@@ -248,62 +322,50 @@ int32_t br_kv_read(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_tokens 
 }
 
 int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *a) {
-  if (!ctx || !layer_ok(layer) || !a || a->n_tokens < 0 || a->max_count < 1 || a->window < 0 || !std::isfinite(a->scale)) return BR_EINVAL;
-  if (a->dtype != BR_KV_F16 && a->dtype != BR_KV_BF16) return BR_EINVAL;
-  if ((a->start == nullptr) != (a->count == nullptr)) return BR_EINVAL;
+  if (!attention_ok(ctx, layer, a)) return BR_EINVAL;
   if (a->n_tokens == 0) return BR_OK;
-  if (!a->q || !a->out || (((uintptr_t)a->q | (uintptr_t)a->out) & 1u) || ((uintptr_t)a->lse & 3u)) return BR_EINVAL;
+  BrKvAttend args;
+  if (!attention_of(ctx, layer, a, 1, args)) return BR_EINVAL;
+  return attend_by_rows(ctx, args, a->max_count, [&](const BrKvAttend &p, int tile) { BR_KV_BY_DIM(br_kv_launch_attend) });
+}
+
+int32_t br_kv_attend_diff(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *a, const br_kv_diff *diff) {
+  if (!attention_ok(ctx, layer, a) || !diff) return BR_EINVAL;
+  if (a->n_tokens == 0) return BR_OK;
+  if (!diff->lambda || ((uintptr_t)diff->lambda & 3u)) return BR_EINVAL;
+  BrKvAttend args;
+  if (!attention_of(ctx, layer, a, 2, args)) return BR_EINVAL;
+  args.lambda = diff->lambda, args.lambda_token = diff->lambda_token;
+  return attend_by_rows(ctx, args, a->max_count, [&](const BrKvAttend &p, int tile) { BR_KV_BY_DIM(br_kv_launch_diff) });
+}
+
+int32_t br_kv_plan(br_kv_ctx *ctx, const br_kv_families *in) {
+  if (!ctx || !ctx->shared || !in || in->members < 1 || (in->start == nullptr) != (in->count == nullptr)) return BR_EINVAL;
   const br_kv_config &c = ctx->cfg;
-  const int group = c.n_q_heads / c.n_kv_heads;
-  if ((int64_t)a->n_tokens * group > INT32_MAX - 256) return BR_EINVAL;
+  const int group = c.n_q_heads / c.n_kv_heads, members = in->members < c.rows ? in->members : c.rows;
+  const int rows = members * group;  // (both at most 1024)
+  const int tile = rows <= 16 ? BR_KV_TILE_16 : rows <= 32 ? BR_KV_TILE_32 : BR_KV_TILE_64, fit = (16 << tile) / group;
   char *base = (char *)c.workspace;
+  BrKvPlan x;
+  x.lead = in->lead, x.start = in->start, x.count = in->count;
+  x.common = (int *)(base + ctx->at.common);
+  x.companies = (int4 *)(base + ctx->at.companies);
+  x.members = (int4 *)(base + ctx->at.members);
+  x.most = fit < 1 ? 1 : fit < members ? fit : members;
+  const int32_t rc = enqueue(ctx, [&] { br_kv_launch_plan(ctx->t, x, ctx->st); });
+  if (rc == BR_OK) ctx->plan_tile = tile;
+  return rc;
+}
+
+int32_t br_kv_attend_shared(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *a) {
+  if (!attention_ok(ctx, layer, a) || !ctx->shared || ctx->plan_tile < 0 || a->start || a->lens || a->table) return BR_EINVAL;
+  if (a->n_tokens == 0) return BR_OK;
   BrKvAttend p;
-  p.q = (const unsigned short *)a->q;
-  p.out = (unsigned short *)a->out;
-  p.lse = a->lse;
-  p.start = a->start, p.count = a->count;
-  p.lens = a->lens ? a->lens : ctx->t.lens;
-  p.table = a->table ? a->table : ctx->t.table;
-  p.k = layer->k, p.v = layer->v, p.ks = layer->k_scale, p.vs = layer->v_scale;
-  p.part = (float *)(base + ctx->at.part);
-  p.ml = (float *)(base + ctx->at.ml);
-  p.arrived = ctx->t.arrived;
-  p.q_token = a->q_token, p.q_head = a->q_head, p.out_token = a->out_token, p.out_head = a->out_head;
-  p.n_rows = c.n_workers * c.rows, p.rows = c.rows, p.n_tokens = a->n_tokens;
-  p.window = a->window < c.max_blocks << ctx->t.shift ? a->window : 0;  // (a longer one hides nothing)
-  p.group = group, p.kv_heads = c.n_kv_heads, p.shift = ctx->t.shift, p.n_blocks = c.n_blocks, p.max_blocks = c.max_blocks;
-  p.group_shift = (unsigned)log2_of(group);
-  p.group_mul = (unsigned)((((uint64_t)1 << 32) * (((uint64_t)1 << p.group_shift) - group)) / group + 1);
-  p.bf16 = a->dtype == BR_KV_BF16;
-  p.q_wide = ((uintptr_t)a->q & 15u) == 0 && ((a->q_token | a->q_head) & 7) == 0;
-  p.out_wide = ((uintptr_t)a->out & 7u) == 0 && ((a->out_token | a->out_head) & 3) == 0;
-  p.scale2 = a->scale * 1.4426950408889634f;
-  // Rows of many queries share their block's token tiles, those of few have waves of their own: two launches where a call may have
-  // both (two chunks of 512 tokens beside 46 single ones: 375 us in one launch).
-  const int64_t rows = (int64_t)a->max_count * group;
-  const bool fp8 = c.fmt == BR_KV_E4M3;
-  auto launch = [&](int tile) {
-    switch (c.head_dim) {
-      case 64: br_kv_launch_attend_64(p, tile, fp8, ctx->cus, ctx->st); break;
-      case 96: br_kv_launch_attend_96(p, tile, fp8, ctx->cus, ctx->st); break;
-      case 128: br_kv_launch_attend_128(p, tile, fp8, ctx->cus, ctx->st); break;
-      case 192: br_kv_launch_attend_192(p, tile, fp8, ctx->cus, ctx->st); break;
-      default: br_kv_launch_attend_256(p, tile, fp8, ctx->cus, ctx->st); break;
-    }
-  };
-  // One does where the tables span few tiles: 10 rows of up to 110 tokens and 6 key heads 13.4 us, in two launches 24; 30 rows of 470 and
-  // 8 key heads, near the line, 27 to 33 us and 38.
-  const int64_t tiles = (int64_t)p.n_rows * c.n_kv_heads * ((((int64_t)c.max_blocks << ctx->t.shift) + BR_KV_TILE - 1) / BR_KV_TILE);
-  const bool both = rows > 64 && tiles > 8 * ctx->cus;
-  const int few = both ? 16 / group : 0;  // query tokens up to which a row of a mixed call goes with the few
-  p.least = 1, p.most = both ? few : INT32_MAX;
-  if (rows <= 64 || few > 0) {
-    const int64_t most = both ? 16 : rows;
-    const int32_t rc = enqueue(ctx, [&] { launch(most <= 16 ? BR_KV_TILE_16 : most <= 32 ? BR_KV_TILE_32 : BR_KV_TILE_64); });
-    if (rc != BR_OK || rows <= 64) return rc;
-  }
-  p.least = few + 1, p.most = INT32_MAX;
-  return enqueue(ctx, [&] { launch(BR_KV_TILE_128); });
+  if (!attention_of(ctx, layer, a, 1, p)) return BR_EINVAL;
+  p.companies = (const int4 *)((char *)ctx->cfg.workspace + ctx->at.companies);
+  p.members = (const int4 *)((char *)ctx->cfg.workspace + ctx->at.members);
+  const int tile = ctx->plan_tile;
+  return enqueue(ctx, [&] { BR_KV_BY_DIM(br_kv_launch_shared) });
 }
 
 void br_kv_free(br_kv_ctx *ctx) { delete ctx; }

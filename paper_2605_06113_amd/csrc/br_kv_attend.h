@@ -26,13 +26,43 @@
 #define BR_KV_NEG (-__builtin_inff())
 #define BR_KV_LEAST_TILES 8  // of a block with many query rows: its pieces are large
 
+// What the kernels below are instantiated for.
+//   PLAIN   a row's queries, and its tokens
+//   DIFF    two maps for each query head: `group` counts query rows, two to a head, the first with the first half of the query's channels, the second
+//           with the other (the rest is 0); what is written is the first's result less lambda times the second's
+//   SHARED  the rows that br_kv_plan took together, as one: each has one query token, and the tokens are those that all of them hold, then each one's
+//           others, which only its own query sees.  A row here is such a company, its first token a place in the list of members.
+enum { BR_KV_PLAIN = 0, BR_KV_DIFF = 1, BR_KV_SHARED = 2 };
+
 struct BrKvRow {
-  int n, len, start;  // query tokens, cached tokens, first token
+  int n, len, start;  // query tokens, cached tokens, first token; SHARED: members, tiles that they hold together, place of the first
+  int tiles;          // SHARED: all that any of them sees
 };
 
+__device__ __forceinline__ int br_kv_tiles_of(int tokens) { return (tokens + BR_KV_TILE - 1) / BR_KV_TILE; }
+
+// SHARED: the first tile that a member of that many tokens sees
+__device__ __forceinline__ int br_kv_first_tile(const BrKvAttend &p, int len) { return p.window > 0 ? max(0, len - p.window) / BR_KV_TILE : 0; }
+
 // (a row that is not this launch's has no queries here)
+template <int MODE>
 __device__ __forceinline__ BrKvRow br_kv_row(const BrKvAttend &p, int r) {
   BrKvRow w;
+  if (MODE == BR_KV_SHARED) {
+    const int4 c = p.companies[r];
+    w.n = c.x, w.start = c.y, w.len = c.z, w.tiles = c.w;
+    if (p.window > 0) {
+      int lo = w.len;
+      w.tiles = 0;
+      for (int i = 0; i < w.n; ++i) {
+        const int len = p.members[w.start + i].z, first = br_kv_first_tile(p, len);
+        lo = min(lo, first), w.tiles += max(0, br_kv_tiles_of(len) - max(w.len, first));
+      }
+      w.tiles += w.len - lo;
+    }
+    return w;
+  }
+  w.tiles = 0;
   w.n = p.count ? min(max(p.count[r], 0), p.n_tokens) : 1;
   if (w.n < p.least || w.n > p.most) w.n = 0;
   w.start = p.start ? p.start[r] : r;
@@ -45,8 +75,12 @@ __device__ __forceinline__ int br_kv_token(const BrKvAttend &p, int row) { retur
 
 // First token tile of a query tile, one past the last, and what it counts in the division of the work: a tile that sees nothing still has
 // zeros to write.
-template <int TQ>
+template <int TQ, int MODE>
 __device__ __forceinline__ int br_kv_span(const BrKvAttend &p, const BrKvRow &w, int qi, int &t0, int &t1) {
+  if (MODE == BR_KV_SHARED) {
+    t0 = 0, t1 = w.tiles;
+    return max(1, t1);
+  }
   const int i0 = br_kv_token(p, qi * TQ), i1 = min(w.n - 1, br_kv_token(p, qi * TQ + TQ - 1)), at = w.len - w.n;
   const int hi = max(0, at + i1 + 1), lo = p.window > 0 ? max(0, max(at + i0, 0) - p.window + 1) : 0;
   t0 = lo / BR_KV_TILE;
@@ -55,13 +89,17 @@ __device__ __forceinline__ int br_kv_span(const BrKvAttend &p, const BrKvRow &w,
 }
 
 // Query tiles of one row and key head; the token tiles of every `step`-th from `first` on, and the most that one of them has.
-template <int TQ>
+template <int TQ, int MODE>
 __device__ __forceinline__ int br_kv_row_tiles(const BrKvAttend &p, const BrKvRow &w, long long &tiles, int &most, int first = 0, int step = 1) {
   const int nq = (int)(((long long)w.n * p.group + TQ - 1) / TQ);
   tiles = 0, most = 0;
+  if (MODE == BR_KV_SHARED) {  // (the same for all of a company's query tiles)
+    if (nq > 0) most = max(1, w.tiles), tiles = (long long)nq * most;
+    return nq;
+  }
   for (int qi = first; qi < nq; qi += step) {
     int t0, t1;
-    const int size = br_kv_span<TQ>(p, w, qi, t0, t1);
+    const int size = br_kv_span<TQ, MODE>(p, w, qi, t0, t1);
     tiles += size, most = max(most, size);
   }
   return nq;
@@ -75,12 +113,43 @@ __device__ __forceinline__ uint4 br_kv_load16(const unsigned char *at) {
   return make_uint4(x[0], x[1], x[2], x[3]);
 }
 
-// One query row's place in the output: its 4 N channels d, d + 16, ..., of the lane, times inv.
-template <int N>
-__device__ __forceinline__ void br_kv_store(const BrKvAttend &p, const BrKvRow &w, int h, int ri, int d, const br_f4 (&x)[N], float inv) {
-  const int i = br_kv_token(p, ri), t = w.start + i;
+// The token of a row's i-th query.
+template <int MODE>
+__device__ __forceinline__ int br_kv_place(const BrKvAttend &p, const BrKvRow &w, int i) {
+  return MODE == BR_KV_SHARED ? p.members[w.start + min(i, max(w.n - 1, 0))].y : w.start + i;
+}
+
+// x times inv, and of DIFF less lambda times y times inv_y: zero where nothing was seen, whatever lambda is.
+__device__ __forceinline__ float br_kv_lambda(const BrKvAttend &p, int t, int head, float inv) {
+  return inv == 0.0f ? 0.0f : p.lambda[(long long)t * p.lambda_token + head];
+}
+
+// Over neighbouring lanes: what the other one has
+__device__ __forceinline__ float br_kv_other(float x) { return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0xB1, 0xf, 0xf, true)); }
+
+// One query row's place in the output: its 4 N channels d, d + 16, ..., of the lane, times inv.  DIFF: a head's two rows are neighbouring lanes', the
+// first of which writes (WHOLE: this lane has made one of both, of row ri, and inv is 1 or 0).
+template <int N, int MODE, bool WHOLE = false>
+__device__ __forceinline__ void br_kv_store(const BrKvAttend &p, const BrKvRow &w, int h, int ri, int d, br_f4 (&x)[N], float inv) {
+  const int i = br_kv_token(p, ri), t = br_kv_place<MODE>(p, w, i);
   if (i >= w.n || t < 0 || t >= p.n_tokens) return;
-  unsigned short *at = p.out + (long long)t * p.out_token + (long long)(h * p.group + ri - i * p.group) * p.out_head + d;
+  int head = h * p.group + ri - i * p.group;
+  if (MODE == BR_KV_DIFF) {
+    if (!WHOLE) {
+      const float lambda = br_kv_lambda(p, t, head >> 1, inv);
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float y = x[k][j] * inv;
+          x[k][j] = __builtin_fmaf(-lambda, br_kv_other(y), y);
+        }
+      if (head & 1) return;
+      inv = 1.0f;
+    }
+    head >>= 1;
+  }
+  unsigned short *at = p.out + (long long)t * p.out_token + (long long)head * p.out_head + d;
   uint2 y[N];
   if (p.bf16) {
 #pragma unroll
@@ -99,8 +168,9 @@ __device__ __forceinline__ void br_kv_store(const BrKvAttend &p, const BrKvRow &
   }
 }
 
+template <int MODE>
 __device__ __forceinline__ void br_kv_store_lse(const BrKvAttend &p, const BrKvRow &w, int h, int ri, float m, float l) {
-  const int i = br_kv_token(p, ri), t = w.start + i;
+  const int i = br_kv_token(p, ri), t = br_kv_place<MODE>(p, w, i);
   if (!p.lse || i >= w.n || t < 0 || t >= p.n_tokens) return;
   p.lse[(long long)t * p.kv_heads * p.group + h * p.group + ri - i * p.group] = l == 0.0f ? BR_KV_NEG : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
@@ -185,24 +255,30 @@ __device__ __forceinline__ void BrKvSums<D, NQ>::close() {
   }
 }
 
+// Which of a wave's 16 NQ query rows lane n of group x has.  DIFF with two groups: both maps of a head in one lane, so that their difference is made there.
+template <int MODE, int NQ>
+__device__ __forceinline__ int br_kv_query(int x, int n) { return MODE == BR_KV_DIFF && NQ == 2 ? 2 * n + x : 16 * x + n; }
+
 // The queries of 16 NQ rows from row0 on in f16, one row's to four lanes: channels 64 i + 16 g .. + 15 of its row for each lane, then
 // 8 g .. + 7 of the last 32; what their scores are multiplied by (in powers of two; never below zero), and their positions.
-template <int D, int NQ>
+template <int D, int NQ, int MODE>
 struct BrKvQueries {
   static constexpr int NI = D / 64, NK = D / 32;
   br_h8 qf[NQ][NK];
   float qs[NQ];
-  int pos[NQ];
+  int pos[NQ], member[NQ];
 
   template <class Fn>
   __device__ __forceinline__ void load(const BrKvAttend &p, const BrKvRow &w, int h, int row0, Fn &&meanwhile) {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-      const int ri = row0 + 16 * x + n, i = br_kv_token(p, ri), t = w.start + i;
+      const int ri = row0 + br_kv_query<MODE, NQ>(x, n), i = br_kv_token(p, ri), t = br_kv_place<MODE>(p, w, i);
       const bool in = i < w.n && t >= 0 && t < p.n_tokens;
-      pos[x] = in ? max(w.len - w.n + i, -1) : -1;
-      const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(h * p.group + ri - i * p.group) * p.q_head : 0);
+      const int head = h * p.group + ri - i * p.group;
+      if (MODE == BR_KV_SHARED) pos[x] = in ? p.members[w.start + i].z - 1 : -1, member[x] = i;
+      else pos[x] = in ? max(w.len - w.n + i, -1) : -1;
+      const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(MODE == BR_KV_DIFF ? head >> 1 : head) * p.q_head : 0);
       uint4 e[NK];
       auto channel = [&](int c) { return c < 2 * NI ? (c / 2) * 64 + g * 16 + (c & 1) * 8 : NI * 64 + g * 8; };
       if (p.q_wide) {
@@ -214,6 +290,11 @@ struct BrKvQueries {
           const unsigned short *y = at + channel(c);
           e[c] = make_uint4(y[0] | (unsigned)y[1] << 16, y[2] | (unsigned)y[3] << 16, y[4] | (unsigned)y[5] << 16, y[6] | (unsigned)y[7] << 16);
         }
+      }
+      if (MODE == BR_KV_DIFF) {  // (halves of 32, 48, 64, 96 or 128 channels: eight neighbours are in one)
+#pragma unroll
+        for (int c = 0; c < NK; ++c)
+          if ((channel(c) >= D / 2) != (bool)(head & 1)) e[c] = make_uint4(0u, 0u, 0u, 0u);
       }
       if (x == 0) meanwhile();
       float f[NK * 8], top = 0.0f;
@@ -245,9 +326,10 @@ struct BrKvQueries {
 
 // Weights of a tile from its scores: s [16 tokens 4 y + i of the lane's group][query n of group x]; ks, vs the scales of the lane's tokens,
 // `have` of them; exist: all of the tile's blocks do.  Moves m and c, and the sums with them.
-template <int D, int NQ>
-__device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQueries<D, NQ> &q, const br_f4 (&s)[NQ][4], float ks, float vs, int have, int t, int first_pos,
-                                              int last_pos, bool exist, BrKvSums<D, NQ> &sums, br_h8 (&pf)[NQ][2]) {
+// SHARED: `owner` is the member whose tile it is; -1: all of them hold it.
+template <int D, int NQ, int MODE>
+__device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQueries<D, NQ, MODE> &q, const br_f4 (&s)[NQ][4], float ks, float vs, int have, int t, int first_pos,
+                                              int last_pos, int owner, bool exist, BrKvSums<D, NQ> &sums, br_h8 (&pf)[NQ][2]) {
   constexpr int ND = D / 16;
   constexpr float ROOM = BrKvSums<D, NQ>::ROOM, UNIT = BrKvSums<D, NQ>::UNIT;
   const int token = t * BR_KV_TILE + 16 * ((threadIdx.x & 63) >> 4);
@@ -257,7 +339,7 @@ __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQue
   auto &c = sums.c;
   const float vmax = br_kv_max4(have > 0 ? vs : 0.0f);  // (of who sees what is asked below, where it matters)
   // inside: every query of the tile sees all of its tokens, and all exist
-  const bool inside = t * BR_KV_TILE + BR_KV_TILE - 1 <= first_pos && (p.window == 0 || t * BR_KV_TILE > last_pos - p.window) && exist;
+  const bool inside = owner < 0 && t * BR_KV_TILE + BR_KV_TILE - 1 <= first_pos && (p.window == 0 || t * BR_KV_TILE > last_pos - p.window) && exist;
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
     float f = q.qs[x] * ks;  // (not below zero: the sign of the caller's scale is in the queries)
@@ -265,7 +347,8 @@ __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQue
 #pragma unroll
     for (int j = 0; j < 16; ++j) z[j] = s[x][j >> 2][j & 3];
     if (!inside) {  // of the lane's tokens, those from `lo` on, `seen` of them
-      const int lo = p.window > 0 ? max(q.pos[x] - p.window + 1 - token, 0) : 0, seen = max(min(have, q.pos[x] + 1 - token) - lo, 0);
+      const int pos = MODE == BR_KV_SHARED && owner >= 0 && owner != q.member[x] ? -1 : q.pos[x];
+      const int lo = p.window > 0 ? max(pos - p.window + 1 - token, 0) : 0, seen = max(min(have, pos + 1 - token) - lo, 0);
 #pragma unroll
       for (int j = 0; j < 16; ++j) z[j] = (unsigned)(j - lo) < (unsigned)seen ? z[j] * f : BR_KV_NEG;
       f = 1.0f;
@@ -313,7 +396,7 @@ __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQue
 
 // ONCE: nobody else reads these codes; ONCE_V: nor these values' lines (blocks of 128 tokens have two tiles' in one).
 // Token tiles t .. stop - 1 of row r and key head h for the query rows from row0 on, whose positions lie in first_pos .. last_pos.
-template <int D, int NQ, bool FP8, bool ONCE_V, bool ONCE>
+template <int D, int NQ, bool FP8, bool ONCE_V, bool ONCE, int MODE>
 __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int r, int h, int row0, int first_pos, int last_pos, int t, int stop,
                                             BrKvSums<D, NQ> &sums) {
   constexpr int NI = D / 64, REST = D % 64 / 32, NK = 2 * NI + REST, ND = D / 16;
@@ -326,9 +409,34 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   auto &o = sums.o;
   sums.clear();
 
-  const int worker = r / p.rows;
-  const int *table = p.table + (long long)r * p.max_blocks;
-  const int last_block = max(0, (w.len - 1) >> p.shift);
+  // Where tile t is: the row of the tables, the tile of its tokens, how many it has, whose it is.
+  struct Tile {
+    int row, tile, len, owner;
+  };
+  int4 member = make_int4(0, 0, 0, 0);  // SHARED: lane i's
+  int begins = 0, first_tile = 0, together = 0;
+  if (MODE == BR_KV_SHARED) {
+    // (a company has no more members than a wave has lanes)
+    member = lane < w.n ? p.members[w.start + lane] : make_int4(0, 0, 0, 0);
+    const int lo = lane < w.n ? br_kv_first_tile(p, member.z) : w.len, own = lane < w.n ? max(0, br_kv_tiles_of(member.z) - max(w.len, lo)) : 0;
+    first_tile = scalar(-(int)br_kv_max64((float)-min(lo, w.len)));  // (below 2^24: exact)
+    together = w.len - first_tile;
+    begins = together + br_kv_wave_scan(own) - own;
+    // what all of them see: one member's own tokens, of several what they hold together, if no window ends there
+    first_pos = last_pos = w.n > 1 ? w.len * BR_KV_TILE - 1 : __builtin_amdgcn_readlane(member.z, 0) - 1;
+    if (w.n > 1 && p.window > 0) last_pos = INT32_MAX;
+  }
+  auto tile_at = [&](int t) {
+    Tile x = {r, t, w.len, -1};
+    if (MODE == BR_KV_SHARED) {
+      const int i = t < together ? 0 : max(__popcll(__ballot(lane < w.n && begins <= t)) - 1, 0);
+      x.row = __builtin_amdgcn_readlane(member.x, i), x.len = __builtin_amdgcn_readlane(member.z, i);
+      if (t < together) x.tile = first_tile + t, x.len = w.len * BR_KV_TILE;
+      else x.tile = max(w.len, br_kv_first_tile(p, x.len)) + t - __builtin_amdgcn_readlane(begins, i), x.owner = w.n > 1 ? i : -1;
+    }
+    return x;
+  };
+  const int worker = (MODE == BR_KV_SHARED ? tile_at(0).row : r) / p.rows;
   const long long cache0 = (long long)worker * p.n_blocks;
   const int mask = (1 << p.shift) - 1;
   const int kg = n >> 2, kr = n & 3;  // the token group, and the place in fours, of the lane's row of K
@@ -337,7 +445,9 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   uint2 kx[4];
   uint4 vc[ND];
   // block of a lane's 16 tokens, as the table has it; where it is read, one that does not exist is block 0
-  auto id_of = [&](int token) { return table[min(token >> p.shift, last_block)]; };
+  auto id_of = [&](const Tile &x, int in) {
+    return p.table[(long long)x.row * p.max_blocks + min((x.tile * BR_KV_TILE + in) >> p.shift, max(0, (x.len - 1) >> p.shift))];
+  };
   auto there = [&](int id) { return (unsigned)id < (unsigned)p.n_blocks; };
   auto load_k = [&](int t, int id, bool live) {
     const unsigned char *at =
@@ -360,29 +470,30 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   };
   const bool t_any = t < stop;
   int kid = 0;
+  Tile now = tile_at(t), next = now;
   if (t_any) {
-    const int next = t + 1 < stop ? t + 1 : t;
-    kid = id_of(t * BR_KV_TILE + 16 * kg), vid = id_of(t * BR_KV_TILE + 16 * g);
-    kid1 = id_of(next * BR_KV_TILE + 16 * kg), vid1 = id_of(next * BR_KV_TILE + 16 * g);
+    next = tile_at(t + 1 < stop ? t + 1 : t);
+    kid = id_of(now, 16 * kg), vid = id_of(now, 16 * g);
+    kid1 = id_of(next, 16 * kg), vid1 = id_of(next, 16 * g);
   }
   auto load_first = [&]() {
-    load_k(t, kid, true);
+    load_k(now.tile, kid, true);
     load_scales(vid);
   };
-  BrKvQueries<D, NQ> q;
+  BrKvQueries<D, NQ, MODE> q;
   q.load(p, w, h, row0, [&] {
     if (t_any) load_first();  // (while the queries are on their way)
   });
 
   for (; t < stop; ++t) {
-    const int token = t * BR_KV_TILE + 16 * g;  // of the lane's first weight
+    const int token = now.tile * BR_KV_TILE + 16 * g;  // of the lane's first weight
     {
       const unsigned char *at = p.v + ((((cache0 + (there(vid) ? vid : 0)) * p.kv_heads + h) * D + n) << p.shift) + (token & mask);
 #pragma unroll
       for (int d = 0; d < ND; ++d) vc[d] = br_kv_load16<ONCE_V>(at + ((16 * d) << p.shift));
     }
     const float ks = there(vid) ? br_kv_sound(ks1) : 0.0f, vs = there(vid) ? br_kv_sound(vs1) : 0.0f;
-    const int have = there(vid) ? min(max(w.len - token, 0), 16) : 0;  // of the lane's tokens, those that exist
+    const int have = there(vid) ? min(max(now.len - token, 0), 16) : 0;  // of the lane's tokens, those that exist
 
     br_f4 s[NQ][4];
 #pragma unroll
@@ -401,15 +512,14 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
         for (int x = 0; x < NQ; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q.qf[x][c], s[x][y], 0, 0, 0);
       }
     }
-    const int next = t + 1 < stop ? t + 1 : t, after = next + 1 < stop ? next + 1 : next;
-    load_k(next, kid1, t + 1 < stop);
+    const Tile after = tile_at(min(t + 2, stop - 1));
+    load_k(next.tile, kid1, t + 1 < stop);
     load_scales(vid1);
-    kid1 = id_of(after * BR_KV_TILE + 16 * kg);
-    const int vid2 = id_of(after * BR_KV_TILE + 16 * g);
-
+    kid1 = id_of(after, 16 * kg);
+    const int vid2 = id_of(after, 16 * g);
 
     br_h8 pf[NQ][2];
-    br_kv_weights<D, NQ>(p, q, s, ks, vs, have, t, first_pos, last_pos, !__any(!there(vid)), sums, pf);
+    br_kv_weights<D, NQ, MODE>(p, q, s, ks, vs, have, now.tile, first_pos, last_pos, now.owner, !__any(!there(vid)), sums, pf);
     // bytes behind the row's end are whatever memory held: an 8-bit float may be a NaN there
     if (FP8 && __any(have < 16)) {
       const unsigned long long full = ~0ull;
@@ -430,6 +540,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
         }
     }
     vid = vid1, vid1 = vid2;
+    now = next, next = after;
   }
   sums.close();
 }
@@ -437,7 +548,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 // Joins the pieces of a query tile, of blocks first .. first + parts - 1, into its result (all of the block's threads; sums and ml: NT of
 // each in LDS).  A thread has four channels of a row; where those are less than half of the threads the pieces are shared out as
 // well.  One way to memory and back: each thread weighs its pieces against the largest maximum among them.
-template <int D, int TQ, int NT>
+template <int D, int TQ, int NT, int MODE>
 __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int rows_q, int first, int parts, br_f4 *sums, float2 *ml) {
   // few rows have many pieces (up to a block of the launch each), many rows few: places asked for at once are AT_ONCE pieces of ROWS rows
   constexpr int ROWS = TQ > 64 ? 8 : TQ > 32 ? 4 : 1, AT_ONCE = TQ > 32 ? 2 : 8, STEP = NT * ROWS;
@@ -520,9 +631,9 @@ __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w
       int row, d;
       pieces.place(it, row, d);
       if (row >= rows_q) continue;
-      const br_f4 one[1] = {ys[q]};
-      br_kv_store<1>(p, w, h, qi * TQ + row, d, one, ls[q] != 0.0f ? 1.0f / ls[q] : 0.0f);
-      if (d == 0) br_kv_store_lse(p, w, h, qi * TQ + row, ms[q], ls[q]);
+      br_f4 one[1] = {ys[q]};
+      br_kv_store<1, MODE>(p, w, h, qi * TQ + row, d, one, ls[q] != 0.0f ? 1.0f / ls[q] : 0.0f);
+      if (d == 0) br_kv_store_lse<MODE>(p, w, h, qi * TQ + row, ms[q], ls[q]);
     }
   }
 }
@@ -538,7 +649,7 @@ __device__ __forceinline__ T br_kv_scalar(T x) {
 // none is much longer than an equal share, each goes to a block, in NR parts: nothing is left to be joined through memory, which
 // takes about as long as SLACK tiles.  Else the workers get runs of tiles that differ by one at most.  What is dealt are units: tiles, or a
 // query tile's NR parts.
-template <int TQ, int NT, int NR, int SLACK>
+template <int TQ, int NT, int NR, int SLACK, int MODE>
 struct BrKvRuns {
   static constexpr bool MANY = TQ > 64;  // a row may well have more than one query tile
   struct Shared {
@@ -562,12 +673,12 @@ struct BrKvRuns {
     long long mine = 0;
     int mine_q = 0, most = 0;
     for (int r = at * per; r < min(p.n_rows, (at + 1) * per); ++r) {
-      const BrKvRow w = br_kv_row(p, r);
-      s.row[at] = make_int4(w.n, w.len, w.start, 0);
+      const BrKvRow w = br_kv_row<MODE>(p, r);
+      s.row[at] = make_int4(w.n, w.len, w.start, w.tiles);
       if (w.n <= 0) continue;
       long long tiles;
       int longest;
-      mine_q = min(mine_q + br_kv_row_tiles<TQ>(p, w, tiles, longest, one, 1 << log_per_row), 4096);
+      mine_q = min(mine_q + br_kv_row_tiles<TQ, MODE>(p, w, tiles, longest, one, 1 << log_per_row), 4096);
       mine += tiles, most = max(most, longest);
     }
     if (MANY) {
@@ -622,10 +733,10 @@ struct BrKvRuns {
     int most;
     if (parts) return (int)(((long long)w.n * p.group + TQ - 1) / TQ) * NR;
     if (MANY) {
-      br_kv_row_tiles<TQ>(p, w, tiles, most, threadIdx.x & 63, 64);
+      br_kv_row_tiles<TQ, MODE>(p, w, tiles, most, threadIdx.x & 63, 64);
       for (int d = 1; d < 64; d <<= 1) tiles += __shfl_xor(tiles, d, 64);
     } else {
-      br_kv_row_tiles<TQ>(p, w, tiles, most);
+      br_kv_row_tiles<TQ, MODE>(p, w, tiles, most);
     }
     return tiles;
   }
@@ -649,14 +760,14 @@ struct BrKvRuns {
     return k;
   }
   __device__ __forceinline__ BrKvRow row_of(const BrKvAttend &p, int r) const {
-    if (per > 1) return br_kv_row(p, r);
+    if (per > 1) return br_kv_row<MODE>(p, r);
     const int4 x = s.row[r];
-    return BrKvRow{x.x, x.y, x.z};
+    return BrKvRow{x.x, x.y, x.z, x.w};
   }
 };
 
 // Where a run stands: query tile qi of row r and key head h, tiles t0 .. t1 - 1 of its tokens, the first of which is tile `seg` of the call.
-template <int TQ, int NT, class Runs>
+template <int TQ, int NT, class Runs, int MODE>
 struct BrKvPlace {
   BrKvRow w;
   long long base, seg, tiles;
@@ -681,14 +792,14 @@ struct BrKvPlace {
     if (Runs::MANY) {  // 64 query tiles at a time
       const int last = (int)(((long long)w.n * p.group + TQ - 1) / TQ) - 1;
       for (int k = 64; k == 64; qi += k) {
-        const int sum = br_kv_wave_scan(runs.units_of(br_kv_span<TQ>(p, w, min(qi + (int)(threadIdx.x & 63), last), t0, t1)));
+        const int sum = br_kv_wave_scan(runs.units_of(br_kv_span<TQ, MODE>(p, w, min(qi + (int)(threadIdx.x & 63), last), t0, t1)));
         k = __popcll(__ballot(seg + sum <= u));
         if (k > 0) seg += __shfl(sum, k - 1, 64);
       }
-      size = runs.units_of(br_kv_span<TQ>(p, w, qi, t0, t1));
+      size = runs.units_of(br_kv_span<TQ, MODE>(p, w, qi, t0, t1));
     } else {
-      size = runs.units_of(br_kv_span<TQ>(p, w, 0, t0, t1));
-      while (u >= seg + size) seg += size, size = runs.units_of(br_kv_span<TQ>(p, w, ++qi, t0, t1));
+      size = runs.units_of(br_kv_span<TQ, MODE>(p, w, 0, t0, t1));
+      while (u >= seg + size) seg += size, size = runs.units_of(br_kv_span<TQ, MODE>(p, w, ++qi, t0, t1));
     }
     return true;
   }
@@ -709,7 +820,7 @@ struct BrKvPlace {
         if (r >= p.n_rows) return false;
       }
     }
-    size = runs.units_of(br_kv_span<TQ>(p, w, qi, t0, t1));
+    size = runs.units_of(br_kv_span<TQ, MODE>(p, w, qi, t0, t1));
     return true;
   }
   // the first tile of its unit k (one past the last, for k = size)
@@ -720,33 +831,46 @@ struct BrKvPlace {
 };
 
 // A wave's result of query rows row.. of the tile, to its place, or as piece `piece` to memory
-template <int D, int NQ, int TQ>
-__device__ __forceinline__ void br_kv_result(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int row, int rows_q, const BrKvSums<D, NQ> &s) {
+template <int D, int NQ, int TQ, int MODE>
+__device__ __forceinline__ void br_kv_result(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int row, int rows_q, BrKvSums<D, NQ> &s) {
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
-    const int at = row + 16 * x + n;
+    const int at = row + br_kv_query<MODE, NQ>(x, n);
     if (at >= rows_q) continue;
     const float inv = s.l[x] != 0.0f ? s.c[x] / s.l[x] : 0.0f;
-    br_kv_store<D / 16>(p, w, h, qi * TQ + at, 4 * g, s.o[x], inv);
-    if (g == 0) br_kv_store_lse(p, w, h, qi * TQ + at, s.m[x], s.l[x]);
+    if (MODE == BR_KV_DIFF && NQ == 2) {
+      if (x == 0) {
+        const int i = br_kv_token(p, qi * TQ + at), t = w.start + i;
+        const float lambda = i < w.n && t >= 0 && t < p.n_tokens ? br_kv_lambda(p, t, (h * p.group + qi * TQ + at - i * p.group) >> 1, inv) : 0.0f;
+        const float less = -lambda * (s.l[NQ - 1] != 0.0f ? s.c[NQ - 1] / s.l[NQ - 1] : 0.0f);
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s.o[0][d][j] = __builtin_fmaf(s.o[NQ - 1][d][j], less, s.o[0][d][j] * inv);
+        br_kv_store<D / 16, MODE, true>(p, w, h, qi * TQ + at, 4 * g, s.o[0], 1.0f);
+      }
+    } else {
+      br_kv_store<D / 16, MODE>(p, w, h, qi * TQ + at, 4 * g, s.o[x], inv);
+    }
+    if (g == 0) br_kv_store_lse<MODE>(p, w, h, qi * TQ + at, s.m[x], s.l[x]);
   }
 }
 
-template <int D, int NQ, int TQ>
+template <int D, int NQ, int TQ, int MODE>
 __device__ __forceinline__ void br_kv_piece(const BrKvAttend &p, int piece, int row, int rows_q, const BrKvSums<D, NQ> &s) {
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const BrKvPieces<D, TQ> pieces(p, rows_q);
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
-    const int at = row + 16 * x + n;
+    const int at = row + br_kv_query<MODE, NQ>(x, n);
     if (at >= rows_q) continue;
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) {
       br_f4 y = s.o[x][d];
 #pragma unroll
       for (int j = 0; j < 4; ++j) y[j] *= s.c[x];
-      pieces.put(piece, pieces.item(row / 16 + x, d, g, n), y);
+      pieces.put(piece, MODE == BR_KV_DIFF ? pieces.item(at / 16, d, g, at % 16) : pieces.item(row / 16 + x, d, g, n), y);
     }
     if (g == 0) br_kv_put2(p.ml + (piece * TQ + at) * 2, s.m[x], s.l[x]);
   }
@@ -763,10 +887,10 @@ struct BrKvShare {
 // of 256 to 8192 tokens, 8 key heads of 128 channels, groups of 8: 128 us, 691 MB = 5.4 TB/s (a large copy: 5.1).  One row of 40 thousand
 // tokens: 26 us, 87 MB, of them some 6 us for the pieces' way through LDS and memory; one of 500 13 us, a launch and a chain
 // of loads (lengths, ids, codes, the join).
-template <int D, int SHARE, bool FP8, bool HALF, int NW, int WAVES>
+template <int D, int SHARE, bool FP8, bool HALF, int NW, int WAVES, int MODE>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   constexpr int TQ = 16 * SHARE, NT = 64 * NW, ND = D / 16, NR = NW / SHARE;  // NR: runs of a block
-  using Runs = BrKvRuns<TQ, NT, NR, 6>;
+  using Runs = BrKvRuns<TQ, NT, NR, 6, MODE>;
   __shared__ typename Runs::Shared shared;
   __shared__ br_f4 kept[2 * NW * ND * 64];  // piece 2 k: taken up by run k, 2 k + 1: begun by it
   __shared__ float2 kept_ml[2 * NW * 16];
@@ -786,16 +910,16 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
 
   bool open = false;  // the query tile that was taken up goes on in the next wave
   {
-    BrKvPlace<TQ, NT, Runs> at;
+    BrKvPlace<TQ, NT, Runs, MODE> at;
     BrKvSums<D, 1> s;
     if (u < end && at.find(p, runs, u)) {
       for (;;) {
         const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg);
         const int rows_q = at.rows_q(p);
-        br_kv_tiles<D, 1, FP8, SHARE == 1 && !HALF, SHARE == 1>(p, at.w, at.r, at.h, at.qi * TQ + row, at.pos_of(p, row), at.pos_of(p, row + 15), at.tile_of(runs, a),
+        br_kv_tiles<D, 1, FP8, SHARE == 1 && !HALF, SHARE == 1, MODE>(p, at.w, at.r, at.h, at.qi * TQ + row, at.pos_of(p, row), at.pos_of(p, row + 15), at.tile_of(runs, a),
                                                                row < rows_q ? at.tile_of(runs, b) : 0, s);
         if (a == 0 && b == at.size) {
-          br_kv_result<D, 1, TQ>(p, at.w, at.h, at.qi, row, rows_q, s);
+          br_kv_result<D, 1, TQ, MODE>(p, at.w, at.h, at.qi, row, rows_q, s);
         } else {
           const int piece = (2 * rn + (a == 0)) * SHARE + wv % SHARE;
 #pragma unroll
@@ -857,8 +981,8 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
       if (row >= rows_q) continue;
       if (top == BR_KV_NEG) top = 0.0f;
       if (chain.parts == 1) {
-        br_kv_store<1>(p, w, chain.h, chain.qi * TQ + row, 16 * d + 4 * g, y, l != 0.0f ? 1.0f / l : 0.0f);
-        if (d == 0 && g == 0) br_kv_store_lse(p, w, chain.h, chain.qi * TQ + row, top, l);
+        br_kv_store<1, MODE>(p, w, chain.h, chain.qi * TQ + row, 16 * d + 4 * g, y, l != 0.0f ? 1.0f / l : 0.0f);
+        if (d == 0 && g == 0) br_kv_store_lse<MODE>(p, w, chain.h, chain.qi * TQ + row, top, l);
       } else {
         const int piece = 2 * wg + (c < NR);
         const BrKvPieces<D, TQ> pieces(p, rows_q);
@@ -882,7 +1006,7 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
     const BrKvShare c = chains[k ? which : NR];
     if ((k ? !goes : !came) || arrived[k] != c.parts - 1) continue;
     const BrKvRow w = runs.row_of(p, c.r);
-    br_kv_join<D, TQ, NT>(p, w, c.h, c.qi, (int)min((long long)TQ, (long long)w.n * p.group - (long long)c.qi * TQ), c.first, c.parts, kept, (float2 *)(kept + NT));
+    br_kv_join<D, TQ, NT, MODE>(p, w, c.h, c.qi, (int)min((long long)TQ, (long long)w.n * p.group - (long long)c.qi * TQ), c.first, c.parts, kept, (float2 *)(kept + NT));
     if (tid == 0) p.arrived[c.first] = 0;  // (for the next launch)
     __syncthreads();
   }
@@ -908,10 +1032,10 @@ __device__ __forceinline__ void br_kv_ahead(Get &&get, Use &&use) {
 // tile.  Bound by the issue of vector instructions between the products (310 a tile and wave, 32 of them exponentials, to 64 products): chunks
 // of 512 tokens of two rows, groups of 4, 8 key heads of 128 channels behind up to 8192 tokens 207 us, 0.61 PFLOP/s; a wave issues in 44 %
 // of its time and waits for its turn, beside the other wave of its SIMD, in 30 %; the matrix units are busy a third.
-template <int D, int NQ, bool FP8, int WAVES>
+template <int D, int NQ, bool FP8, int WAVES, int MODE>
 __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) {
   constexpr int TQ = 64 * NQ, NT = 256, NI = D / 64, REST = D % 64 / 32, NK = D / 32, ND = D / 16, VG = (ND + 3) / 4, AHEAD = WAVES == 1 ? 2 : 1;  // VG: groups of 16 channels of values that a wave brings
-  using Runs = BrKvRuns<TQ, NT, 1, 8>;
+  using Runs = BrKvRuns<TQ, NT, 1, 8, MODE>;
   __shared__ typename Runs::Shared shared;
   __shared__ br_h8 tile[2][(4 * NK + 2 * ND) * 64];
   __shared__ int arrived;
@@ -921,7 +1045,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
   if (wg >= blocks) return;
   long long u = runs.begin_of(wg);
   const long long end = runs.begin_of(wg + 1);
-  BrKvPlace<TQ, NT, Runs> at;
+  BrKvPlace<TQ, NT, Runs, MODE> at;
   if (u >= end || !at.find(p, runs, u)) return;
   const int kg = n >> 2, kr = n & 3, mask = (1 << p.shift) - 1;
   // Of two blocks on a compute unit the one that came first would have its way, and be done long before the other: they go first in turns.
@@ -998,7 +1122,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
       kid2 = id_of(after * BR_KV_TILE + 16 * kg), vid2 = id_of(after * BR_KV_TILE + 16 * g);
       fetch(first, kid, vid);
     }
-    BrKvQueries<D, NQ> q;
+    BrKvQueries<D, NQ, MODE> q;
     q.load(p, at.w, h, at.qi * TQ + row, [] {});
     if (first < stop) {
       ks = ks1, vs = vs1;
@@ -1036,7 +1160,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
             });
         const int have = there(vid) ? min(max(len - t * BR_KV_TILE - 16 * g, 0), 16) : 0;
         br_h8 pf[NQ][2];
-        br_kv_weights<D, NQ>(p, q, z, there(vid) ? br_kv_sound(ks) : 0.0f, there(vid) ? br_kv_sound(vs) : 0.0f, have, t, first_pos, last_pos, !__any(!there(vid)), s, pf);
+        br_kv_weights<D, NQ, MODE>(p, q, z, there(vid) ? br_kv_sound(ks) : 0.0f, there(vid) ? br_kv_sound(vs) : 0.0f, have, t, first_pos, last_pos, -1, !__any(!there(vid)), s, pf);
         br_kv_ahead<ND / 2, AHEAD>(
             [&](int d, br_h8 (&f)[4]) {
 #pragma unroll
@@ -1058,16 +1182,16 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
     }
     s.close();
     if (whole) {
-      br_kv_result<D, NQ, TQ>(p, at.w, at.h, at.qi, row, rows_q, s);
+      br_kv_result<D, NQ, TQ, MODE>(p, at.w, at.h, at.qi, row, rows_q, s);
     } else {
       const int from = runs.owner_of(at.seg), parts = runs.owner_of(at.seg + at.size - 1) - from + 1;
-      br_kv_piece<D, NQ, TQ>(p, 2 * wg + (a == 0 ? 1 : 0), row, rows_q, s);
+      br_kv_piece<D, NQ, TQ, MODE>(p, 2 * wg + (a == 0 ? 1 : 0), row, rows_q, s);
       br_kv_stores_done();
       __syncthreads();
       if (tid == 0) arrived = __hip_atomic_fetch_add(&p.arrived[from], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       __syncthreads();
       if (arrived == parts - 1) {
-        br_kv_join<D, TQ, NT>(p, at.w, at.h, at.qi, rows_q, from, parts, (br_f4 *)tile[0], (float2 *)tile[1]);
+        br_kv_join<D, TQ, NT, MODE>(p, at.w, at.h, at.qi, rows_q, from, parts, (br_f4 *)tile[0], (float2 *)tile[1]);
         if (tid == 0) p.arrived[from] = 0;  // (for the next launch)
       }
       __syncthreads();
@@ -1078,36 +1202,36 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
 }
 
 // WAVES on a SIMD, by the registers that the tile needs; PER blocks of NW waves on a compute unit
-template <int D, int SHARE, int NW, int WAVES>
+template <int D, int SHARE, int NW, int WAVES, int MODE>
 void br_kv_attend_few(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
   constexpr int PER = 4 * WAVES / NW;
   const int blocks = PER * cus < BR_KV_SPLIT_WGS_OF(D) ? PER * cus : BR_KV_SPLIT_WGS_OF(D);
   const bool half = SHARE == 1 && p.shift == 7;
   if constexpr (SHARE == 1) {
     if (half) {
-      if (fp8) br_kv_k_attend<D, SHARE, true, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
-      else br_kv_k_attend<D, SHARE, false, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+      if (fp8) br_kv_k_attend<D, SHARE, true, true, NW, WAVES, MODE><<<blocks, 64 * NW, 0, st>>>(p);
+      else br_kv_k_attend<D, SHARE, false, true, NW, WAVES, MODE><<<blocks, 64 * NW, 0, st>>>(p);
       return;
     }
   }
-  if (fp8) br_kv_k_attend<D, SHARE, true, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
-  else br_kv_k_attend<D, SHARE, false, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+  if (fp8) br_kv_k_attend<D, SHARE, true, false, NW, WAVES, MODE><<<blocks, 64 * NW, 0, st>>>(p);
+  else br_kv_k_attend<D, SHARE, false, false, NW, WAVES, MODE><<<blocks, 64 * NW, 0, st>>>(p);
 }
 
-template <int D, int NQ, int WAVES>
+template <int D, int NQ, int WAVES, int MODE>
 void br_kv_attend_rows(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
   const int blocks = WAVES * cus < BR_KV_SPLIT_WGS_OF(D) ? WAVES * cus : BR_KV_SPLIT_WGS_OF(D);
-  if (fp8) br_kv_k_attend_rows<D, NQ, true, WAVES><<<blocks, 256, 0, st>>>(p);
-  else br_kv_k_attend_rows<D, NQ, false, WAVES><<<blocks, 256, 0, st>>>(p);
+  if (fp8) br_kv_k_attend_rows<D, NQ, true, WAVES, MODE><<<blocks, 256, 0, st>>>(p);
+  else br_kv_k_attend_rows<D, NQ, false, WAVES, MODE><<<blocks, 256, 0, st>>>(p);
 }
 
-template <int D>
+template <int D, int MODE = BR_KV_PLAIN>
 void br_kv_attend_dim(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st) {
   constexpr int NW = D <= 64 ? 12 : D <= 128 ? 8 : 4, WAVES = D <= 64 ? 3 : D <= 128 ? 2 : 1;
-  if (tile == BR_KV_TILE_16) br_kv_attend_few<D, 1, NW, WAVES>(p, fp8, cus, st);
-  else if (tile == BR_KV_TILE_32) br_kv_attend_few<D, 2, NW, WAVES>(p, fp8, cus, st);
-  else if (tile == BR_KV_TILE_64) br_kv_attend_few<D, 4, NW, WAVES>(p, fp8, cus, st);
-  else br_kv_attend_rows<D, 2, D <= 128 ? 2 : 1>(p, fp8, cus, st);
+  if (tile == BR_KV_TILE_16) br_kv_attend_few<D, 1, NW, WAVES, MODE>(p, fp8, cus, st);
+  else if (tile == BR_KV_TILE_32) br_kv_attend_few<D, 2, NW, WAVES, MODE>(p, fp8, cus, st);
+  else if (MODE == BR_KV_SHARED || tile == BR_KV_TILE_64) br_kv_attend_few<D, 4, NW, WAVES, MODE>(p, fp8, cus, st);
+  else if constexpr (MODE != BR_KV_SHARED) br_kv_attend_rows<D, 2, D <= 128 ? 2 : 1, MODE>(p, fp8, cus, st);
 }
 
 #endif

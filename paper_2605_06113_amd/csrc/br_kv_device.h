@@ -32,6 +32,15 @@ struct BrKvNext {
   int *least;     // [W] blocks from this id on have moved, if they are in use
 };
 
+// Which rows are read together (br_kv_plan).
+struct BrKvPlan {
+  const int *lead, *start, *count;
+  int *common;      // [W][B] tokens that the row holds in its leader's blocks
+  int4 *companies;  // [W][B] members, place of the first in the list, tiles that all of them hold, all tiles; behind the last: no members
+  int4 *members;    // [W][B] row of all workers', token, cached tokens
+  int most;         // members of a company
+};
+
 struct BrKvMoves {
   int *src, *dst;
   const int *src_worker;
@@ -78,6 +87,10 @@ struct BrKvAttend {
   int bf16, q_wide, out_wide;  // wide: rows of q (out) can be read (written) 16 (8) bytes at a time
   unsigned group_mul, group_shift;  // x / group = (high word of group_mul x + x) >> group_shift for 0 <= x < 2^31
   float scale2;                // scale * log2(e)
+  const float *lambda;         // of differential attention: of token t and query head h at t * lambda_token + h
+  long long lambda_token;
+  const int4 *companies;       // of rows that are read together, see br_kv_k_plan: n_rows of them
+  const int4 *members;
 };
 
 void br_kv_launch_clear(const BrKvTables &t, hipStream_t st);
@@ -85,6 +98,7 @@ void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, h
 void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st);
 void br_kv_launch_fork(const BrKvTables &t, const BrKvNext &x, const int *from, const int *len, hipStream_t st);
 void br_kv_launch_compact(const BrKvTables &t, const BrKvNext &x, const BrKvMoves &m, hipStream_t st);
+void br_kv_launch_plan(const BrKvTables &t, const BrKvPlan &x, hipStream_t st);
 void br_kv_launch_copy(const BrKvCache &c, const BrKvMoves &m, int W, hipStream_t st);
 void br_kv_launch_append(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st);
 void br_kv_launch_read(const BrKvCache &c, const BrKvTokens &t, int rows, bool fp8, hipStream_t st);
@@ -96,6 +110,17 @@ void br_kv_launch_attend_96(const BrKvAttend &p, int tile, bool fp8, int cus, hi
 void br_kv_launch_attend_128(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
 void br_kv_launch_attend_192(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
 void br_kv_launch_attend_256(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+// br_kv_diff_*.hip, br_kv_shared_*.hip: the same kernels for two maps a head, and for rows that are read together
+void br_kv_launch_diff_64(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_diff_96(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_diff_128(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_diff_192(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_diff_256(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_shared_64(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_shared_96(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_shared_128(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_shared_192(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
+void br_kv_launch_shared_256(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st);
 
 #ifdef __HIPCC__
 typedef _Float16 br_h2 __attribute__((ext_vector_type(2)));
@@ -159,6 +184,15 @@ __device__ __forceinline__ int br_kv_wave_scan(int x) {
   BR_KV_STEP(0x143, 0xc);  // rows 2 and 3: the last of row 1
 #undef BR_KV_STEP
   return x;
+}
+
+// Cached tokens of a row of all workers', as far as its table spans
+__device__ __forceinline__ int br_kv_len(const BrKvTables &t, int r) { return min(max(t.lens[r], 0), t.max_blocks << t.shift); }
+
+// The row that leads row r of worker w: itself, if none is said.
+__device__ __forceinline__ int br_kv_leader(const BrKvTables &t, const BrKvPlan &x, int w, int r) {
+  const int f = x.lead ? x.lead[(long long)w * t.B + r] : r;
+  return (unsigned)f < (unsigned)t.B ? f : r;
 }
 
 // Inclusive sums of K values each over the block's threads; total: all of them.  One barrier (part: 2 x K x NT / 64 words, used in turn).

@@ -13,8 +13,6 @@ __device__ __forceinline__ void br_kv_rows(const BrKvTables &t, int slices, Fn &
   }
 }
 
-__device__ __forceinline__ int br_kv_len(const BrKvTables &t, int r) { return min(max(t.lens[r], 0), t.max_blocks << t.shift); }
-
 // What each row is to hold, beside the tables: its entries, and one holder more of each block that the row does not hold in that place.
 __global__ __launch_bounds__(256) void br_kv_k_fork_take(BrKvTables t, BrKvNext x, const int *from, const int *len, int slices) {
   br_kv_rows(t, slices, [&](int r, int w, int first) {

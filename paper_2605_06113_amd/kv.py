@@ -41,7 +41,7 @@ ST = dict(tokens=0, used=1, free=2, rows=3, added=4, refused=5, no_blocks=6, tak
 STATUS = dict(taken=0, no_blocks=1, too_long=2, no_room=3)
 EXPORTS = ("br_kv_workspace_bytes", "br_kv_init", "br_kv_step", "br_kv_append", "br_kv_read", "br_kv_attend", "br_kv_free",
            "br_kv_last_hip_error", "br_kv_get_layout", "br_kv_shared_workspace_bytes", "br_kv_init_shared", "br_kv_get_shared_layout", "br_kv_fork", "br_kv_step_shared",
-           "br_kv_compact", "br_kv_copy")
+           "br_kv_compact", "br_kv_copy", "br_kv_plan", "br_kv_attend_shared", "br_kv_attend_diff")
 
 _P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
 
@@ -88,13 +88,21 @@ class _Forks(C.Structure):
     _fields_ = [("from_", _P), ("len", _P)]
 
 
+class _Families(C.Structure):
+    _fields_ = [(k, _P) for k in ("lead", "start", "count")] + [("members", _I), ("pad", _I)]
+
+
+class _Diff(C.Structure):
+    _fields_ = [("lam", _P), ("lambda_token", _L)]
+
+
 class _Moves(C.Structure):
     _fields_ = [(k, _P) for k in ("src", "dst", "src_worker")] + [("n", _I), ("pad", _I)]
 
 
 # The structs of the calls of a decode loop, packed in one go (a ctypes struct costs as much as the call): pointers, strides, numbers.
 _PACK_LENGTHS, _PACK_STEP, _PACK_TOKENS, _PACK_ATTENTION = (struct.Struct(f) for f in ("@2P", "@6P2i", "@3P4q2i", "@7P4q4ifi"))
-_PACK_FORKS, _PACK_MOVES = (struct.Struct(f) for f in ("@2P", "@3P2i"))
+_PACK_FORKS, _PACK_MOVES, _PACK_FAMILIES, _PACK_DIFF = (struct.Struct(f) for f in ("@2P", "@3P2i", "@3P2i", "@Pq"))
 _lib = None
 
 
@@ -111,10 +119,11 @@ def load():
         getattr(lib, name).argtypes = [C.POINTER(_Config)]
     for name in ("br_kv_init", "br_kv_init_shared"):
         getattr(lib, name).argtypes = [C.POINTER(_Config), C.POINTER(_State), C.POINTER(_P)]
-    for name in ("br_kv_step", "br_kv_append", "br_kv_read", "br_kv_attend", "br_kv_copy"):
+    for name in ("br_kv_step", "br_kv_append", "br_kv_read", "br_kv_attend", "br_kv_copy", "br_kv_attend_shared"):
         getattr(lib, name).argtypes = [_P, _P, _P]
-    lib.br_kv_step_shared.argtypes = [_P, _P, _P, _P]
-    for name in ("br_kv_fork", "br_kv_compact"):
+    for name in ("br_kv_step_shared", "br_kv_attend_diff"):
+        getattr(lib, name).argtypes = [_P, _P, _P, _P]
+    for name in ("br_kv_fork", "br_kv_compact", "br_kv_plan"):
         getattr(lib, name).argtypes = [_P, _P]
     lib.br_kv_get_shared_layout.argtypes = [_P, C.POINTER(_SharedLayout)]
     lib.br_kv_free.restype = None
@@ -219,7 +228,7 @@ class KvCache:
         self._i32, self._f32, self._i64 = torch.int32, torch.float32, torch.int64
         W, B = cfg.n_workers, cfg.rows
         self._rows, self._stats, self._tables = torch.Size((W, B)), torch.Size((W, NSTATS)), torch.Size((W, B, cfg.max_blocks))
-        self._scale = cfg.head_dim ** -0.5
+        self._scale, self._half_scale = cfg.head_dim ** -0.5, (cfg.head_dim / 2) ** -0.5
         self._layer = (torch.Size((W * cfg.n_blocks, cfg.n_kv_heads, cfg.block_tokens, cfg.head_dim)), self._index)
         self._args = C.create_string_buffer(256)
         self._at = C.addressof(self._args)
@@ -377,6 +386,12 @@ class KvCache:
 
         start, count [n_workers, rows] (step_device's): a row's query tokens; none: token r belongs to row r.  lse [tokens, n_q_heads] float32.
         scale: 1 / sqrt(head_dim) if not given.  lens, table: instead of the cache's own."""
+        self._pack_attention(layer, q, out, lse, (), start, count, max_count, scale, self._scale, window, lens, table)
+        rc = self.lib.br_kv_attend(self.ctx, layer.at, self._at)
+        if rc:
+            self._done(rc, "br_kv_attend")
+
+    def _pack_attention(self, layer, q, out, lse, lse_maps, start, count, max_count, scale, own_scale, window, lens, table) -> None:
         if layer.sizes != self._layer:
             raise BrError("the layer is one of another cache's sizes")
         heads = self.cfg.n_q_heads
@@ -387,20 +402,61 @@ class KvCache:
         out_dtype, out_token, out_head = self._tokens(out, "out", n, heads)
         if out_dtype != dtype:
             raise BrError("q and out must have one type")
-        if (start is None) != (count is None):
-            raise BrError("start and count come together")
         check, i32, rows = self._check, self._i32, self._rows
-        at = (q.data_ptr(), out.data_ptr(), 0 if lse is None else check(lse, "lse", (n, heads), self._f32),
-              0 if start is None else check(start.view(rows) if start.shape != rows and start.numel() == rows.numel() else start, "start", rows, i32),
-              0 if count is None else check(count.view(rows) if count.shape != rows and count.numel() == rows.numel() else count, "count", rows, i32),
+        at = (q.data_ptr(), out.data_ptr(), 0 if lse is None else check(lse, "lse", (n, heads, *lse_maps), self._f32), *self._check_lists(start, count),
               0 if lens is None else check(lens, "lens", rows, i32), 0 if table is None else check(table, "table", self._tables, i32), q_token, q_head, out_token, out_head, n)
         try:
-            _PACK_ATTENTION.pack_into(self._args, 0, *at, max_count, window, dtype, self._scale if scale is None else scale, 0)
+            _PACK_ATTENTION.pack_into(self._args, 0, *at, max_count, window, dtype, own_scale if scale is None else scale, 0)
         except (struct.error, OverflowError):
             raise BrError("max_count and window must be whole numbers of 32 bits, scale a number of 32 bits") from None
-        rc = self.lib.br_kv_attend(self.ctx, layer.at, self._at)
+
+    def _check_lists(self, start, count):
+        """Addresses of a step's start and count, in any shape of as many numbers; 0 without them."""
+        if (start is None) != (count is None):
+            raise BrError("start and count come together")
+        if start is None:
+            return 0, 0
+        check, i32, rows = self._check, self._i32, self._rows
+        return (check(start.view(rows) if start.shape != rows and start.numel() == rows.numel() else start, "start", rows, i32),
+                check(count.view(rows) if count.shape != rows and count.numel() == rows.numel() else count, "count", rows, i32))
+
+    def plan_device(self, lead, members: int, start=None, count=None) -> None:
+        """Which rows attend_shared_device reads together (br_kv_plan), for all layers of a step: behind step_device.
+
+        lead [n_workers, rows] int32: the row that row r shares its first blocks with (its family's first, itself, or -1); at most `members` rows together.
+        start, count: step_device's; rows whose count is not 1 are left out; none: token r belongs to row r."""
+        self._is_shared()
+        at = (self._check(lead, "lead", self._rows, self._i32), *self._check_lists(start, count))
+        try:
+            _PACK_FAMILIES.pack_into(self._args, 0, *at, members, 0)
+        except struct.error:
+            raise BrError("members must be a whole number of 32 bits") from None
+        rc = self.lib.br_kv_plan(self.ctx, self._at)
         if rc:
-            self._done(rc, "br_kv_attend")
+            self._done(rc, "br_kv_plan")
+
+    def attend_shared_device(self, layer: KvLayer, q, out, lse=None, scale: Optional[float] = None, window: int = 0) -> None:
+        """attend_device of the planned rows' tokens (br_kv_attend_shared): what rows hold together is read once for all of them."""
+        self._is_shared()
+        self._pack_attention(layer, q, out, lse, (), None, None, 1, scale, self._scale, window, None, None)
+        rc = self.lib.br_kv_attend_shared(self.ctx, layer.at, self._at)
+        if rc:
+            self._done(rc, "br_kv_attend_shared")
+
+    def attend_diff_device(self, layer: KvLayer, q, out, lam, lse=None, start=None, count=None, max_count: int = 1, scale: Optional[float] = None, window: int = 0,
+                           lens=None, table=None) -> None:
+        """Differential attention (br_kv_attend_diff): the first halves of the channels' map less lam times the second halves'.
+
+        lam: float32 [n_q_heads], or [tokens, n_q_heads] with contiguous heads.  lse [tokens, n_q_heads, 2].  scale: 1 / sqrt(head_dim / 2) if not given.
+        The rest as attend_device's."""
+        n, heads = q.shape[0], self.cfg.n_q_heads
+        self._pack_attention(layer, q, out, lse, (2,), start, count, max_count, scale, self._half_scale, window, lens, table)
+        if lam.dtype is not self._f32 or lam.get_device() != self._index or lam.shape not in ((heads,), (n, heads)) or (lam.stride(-1) != 1 and heads > 1):
+            raise BrError(f"lam must be a torch.float32 tensor of shape {(heads,)} or {(n, heads)} on {self.device}, its heads contiguous")
+        _PACK_DIFF.pack_into(self._args, 160, lam.data_ptr(), lam.stride(0) if lam.dim() == 2 else 0)
+        rc = self.lib.br_kv_attend_diff(self.ctx, layer.at, self._at, self._at + 160)
+        if rc:
+            self._done(rc, "br_kv_attend_diff")
 
     def close(self) -> None:
         if getattr(self, "ctx", None):

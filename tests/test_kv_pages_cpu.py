@@ -11,6 +11,7 @@ GOOD = dict(rows=96, n_blocks=512, max_blocks=64, n_kv_heads=8, n_q_heads=32, he
 
 
 def test_structs():
+    assert C.sizeof(kv._Families) == kv._PACK_FAMILIES.size == 32 and C.sizeof(kv._Diff) == kv._PACK_DIFF.size == 16
     assert C.sizeof(kv._Forks) == kv._PACK_FORKS.size == 16 and C.sizeof(kv._Moves) == kv._PACK_MOVES.size == 32 and C.sizeof(kv._SharedLayout) == 16
     m = kv._Moves.from_buffer_copy(kv._PACK_MOVES.pack(1, 2, 3, 4, 5))
     assert [getattr(m, f) for f, _ in kv._Moves._fields_] == [1, 2, 3, 4, 5]
@@ -18,9 +19,9 @@ def test_structs():
 
 def test_workspaces():
     one, more = kv.workspace_bytes(kv.KvConfig(**GOOD)), kv.workspace_bytes(kv.KvConfig(**GOOD, shared=True))
-    # a second table, lengths twice, two numbers for each block, one for each worker
-    need = 4 * (96 * 64 + 2 * 96 + 2 * 512 + 1)
-    assert one + need <= more <= one + need + 5 * 256
+    # a second table, lengths twice, two numbers for each block, one for each worker, nine for each row's part in a plan
+    need = 4 * (96 * 64 + 2 * 96 + 2 * 512 + 1 + 9 * 96)
+    assert one + need <= more <= one + need + 8 * 256
     for bad in (dict(rows=0), dict(head_dim=32), dict(n_blocks=262145), dict(block_tokens=8)):
         assert kv.workspace_bytes(kv.KvConfig(**{**GOOD, **bad}, shared=True)) == 0
 
@@ -35,8 +36,9 @@ def test_init_refusals():
     assert lib.br_kv_init_shared(C.byref(c), None, None) == binding.BR_EINVAL
     half = kv._State(lens=256, table=0)
     assert lib.br_kv_init_shared(C.byref(c), C.byref(half), C.byref(ctx)) == binding.BR_EINVAL
-    for call in (lib.br_kv_fork, lib.br_kv_compact):
+    for call in (lib.br_kv_fork, lib.br_kv_compact, lib.br_kv_plan):
         assert call(None, None) == binding.BR_EINVAL
+    assert lib.br_kv_attend_shared(None, None, None) == binding.BR_EINVAL
     assert lib.br_kv_copy(None, None, None) == binding.BR_EINVAL and lib.br_kv_step_shared(None, None, None, None) == binding.BR_EINVAL
     assert lib.br_kv_get_shared_layout(None, None) == binding.BR_EINVAL
 
@@ -58,7 +60,7 @@ def test_binding_refuses_what_does_not_fit():
     out = c.alloc_step(7)
     assert set(out) - set(plain.alloc_step(7)) == {"copy_src", "copy_dst"} and out["copy_src"].shape == (1, 96)
     layer = c.layer(u8(512, 8, 16, 128), u8(512, 8, 128, 16), torch.zeros(512, 8), torch.zeros(512, 8))
-    moves = c.alloc_moves(5)
+    moves, q = c.alloc_moves(5), torch.zeros((5, 32, 128), dtype=torch.float16)
     refused = [
         lambda: plain.fork_device(i32(1, 96)), lambda: plain.compact_device(moves),  # one holder each
         lambda: c.fork_device(i32(96)), lambda: c.fork_device(i32(1, 95)), lambda: c.fork_device(i32(1, 96).long()), lambda: c.fork_device(i32(1, 96), i32(1, 97)),
@@ -68,6 +70,12 @@ def test_binding_refuses_what_does_not_fit():
         lambda: c.copy_device(layer, i32(5), i32(5)), lambda: c.copy_device(layer, i32(1, 5), i32(1, 6)), lambda: c.copy_device(layer, i32(1, 5).long(), i32(1, 5)),
         lambda: c.copy_device(layer, i32(1, 5), i32(1, 5), src_worker=i32(1, 4)), lambda: c.copy_device(layer, i32(2, 5), i32(2, 5)),
         lambda: two.copy_device(layer, i32(2, 5), i32(2, 5)),  # another cache's layer
+        lambda: plain.plan_device(i32(1, 96), 4), lambda: plain.attend_shared_device(layer, q, q),
+        lambda: c.plan_device(i32(1, 95), 4), lambda: c.plan_device(i32(1, 96).long(), 4), lambda: c.plan_device(i32(1, 96), 4, start=i32(1, 96)),
+        lambda: c.plan_device(i32(1, 96), 4, count=i32(1, 96)), lambda: c.plan_device(i32(1, 96), 4, start=i32(1, 96), count=i32(95)), lambda: c.plan_device(i32(1, 96), 1.5),
+        lambda: c.plan_device(i32(1, 96), 2 ** 31),
+        lambda: c.attend_shared_device(layer, q[:, :31], q), lambda: c.attend_shared_device(layer, q, q.bfloat16()), lambda: c.attend_shared_device(layer, q, q, lse=torch.zeros(5, 31)),
+        lambda: c.attend_shared_device(layer, q, q, window=2 ** 31), lambda: c.attend_shared_device(layer, q.float(), q.float()),
     ]
     for call in refused:
         with pytest.raises(kv.BrError):
