@@ -61,7 +61,7 @@ Places make_layout(const br_kv_config &c, bool shared) {
     l.moved = take(blocks);
     l.least = take((uint64_t)c.n_workers);
     l.common = take(rows);
-    l.companies = take(4 * rows);
+    l.companies = take(8 * rows);
     l.members = take(4 * rows);
   }
   l.total = off;
@@ -351,6 +351,7 @@ int32_t br_kv_plan(br_kv_ctx *ctx, const br_kv_families *in) {
   x.common = (int *)(base + ctx->at.common);
   x.companies = (int4 *)(base + ctx->at.companies);
   x.members = (int4 *)(base + ctx->at.members);
+  x.group = group;
   x.most = fit < 1 ? 1 : fit < members ? fit : members;
   const int32_t rc = enqueue(ctx, [&] { br_kv_launch_plan(ctx->t, x, ctx->st); });
   if (rc == BR_OK) ctx->plan_tile = tile;

@@ -32,7 +32,10 @@
 //           with the other (the rest is 0); what is written is the first's result less lambda times the second's
 //   SHARED  the rows that br_kv_plan took together, as one: each has one query token, and the tokens are those that all of them hold, then each one's
 //           others, which only its own query sees.  A row here is such a company, its first token a place in the list of members.
-enum { BR_KV_PLAIN = 0, BR_KV_DIFF = 1, BR_KV_SHARED = 2 };
+//   SHARED_16, SHARED_32  the same by waves of 16 or 32 query rows, each with its own members' tokens only behind those that all hold: a tile is a
+//           step of all waves, and a company has as many as the wave with most
+enum { BR_KV_PLAIN = 0, BR_KV_DIFF = 1, BR_KV_SHARED = 2, BR_KV_SHARED_16 = 3, BR_KV_SHARED_32 = 4 };
+constexpr bool br_kv_shared(int mode) { return mode >= BR_KV_SHARED; }
 
 struct BrKvRow {
   int n, len, start;  // query tokens, cached tokens, first token; SHARED: members, tiles that they hold together, place of the first
@@ -48,17 +51,20 @@ __device__ __forceinline__ int br_kv_first_tile(const BrKvAttend &p, int len) { 
 template <int MODE>
 __device__ __forceinline__ BrKvRow br_kv_row(const BrKvAttend &p, int r) {
   BrKvRow w;
-  if (MODE == BR_KV_SHARED) {
-    const int4 c = p.companies[r];
-    w.n = c.x, w.start = c.y, w.len = c.z, w.tiles = c.w;
+  if (br_kv_shared(MODE)) {
+    const int4 c = p.companies[2 * r], sizes = p.companies[2 * r + 1];
+    w.n = c.x, w.start = c.y, w.len = c.z, w.tiles = MODE == BR_KV_SHARED ? c.w : MODE == BR_KV_SHARED_16 ? sizes.x : sizes.y;
     if (p.window > 0) {
-      int lo = w.len;
-      w.tiles = 0;
+      constexpr int PART = MODE == BR_KV_SHARED_16 ? 16 : 32;
+      int lo = w.len, own[4] = {0, 0, 0, 0};  // (several members have 64 query rows at most; one has the same tiles for all of its rows)
       for (int i = 0; i < w.n; ++i) {
-        const int len = p.members[w.start + i].z, first = br_kv_first_tile(p, len);
-        lo = min(lo, first), w.tiles += max(0, br_kv_tiles_of(len) - max(w.len, first));
+        const int len = p.members[w.start + i].z, first = br_kv_first_tile(p, len), tiles = max(0, br_kv_tiles_of(len) - max(w.len, first));
+        lo = min(lo, first);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (MODE == BR_KV_SHARED ? k == 0 : k >= i * p.group / PART && k <= (i * p.group + p.group - 1) / PART) own[k] += tiles;
       }
-      w.tiles += w.len - lo;
+      w.tiles = max(max(own[0], own[1]), max(own[2], own[3])) + w.len - lo;
     }
     return w;
   }
@@ -77,7 +83,7 @@ __device__ __forceinline__ int br_kv_token(const BrKvAttend &p, int row) { retur
 // zeros to write.
 template <int TQ, int MODE>
 __device__ __forceinline__ int br_kv_span(const BrKvAttend &p, const BrKvRow &w, int qi, int &t0, int &t1) {
-  if (MODE == BR_KV_SHARED) {
+  if (br_kv_shared(MODE)) {
     t0 = 0, t1 = w.tiles;
     return max(1, t1);
   }
@@ -93,7 +99,7 @@ template <int TQ, int MODE>
 __device__ __forceinline__ int br_kv_row_tiles(const BrKvAttend &p, const BrKvRow &w, long long &tiles, int &most, int first = 0, int step = 1) {
   const int nq = (int)(((long long)w.n * p.group + TQ - 1) / TQ);
   tiles = 0, most = 0;
-  if (MODE == BR_KV_SHARED) {  // (the same for all of a company's query tiles)
+  if (br_kv_shared(MODE)) {  // (the same for all of a company's query tiles)
     if (nq > 0) most = max(1, w.tiles), tiles = (long long)nq * most;
     return nq;
   }
@@ -116,7 +122,7 @@ __device__ __forceinline__ uint4 br_kv_load16(const unsigned char *at) {
 // The token of a row's i-th query.
 template <int MODE>
 __device__ __forceinline__ int br_kv_place(const BrKvAttend &p, const BrKvRow &w, int i) {
-  return MODE == BR_KV_SHARED ? p.members[w.start + min(i, max(w.n - 1, 0))].y : w.start + i;
+  return br_kv_shared(MODE) ? p.members[w.start + min(i, max(w.n - 1, 0))].y : w.start + i;
 }
 
 // x times inv, and of DIFF less lambda times y times inv_y: zero where nothing was seen, whatever lambda is.
@@ -276,7 +282,7 @@ struct BrKvQueries {
       const int ri = row0 + br_kv_query<MODE, NQ>(x, n), i = br_kv_token(p, ri), t = br_kv_place<MODE>(p, w, i);
       const bool in = i < w.n && t >= 0 && t < p.n_tokens;
       const int head = h * p.group + ri - i * p.group;
-      if (MODE == BR_KV_SHARED) pos[x] = in ? p.members[w.start + i].z - 1 : -1, member[x] = i;
+      if (br_kv_shared(MODE)) pos[x] = in ? p.members[w.start + i].z - 1 : -1, member[x] = i;
       else pos[x] = in ? max(w.len - w.n + i, -1) : -1;
       const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(MODE == BR_KV_DIFF ? head >> 1 : head) * p.q_head : 0);
       uint4 e[NK];
@@ -347,7 +353,7 @@ __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQue
 #pragma unroll
     for (int j = 0; j < 16; ++j) z[j] = s[x][j >> 2][j & 3];
     if (!inside) {  // of the lane's tokens, those from `lo` on, `seen` of them
-      const int pos = MODE == BR_KV_SHARED && owner >= 0 && owner != q.member[x] ? -1 : q.pos[x];
+      const int pos = br_kv_shared(MODE) && owner >= 0 && owner != q.member[x] ? -1 : q.pos[x];
       const int lo = p.window > 0 ? max(pos - p.window + 1 - token, 0) : 0, seen = max(min(have, pos + 1 - token) - lo, 0);
 #pragma unroll
       for (int j = 0; j < 16; ++j) z[j] = (unsigned)(j - lo) < (unsigned)seen ? z[j] * f : BR_KV_NEG;
@@ -394,11 +400,59 @@ __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQue
   }
 }
 
+// A token tile: the row of the tables, its place among that row's tiles, how many tokens the row has (as far as it goes for this tile), whose it is.
+struct BrKvTile {
+  int row, tile, len, owner;
+  // block of the tile's token `in`, as the table has it
+  __device__ __forceinline__ int id_of(const BrKvAttend &p, int in) const {
+    return p.table[(long long)row * p.max_blocks + min((tile * BR_KV_TILE + in) >> p.shift, max(0, (len - 1) >> p.shift))];
+  }
+};
+
+// Where the tiles of a row, or a company, are.  Of a company: first what all hold together, then each member's own, those of the first member first; lane i
+// has member i (there are no more than 64), and who has tile t is counted.  By waves: the own ones of members `from` to `to`.
+template <int MODE>
+struct BrKvMap {
+  int r, begins, first_tile, together, tiles;
+  int4 member;
+  __device__ __forceinline__ BrKvMap(const BrKvAttend &p, const BrKvRow &w, int r, int from, int to)
+      : r(r), begins(0), first_tile(0), together(0), tiles(0), member(make_int4(0, 0, 0, 0)) {
+    if (br_kv_shared(MODE)) {
+      const int lane = threadIdx.x & 63;
+      const bool mine = lane < w.n && (MODE == BR_KV_SHARED || (lane >= from && lane <= to));
+      if (lane < w.n) member = p.members[w.start + lane];
+      const int lo = lane < w.n ? br_kv_first_tile(p, member.z) : w.len, own = mine ? max(0, br_kv_tiles_of(member.z) - max(w.len, lo)) : 0;
+      first_tile = __builtin_amdgcn_readfirstlane(-(int)br_kv_max64((float)-min(lo, w.len)));  // (below 2^24: exact)
+      together = w.len - first_tile;
+      const int sum = together + br_kv_wave_scan(own);
+      begins = sum - own;
+      tiles = __builtin_amdgcn_readlane(sum, 63);
+    }
+  }
+  // Of a company what all see is what they hold together, if no window ends there; of one row its tokens
+  __device__ __forceinline__ void sight(const BrKvAttend &p, const BrKvRow &w, int &first_pos, int &last_pos) const {
+    if (!br_kv_shared(MODE)) return;
+    first_pos = last_pos = w.n > 1 ? w.len * BR_KV_TILE - 1 : __builtin_amdgcn_readlane(member.z, 0) - 1;
+    if (w.n > 1 && p.window > 0) last_pos = INT32_MAX;
+  }
+  __device__ __forceinline__ BrKvTile at(const BrKvAttend &p, const BrKvRow &w, int t) const {
+    BrKvTile x = {r, t, w.len, -1};
+    if (br_kv_shared(MODE)) {
+      const int i = t < together ? 0 : max(__popcll(__ballot((int)(threadIdx.x & 63) < w.n && begins <= t)) - 1, 0);
+      x.row = __builtin_amdgcn_readlane(member.x, i), x.len = __builtin_amdgcn_readlane(member.z, i);
+      if (t < together) x.tile = first_tile + t, x.len = w.len * BR_KV_TILE;
+      else x.tile = max(w.len, br_kv_first_tile(p, x.len)) + t - __builtin_amdgcn_readlane(begins, i), x.owner = w.n > 1 ? i : -1;
+    }
+    return x;
+  }
+};
+
 // ONCE: nobody else reads these codes; ONCE_V: nor these values' lines (blocks of 128 tokens have two tiles' in one).
 // Token tiles t .. stop - 1 of row r and key head h for the query rows from row0 on, whose positions lie in first_pos .. last_pos.
-template <int D, int NQ, bool FP8, bool ONCE_V, bool ONCE, int MODE>
+// PHASES > 0: every PHASES-th of them, from the phase-th on.
+template <int D, int NQ, bool FP8, bool ONCE_V, bool ONCE, int MODE, int PHASES = 0>
 __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int r, int h, int row0, int first_pos, int last_pos, int t, int stop,
-                                            BrKvSums<D, NQ> &sums) {
+                                            BrKvSums<D, NQ> &sums, int phase = 0, br_h8 *q_lds = nullptr) {
   constexpr int NI = D / 64, REST = D % 64 / 32, NK = 2 * NI + REST, ND = D / 16;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   // (what is the same for the wave, in scalar registers)
@@ -409,34 +463,12 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   auto &o = sums.o;
   sums.clear();
 
-  // Where tile t is: the row of the tables, the tile of its tokens, how many it has, whose it is.
-  struct Tile {
-    int row, tile, len, owner;
-  };
-  int4 member = make_int4(0, 0, 0, 0);  // SHARED: lane i's
-  int begins = 0, first_tile = 0, together = 0;
-  if (MODE == BR_KV_SHARED) {
-    // (a company has no more members than a wave has lanes)
-    member = lane < w.n ? p.members[w.start + lane] : make_int4(0, 0, 0, 0);
-    const int lo = lane < w.n ? br_kv_first_tile(p, member.z) : w.len, own = lane < w.n ? max(0, br_kv_tiles_of(member.z) - max(w.len, lo)) : 0;
-    first_tile = scalar(-(int)br_kv_max64((float)-min(lo, w.len)));  // (below 2^24: exact)
-    together = w.len - first_tile;
-    begins = together + br_kv_wave_scan(own) - own;
-    // what all of them see: one member's own tokens, of several what they hold together, if no window ends there
-    first_pos = last_pos = w.n > 1 ? w.len * BR_KV_TILE - 1 : __builtin_amdgcn_readlane(member.z, 0) - 1;
-    if (w.n > 1 && p.window > 0) last_pos = INT32_MAX;
-  }
-  auto tile_at = [&](int t) {
-    Tile x = {r, t, w.len, -1};
-    if (MODE == BR_KV_SHARED) {
-      const int i = t < together ? 0 : max(__popcll(__ballot(lane < w.n && begins <= t)) - 1, 0);
-      x.row = __builtin_amdgcn_readlane(member.x, i), x.len = __builtin_amdgcn_readlane(member.z, i);
-      if (t < together) x.tile = first_tile + t, x.len = w.len * BR_KV_TILE;
-      else x.tile = max(w.len, br_kv_first_tile(p, x.len)) + t - __builtin_amdgcn_readlane(begins, i), x.owner = w.n > 1 ? i : -1;
-    }
-    return x;
-  };
-  const int worker = (MODE == BR_KV_SHARED ? tile_at(0).row : r) / p.rows;
+  const BrKvMap<MODE> map(p, w, r, scalar(br_kv_token(p, row0)), scalar(br_kv_token(p, row0 + 16 * NQ - 1)));
+  map.sight(p, w, first_pos, last_pos);
+  constexpr int STEP = PHASES > 0 ? PHASES : 1;
+  if (PHASES > 0) t += scalar(phase), stop = min(stop, map.tiles);
+  auto tile_at = [&](int t) { return map.at(p, w, t); };
+  const int worker = tile_at(0).row / p.rows;
   const long long cache0 = (long long)worker * p.n_blocks;
   const int mask = (1 << p.shift) - 1;
   const int kg = n >> 2, kr = n & 3;  // the token group, and the place in fours, of the lane's row of K
@@ -445,9 +477,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   uint2 kx[4];
   uint4 vc[ND];
   // block of a lane's 16 tokens, as the table has it; where it is read, one that does not exist is block 0
-  auto id_of = [&](const Tile &x, int in) {
-    return p.table[(long long)x.row * p.max_blocks + min((x.tile * BR_KV_TILE + in) >> p.shift, max(0, (x.len - 1) >> p.shift))];
-  };
+  auto id_of = [&](const BrKvTile &x, int in) { return x.id_of(p, in); };
   auto there = [&](int id) { return (unsigned)id < (unsigned)p.n_blocks; };
   auto load_k = [&](int t, int id, bool live) {
     const unsigned char *at =
@@ -470,9 +500,9 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   };
   const bool t_any = t < stop;
   int kid = 0;
-  Tile now = tile_at(t), next = now;
+  BrKvTile now = tile_at(t), next = now;
   if (t_any) {
-    next = tile_at(t + 1 < stop ? t + 1 : t);
+    next = tile_at(t + STEP < stop ? t + STEP : t);
     kid = id_of(now, 16 * kg), vid = id_of(now, 16 * g);
     kid1 = id_of(next, 16 * kg), vid1 = id_of(next, 16 * g);
   }
@@ -484,8 +514,16 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   q.load(p, w, h, row0, [&] {
     if (t_any) load_first();  // (while the queries are on their way)
   });
+  if (PHASES > 0) {  // the queries' channels wait in LDS: 32 registers that the codes need
+    if (phase == 0)
+#pragma unroll
+      for (int x = 0; x < NQ; ++x)
+#pragma unroll
+        for (int c = 0; c < NK; ++c) q_lds[(x * NK + c) * 64 + lane] = q.qf[x][c];
+    __syncthreads();
+  }
 
-  for (; t < stop; ++t) {
+  for (; t < stop; t += STEP) {
     const int token = now.tile * BR_KV_TILE + 16 * g;  // of the lane's first weight
     {
       const unsigned char *at = p.v + ((((cache0 + (there(vid) ? vid : 0)) * p.kv_heads + h) * D + n) << p.shift) + (token & mask);
@@ -500,9 +538,13 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     for (int x = 0; x < NQ; ++x)
 #pragma unroll
       for (int y = 0; y < 4; ++y) s[x][y] = br_f4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (PHASES > 0) __asm__ volatile("" ::: "memory");  // (or they are read once)
     // (products into one sum do not follow each other directly)
 #pragma unroll
     for (int c = 0; c < NK; ++c) {
+      if (PHASES > 0)
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) q.qf[x][c] = q_lds[(x * NK + c) * 64 + lane];
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
         br_h8 kf;
@@ -512,8 +554,8 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
         for (int x = 0; x < NQ; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q.qf[x][c], s[x][y], 0, 0, 0);
       }
     }
-    const Tile after = tile_at(min(t + 2, stop - 1));
-    load_k(next.tile, kid1, t + 1 < stop);
+    const BrKvTile after = tile_at(min(t + 2 * STEP, stop - 1));
+    load_k(next.tile, kid1, t + STEP < stop);
     load_scales(vid1);
     kid1 = id_of(after, 16 * kg);
     const int vid2 = id_of(after, 16 * g);
@@ -1201,6 +1243,99 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
   }
 }
 
+// Companies of more than 16 query rows: a run for each block, whose waves have 16 NQ of its TQ rows each and every P-th of the tiles that those see; nothing passes
+// between them before the run's end, where the P sums of a row are joined in LDS.  A tile is decoded TQ / (16 NQ) times.  The queries are in LDS: in
+// registers they drove others out to memory, and every reload of those waited for the codes on their way (96 rows of 8 to a company, groups of 8, up to 16384
+// tokens together, 8 key heads of 128 channels, fp8: 72 us, 66 with them in LDS; a tile through LDS for all four waves of a block, as for many rows above: 84, and 98 by
+// the kernel of few rows).  Such a call, 184 MB, out of memory 75 us: two waves on a SIMD, each waits for its values' codes about as long as it computes.
+template <int D, int TQ, int NQ, bool FP8, int NW, int WAVES>
+__global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend_together(BrKvAttend p) {
+  constexpr int MODE = NQ == 2 ? BR_KV_SHARED_32 : BR_KV_SHARED_16, NT = 64 * NW, ND = D / 16, NH = TQ / (16 * NQ), P = NW / NH;
+  using Runs = BrKvRuns<TQ, NT, 1, 16, MODE>;
+  __shared__ typename Runs::Shared shared;
+  __shared__ br_f4 kept[NW * NQ * ND * 64];
+  __shared__ float2 kept_ml[NW * NQ * 16];
+  __shared__ br_h8 q_lds[NH * NQ * (D / 32) * 64];
+  __shared__ int arrived;
+  const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int phase = wv / NH, row = 16 * NQ * (wv % NH);
+  Runs runs(p, shared, gridDim.x, BR_KV_LEAST_TILES);
+  const int blocks = runs.workers, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
+  if (wg >= blocks) return;
+  long long u = runs.begin_of(wg);
+  const long long end = runs.begin_of(wg + 1);
+  BrKvPlace<TQ, NT, Runs, MODE> at;
+  if (u >= end || !at.find(p, runs, u)) return;
+  for (;;) {
+    const int a = (int)(u - at.seg), b = (int)min((long long)at.size, end - at.seg), rows_q = at.rows_q(p);
+    const bool whole = a == 0 && b == at.size;
+    {
+      BrKvSums<D, NQ> s;
+      br_kv_tiles<D, NQ, FP8, false, false, MODE, P>(p, at.w, at.r, at.h, at.qi * TQ + row, 0, 0, at.tile_of(runs, a), row < rows_q ? at.tile_of(runs, b) : 0, s, phase, q_lds + wv % NH * (NQ * (D / 32) * 64));
+#pragma unroll
+      for (int x = 0; x < NQ; ++x) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          br_f4 y = s.o[x][d];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] *= s.c[x];
+          kept[((wv * NQ + x) * ND + d) * 64 + lane] = y;
+        }
+        if (g == 0) kept_ml[(wv * NQ + x) * 16 + n] = make_float2(s.m[x], s.l[x]);
+      }
+    }
+    __syncthreads();
+    const int from = whole ? 0 : runs.owner_of(at.seg), parts = whole ? 1 : runs.owner_of(at.seg + at.size - 1) - from + 1;
+    const BrKvPieces<D, TQ> pieces(p, rows_q);
+#pragma unroll 4
+    for (int it = wv; it < NH * NQ * ND; it += NW) {
+      const int d = it % ND, x = it / ND, rq = 16 * x + n;  // group x of 16 rows: wave x / NQ of each phase, its group x % NQ
+      float2 mls[P];
+      br_f4 vs[P];
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const int piece = (i * NH + x / NQ) * NQ + x % NQ;
+        mls[i] = kept_ml[piece * 16 + n], vs[i] = kept[(piece * ND + d) * 64 + lane];
+      }
+      float top = BR_KV_NEG, l = 0.0f;
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+        if (mls[i].y != 0.0f) top = fmaxf(top, mls[i].x);
+      br_f4 y[1] = {{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const float e = mls[i].y != 0.0f ? __builtin_amdgcn_exp2f(mls[i].x - top) : 0.0f;
+        l += mls[i].y * e;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[0][j] = __builtin_fmaf(vs[i][j], e, y[0][j]);
+      }
+      if (rq >= rows_q) continue;
+      if (top == BR_KV_NEG) top = 0.0f;
+      if (whole) {
+        br_kv_store<1, MODE>(p, at.w, at.h, at.qi * TQ + rq, 16 * d + 4 * g, y, l != 0.0f ? 1.0f / l : 0.0f);
+        if (d == 0 && g == 0) br_kv_store_lse<MODE>(p, at.w, at.h, at.qi * TQ + rq, top, l);
+      } else {
+        const int piece = 2 * wg + (a == 0);
+        pieces.put(piece, pieces.item(x, d, g, n), y[0]);
+        if (d == 0 && g == 0) br_kv_put2(p.ml + (piece * TQ + rq) * 2, top, l);
+      }
+    }
+    if (!whole) {
+      br_kv_stores_done();
+      __syncthreads();
+      if (tid == 0) arrived = __hip_atomic_fetch_add(&p.arrived[from], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __syncthreads();
+      if (arrived == parts - 1) {
+        br_kv_join<D, TQ, NT, MODE>(p, at.w, at.h, at.qi, rows_q, from, parts, kept, (float2 *)(kept + NT));
+        if (tid == 0) p.arrived[from] = 0;  // (for the next launch)
+      }
+    }
+    __syncthreads();
+    u = at.seg + b;
+    if (u >= end || !at.next(p, runs)) break;
+  }
+}
+
 // WAVES on a SIMD, by the registers that the tile needs; PER blocks of NW waves on a compute unit
 template <int D, int SHARE, int NW, int WAVES, int MODE>
 void br_kv_attend_few(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
@@ -1225,13 +1360,24 @@ void br_kv_attend_rows(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
   else br_kv_k_attend_rows<D, NQ, false, WAVES, MODE><<<blocks, 256, 0, st>>>(p);
 }
 
+template <int D, int TQ>
+void br_kv_attend_together(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
+  constexpr int NQ = D <= 128 ? 2 : 1, NW = D <= 128 ? 8 : 4, WAVES = D <= 128 ? 2 : 1;
+  const int blocks = cus < BR_KV_SPLIT_WGS_OF(D) ? cus : BR_KV_SPLIT_WGS_OF(D);
+  if (fp8) br_kv_k_attend_together<D, TQ, NQ, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+  else br_kv_k_attend_together<D, TQ, NQ, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
+}
+
 template <int D, int MODE = BR_KV_PLAIN>
 void br_kv_attend_dim(const BrKvAttend &p, int tile, bool fp8, int cus, hipStream_t st) {
   constexpr int NW = D <= 64 ? 12 : D <= 128 ? 8 : 4, WAVES = D <= 64 ? 3 : D <= 128 ? 2 : 1;
   if (tile == BR_KV_TILE_16) br_kv_attend_few<D, 1, NW, WAVES, MODE>(p, fp8, cus, st);
-  else if (tile == BR_KV_TILE_32) br_kv_attend_few<D, 2, NW, WAVES, MODE>(p, fp8, cus, st);
-  else if (MODE == BR_KV_SHARED || tile == BR_KV_TILE_64) br_kv_attend_few<D, 4, NW, WAVES, MODE>(p, fp8, cus, st);
-  else if constexpr (MODE != BR_KV_SHARED) br_kv_attend_rows<D, 2, D <= 128 ? 2 : 1, MODE>(p, fp8, cus, st);
+  else if constexpr (MODE == BR_KV_SHARED) {
+    if (tile == BR_KV_TILE_32) br_kv_attend_together<D, 32>(p, fp8, cus, st);
+    else br_kv_attend_together<D, 64>(p, fp8, cus, st);
+  } else if (tile == BR_KV_TILE_32) br_kv_attend_few<D, 2, NW, WAVES, MODE>(p, fp8, cus, st);
+  else if (tile == BR_KV_TILE_64) br_kv_attend_few<D, 4, NW, WAVES, MODE>(p, fp8, cus, st);
+  else br_kv_attend_rows<D, 2, D <= 128 ? 2 : 1, MODE>(p, fp8, cus, st);
 }
 
 #endif

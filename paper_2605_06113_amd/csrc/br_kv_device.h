@@ -36,9 +36,10 @@ struct BrKvNext {
 struct BrKvPlan {
   const int *lead, *start, *count;
   int *common;      // [W][B] tokens that the row holds in its leader's blocks
-  int4 *companies;  // [W][B] members, place of the first in the list, tiles that all of them hold, all tiles; behind the last: no members
+  int4 *companies;  // [W][B][2] members (behind the last company: none), place of the first in the list, tiles that all of them hold, those and each
+                    // one's own; tiles for waves of 16 query rows, each with its own members' only: the most of any, for waves of 32
   int4 *members;    // [W][B] row of all workers', token, cached tokens
-  int most;         // members of a company
+  int most, group;  // members of a company, query rows of each
 };
 
 struct BrKvMoves {

@@ -19,8 +19,8 @@ def test_structs():
 
 def test_workspaces():
     one, more = kv.workspace_bytes(kv.KvConfig(**GOOD)), kv.workspace_bytes(kv.KvConfig(**GOOD, shared=True))
-    # a second table, lengths twice, two numbers for each block, one for each worker, nine for each row's part in a plan
-    need = 4 * (96 * 64 + 2 * 96 + 2 * 512 + 1 + 9 * 96)
+    # a second table, lengths twice, two numbers for each block, one for each worker, thirteen for each row's part in a plan
+    need = 4 * (96 * 64 + 2 * 96 + 2 * 512 + 1 + 13 * 96)
     assert one + need <= more <= one + need + 8 * 256
     for bad in (dict(rows=0), dict(head_dim=32), dict(n_blocks=262145), dict(block_tokens=8)):
         assert kv.workspace_bytes(kv.KvConfig(**{**GOOD, **bad}, shared=True)) == 0
