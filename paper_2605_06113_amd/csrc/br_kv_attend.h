@@ -1054,6 +1054,14 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   }
 }
 
+// Whether any of the channels of step c of a score is in the half that group x of a wave's queries reads (the others' are 0).
+template <int D, int MODE>
+constexpr bool br_kv_has(int x, int c) {
+  if (MODE != BR_KV_DIFF) return true;
+  const int whole = D / 64 * 2, lo = c < whole ? c / 2 * 64 : whole * 32, hi = c < whole ? lo + 64 : D;
+  return x == 0 ? lo < D / 2 : hi > D / 2;
+}
+
 // Steps 0 .. N - 1 with four operands from LDS each, asked for AHEAD steps before.
 template <int N, int AHEAD, class Get, class Use>
 __device__ __forceinline__ void br_kv_ahead(Get &&get, Use &&use) {
@@ -1198,7 +1206,8 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
 #pragma unroll
               for (int y = 0; y < 4; ++y)
 #pragma unroll
-                for (int x = 0; x < NQ; ++x) z[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[y], q.qf[x][c], z[x][y], 0, 0, 0);
+                for (int x = 0; x < NQ; ++x)
+                  if (br_kv_has<D, MODE>(x, c)) z[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[y], q.qf[x][c], z[x][y], 0, 0, 0);
             });
         const int have = there(vid) ? min(max(len - t * BR_KV_TILE - 16 * g, 0), 16) : 0;
         br_h8 pf[NQ][2];
