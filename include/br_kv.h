@@ -292,7 +292,8 @@ int32_t br_kv_step_shared(br_kv_ctx *ctx, const br_kv_lengths *in, const br_kv_s
 /*
  * The blocks in use become, as far as the list reaches, those of the lowest ids.  With u = blocks in use of the worker: the k-th highest id in use not below u
  * becomes the k-th lowest free id below u, for k < n; tables and holders change accordingly, and list k says so (src, dst; -1 behind the last).  br_kv_copy with
- * this list, for every layer, comes before anything else is done with the layer.  Sources and destinations are different blocks.
+ * this list, for every layer, comes before anything else is done with the layer.  Sources and destinations are different blocks.  Slots of an earlier step name
+ * the places before: its tokens are appended first.
  */
 int32_t br_kv_compact(br_kv_ctx *ctx, const br_kv_moves *out);
 

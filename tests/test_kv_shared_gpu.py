@@ -204,6 +204,38 @@ def test_after_forks_and_steps_captured_with_them():
     cache.close()
 
 
+def test_a_captured_attention_follows_the_last_plan():
+    """Plans with fewer or more members between its replays: the kernel is another plan's, the results are not."""
+    torch = _torch()
+    for D, group, members in ((64, 4, 8), (128, 2, 4), (192, 4, 16), (128, 4, 2)):
+        rng = np.random.default_rng(D + group)
+        lens = 200 + rng.integers(0, 200, (1, 16))
+        cache, layer, h = _shared_cache(rng, "int8", 1, 16, 16, D, 2, group, lens, _families(16, 16), np.full((1, 16), 12))
+        lead = _i32(_families(16, 16))
+        q = torch.tensor(rng.normal(size=(16, 2 * group, D)), dtype=torch.float16, device="cuda:0")
+        out, lse = torch.empty_like(q), torch.empty((16, 2 * group), device="cuda:0")
+        side = torch.cuda.Stream()
+        own = kv.KvCache(cache.cfg, lens=cache.lens.clone(), table=cache.table.clone(), stream=side)
+        torch.cuda.synchronize()
+        own.plan_device(lead, members)
+        torch.cuda.synchronize()
+        for window in (0, 150):
+            ref = _reference(q.double().cpu().numpy(), h, lens, np.arange(16), np.ones(16, np.int64), 1, group, 16, "int8", window, None)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                own.attend_shared_device(layer, q, out, lse=lse, window=window)
+            for other in (members, 1, 16, 3, 64):
+                with torch.cuda.stream(side):
+                    own.plan_device(lead, other)
+                    out.fill_(7.0), lse.fill_(7.0)
+                    graph.replay()
+                torch.cuda.synchronize()
+                _check_attention((D, group, members, other, window), own, q, out, lse, ref, "float16")
+            own.plan_device(lead, members)
+            torch.cuda.synchronize()
+        cache.close(), own.close()
+
+
 def test_refusals():
     torch = _torch()
     sizes = dict(rows=2, n_blocks=4, max_blocks=2, head_dim=64)
