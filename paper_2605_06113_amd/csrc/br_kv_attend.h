@@ -523,10 +523,18 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
     __syncthreads();
   }
 
+  auto values_at = [&](const BrKvTile &x, int id) {
+    return p.v + ((((cache0 + (there(id) ? id : 0)) * p.kv_heads + h) * D + n) << p.shift) + ((x.tile * BR_KV_TILE + 16 * g) & mask);
+  };
+  if (PHASES > 0 && t_any) {
+    const unsigned char *at = values_at(now, vid);
+#pragma unroll
+    for (int d = 0; d < ND; ++d) vc[d] = br_kv_load16<ONCE_V>(at + ((16 * d) << p.shift));
+  }
   for (; t < stop; t += STEP) {
     const int token = now.tile * BR_KV_TILE + 16 * g;  // of the lane's first weight
-    {
-      const unsigned char *at = p.v + ((((cache0 + (there(vid) ? vid : 0)) * p.kv_heads + h) * D + n) << p.shift) + (token & mask);
+    if (PHASES == 0) {
+      const unsigned char *at = values_at(now, vid);
 #pragma unroll
       for (int d = 0; d < ND; ++d) vc[d] = br_kv_load16<ONCE_V>(at + ((16 * d) << p.shift));
     }
@@ -570,6 +578,8 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 #pragma unroll
       for (int d = 0; d < ND; ++d) vc[d].x &= (unsigned)m0, vc[d].y &= (unsigned)(m0 >> 32), vc[d].z &= (unsigned)m1, vc[d].w &= (unsigned)(m1 >> 32);
     }
+    // PHASES: the next tile's values take these ones' registers as they are used up, and have a whole tile's time to come
+    const unsigned char *coming = PHASES > 0 && t + STEP < stop ? values_at(next, vid1) : p.v;
 #pragma unroll
     for (int d0 = 0; d0 < ND; d0 += 2) {
 #pragma unroll
@@ -580,6 +590,10 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 #pragma unroll
           for (int x = 0; x < NQ; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pf[x][k], o[x][d], 0, 0, 0);
         }
+      if (PHASES > 0) {
+#pragma unroll
+        for (int d = d0; d < d0 + 2; ++d) vc[d] = br_kv_load16<ONCE_V>(coming + ((16 * d) << p.shift));
+      }
     }
     vid = vid1, vid1 = vid2;
     now = next, next = after;
