@@ -14,32 +14,57 @@ __device__ __forceinline__ void br_kv_rows(const BrKvTables &t, int slices, Fn &
   }
 }
 
-// What row r of worker w becomes, its `held` tokens aside: tokens, -1 where it stays as it is; f: whose.
+// What row r of worker w becomes: tokens, -1 where it stays as it is; f: whose.
 __device__ __forceinline__ int br_kv_forked(const BrKvTables &t, int w, int r, int f, const int *len) {
   if ((unsigned)f >= (unsigned)t.B) return -1;
   const int n = br_kv_len(t, w * t.B + f), cut = len ? len[r] : -1;
   return cut >= 0 ? min(n, cut) : n;
 }
 
-// Entry j of a row: what is to come (-> x.table), counted; false where the row holds that block there already, and nothing is to be done.
-__device__ __forceinline__ bool br_kv_take(const BrKvTables &t, const BrKvNext &x, int w, int r, long long src, int j, int had, int blocks) {
-  const long long at = (long long)r * t.max_blocks + j;
-  const int id = t.table[src + j], was = t.table[at];
-  if (j == blocks - 1) t.tail[r] = id;
-  if (j < had && was == id) return false;
-  x.table[at] = id;
-  if ((unsigned)id < (unsigned)t.n_blocks) atomicAdd(&t.holders[(long long)w * t.n_blocks + id], 1);
-  return true;
-}
+// Four entries of a row, j, j + step, ..., below `blocks`: asked for, all before any is acted on; then what is to come (-> x.table), counted, bit k of the
+// result: entry k changes.
+struct BrKvFour {
+  int id[4], was[4];
+  __device__ __forceinline__ void ask(const BrKvTables &t, int r, long long src, int j, int step, int blocks) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e = min(j + k * step, blocks - 1);
+      id[k] = t.table[src + e], was[k] = t.table[(long long)r * t.max_blocks + e];
+    }
+  }
+  __device__ __forceinline__ unsigned take(const BrKvTables &t, const BrKvNext &x, int w, int r, int j, int step, int had, int blocks) const {
+    unsigned changes = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e = j + k * step;
+      if (e == blocks - 1) t.tail[r] = id[k];
+      if (e >= blocks || (e < had && was[k] == id[k])) continue;
+      changes |= 1u << k;
+      x.table[(long long)r * t.max_blocks + e] = id[k];
+      if ((unsigned)id[k] < (unsigned)t.n_blocks) atomicAdd(&t.holders[(long long)w * t.n_blocks + id[k]], 1);
+    }
+    return changes;
+  }
+};
 
-// ... into the table, and the block that stood there given back.
-__device__ __forceinline__ void br_kv_put(const BrKvTables &t, const BrKvNext &x, int w, int r, int j, int had, int blocks) {
-  const long long at = (long long)r * t.max_blocks + j;
-  const int stood = t.table[at], next = x.table[at];  // (both are memory, whatever they hold)
-  const int was = j < had ? stood : -1;
-  t.table[at] = j < blocks ? next : -1;
-  if ((unsigned)was < (unsigned)t.n_blocks && atomicSub(&t.holders[(long long)w * t.n_blocks + was], 1) == 1)
-    atomicAnd(&t.used[(long long)w * t.words + (was >> 5)], ~(1u << (was & 31)));
+// ... those of them that change into the table, and the blocks that stood there given back.
+__device__ __forceinline__ void br_kv_put4(const BrKvTables &t, const BrKvNext &x, int w, int r, int j, int step, int had, int blocks, int end, unsigned changes) {
+  const long long at = (long long)r * t.max_blocks;
+  int stood[4], next[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int e = min(j + k * step, end - 1);
+    stood[k] = t.table[at + e], next[k] = x.table[at + e];  // (both are memory, whatever they hold)
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int e = j + k * step;
+    if (e >= end || !(changes >> k & 1) || (e < blocks && next[k] == INT32_MIN)) continue;
+    t.table[at + e] = e < blocks ? next[k] : -1;
+    const int was = e < had ? stood[k] : -1;
+    if ((unsigned)was < (unsigned)t.n_blocks && atomicSub(&t.holders[(long long)w * t.n_blocks + was], 1) == 1)
+      atomicAnd(&t.used[(long long)w * t.words + (was >> 5)], ~(1u << (was & 31)));
+  }
 }
 
 // What each row is to hold, beside the tables: its entries, and one holder more of each block that the row does not hold in that place.
@@ -50,9 +75,15 @@ __global__ __launch_bounds__(256) void br_kv_k_fork_take(BrKvTables t, BrKvNext 
     if (first == 0) x.lens[r] = make_int2(held, n);
     const long long src = ((long long)w * t.B + f) * t.max_blocks;
     const int blocks = (n + b1) >> t.shift, had = (held + b1) >> t.shift;
-#pragma unroll 4
-    for (int j = first; j < blocks; j += slices * G)
-      if (!br_kv_take(t, x, w, r, src, j, had, blocks)) x.table[(long long)r * t.max_blocks + j] = INT32_MIN;  // (no block's id: stays)
+    const int step = slices * G;
+    for (int j = first; j < blocks; j += 4 * step) {
+      BrKvFour four;
+      four.ask(t, r, src, j, step, blocks);
+      const unsigned changes = four.take(t, x, w, r, j, step, had, blocks);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (!(changes >> k & 1) && j + k * step < blocks) x.table[(long long)r * t.max_blocks + j + k * step] = INT32_MIN;  // (no block's id: stays)
+    }
   });
 }
 
@@ -64,9 +95,7 @@ __global__ __launch_bounds__(256) void br_kv_k_fork_put(BrKvTables t, BrKvNext x
     const int2 n = x.lens[r];
     if (n.y < 0) return;
     const int blocks = (n.y + b1) >> t.shift, had = (n.x + b1) >> t.shift;
-#pragma unroll 4
-    for (int j = first; j < max(blocks, had); j += slices * G)
-      if (j >= blocks || x.table[(long long)r * t.max_blocks + j] != INT32_MIN) br_kv_put(t, x, w, r, j, had, blocks);
+    for (int j = first; j < max(blocks, had); j += 4 * slices * G) br_kv_put4(t, x, w, r, j, slices * G, had, blocks, max(blocks, had), 15u);
     if (first == 0) {
       t.lens[r] = n.y;
       if (blocks == 0) t.tail[r] = -1;
@@ -74,7 +103,9 @@ __global__ __launch_bounds__(256) void br_kv_k_fork_put(BrKvTables t, BrKvNext x
   });
 }
 
-// Both for one worker by one block, 16 lanes to a row: no row's entries are written before all have been read.  A lane notes which of its first 63 entries
+// Bound by the way to memory: 512 workers of 144 rows, up to 133 entries each, 19.6 us, some 45 MB of lines of own and others' rows, a launch and four dependent
+// trips.  The next four entries on their way beside these ones' work did not change that.
+// Both for one worker by one block, 16 lanes to a row: no row's entries are written before all have been read.  A lane notes which of its first 60 entries
 // change: rows of one family differ in a few, and the others are not looked at again.
 template <int NT>
 __global__ __launch_bounds__(NT) void br_kv_k_fork(BrKvTables t, BrKvNext x, const int *from, const int *len) {
@@ -94,11 +125,17 @@ __global__ __launch_bounds__(NT) void br_kv_k_fork(BrKvTables t, BrKvNext x, con
     const int2 n = lens[r];  // (a row that stays has -1 tokens here: no blocks)
     const int blocks = (n.y + b1) >> t.shift, had = (n.x + b1) >> t.shift;
     const long long src = (long long)(row0 + whose[r]) * t.max_blocks;
-#pragma unroll 4
-    for (int j = lane; j < blocks; j += G, ++i) {
-      const bool changed = br_kv_take(t, x, w, row0 + r, src, j, had, blocks);
-      if (i < 63) changes |= (unsigned long long)changed << i;
-      else if (!changed) x.table[(long long)(row0 + r) * t.max_blocks + j] = INT32_MIN;  // (no block's id: stays)
+    for (int j = lane; j < blocks; j += 4 * G, i += 4) {
+      BrKvFour four;
+      four.ask(t, row0 + r, src, j, G, blocks);
+      const unsigned some = four.take(t, x, w, row0 + r, j, G, had, blocks);
+      if (i < 60) {
+        changes |= (unsigned long long)some << i;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (!(some >> k & 1) && j + k * G < blocks) x.table[(long long)(row0 + r) * t.max_blocks + j + k * G] = INT32_MIN;  // (no block's id: stays)
+      }
     }
   }
   __syncthreads();
@@ -107,12 +144,11 @@ __global__ __launch_bounds__(NT) void br_kv_k_fork(BrKvTables t, BrKvNext x, con
     const int2 n = lens[r];
     if (n.y < 0) continue;
     const int blocks = (n.y + b1) >> t.shift, had = (n.x + b1) >> t.shift;
-    for (int j = lane; j < blocks; j += G, ++i) {
-      const bool changed = i < 63 ? changes >> i & 1 : x.table[(long long)(row0 + r) * t.max_blocks + j] != INT32_MIN;
-      if (changed) br_kv_put(t, x, w, row0 + r, j, had, blocks);
+    for (int j = lane; j < blocks; j += 4 * G, i += 4) {
+      const unsigned four = i < 60 ? (unsigned)(changes >> i) & 15u : 15u;
+      if (four) br_kv_put4(t, x, w, row0 + r, j, G, had, blocks, blocks, four);
     }
-#pragma unroll 4
-    for (int j = blocks + lane; j < had; j += G) br_kv_put(t, x, w, row0 + r, j, had, blocks);
+    for (int j = blocks + lane; j < had; j += 4 * G) br_kv_put4(t, x, w, row0 + r, j, G, had, blocks, had, 15u);
     if (lane == 0) {
       t.lens[row0 + r] = n.y;
       if (blocks == 0) t.tail[row0 + r] = -1;
@@ -186,13 +222,22 @@ __global__ __launch_bounds__(256) void br_kv_k_compact_tables(BrKvTables t, BrKv
     const int least = x.least[w], blocks = (br_kv_len(t, r) + (1 << t.shift) - 1) >> t.shift;
     const int *moved = x.moved + (long long)w * t.n_blocks;
     int *table = t.table + (long long)r * t.max_blocks;
-#pragma unroll 4
-    for (int j = first; j < blocks; j += slices * G) {
-      const int id = table[j];
-      if (id < least || id >= t.n_blocks) continue;
-      const int to = moved[id];
-      table[j] = to;
-      if (j == blocks - 1) t.tail[r] = to;
+    const int step = slices * G;
+    for (int j = first; j < blocks; j += 4 * step) {
+      int id[4], to[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) id[k] = table[min(j + k * step, blocks - 1)];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        to[k] = -1;
+        if (j + k * step < blocks && id[k] >= least && id[k] < t.n_blocks) to[k] = moved[id[k]];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (to[k] < 0) continue;
+        table[j + k * step] = to[k];
+        if (j + k * step == blocks - 1) t.tail[r] = to[k];
+      }
     }
   });
 }
@@ -280,8 +325,8 @@ struct BrKvGrid {
 
 void br_kv_launch_fork(const BrKvTables &t, const BrKvNext &x, const int *from, const int *len, hipStream_t st) {
   // A block for a worker goes over its rows' entries in rounds of some 1.2 us; two launches spread one worker over the card.  64 rows of up to 2048 tokens in
-  // blocks of 64: one worker 5.7 us and 9.7, 512 of them 9.9 and 14.9; 256 rows of up to 8192: one 14.4 and 9.7, 256 workers 22 and 29; 64 rows
-  // of up to 16384 tokens in blocks of 16, 128 workers 27 and 20, 300 of them 30 and 45.  Workers of a few rows fill no blocks: 16384 of 4 rows 29 and 20.
+  // blocks of 64: one worker 5.1 us and 9.7, 512 of them 9.9 and 14.9; 256 rows of up to 8192: 14.4 and 8.4, 256 workers 20 and 29; 64 rows
+  // of up to 16384 tokens in blocks of 16, 128 workers 27 and 17, 300 of them 16 and 45.  Workers of a few rows fill no blocks: 16384 of 4 rows 29 and 18.
   const long long rounds = (long long)((t.B + 63) / 64) * ((t.max_blocks + 63) / 64);
   if ((rounds <= 2 && t.W <= 4096) || (rounds <= 16 && t.W >= 256 && t.B > 32)) {
     if (t.B <= 16) br_kv_k_fork<256><<<t.W, 256, 0, st>>>(t, x, from, len);
