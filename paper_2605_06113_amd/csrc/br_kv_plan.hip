@@ -124,13 +124,13 @@ __global__ __launch_bounds__(NT) void br_kv_k_plan(BrKvTables t, BrKvPlan x) {
 
 void br_kv_launch_plan(const BrKvTables &t, const BrKvPlan &x, hipStream_t st) {
   // A wave takes some 1.2 us for what a row has in common with its leader.  One worker's rows by its one block, in one launch, or by the card, in two: 16 rows
-  // 5.3 us and 8.9, 64 rows (a block of 16 waves) 6.7 and 8.6, 256 rows 16 and 10.  Many workers fill the card by themselves, with blocks of four waves if
+  // 5.3 us and 8.9, 64 rows (a block of 16 waves) 6.7 and 8.6, 96 rows with tables out of memory 11.6 and 9.6, 256 rows 16 and 10.  Many workers fill the card by themselves, with blocks of four waves if
   // they are very many: 512 of 144 rows 18 us and 27, 4096 of 32 rows 25, 43 with 16 waves each, and 45.
   if (t.B <= 16 || (t.W >= 1024 && t.B <= 256)) {
     br_kv_k_plan<256, 1, true><<<t.W, 256, 0, st>>>(t, x);
     return;
   }
-  if (t.B <= 96 || (t.W >= 128 && t.B <= 256)) {
+  if (t.B <= 64 || (t.W >= 128 && t.B <= 256)) {
     br_kv_k_plan<1024, 1, true><<<t.W, 1024, 0, st>>>(t, x);
     return;
   }
