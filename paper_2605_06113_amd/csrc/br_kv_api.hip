@@ -194,9 +194,9 @@ bool attention_ok(const br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_at
 #define BR_KV_ARGS (p, tile, ctx->cfg.fmt == BR_KV_E4M3, ctx->cus, ctx->st)
 
 // Rows of many queries share their block's token tiles, those of few have waves of their own: two launches where a call may have
-// both (two chunks of 512 tokens beside 46 single ones: 375 us in one launch).
+// both (two chunks of 512 tokens beside 46 single ones: 375 us in one launch).  few_rows: query rows up to which a row goes with the few.
 template <class Fn>
-int32_t attend_by_rows(br_kv_ctx *ctx, BrKvAttend &p, int max_count, Fn &&launch) {
+int32_t attend_by_rows(br_kv_ctx *ctx, BrKvAttend &p, int max_count, int few_rows, Fn &&launch) {
   const br_kv_config &c = ctx->cfg;
   const int group = p.group;
   const int64_t rows = (int64_t)max_count * group;
@@ -204,10 +204,10 @@ int32_t attend_by_rows(br_kv_ctx *ctx, BrKvAttend &p, int max_count, Fn &&launch
   // 8 key heads, near the line, 27 to 33 us and 38.
   const int64_t tiles = (int64_t)p.n_rows * c.n_kv_heads * ((((int64_t)c.max_blocks << ctx->t.shift) + BR_KV_TILE - 1) / BR_KV_TILE);
   const bool both = rows > 64 && tiles > 8 * ctx->cus;
-  const int few = both ? 16 / group : 0;  // query tokens up to which a row of a mixed call goes with the few
+  const int few = both ? few_rows / group : 0;  // query tokens up to which a row of a mixed call goes with the few
   p.least = 1, p.most = both ? few : INT32_MAX;
   if (rows <= 64 || few > 0) {
-    const int64_t most = both ? 16 : rows;
+    const int64_t most = both ? few_rows : rows;
     const int32_t rc = enqueue(ctx, [&] { launch(p, most <= 16 ? BR_KV_TILE_16 : most <= 32 ? BR_KV_TILE_32 : BR_KV_TILE_64); });
     if (rc != BR_OK || rows <= 64) return rc;
   }
@@ -326,7 +326,7 @@ int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_atten
   if (a->n_tokens == 0) return BR_OK;
   BrKvAttend args;
   if (!attention_of(ctx, layer, a, 1, args)) return BR_EINVAL;
-  return attend_by_rows(ctx, args, a->max_count, [&](const BrKvAttend &p, int tile) { BR_KV_BY_DIM(br_kv_launch_attend) });
+  return attend_by_rows(ctx, args, a->max_count, 16, [&](const BrKvAttend &p, int tile) { BR_KV_BY_DIM(br_kv_launch_attend) });
 }
 
 int32_t br_kv_attend_diff(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *a, const br_kv_diff *diff) {
@@ -336,7 +336,8 @@ int32_t br_kv_attend_diff(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_
   BrKvAttend args;
   if (!attention_of(ctx, layer, a, 2, args)) return BR_EINVAL;
   args.lambda = diff->lambda, args.lambda_token = diff->lambda_token;
-  return attend_by_rows(ctx, args, a->max_count, [&](const BrKvAttend &p, int tile) { BR_KV_BY_DIM(br_kv_launch_diff) });
+  const int few_rows = args.group <= 16 ? 16 : args.group <= 32 ? 32 : 64;
+  return attend_by_rows(ctx, args, a->max_count, few_rows, [&](const BrKvAttend &p, int tile) { BR_KV_BY_DIM(br_kv_launch_diff) });
 }
 
 int32_t br_kv_plan(br_kv_ctx *ctx, const br_kv_families *in) {
