@@ -607,7 +607,8 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
 template <int D, int TQ, int NT, int MODE>
 __device__ __forceinline__ void br_kv_join(const BrKvAttend &p, const BrKvRow &w, int h, int qi, int rows_q, int first, int parts, br_f4 *sums, float2 *ml) {
   // few rows have many pieces (up to a block of the launch each), many rows few: places asked for at once are AT_ONCE pieces of ROWS rows
-  constexpr int ROWS = TQ > 64 ? 8 : TQ > 32 ? 4 : 1, AT_ONCE = TQ > 32 ? 2 : 8, STEP = NT * ROWS;
+  // (two rows for 32: one of 40000 tokens, 8 key heads of 128 channels in groups of 16, two maps 43 us, 39 so; three of up to 18584, 7 of 256 in groups of 12, 115 and 90)
+  constexpr int ROWS = TQ > 64 ? 8 : TQ > 32 ? 4 : TQ > 16 && MODE != BR_KV_PLAIN ? 2 : 1, AT_ONCE = TQ > 32 ? 2 : 8, STEP = NT * ROWS;
   const BrKvPieces<D, TQ> pieces(p, rows_q);
   const int tid = threadIdx.x, items = pieces.items(), S = items < NT ? max(1, NT / items) : 1;
   for (int at0 = tid; at0 < max(items, NT); at0 += STEP) {
@@ -1274,7 +1275,11 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
 template <int D, int TQ, int NQ, bool FP8, int NW, int WAVES>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend_together(BrKvAttend p) {
   constexpr int MODE = NQ == 2 ? BR_KV_SHARED_32 : BR_KV_SHARED_16, NT = 64 * NW, ND = D / 16, NH = TQ / (16 * NQ), P = NW / NH;
-  using Runs = BrKvRuns<TQ, NT, 1, 16, MODE>;
+  // A block that has fewer than LEAST tiles pays more for its pieces than it saves, one with P phases takes P tiles at a time: with 8 for all,
+  // 20 rows of 11 key heads that hold 4339 tokens together (D 256, 6 query heads each) 96 us, here 57; 152 rows of 5 (1103 tokens, D 128,
+  // 12 query heads) 99, here 56; with P for one column tile too, 16 rows of 4 (4000, D 192) 43, then 50.
+  constexpr int LEAST = 2 * P / NQ;
+  using Runs = BrKvRuns<TQ, NT, 1, (5 * P + 1) / 2, MODE>;
   __shared__ typename Runs::Shared shared;
   __shared__ br_f4 kept[NW * NQ * ND * 64];
   __shared__ float2 kept_ml[NW * NQ * 16];
@@ -1282,7 +1287,7 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend_together(BrKvAt
   __shared__ int arrived;
   const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int phase = wv / NH, row = 16 * NQ * (wv % NH);
-  Runs runs(p, shared, gridDim.x, BR_KV_LEAST_TILES);
+  Runs runs(p, shared, gridDim.x, LEAST);
   const int blocks = runs.workers, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
   if (wg >= blocks) return;
   long long u = runs.begin_of(wg);
