@@ -325,7 +325,7 @@ int32_t br_kv_plan(br_kv_ctx *ctx, const br_kv_families *in);
 /*
  * br_kv_attend of the planned rows' tokens (start, count, lens and table are NULL, max_count 1 or more): whole tiles of 64 tokens that the rows read together hold in
  * the same blocks are read once for all of them.  Results are br_kv_attend's but for the order of the sums, which the families have a say in; equal plans and inputs give
- * equal outputs.  Before the first plan: BR_EINVAL.
+ * equal outputs.  Before the first plan: BR_EINVAL; behind one that was captured and has not run, no row has a part in it.
  */
 int32_t br_kv_attend_shared(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *args);
 

@@ -248,7 +248,7 @@ static int32_t init_context(const br_kv_config *cfg, const br_kv_state *init, bo
   t.used = (unsigned *)(base + at.used);
   t.arrived = (int *)(base + at.arrived);
   t.holders = shared ? (int *)(base + at.holders) : nullptr;
-  int32_t rc = enqueue(ctx, [&] { br_kv_launch_clear(t, ctx->st); });
+  int32_t rc = enqueue(ctx, [&] { br_kv_launch_clear(t, shared ? (int4 *)(base + at.companies) : nullptr, ctx->st); });
   if (rc == BR_OK && init) rc = enqueue(ctx, [&] { br_kv_launch_load(t, init->lens, init->table, ctx->st); });
   if (rc != BR_OK) {
     delete ctx;

@@ -94,7 +94,7 @@ struct BrKvAttend {
   const int4 *members;
 };
 
-void br_kv_launch_clear(const BrKvTables &t, hipStream_t st);
+void br_kv_launch_clear(const BrKvTables &t, int4 *companies, hipStream_t st);
 void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, hipStream_t st);
 void br_kv_launch_step(const BrKvTables &t, const BrKvStep &s, hipStream_t st);
 void br_kv_launch_fork(const BrKvTables &t, const BrKvNext &x, const int *from, const int *len, hipStream_t st);

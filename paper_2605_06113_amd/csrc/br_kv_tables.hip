@@ -4,7 +4,7 @@
 #include "br_kv_device.h"
 
 // Every row empty, every block free; nothing begun.
-__global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t) {
+__global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t, int4 *companies) {
   const long long n = (long long)t.W * t.B * t.max_blocks, rows = (long long)t.W * t.B, words = (long long)t.W * t.words;
   const long long step = (long long)gridDim.x * 256;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
@@ -15,6 +15,8 @@ __global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t) {
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < BR_KV_SPLIT_WGS; i += step) t.arrived[i] = 0;
   if (t.holders)
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)t.W * t.n_blocks; i += step) t.holders[i] = 0;
+  if (companies)  // (a plan that was captured and not run yet has planned nothing)
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < 2ll * t.W * t.B; i += step) companies[i] = make_int4(0, 0, 0, 0);
 }
 
 // The rows held at the start (behind br_kv_k_clear).
@@ -322,8 +324,8 @@ __global__ __launch_bounds__(256) void br_kv_k_list(BrKvTables t, BrKvStep s) {
 
 static int grid_for(long long n) { return (int)(n < 1 ? 1 : n > 4096ll * 256 ? 4096 : (n + 255) / 256); }
 
-void br_kv_launch_clear(const BrKvTables &t, hipStream_t st) {
-  br_kv_k_clear<<<grid_for((long long)t.W * t.B * t.max_blocks), 256, 0, st>>>(t);
+void br_kv_launch_clear(const BrKvTables &t, int4 *companies, hipStream_t st) {
+  br_kv_k_clear<<<grid_for((long long)t.W * t.B * t.max_blocks), 256, 0, st>>>(t, companies);
 }
 
 void br_kv_launch_load(const BrKvTables &t, const int *lens, const int *table, hipStream_t st) {

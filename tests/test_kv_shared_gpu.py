@@ -236,6 +236,34 @@ def test_a_captured_attention_follows_the_last_plan():
         cache.close(), own.close()
 
 
+def test_a_plan_that_was_captured_and_has_not_run():
+    """It has planned nothing: the attention behind it writes no row; once it has run it does."""
+    torch = _torch()
+    for members in (2, 6, 16):
+        rng = np.random.default_rng(members)
+        lens = 100 + rng.integers(0, 200, (1, 16))
+        cache, layer, h = _shared_cache(rng, "fp8", 1, 16, 16, 128, 2, 4, lens, _families(16, 16), np.full((1, 16), 6))
+        side = torch.cuda.Stream()
+        own = kv.KvCache(cache.cfg, lens=cache.lens.clone(), table=cache.table.clone(), stream=side)
+        lead = _i32(_families(16, 16))
+        q = torch.tensor(rng.normal(size=(16, 8, 128)), dtype=torch.float16, device="cuda:0")
+        out, lse = torch.full_like(q, 7.0), torch.full((16, 8), 7.0, device="cuda:0")
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            own.plan_device(lead, members)
+        own.attend_shared_device(layer, q, out, lse=lse)
+        torch.cuda.synchronize()
+        assert bool((out == 7.0).all()) and bool((lse == 7.0).all())
+        with torch.cuda.stream(side):
+            graph.replay()
+            own.attend_shared_device(layer, q, out, lse=lse)
+        torch.cuda.synchronize()
+        ref = _reference(q.double().cpu().numpy(), h, lens, np.arange(16), np.ones(16, np.int64), 1, 4, 16, "fp8", 0, None)
+        _check_attention(("captured", members), own, q, out, lse, ref, "float16")
+        cache.close(), own.close()
+
+
 def test_refusals():
     torch = _torch()
     sizes = dict(rows=2, n_blocks=4, max_blocks=2, head_dim=64)
