@@ -275,14 +275,15 @@ struct BrKvQueries {
   int pos[NQ], member[NQ];
 
   template <class Fn>
-  __device__ __forceinline__ void load(const BrKvAttend &p, const BrKvRow &w, int h, int row0, Fn &&meanwhile) {
+  __device__ __forceinline__ void load(const BrKvAttend &p, const BrKvRow &w, int h, int row0, Fn &&meanwhile, const int4 &members = int4()) {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-      const int ri = row0 + br_kv_query<MODE, NQ>(x, n), i = br_kv_token(p, ri), t = br_kv_place<MODE>(p, w, i);
+      const int ri = row0 + br_kv_query<MODE, NQ>(x, n), i = br_kv_token(p, ri);
+      const int t = br_kv_shared(MODE) ? __shfl(members.y, min(i, 63), 64) : w.start + i, cached = br_kv_shared(MODE) ? __shfl(members.z, min(i, 63), 64) : 0;
       const bool in = i < w.n && t >= 0 && t < p.n_tokens;
       const int head = h * p.group + ri - i * p.group;
-      if (br_kv_shared(MODE)) pos[x] = in ? p.members[w.start + i].z - 1 : -1, member[x] = i;
+      if (br_kv_shared(MODE)) pos[x] = in ? cached - 1 : -1, member[x] = i;
       else pos[x] = in ? max(w.len - w.n + i, -1) : -1;
       const unsigned short *at = p.q + (in ? (long long)t * p.q_token + (long long)(MODE == BR_KV_DIFF ? head >> 1 : head) * p.q_head : 0);
       uint4 e[NK];
@@ -348,6 +349,10 @@ __device__ __forceinline__ void br_kv_weights(const BrKvAttend &p, const BrKvQue
   const bool inside = owner < 0 && t * BR_KV_TILE + BR_KV_TILE - 1 <= first_pos && (p.window == 0 || t * BR_KV_TILE > last_pos - p.window) && exist;
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
+    if (br_kv_shared(MODE) && NQ > 1 && owner >= 0 && !__any(owner == q.member[x])) {  // (none of these 16 rows is the owner's: weights of zero, nothing moves)
+      pf[x][0] = br_h8{}, pf[x][1] = br_h8{};
+      continue;
+    }
     float f = q.qs[x] * ks;  // (not below zero: the sign of the caller's scale is in the queries)
     float z[16], mx = BR_KV_NEG, vx = vs;
 #pragma unroll
@@ -513,7 +518,7 @@ __device__ __forceinline__ void br_kv_tiles(const BrKvAttend &p, BrKvRow w0, int
   BrKvQueries<D, NQ, MODE> q;
   q.load(p, w, h, row0, [&] {
     if (t_any) load_first();  // (while the queries are on their way)
-  });
+  }, map.member);
   if (PHASES > 0) {  // the queries' channels wait in LDS: 32 registers that the codes need
     if (phase == 0)
 #pragma unroll
@@ -1277,11 +1282,12 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
 template <int D, int TQ, int NQ, bool FP8, int NW, int WAVES>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend_together(BrKvAttend p) {
   constexpr int MODE = NQ == 2 ? BR_KV_SHARED_32 : BR_KV_SHARED_16, NT = 64 * NW, ND = D / 16, NH = TQ / (16 * NQ), P = NW / NH;
-  // A block that has fewer than LEAST tiles pays more for its pieces than it saves, one with P phases takes P tiles at a time: with 8 for all,
-  // 20 rows of 11 key heads that hold 4339 tokens together (D 256, 6 query heads each) 96 us, here 57; 152 rows of 5 (1103 tokens, D 128,
-  // 12 query heads) 99, here 56; with P for one column tile too, 16 rows of 4 (4000, D 192) 43, then 50.
-  constexpr int LEAST = 2 * P / NQ;
-  using Runs = BrKvRuns<TQ, NT, 1, (5 * P + 1) / 2, MODE>;
+  // A block that has fewer than LEAST tiles pays more for its pieces than it saves: with 8 for all, 20 rows of 11 key heads that hold 4339 tokens
+  // together (D 256, 6 query heads each) 96 us, here 57; 152 rows of 5 (1103 tokens, D 128, 12 query heads) 99, here 56; 2 / NH to 4 / NH: 4 rows of 8
+  // (30000 tokens, D 128) 40 as here, 16 rows of 4 (4000, D 192) 50 and 43.  And one whose company is no more than SLACK tiles over an equal share keeps it: 32
+  // rows of 8 (500 tokens, D 128, 4 query heads) 30 us with half of that, 25 so, and 16 of 8 (500, D 192, 2 query heads) 31 with twice that, 22 so.
+  constexpr int LEAST = 8 / NH, SLACK = 20 / NH;
+  using Runs = BrKvRuns<TQ, NT, 1, SLACK, MODE>;
   __shared__ typename Runs::Shared shared;
   __shared__ br_f4 kept[NW * NQ * ND * 64];
   __shared__ float2 kept_ml[NW * NQ * 16];
@@ -1392,7 +1398,9 @@ void br_kv_attend_rows(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
 
 template <int D, int TQ>
 void br_kv_attend_together(const BrKvAttend &p, bool fp8, int cus, hipStream_t st) {
-  constexpr int NQ = D <= 128 ? 2 : 1, NW = D <= 128 ? 8 : 4, WAVES = D <= 128 ? 2 : 1;
+  // (two column tiles a wave where registers do; eight waves where their sums fit LDS: D 192 by four, with twice the registers, 16 rows of 8 that hold 500
+  // tokens together 40 us, here 22; 96 rows of 8, 4000 tokens, 8 query heads each, 81 and 68)
+  constexpr int NQ = D <= 128 ? 2 : 1, NW = D <= 192 ? 8 : 4, WAVES = D <= 192 ? 2 : 1;
   const int blocks = cus < BR_KV_SPLIT_WGS_OF(D) ? cus : BR_KV_SPLIT_WGS_OF(D);
   if (fp8) br_kv_k_attend_together<D, TQ, NQ, true, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
   else br_kv_k_attend_together<D, TQ, NQ, false, NW, WAVES><<<blocks, 64 * NW, 0, st>>>(p);
