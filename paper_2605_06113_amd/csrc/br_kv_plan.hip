@@ -36,106 +36,81 @@ __global__ __launch_bounds__(256) void br_kv_k_plan_common(BrKvTables t, BrKvPla
   }
 }
 
-// One block for each worker: a family's rows in companies of at most `most`, evenly, in the order of the rows.
-// ALONE: what rows have in common is found here too (else by br_kv_k_plan_common, before).
-template <int NT, int RPT, bool ALONE>
+// One block for each worker, a thread for each row: a family's rows in companies of at most `most`, evenly, in the order of the rows.
+// ALONE: what rows have in common is found here too (else by br_kv_k_plan_common, before).  Bound by its chain of loads and barriers: four rows of one worker
+// 4.1 us, a launch that does nothing 3.9; 96 rows in two launches 4.8 and 5.2.
+template <int NT, bool ALONE>
 __global__ __launch_bounds__(NT) void br_kv_k_plan(BrKvTables t, BrKvPlan x) {
-  constexpr int ROWS = NT * RPT;
-  __shared__ __attribute__((aligned(16))) int family[ROWS];
-  __shared__ int part[16 * (NT / 64)], common[ALONE ? ROWS : 1], size[ROWS], before[ROWS], first_of[ROWS], least[ROWS], tiles[ROWS], n_of[ROWS], begin_of[ROWS], by16[4 * ROWS], by32[2 * ROWS];
-  const int w = blockIdx.x, tid = threadIdx.x, B = t.B;
+  __shared__ __attribute__((aligned(16))) int family[NT];
+  __shared__ int part[16 * (NT / 64)], common[ALONE ? NT : 1], size[NT], before[NT], first_of[NT], least[NT], tiles[NT], n_of[NT], begin_of[NT], by16[4 * NT], by32[2 * NT];
+  const int w = blockIdx.x, r = threadIdx.x, B = t.B;
+  const long long at = (long long)w * B + r;
   int turn = 0;
-#pragma unroll
-  for (int i = 0; i < RPT; ++i) {
-    const int r = tid * RPT + i;
-    family[r] = r < B && (!x.count || x.count[(long long)w * B + r] == 1) ? br_kv_leader(t, x, w, r) : -1;
-    size[r] = n_of[r] = begin_of[r] = tiles[r] = 0, least[r] = INT32_MAX;
-    by16[4 * r] = by16[4 * r + 1] = by16[4 * r + 2] = by16[4 * r + 3] = by32[2 * r] = by32[2 * r + 1] = 0;
-  }
+  const int f = r < B && (!x.count || x.count[at] == 1) ? br_kv_leader(t, x, w, r) : -1;
+  family[r] = f;
+  size[r] = n_of[r] = begin_of[r] = tiles[r] = 0, least[r] = INT32_MAX;
+  by16[4 * r] = by16[4 * r + 1] = by16[4 * r + 2] = by16[4 * r + 3] = by32[2 * r] = by32[2 * r + 1] = 0;
   __syncthreads();
   if (ALONE)
-    for (int r = __builtin_amdgcn_readfirstlane(tid >> 6); r < B; r += NT / 64) {
-      if (family[r] < 0) continue;
-      const int same = br_kv_common(t, x, w, r);
-      if ((tid & 63) == 0) common[r] = same;
+    for (int k = __builtin_amdgcn_readfirstlane(r >> 6); k < B; k += NT / 64) {
+      if (family[k] < 0) continue;
+      const int same = br_kv_common(t, x, w, k);
+      if ((r & 63) == 0) common[k] = same;
     }
-  int rank[RPT];
-#pragma unroll
-  for (int i = 0; i < RPT; ++i) {
-    const int r = tid * RPT + i, f = family[r];
-    rank[i] = 0;
-    if (f < 0) continue;
+  int rank = 0;
+  if (f >= 0) {
     for (int k = 0; k < r; k += 4) {  // (up to three rows from r on are looked at and not counted)
       const int4 x4 = *(const int4 *)(family + k);
-      rank[i] += (x4.x == f) + (x4.y == f && k + 1 < r) + (x4.z == f && k + 2 < r) + (x4.w == f && k + 3 < r);
+      rank += (x4.x == f) + (x4.y == f && k + 1 < r) + (x4.z == f && k + 2 < r) + (x4.w == f && k + 3 < r);
     }
     atomicAdd(&size[f], 1);
   }
   __syncthreads();
-  int sum[2] = {0, 0}, all[2];
-#pragma unroll
-  for (int i = 0; i < RPT; ++i) sum[0] += size[tid * RPT + i], sum[1] += (size[tid * RPT + i] + x.most - 1) / x.most;
-  const int mine[2] = {sum[0], sum[1]};
+  const int mine[2] = {size[r], (size[r] + x.most - 1) / x.most};
+  int sum[2] = {mine[0], mine[1]}, all[2];
   br_kv_scan<NT, 2>(sum, all, part, turn);
-  int a = sum[0] - mine[0], b = sum[1] - mine[1];
-#pragma unroll
-  for (int i = 0; i < RPT; ++i) {
-    const int r = tid * RPT + i;
-    before[r] = a, first_of[r] = b;
-    a += size[r], b += (size[r] + x.most - 1) / x.most;
+  before[r] = sum[0] - mine[0], first_of[r] = sum[1] - mine[1];
+  __syncthreads();
+  int company = -1, tokens = 0, place = 0;
+  if (f >= 0) {
+    const int companies = (size[f] + x.most - 1) / x.most, per = (size[f] + companies - 1) / companies, k = rank / per;
+    company = first_of[f] + k, place = rank - k * per;
+    tokens = br_kv_len(t, (int)at);
+    atomicMin(&least[company], ALONE ? common[r] : x.common[at]);
+    if (place == 0) n_of[company] = min(per, size[f] - k * per), begin_of[company] = before[f] + k * per;
+    x.members[(long long)w * B + before[f] + rank] = make_int4((int)at, x.start ? x.start[at] : (int)at, tokens, 0);
   }
   __syncthreads();
-  int company[RPT], tokens[RPT], place[RPT];
-#pragma unroll
-  for (int i = 0; i < RPT; ++i) {
-    const int r = tid * RPT + i, f = family[r];
-    company[i] = -1;
-    if (f < 0) continue;
-    const long long at = (long long)w * B + r;
-    const int companies = (size[f] + x.most - 1) / x.most, per = (size[f] + companies - 1) / companies, k = rank[i] / per;
-    company[i] = first_of[f] + k, place[i] = rank[i] - k * per;
-    tokens[i] = br_kv_len(t, (int)at);
-    atomicMin(&least[company[i]], ALONE ? common[r] : x.common[at]);
-    if (rank[i] == k * per) n_of[company[i]] = min(per, size[f] - k * per), begin_of[company[i]] = before[f] + k * per;
-    x.members[(long long)w * B + before[f] + rank[i]] = make_int4((int)at, x.start ? x.start[at] : (int)at, tokens[i], 0);
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < RPT; ++i) {
-    if (company[i] < 0) continue;
-    const int together = n_of[company[i]] > 1 ? least[company[i]] / BR_KV_TILE : 0, own = (tokens[i] + BR_KV_TILE - 1) / BR_KV_TILE - together;
-    atomicAdd(&tiles[company[i]], own);
+  if (company >= 0) {
+    const int together = n_of[company] > 1 ? least[company] / BR_KV_TILE : 0, own = (tokens + BR_KV_TILE - 1) / BR_KV_TILE - together;
+    atomicAdd(&tiles[company], own);
     // (of one member all waves have the same; several have 64 query rows at most)
-    const int first = place[i] * x.group, last = n_of[company[i]] > 1 ? first + x.group - 1 : first;
-    for (int k = first / 16; k <= min(last / 16, 3); ++k) atomicAdd(&by16[4 * company[i] + k], own);
-    for (int k = first / 32; k <= min(last / 32, 1); ++k) atomicAdd(&by32[2 * company[i] + k], own);
+    const int first = place * x.group, last = n_of[company] > 1 ? first + x.group - 1 : first;
+    for (int k = first / 16; k <= min(last / 16, 3); ++k) atomicAdd(&by16[4 * company + k], own);
+    for (int k = first / 32; k <= min(last / 32, 1); ++k) atomicAdd(&by32[2 * company + k], own);
   }
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < RPT; ++i) {
-    const int c = tid * RPT + i;
-    if (c >= B) continue;
-    const int together = n_of[c] > 1 ? least[c] / BR_KV_TILE : 0;
-    int4 *to = x.companies + 2 * ((long long)w * B + c);
-    to[0] = make_int4(n_of[c], w * B + begin_of[c], together, together + tiles[c]);
-    to[1] = make_int4(together + max(max(by16[4 * c], by16[4 * c + 1]), max(by16[4 * c + 2], by16[4 * c + 3])), together + max(by32[2 * c], by32[2 * c + 1]), 0, 0);
-  }
+  if (r >= B) return;
+  const int together = n_of[r] > 1 ? least[r] / BR_KV_TILE : 0;
+  int4 *to = x.companies + 2 * at;
+  to[0] = make_int4(n_of[r], w * B + begin_of[r], together, together + tiles[r]);
+  to[1] = make_int4(together + max(max(by16[4 * r], by16[4 * r + 1]), max(by16[4 * r + 2], by16[4 * r + 3])), together + max(by32[2 * r], by32[2 * r + 1]), 0, 0);
 }
 
 void br_kv_launch_plan(const BrKvTables &t, const BrKvPlan &x, hipStream_t st) {
   // A wave takes some 1.2 us for what a row has in common with its leader.  One worker's rows by its one block, in one launch, or by the card, in two: 16 rows
-  // 5.3 us and 8.9, 64 rows (a block of 16 waves) 6.7 and 8.6, 96 rows with tables out of memory 11.6 and 9.6, 256 rows 16 and 10.  Many workers fill the card by themselves, with blocks of four waves if
-  // they are very many: 512 of 144 rows 18 us and 27, 4096 of 32 rows 25, 43 with 16 waves each, and 45.
+  // 5.1 us and 8.5, 64 rows (a block of 16 waves) 6.7 and 8.7, 96 rows with tables out of memory 11.6 and 9.6, 256 rows 16 and 11.  Many workers fill the card by
+  // themselves, with blocks of four waves if they are very many: 512 of 144 rows 23 us and 28, 4096 of 32 rows 27, 67 with 16 waves each, and 46.
   if (t.B <= 16 || (t.W >= 1024 && t.B <= 256)) {
-    br_kv_k_plan<256, 1, true><<<t.W, 256, 0, st>>>(t, x);
+    br_kv_k_plan<256, true><<<t.W, 256, 0, st>>>(t, x);
     return;
   }
   if (t.B <= 64 || (t.W >= 128 && t.B <= 256)) {
-    br_kv_k_plan<1024, 1, true><<<t.W, 1024, 0, st>>>(t, x);
+    br_kv_k_plan<1024, true><<<t.W, 1024, 0, st>>>(t, x);
     return;
   }
   const long long blocks = ((long long)t.W * t.B + 3) / 4;
   br_kv_k_plan_common<<<(unsigned)(blocks < 1 << 20 ? blocks : 1 << 20), 256, 0, st>>>(t, x);
-  if (t.B <= 256) br_kv_k_plan<256, 1, false><<<t.W, 256, 0, st>>>(t, x);
-  else br_kv_k_plan<1024, 1, false><<<t.W, 1024, 0, st>>>(t, x);
+  if (t.B <= 256) br_kv_k_plan<256, false><<<t.W, 256, 0, st>>>(t, x);
+  else br_kv_k_plan<1024, false><<<t.W, 1024, 0, st>>>(t, x);
 }
