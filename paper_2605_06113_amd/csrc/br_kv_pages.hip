@@ -67,7 +67,8 @@ __device__ __forceinline__ void br_kv_put4(const BrKvTables &t, const BrKvNext &
   }
 }
 
-// What each row is to hold, beside the tables: its entries, and one holder more of each block that the row does not hold in that place.
+// What each row is to hold, beside the tables: its entries, and one holder more of each block that the row does not hold in that place.  Bound by a launch and its
+// chain (lengths and whose, entries, counts), 80 % waiting: one worker of 96 rows, up to 250 entries each, 3.6 us, and 3.4 for the second half below.
 template <int G>
 __global__ __launch_bounds__(256) void br_kv_k_fork_take(BrKvTables t, BrKvNext x, const int *from, const int *len, int slices) {
   br_kv_rows<G>(t, slices, [&](int r, int w, int first) {
@@ -156,7 +157,8 @@ __global__ __launch_bounds__(NT) void br_kv_k_fork(BrKvTables t, BrKvNext x, con
   }
 }
 
-// One block for each worker: which blocks go where, the used bits and the counts.  The used bits are in LDS.
+// One block for each worker: which blocks go where, the used bits and the counts.  The used bits are in LDS.  Bound by four scans and the trips between them, not
+// by what they move: one worker of 96 rows 3.6 us, 300 of 31 rows 6.0, 80 to 87 % of the time waiting.
 template <int NT>
 __global__ __launch_bounds__(NT) void br_kv_k_compact(BrKvTables t, BrKvNext x, BrKvMoves m) {
   extern __shared__ unsigned used[];
@@ -215,7 +217,7 @@ __global__ __launch_bounds__(NT) void br_kv_k_compact(BrKvTables t, BrKvNext x, 
     for (int i = tid; i < t.words; i += NT) gused[i] = used[i];
 }
 
-// The tables' entries, by where the blocks have gone (behind br_kv_k_compact).
+// The tables' entries, by where the blocks have gone (behind br_kv_k_compact): three dependent trips, 2.6 us of one worker, 4.1 of 300 of 31 rows.
 template <int G>
 __global__ __launch_bounds__(256) void br_kv_k_compact_tables(BrKvTables t, BrKvNext x, int slices) {
   br_kv_rows<G>(t, slices, [&](int r, int w, int first) {
@@ -242,7 +244,8 @@ __global__ __launch_bounds__(256) void br_kv_k_compact_tables(BrKvTables t, BrKv
   });
 }
 
-// Large blocks: a block of threads has one piece of a pair's keys or values, all of it on its way at once; the scales go with the first.
+// Large blocks: a block of threads has one piece of a pair's keys or values, all of it on its way at once; the scales go with the first.  Bound by memory: requests
+// of 64 KB a block, 1.39 GB read and written, 278 us = 5.0 TB/s (a large copy 5.1).
 template <int AT_ONCE>
 __global__ __launch_bounds__(256) void br_kv_k_copy(BrKvCache c, BrKvMoves m, int W, int chunks, long long units) {
   constexpr int CHUNK = AT_ONCE * 256 * 16;
@@ -269,7 +272,8 @@ __global__ __launch_bounds__(256) void br_kv_k_copy(BrKvCache c, BrKvMoves m, in
   }
 }
 
-// Pairs' codes in pieces of 1 KB, 16 bytes a lane: a block's keys, its values, then its scales as one piece.  A wave has eight pieces on their way at once.
+// Pairs' codes in pieces of 1 KB, 16 bytes a lane: a block's keys, its values, then its scales as one piece.  A wave has eight pieces on their way at once.  Bound by
+// memory: 69 MB in 13.6 us = 5.1 TB/s.
 __global__ __launch_bounds__(256) void br_kv_k_copy_small(BrKvCache c, BrKvMoves m, int W, int half, long long batches) {
   constexpr int AT_ONCE = 8;
   typedef unsigned u4 __attribute__((ext_vector_type(4)));

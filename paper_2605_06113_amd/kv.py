@@ -24,6 +24,9 @@ Of a cache with `shared=True` several rows may hold the same blocks (samples of 
     for layer in layers:
         cache.copy_device(layer, step["copy_src"], step["copy_dst"])   # ... with what it held, before anything is appended
         cache.append_device(layer, k, v, step["slot"])
+    cache.plan_device(lead, members, start=step["start"], count=step["count"])   # for all layers of the step
+    for layer in layers:
+        cache.attend_shared_device(layer, q, out)             # what rows hold together is read once
 """
 from __future__ import annotations
 
@@ -423,7 +426,8 @@ class KvCache:
     def plan_device(self, lead, members: int, start=None, count=None) -> None:
         """Which rows attend_shared_device reads together (br_kv_plan), for all layers of a step: behind step_device.
 
-        lead [n_workers, rows] int32: the row that row r shares its first blocks with (its family's first, itself, or -1); at most `members` rows together.
+        lead [n_workers, rows] int32: the row that row r shares its first blocks with (its family's first, itself, or -1); at most `members` rows together:
+        as many as have 16 query rows of a key head where calls are short, more where they read much.
         start, count: step_device's; rows whose count is not 1 are left out; none: token r belongs to row r."""
         self._is_shared()
         at = (self._check(lead, "lead", self._rows, self._i32), *self._check_lists(start, count))
