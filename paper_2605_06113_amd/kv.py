@@ -21,11 +21,10 @@ Of a cache with `shared=True` several rows may hold the same blocks (samples of 
 
     cache.fork_device(rows, length)                           # row r goes on from the first length[r] tokens of row rows[r]
     cache.step_device(keep, add, step)                        # rows that write into a block that others hold get one of their own
+    cache.plan_device(lead, members, start=step["start"], count=step["count"])   # for all layers of the step
     for layer in layers:
         cache.copy_device(layer, step["copy_src"], step["copy_dst"])   # ... with what it held, before anything is appended
         cache.append_device(layer, k, v, step["slot"])
-    cache.plan_device(lead, members, start=step["start"], count=step["count"])   # for all layers of the step
-    for layer in layers:
         cache.attend_shared_device(layer, q, out)             # what rows hold together is read once
 """
 from __future__ import annotations
