@@ -91,6 +91,52 @@ def test_tables(case):
     cache.close()
 
 
+@pytest.mark.parametrize("case", [(256, 40, 16, 20000, 1024), (256, 1000, 16, 60000, 64), (2, 200, 16, 4000, 12), (4200, 8, 16, 100, 4), (1, 40, 16, 262144, 11000), (5, 16, 32, 3000, 128), (3, 30, 64, 3000, 100)], ids=str)
+def test_forks_of_many_entries(case):
+    """Every way in which a fork's work is divided: lengths, tables, holders, and each row's last block (by what the next step asks to be copied)."""
+    torch = _torch()
+    W, B, b, N, M = case
+    _say("forks", case)
+    g = torch.Generator("cuda").manual_seed(B)
+    r = lambda lo, hi, *shape: torch.randint(lo, hi, shape, generator=g, device="cuda:0", dtype=torch.int32)
+    place = torch.arange(M, device="cuda:0", dtype=torch.int32)
+    lens = r(0, M * b + 1, W, B)
+    lens[:, 0], lens[:, 1] = M * b, 0
+    table = torch.where(place < ((lens + b - 1) // b)[..., None], r(0, N, W, B, M), -1).int()
+    for k in range(0, B - 1, 3):  # (rows that begin alike)
+        n = torch.minimum((lens[:, k] + b - 1) // b, (lens[:, k + 1] + b - 1) // b) // 2
+        table[:, k + 1] = torch.where(place < n[:, None], table[:, k], table[:, k + 1])
+    cache = kv.KvCache(kv.KvConfig(n_workers=W, rows=B, block_tokens=b, n_blocks=N, max_blocks=M, n_kv_heads=1, n_q_heads=1, head_dim=64, shared=True), lens=lens, table=table)
+    step = cache.alloc_step(4 * B)
+    for turn in range(2):
+        frm, cut = r(0, B, W, B), r(-100, M * b + 50, W, B)
+        own = r(0, 10, W, B)
+        frm = torch.where(own < 2, torch.arange(B, device="cuda:0", dtype=torch.int32), torch.where(own == 3, -1, torch.where(own == 4, torch.arange(B, device="cuda:0", dtype=torch.int32) // 3 * 3, frm))).int()
+        stays = (frm < 0) | (frm >= B)
+        take = torch.where(stays, torch.arange(B, device="cuda:0", dtype=torch.int32), frm).long()
+        held = lens.gather(1, take)
+        lens2 = torch.where(stays | (cut < 0), held, torch.minimum(held, cut)).int()
+        table2 = torch.where(place < ((lens2 + b - 1) // b)[..., None], table.gather(1, take[..., None].expand(-1, -1, M)), -1).int()
+        cache.fork_device(frm, cut)
+        lens, table = lens2, table2
+        torch.cuda.synchronize()
+        assert torch.equal(cache.lens, lens) and torch.equal(cache.table, table), (case, turn)
+        ids = torch.where(table >= 0, table, N).view(W, -1).long()
+        holders = torch.zeros((W, N + 1), dtype=torch.int32, device="cuda:0").scatter_add_(1, ids, torch.ones_like(ids, dtype=torch.int32))[:, :N]
+        assert torch.equal(cache.holders, holders), (case, turn)
+    cache.step_device(torch.full_like(lens, -1), ((lens > 0) & (lens < M * b)).int(), step)
+    torch.cuda.synchronize()
+    last = table.gather(2, torch.clamp((lens - 1) // b, min=0)[..., None].long())[..., 0]
+    several = holders.gather(1, torch.clamp(last, min=0).long()) > 1
+    want = torch.where((lens % b != 0) & several, last, -1)
+    assert not bool(step["status"].any()) and torch.equal(step["copy_src"], want.int()), case
+    now = torch.zeros((W, N + 1), dtype=torch.int32, device="cuda:0")
+    ids = torch.where(cache.table >= 0, cache.table, N).view(W, -1).long()
+    now.scatter_add_(1, ids, torch.ones_like(ids, dtype=torch.int32))
+    assert torch.equal(cache.holders, now[:, :N]) and torch.equal(step["stats"][:, 1], (now[:, :N] > 0).sum(1)), case
+    cache.close()
+
+
 def test_requests_at_the_start_may_share_blocks():
     """Ids outside the worker's blocks count as none, lengths are clamped, stale entries are not looked at."""
     b, N, M = 16, 40, 6
@@ -246,7 +292,8 @@ def test_attention_of_rows_that_share_blocks():
 
 
 # -- copies ---------------------------------------------------------------------------
-@pytest.mark.parametrize("case", [(1, 1, 16, 64, 1), (3, 5, 32, 96, 7), (2, 3, 128, 256, 40), (4, 17, 64, 128, 0), (2, 1, 16, 192, 300)], ids=str)
+@pytest.mark.parametrize("case", [(1, 1, 16, 64, 1), (3, 5, 32, 96, 7), (2, 3, 128, 256, 40), (4, 17, 64, 128, 0), (2, 1, 16, 192, 300),
+                                  (7, 1, 16, 96, 300), (3, 1, 32, 64, 700), (9, 1, 16, 64, 230), (2, 2, 16, 64, 1100)], ids=str)
 def test_copies(case):
     """Bytes and scales of blocks, also from worker to worker; pairs that are none; nothing else changes."""
     torch = _torch()
