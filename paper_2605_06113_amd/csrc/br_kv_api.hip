@@ -195,9 +195,9 @@ bool attention_ok(const br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_at
 
 // Rows of many queries share their block's token tiles, those of few have waves of their own: two launches where a call may have
 // both (two chunks of 512 tokens beside 46 single ones: 375 us in one launch).  few_rows: query rows up to which a row goes with the few; most_tiles: query tiles that
-// one launch for many queries may have, at least, where the tables span few token tiles.
+// one launch for many queries may have, at least, where the tables span few token tiles; most_few: query tiles of 64 rows that go with the few there.
 template <class Fn>
-int32_t attend_by_rows(br_kv_ctx *ctx, BrKvAttend &p, int max_count, int few_rows, int64_t most_tiles, Fn &&launch) {
+int32_t attend_by_rows(br_kv_ctx *ctx, BrKvAttend &p, int max_count, int few_rows, int64_t most_tiles, int64_t most_few, Fn &&launch) {
   const br_kv_config &c = ctx->cfg;
   const int group = p.group;
   const int64_t rows = (int64_t)max_count * group;
@@ -205,6 +205,8 @@ int32_t attend_by_rows(br_kv_ctx *ctx, BrKvAttend &p, int max_count, int few_row
   // 8 key heads, near the line, 27 to 33 us and 38.
   const int64_t tiles = (int64_t)p.n_rows * c.n_kv_heads * ((((int64_t)c.max_blocks << ctx->t.shift) + BR_KV_TILE - 1) / BR_KV_TILE);
   const bool both = rows > 64 && (tiles > 8 * ctx->cus || (int64_t)p.n_rows * c.n_kv_heads > most_tiles);
+  const int64_t by64 = (rows + 63) / 64;
+  if (!both && rows > 64 && by64 * p.n_rows * c.n_kv_heads <= most_few && by64 * tiles <= 32 * ctx->cus) return enqueue(ctx, [&] { launch(p, BR_KV_TILE_64); });
   const int few = both ? few_rows / group : 0;  // query tokens up to which a row of a mixed call goes with the few
   p.least = 1, p.most = both ? few : INT32_MAX;
   if (rows <= 64 || few > 0) {
@@ -327,7 +329,7 @@ int32_t br_kv_attend(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_atten
   if (a->n_tokens == 0) return BR_OK;
   BrKvAttend args;
   if (!attention_of(ctx, layer, a, 1, args)) return BR_EINVAL;
-  return attend_by_rows(ctx, args, a->max_count, 16, INT64_MAX, [&](const BrKvAttend &p, int tile) { BR_KV_BY_DIM(br_kv_launch_attend) });
+  return attend_by_rows(ctx, args, a->max_count, 16, INT64_MAX, 0, [&](const BrKvAttend &p, int tile) { BR_KV_BY_DIM(br_kv_launch_attend) });
 }
 
 int32_t br_kv_attend_diff(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *a, const br_kv_diff *diff) {
@@ -341,7 +343,9 @@ int32_t br_kv_attend_diff(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_
   // Where one launch has a block for each query tile nothing is joined: 40 rows of up to 100 tokens, one of them with 16 queries, 7 key heads, D 96, 13.9 us and 33.6 in
   // two; 80 of them 52 and 34, 162 of up to 24 tokens 50 and 20.  D 192, a block to a compute unit: 20 rows 16.3 and 27, 40 rows 78 and 41.
   const int64_t most_tiles = (int64_t)(ctx->cfg.head_dim <= 128 ? 2 : 1) * ctx->cus;
-  return attend_by_rows(ctx, args, a->max_count, few_rows, most_tiles, [&](const BrKvAttend &p, int tile) { BR_KV_BY_DIM(br_kv_launch_diff) });
+  // Few query tiles, spread over the card in parts: one row of 1000 tokens, 32 to 128 of them queries, groups of 4, 8 key heads, D 128, 38 us by the kernel of many rows, 23
+  // to 28 by the other one; with 192 queries 39 and 45.  60 queries behind 12000 tokens, D 192, 112 and 129.
+  return attend_by_rows(ctx, args, a->max_count, few_rows, most_tiles, ctx->cus / 2, [&](const BrKvAttend &p, int tile) { BR_KV_BY_DIM(br_kv_launch_diff) });
 }
 
 int32_t br_kv_plan(br_kv_ctx *ctx, const br_kv_families *in) {

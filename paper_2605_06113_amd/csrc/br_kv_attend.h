@@ -21,6 +21,8 @@
 #ifndef BR_KV_ATTEND_H
 #define BR_KV_ATTEND_H
 
+#include <type_traits>
+
 #include "br_kv_device.h"
 
 #define BR_KV_NEG (-__builtin_inff())
@@ -709,9 +711,9 @@ __device__ __forceinline__ T br_kv_scalar(T x) {
 
 // The division of a call's tiles among `workers` (waves, groups of waves, or blocks: NR to a block).  Where there are few query tiles and
 // none is much longer than an equal share, each goes to a block, in NR parts: nothing is left to be joined through memory, which
-// takes about as long as SLACK tiles.  Else the workers get runs of tiles that differ by one at most.  What is dealt are units: tiles, or a
-// query tile's NR parts.
-template <int TQ, int NT, int NR, int SLACK, int MODE>
+// takes about as long as SLACK tiles.  Else the workers get runs of tiles that differ by one at most, or query tiles in other parts (below).  What is dealt are units: tiles,
+// or a query tile's parts.
+template <int TQ, int NT, int NR, int SLACK, int MODE, int JOIN = SLACK, int ROUNDS = SLACK>
 struct BrKvRuns {
   static constexpr bool MANY = TQ > 64;  // a row may well have more than one query tile
   struct Shared {
@@ -723,7 +725,7 @@ struct BrKvRuns {
   long long all;
   unsigned share, extra;  // a worker has `share` units, and extra / 2^32 of one more
   int per, workers;
-  bool parts;  // the units are parts of query tiles
+  std::conditional_t<MODE == BR_KV_PLAIN, bool, int> parts;  // the units are parts of query tiles, so many to each (NR); 0: tiles
   int log_per_row;  // 2^.. threads count a row's tiles (chunks of thousands of query rows have many: one thread 5 us); the first has the sum
 
   // (a worker gets at least `least` tiles, if there are as many)
@@ -781,9 +783,30 @@ struct BrKvRuns {
     // each: 34 us)
     share = (unsigned)q, extra = (unsigned)((double)left * 4294967296.0 * (1.0 / workers) + 0.5);
     all = total;
-    parts = total_q <= workers_most && (most + NR - 1) / NR <= (int)min(q, 1ll << 20) + SLACK;
-    if (parts) workers = total_q, all = total_q, share = 1, extra = 0, sum = sum_q;
+    const int whole = (most + NR - 1) / NR;
+    parts = total_q <= workers_most && whole <= (int)min(q, 1ll << 20) + SLACK;
+    if constexpr (MODE != BR_KV_PLAIN) {
+      // A run that ends one query tile and begins another goes through two chains of loads and joins, 10 us; so other divisions come first.  K blocks to each query
+      // tile: 32 companies of 8 rows that hold 2000 tokens (D 128, 4 query heads) 30 us in runs, 21 so; two maps of 32 query heads on one key head, one row of 4000
+      // tokens, 57 and 30; 96 rows of 8, 2000 tokens, 36 and 29, though a part is up to 12 tiles over the mean.  One block is better where K save less than JOIN.
+      const int k = 2 * total_q <= workers_most ? max(1, min(workers_most / max(total_q, 1), most / (NR * least))) : 1;
+      const int split = (most + NR * k - 1) / (NR * k);
+      if (k > 1) parts = whole <= split + JOIN;
+      parts *= NR;
+      if (k > 1 && !parts && split <= (int)min(q, 1ll << 20) + 16) parts = NR * k, total_q *= k, sum_q *= k;
+      // More query tiles than blocks: whole ones, one after the other.  152 rows of 2 (300 tokens, D 128, 12 query heads, 5 key heads) 39 us in runs, 30 so; 1103 tokens 52 and 40;
+      // with 40 over the mean for two waves to a tile too, 300 rows of 8 (1103, 8 query heads, 8 key heads) 57 and 67.
+      if (NR == 1 && total_q > workers_most && total_q <= 8 * workers_most) {
+        const int rounds = (total_q + workers_most - 1) / workers_most;
+        if (rounds * most <= (int)min(q, 1ll << 20) + ROUNDS) {
+          parts = 1, workers = workers_most, all = total_q, sum = sum_q;
+          share = total_q / workers, extra = (unsigned)((double)(total_q - (int)share * workers) * 4294967296.0 * (1.0 / workers) + 0.5);
+        }
+      }
+    }
+    if (parts && total_q <= workers_most) workers = total_q, all = total_q, share = 1, extra = 0, sum = sum_q;
     share = br_kv_scalar(share), extra = br_kv_scalar(extra), workers = br_kv_scalar(workers), all = br_kv_scalar(all);
+    if (MODE != BR_KV_PLAIN) parts = br_kv_scalar(parts);
     s.before[tid + 1] = sum;
     if (tid == 0) s.before[0] = 0;
     __syncthreads();
@@ -793,7 +816,7 @@ struct BrKvRuns {
     if (w.n <= 0) return 0;
     long long tiles;
     int most;
-    if (parts) return (int)(((long long)w.n * p.group + TQ - 1) / TQ) * NR;
+    if (parts) return (int)(((long long)w.n * p.group + TQ - 1) / TQ) * (MODE == BR_KV_PLAIN ? NR : parts);
     if (MANY) {
       br_kv_row_tiles<TQ, MODE>(p, w, tiles, most, threadIdx.x & 63, 64);
       for (int d = 1; d < 64; d <<= 1) tiles += __shfl_xor(tiles, d, 64);
@@ -802,7 +825,7 @@ struct BrKvRuns {
     }
     return tiles;
   }
-  __device__ __forceinline__ int units_of(int size) const { return parts ? NR : size; }
+  __device__ __forceinline__ int units_of(int size) const { return parts ? (MODE == BR_KV_PLAIN ? NR : parts) : size; }
   __device__ __forceinline__ long long begin_of(int k) const {
     const long long at = (long long)((unsigned long long)(unsigned)k * share + __umulhi((unsigned)k, extra));
     return k < workers ? at : all;
@@ -953,9 +976,10 @@ struct BrKvShare {
 template <int D, int SHARE, bool FP8, bool HALF, int NW, int WAVES, int MODE>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   constexpr int TQ = 16 * SHARE, NT = 64 * NW, ND = D / 16, NR = NW / SHARE;  // NR: runs of a block
-  // (6 and 2, with two maps and with companies: one row of 2000 tokens beside seven, 8 key heads of 128 channels 24.5 us and 18.1; four beams of 3000 33.3 and 20.7)
-  constexpr int SLACK = MODE == BR_KV_PLAIN ? 6 : 2;
-  using Runs = BrKvRuns<TQ, NT, NR, SLACK, MODE>;
+  // (6 and 1, with two maps and with companies: one row of 2000 tokens beside seven, 8 key heads of 128 channels 24.5 us and 18.1; four beams of 3000 33.3 and 18.6.  Pieces of
+  // many rows are large: two maps of 32 query heads on a key head, D 192, a row of 4000 tokens 69 us with 1 and 54 with 4; of 16 heads 39 with 1 and 32 with 2)
+  constexpr int SLACK = MODE == BR_KV_PLAIN ? 6 : 2, LEAST = MODE == BR_KV_PLAIN || SHARE == 1 ? 1 : SHARE == 2 || D <= 128 ? 2 : 4;
+  using Runs = BrKvRuns<TQ, NT, NR, SLACK, MODE, 0>;
   __shared__ typename Runs::Shared shared;
   __shared__ br_f4 kept[2 * NW * ND * 64];  // piece 2 k: taken up by run k, 2 k + 1: begun by it
   __shared__ float2 kept_ml[2 * NW * 16];
@@ -963,7 +987,7 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   __shared__ BrKvShare chains[NR + 1];  // of the query tile that run k has begun; the last: of one that an earlier block has
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), rn = wv / SHARE, row = 16 * (wv % SHARE);  // the wave's run, its first query row of the tile
-  Runs runs(p, shared, gridDim.x, 1);
+  Runs runs(p, shared, gridDim.x, LEAST);
   // runs that follow each other go to one XCD (blocks go round them), which has what they share in its L2
   const int blocks = (runs.workers + NR - 1) / NR, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
   if (wg >= blocks) return;
@@ -1288,11 +1312,10 @@ template <int D, int TQ, int NQ, bool FP8, int NW, int WAVES>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend_together(BrKvAttend p) {
   constexpr int MODE = NQ == 2 ? BR_KV_SHARED_32 : BR_KV_SHARED_16, NT = 64 * NW, ND = D / 16, NH = TQ / (16 * NQ), P = NW / NH;
   // A block that has fewer than LEAST tiles pays more for its pieces than it saves: with 8 for all, 20 rows of 11 key heads that hold 4339 tokens
-  // together (D 256, 6 query heads each) 96 us, here 57; 152 rows of 5 (1103 tokens, D 128, 12 query heads) 99, here 56; 2 / NH to 4 / NH: 4 rows of 8
-  // (30000 tokens, D 128) 40 as here, 16 rows of 4 (4000, D 192) 50 and 43.  And one whose company is no more than SLACK tiles over an equal share keeps it: 32
-  // rows of 8 (500 tokens, D 128, 4 query heads) 30 us with half of that, 25 so, and 16 of 8 (500, D 192, 2 query heads) 31 with twice that, 22 so.
-  constexpr int LEAST = 8 / NH, SLACK = 20 / NH;
-  using Runs = BrKvRuns<TQ, NT, 1, SLACK, MODE>;
+  // together (D 256, 6 query heads each) 96 us, here 59; for one wave to a tile, 8 rows of 8 (500 tokens, D 128, 4 query heads) 22 and 19; with 2 for two, 8 rows of 8
+  // (2000, 8 query heads) 29 and 27.  JOIN: 96 rows of 8 (500, 4 query heads) 25 us with 12 / NH, 23 so, 32 of them with 20 / NH 23, 20 so.
+  constexpr int LEAST = NH < 2 ? 4 : 8 / NH, SLACK = 20 / NH, JOIN = NH < 2 ? 16 : 12 / NH, ROUNDS = NH < 2 ? 40 : 20 / NH;
+  using Runs = BrKvRuns<TQ, NT, 1, SLACK, MODE, JOIN, ROUNDS>;
   __shared__ typename Runs::Shared shared;
   __shared__ br_f4 kept[NW * NQ * ND * 64];
   __shared__ float2 kept_ml[NW * NQ * 16];

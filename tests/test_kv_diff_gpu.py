@@ -118,6 +118,16 @@ def test_long_rows_that_many_blocks_share():
     _case("long", "fp8", "float16", 96, 1, 9, 32, [[7000, 5000]], [[2, 1]])
 
 
+@pytest.mark.parametrize("D", [64, 128, 192, 256])
+def test_divisions_of_the_work(D):
+    """A query tile to a block, to several blocks, several to a block; few and many query rows; calls of both in one launch and in two."""
+    rng = np.random.default_rng(D)
+    for tag, H, group, lens, counts in (("split", 1, 16, [[2000]], [[1]]), ("split", 2, 32, [[1500, 1600]], [[1, 1]]), ("split", 2, 4, [[1800]], [[12]]), ("split", 1, 8, [[1500, 300]], [[40, 5]]),
+                                        ("many", 2, 4, [[700]], [[300]]), ("rounds", 3, 4, [rng.integers(1, 90, 200)], [[17] + [1] * 199]), ("rounds", 2, 12, [rng.integers(5, 60, 300)], [[1] * 299 + [5]]),
+                                        ("one", 2, 4, [rng.integers(20, 90, 30)], [[20] + [1] * 29])):
+        _case((tag, H, group), "int8" if group % 8 else "fp8", "bfloat16", D, H, group, 32, np.asarray(lens), np.asarray(counts))
+
+
 def test_rows_that_are_not_aligned_and_scales_of_any_sign():
     _case("narrow", "int8", "float16", 64, 2, 3, 16, [[100, 400]], [[1, 2]], wide=False, per_token=True)
     _case("narrow", "fp8", "bfloat16", 128, 1, 2, 32, [[100, 300]], [[40, 70]], wide=False)

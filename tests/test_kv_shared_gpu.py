@@ -142,6 +142,17 @@ def test_many_rows_and_workers():
     _case("rows", "int8", "float16", 64, 1, 1, 64, lens, _families(1024, 1024), 2, 1024)
 
 
+@pytest.mark.parametrize("D", [64, 128, 192, 256])
+def test_divisions_of_the_work(D):
+    """A company to a block, to several blocks, several to a block, and cut wherever a block's share ends."""
+    rng = np.random.default_rng(D)
+    for tag, rows, family, members, group, shared, own, H in (("split", 8, 8, 8, 4, 1920, 100, 1), ("split", 5, 5, 5, 12, 2304, 30, 2), ("split", 4, 4, 4, 4, 1500, 60, 3), ("one each", 24, 8, 8, 4, 128, 60, 2),
+                                                          ("rounds", 264, 2, 2, 12, 64, 40, 2), ("rounds", 180, 4, 4, 16, 64, 70, 7), ("cut", 264, 2, 2, 9, 64, 40, 2), ("cut", 12, 4, 4, 5, 640, 100, 2)):
+        lens = shared + rng.integers(0, own, (1, rows))
+        lens[:, :2] += 4000 * (tag == "cut")
+        _case((tag, rows), "fp8" if group % 8 else "int8", "bfloat16", D, H, group, 64, lens, _families(rows, family), -(-shared // 64), members, seed=rows)
+
+
 def test_long_prefixes_that_many_blocks_share():
     _case("long", "fp8", "bfloat16", 128, 2, 4, 64, [[20000, 20100, 19900, 20001]], [[0] * 4], 300, 4)
     _case("long", "int8", "float16", 64, 1, 8, 16, [[9000, 9500, 30, 9100, 9000]], [[0, 0, 2, 0, 0]], 560, 5, wide=False)
