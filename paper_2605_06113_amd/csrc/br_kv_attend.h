@@ -789,8 +789,8 @@ struct BrKvRuns {
       // A run that ends one query tile and begins another goes through two chains of loads and joins, 10 us; so other divisions come first.  K blocks to each query
       // tile: 32 companies of 8 rows that hold 2000 tokens (D 128, 4 query heads) 30 us in runs, 21 so; two maps of 32 query heads on one key head, one row of 4000
       // tokens, 57 and 30; 96 rows of 8, 2000 tokens, 36 and 29, though a part is up to 12 tiles over the mean.  One block is better where K save less than JOIN.
-      const int k = 2 * total_q <= workers_most ? max(1, min(workers_most / max(total_q, 1), most / (NR * least))) : 1;
-      const int split = (most + NR * k - 1) / (NR * k);
+      const int k = whole > 1 && 2 * total_q <= workers_most ? max(1, min(workers_most / max(total_q, 1), most / (NR * least))) : 1;
+      const int split = k > 1 ? (most + NR * k - 1) / (NR * k) : whole;
       if (k > 1) parts = whole <= split + JOIN;
       parts *= NR;
       if (k > 1 && !parts && split <= (int)min(q, 1ll << 20) + 16) parts = NR * k, total_q *= k, sum_q *= k;
@@ -971,8 +971,8 @@ struct BrKvShare {
 // each its share of the channels.  Bound by memory: each code comes once from there (waves of one run find it in the caches).  144 rows
 // of 256 to 8192 tokens, 8 key heads of 128 channels, groups of 8: 128 us, 691 MB = 5.4 TB/s (a large copy: 5.1).  One row of 40 thousand
 // tokens: 26 us, 87 MB, of them some 6 us for the pieces' way through LDS and memory; one of 500 13 us, a launch and a chain
-// of loads (lengths, ids, codes, the join).  By two maps the same rows 127 us = 5.5 TB/s, and 12.8 the short one; four beams that hold 900 tokens together 20: a block
-// for each key head, whose waves have two or three tiles of 2.5 us (their instructions, not their loads: values a tile ahead change nothing).
+// of loads (lengths, ids, codes, the join).  By two maps the same rows 127 us = 5.4 TB/s, and 13 the short one; four beams that hold 900 tokens together 19: two blocks
+// for each key head, whose waves have one or two tiles of 2.5 us (their instructions, not their loads: values a tile ahead change nothing).
 template <int D, int SHARE, bool FP8, bool HALF, int NW, int WAVES, int MODE>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   constexpr int TQ = 16 * SHARE, NT = 64 * NW, ND = D / 16, NR = NW / SHARE;  // NR: runs of a block
@@ -1129,7 +1129,7 @@ __device__ __forceinline__ void br_kv_ahead(Get &&get, Use &&use) {
 // tile.  Bound by the issue of vector instructions between the products (310 a tile and wave, 32 of them exponentials, to 64 products): chunks
 // of 512 tokens of two rows, groups of 4, 8 key heads of 128 channels behind up to 8192 tokens 207 us, 0.61 PFLOP/s; a wave issues in 44 %
 // of its time and waits for its turn, beside the other wave of its SIMD, in 30 %; the matrix units are busy a third.  By two maps, twice the
-// query rows and weights, 319 us (with 46 single rows beside them 349, and 17 more with
+// query rows and weights, 320 us (with 46 single rows beside them 354, and 17 more with
 // the half of the scores' products that is 0).
 template <int D, int NQ, bool FP8, int WAVES, int MODE>
 __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) {
@@ -1305,7 +1305,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
 // between them before the run's end, where the P sums of a row are joined in LDS.  A tile is decoded TQ / (16 NQ) times.  The queries are in LDS: in
 // registers they drove others out to memory, and every reload of those waited for the codes on their way (96 rows of 8 to a company, groups of 8, up to 16384
 // tokens together, 8 key heads of 128 channels, fp8: 72 us, 66 with them in LDS; a tile through LDS for all four waves of a block, as for many rows above: 84, and 98 by
-// the kernel of few rows).  Such a call, 184 MB, out of memory 75 us: two waves on a SIMD, each waits for its values' codes about as long as it computes.  Calls of a few
+// the kernel of few rows).  Such a call, 184 MB, out of memory 72 us: two waves on a SIMD, each waits for its values' codes about as long as it computes.  Calls of a few
 // companies are bound by a chain instead: division and place 2.3 us, the members 1.2, queries and first codes 4.5, each tile of a wave 2.5 (some 900 vector
 // instructions, two waves to a SIMD), the join in LDS 2, through memory some 7 more.
 template <int D, int TQ, int NQ, bool FP8, int NW, int WAVES>
