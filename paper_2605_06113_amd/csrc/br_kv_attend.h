@@ -976,8 +976,9 @@ struct BrKvShare {
 template <int D, int SHARE, bool FP8, bool HALF, int NW, int WAVES, int MODE>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   constexpr int TQ = 16 * SHARE, NT = 64 * NW, ND = D / 16, NR = NW / SHARE;  // NR: runs of a block
-  // (6 and 1, with two maps and with companies: one row of 2000 tokens beside seven, 8 key heads of 128 channels 24.5 us and 18.1; four beams of 3000 33.3 and 18.6.  Pieces of
-  // many rows are large: two maps of 32 query heads on a key head, D 192, a row of 4000 tokens 69 us with 1 and 54 with 4; of 16 heads 39 with 1 and 32 with 2)
+  // (With two maps and with companies, 6 and 2: one row of 2000 tokens beside seven, 8 key heads of 128 channels 24.5 us and 18.1, four beams of 3000 33.3 and 20.7, 18.6 in parts.
+  // Pieces of many rows are large: two maps of 32 query heads on a key head, D 192, a row of 4000 tokens 69 us with a least of 1 and 54 with 4; of 16 heads 39 with 1 and 32
+  // with 2; 32 heads of D 128 35 with 1, 29 with 2, 30 with 4)
   constexpr int SLACK = MODE == BR_KV_PLAIN ? 6 : 2, LEAST = MODE == BR_KV_PLAIN || SHARE == 1 ? 1 : SHARE == 2 || D <= 128 ? 2 : 4;
   using Runs = BrKvRuns<TQ, NT, NR, SLACK, MODE, 0>;
   __shared__ typename Runs::Shared shared;
