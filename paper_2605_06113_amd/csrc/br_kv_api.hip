@@ -353,7 +353,10 @@ int32_t br_kv_plan(br_kv_ctx *ctx, const br_kv_families *in) {
   const br_kv_config &c = ctx->cfg;
   const int group = c.n_q_heads / c.n_kv_heads, members = in->members < c.rows ? in->members : c.rows;
   const int rows = members * group;  // (both at most 1024)
-  const int tile = rows <= 16 ? BR_KV_TILE_16 : rows <= 32 ? BR_KV_TILE_32 : BR_KV_TILE_64, fit = (16 << tile) / group;
+  // Of wide heads each wave decodes a tile for 16 query rows alone: 32 rows have half of that in a row, and as many blocks again, where four members are among them.
+  // D 256, 16 rows of 8 that hold up to 4000 tokens, 8 query heads 64 us by 64 rows and 36, 96 of 8 114 and 85; D 192 42 and 28, 67 and 57; but 16 query heads, 96 rows of 4: 141 and 154, 87 and 98.
+  const int large = c.head_dim > 128 && 4 * group <= 32 ? BR_KV_TILE_32 : BR_KV_TILE_64;
+  const int tile = rows <= 16 ? BR_KV_TILE_16 : rows <= 32 ? BR_KV_TILE_32 : large, fit = (16 << tile) / group;
   char *base = (char *)c.workspace;
   BrKvPlan x;
   x.lead = in->lead, x.start = in->start, x.count = in->count;
