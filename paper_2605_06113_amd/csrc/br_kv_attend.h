@@ -789,11 +789,13 @@ struct BrKvRuns {
       // A run that ends one query tile and begins another goes through two chains of loads and joins, 10 us; so other divisions come first.  K blocks to each query
       // tile: 32 companies of 8 rows that hold 2000 tokens (D 128, 4 query heads) 30 us in runs, 21 so; two maps of 32 query heads on one key head, one row of 4000
       // tokens, 57 and 30; 96 rows of 8, 2000 tokens, 36 and 29, though a part is up to 12 tiles over the mean.  One block is better where K save less than JOIN.
-      const int k = whole > 1 && 2 * total_q <= workers_most ? max(1, min(workers_most / max(total_q, 1), most / (NR * least))) : 1;
+      // The join goes over K pieces as the blocks go over most / K tiles, so K is about the root of `most`: one row of 40000 tokens, two maps of 32 query heads on a key
+      // head, 100 us with as many as there are blocks for, 54 with 32; of 12000 tokens 44 and, with 16, 36.
+      const int k = whole > 1 && 2 * total_q <= workers_most ? max(1, min(min(workers_most / max(total_q, 1), (int)__builtin_amdgcn_sqrtf((TQ > 16 ? 2.0f : 6.0f) * most)), most / (NR * least))) : 1;
       const int split = k > 1 ? (most + NR * k - 1) / (NR * k) : whole;
       if (k > 1) parts = whole <= split + JOIN;
       parts *= NR;
-      if (k > 1 && !parts && split <= (int)min(q, 1ll << 20) + 16) parts = NR * k, total_q *= k, sum_q *= k;
+      if (k > 1 && !parts && split <= max((int)min(q, 1ll << 20), (int)((float)total * __builtin_amdgcn_rcpf((float)(total_q * k)))) + 16) parts = NR * k, total_q *= k, sum_q *= k;
       // More query tiles than blocks: whole ones, one after the other.  152 rows of 2 (300 tokens, D 128, 12 query heads, 5 key heads) 39 us in runs, 30 so; 1103 tokens 52 and 40;
       // with 40 over the mean for two waves to a tile too, 300 rows of 8 (1103, 8 query heads, 8 key heads) 57 and 67.
       if (NR == 1 && total_q > workers_most && total_q <= 8 * workers_most) {
@@ -1313,7 +1315,7 @@ template <int D, int TQ, int NQ, bool FP8, int NW, int WAVES>
 __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend_together(BrKvAttend p) {
   constexpr int MODE = NQ == 2 ? BR_KV_SHARED_32 : BR_KV_SHARED_16, NT = 64 * NW, ND = D / 16, NH = TQ / (16 * NQ), P = NW / NH;
   // A block that has fewer than LEAST tiles pays more for its pieces than it saves: with 8 for all, 20 rows of 11 key heads that hold 4339 tokens
-  // together (D 256, 6 query heads each) 96 us, here 59; for one wave to a tile, 8 rows of 8 (500 tokens, D 128, 4 query heads) 22 and 19; with 2 for two, 8 rows of 8
+  // together (D 256, 6 query heads each, by 64 rows) 96 us, here 59; for one wave to a tile, 8 rows of 8 (500 tokens, D 128, 4 query heads) 22 and 19; with 2 for two, 8 rows of 8
   // (2000, 8 query heads) 29 and 27.  JOIN: 96 rows of 8 (500, 4 query heads) 25 us with 12 / NH, 23 so, 32 of them with 20 / NH 23, 20 so.
   constexpr int LEAST = NH < 2 ? 4 : 8 / NH, SLACK = 20 / NH, JOIN = NH < 2 ? 16 : 12 / NH, ROUNDS = NH < 2 ? 40 : 20 / NH;
   using Runs = BrKvRuns<TQ, NT, 1, SLACK, MODE, JOIN, ROUNDS>;
