@@ -27,6 +27,7 @@
 
 #define BR_KV_NEG (-__builtin_inff())
 #define BR_KV_LEAST_TILES 8  // of a block with many query rows: its pieces are large
+#define BR_KV_COUNTED 4096   // query tiles that a thread counts, at most: a sum below it is exact
 
 // What the kernels below are instantiated for.
 //   PLAIN   a row's queries, and its tokens
@@ -742,7 +743,7 @@ struct BrKvRuns {
       if (w.n <= 0) continue;
       long long tiles;
       int longest;
-      mine_q = min(mine_q + br_kv_row_tiles<TQ, MODE>(p, w, tiles, longest, one, 1 << log_per_row), 4096);
+      mine_q = min(mine_q + br_kv_row_tiles<TQ, MODE>(p, w, tiles, longest, one, 1 << log_per_row), BR_KV_COUNTED);
       mine += tiles, most = max(most, longest);
     }
     if (MANY) {
@@ -798,7 +799,7 @@ struct BrKvRuns {
       if (k > 1 && !parts && split <= max((int)min(q, 1ll << 20), (int)((float)total * __builtin_amdgcn_rcpf((float)(total_q * k)))) + 16) parts = NR * k, total_q *= k, sum_q *= k;
       // More query tiles than blocks: whole ones, one after the other.  152 rows of 2 (300 tokens, D 128, 12 query heads, 5 key heads) 39 us in runs, 30 so; 1103 tokens 52 and 40;
       // with 40 over the mean for two waves to a tile too, 300 rows of 8 (1103, 8 query heads, 8 key heads) 57 and 67.
-      if (NR == 1 && total_q > workers_most && total_q <= 8 * workers_most) {
+      if (NR == 1 && total_q > workers_most && total_q < min(8 * workers_most, BR_KV_COUNTED)) {
         const int rounds = (total_q + workers_most - 1) / workers_most;
         if (rounds * most <= (int)min(q, 1ll << 20) + ROUNDS) {
           parts = 1, workers = workers_most, all = total_q, sum = sum_q;

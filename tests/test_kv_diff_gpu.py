@@ -135,6 +135,34 @@ def test_rows_that_are_not_aligned_and_scales_of_any_sign():
         _case("scale", "int8", "bfloat16", 64, 1, 4, 16, [[300, 50]], [[1, 40]], scale=scale)
 
 
+def test_more_query_tiles_than_a_thread_counts():
+    """One row of some 5000 query tiles behind a short window: what pieces of it give, every token of it."""
+    torch = _torch()
+    n, step, window, b, D = 330000, 33000, 150, 128, 64
+    _say("diff", "query tiles", n // 64)
+    M = -(-n // b)
+    cache = kv.KvCache(kv.KvConfig(rows=1, block_tokens=b, n_blocks=M, max_blocks=M, n_kv_heads=1, n_q_heads=1, head_dim=D), lens=_dev(np.array([[n]]), torch.int32),
+                       table=_dev(np.arange(M, dtype=np.int32).reshape(1, 1, M)))
+    g = torch.Generator("cuda").manual_seed(5)
+    layer = cache.new_layer()
+    for x in (layer.k, layer.v):
+        x.copy_(torch.randint(0, 256, x.shape, generator=g, device="cuda:0", dtype=torch.uint8))
+    layer.k_scale.fill_(0.01), layer.v_scale.fill_(1 / 128)
+    q = torch.randn((n, 1, D), generator=g, device="cuda:0").half()
+    lam = torch.full((1,), 0.3, device="cuda:0")
+    out, want, lse, lse_want = torch.full_like(q, 7.0), torch.full_like(q, 7.0), torch.zeros((n, 1, 2), device="cuda:0"), torch.ones((n, 1, 2), device="cuda:0")
+    one = lambda x: _dev(np.array([[x]]), torch.int32)
+    cache.attend_diff_device(layer, q, out, lam, lse=lse, start=one(0), count=one(n), max_count=n, window=window)
+    for at in range(0, n, step):
+        cache.attend_diff_device(layer, q, want, lam, lse=lse_want, start=one(at), count=one(step), max_count=step, window=window, lens=one(at + step))
+    torch.cuda.synchronize()
+    # values of 1 at most: in both results the maps' weights are off by 2^-11 + 2^-15 of them (scores and sums of magnitudes up to 24: 2^-20 of 32), the second map's times
+    # 0.3, and each result is rounded by half a step of 1.3
+    assert (out.float() - want.float()).abs().max() <= 2 * 1.3 * (2.0 ** -11 + 2.0 ** -15 + 2.0 ** -11)
+    assert torch.allclose(lse, lse_want, atol=2 * 2.0 ** -15, rtol=0)
+    cache.close()
+
+
 def test_more_queries_than_said():
     _case("more", "int8", "bfloat16", 64, 2, 4, 16, [[300, 200, 100]], [[9, 1, 30]], max_count=1)
 
