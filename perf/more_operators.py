@@ -1,5 +1,4 @@
-"""Measured cases of what a worker does with blocks that several requests hold, of the attention that reads those once, and of differential
-attention over its cache.
+"""Measured cases of what a worker does with blocks that several requests hold, and of differential attention over its cache.
 
 Requests that begin alike (samples of one prompt, beams, turns of one talk) hold the same blocks of the 8-bit cache until they
 write into them.  A pass is one call, or a few in a row, of a program that keeps such a cache:
@@ -9,7 +8,6 @@ write into them.  A pass is one call, or a few in a row, of a program that keeps
            blocks that go with that are copied
   copy     blocks of requests that move from worker to worker
   compact  requests leave, the blocks in use move to the lowest ids, their keys and values with them, requests come
-  shared   a decode step's attention of rows that begin alike: what they hold together is read for all of them
   diff     differential attention: the first map's result less lambda times the second's
 
 Keys of a case:
@@ -18,16 +16,16 @@ Keys of a case:
   block                 tokens of a block
   len_lo, len_hi        cached tokens of a row: spread evenly over the logarithm, in an order drawn from the seed
   idle                  rows that hold nothing
-  fork, branch, shared: family  rows that begin alike; own: tokens of a row that the others of its family do not hold (shared: at most)
-  fork, branch: how     "samples": a family's rows take over its first one, "beams": each takes over any of them; cut: the rows keep so many
-                        of a hundred of the tokens that they take over (100: all)
+  fork, branch: family  rows that begin alike; how: "samples": a family's rows take over its first one, "beams": each takes over any of
+                        them; own: tokens of a row that the others of its family do not hold; cut: the rows keep so many of a hundred of the
+                        tokens that they take over (100: all)
   branch: add           tokens that come to each row
   copy: take            requests that each worker gets from another
   compact: leave        share of the rows that leave; room: of a hundred blocks, those that a list of moves has places for
   heads, group, dim     key heads, query heads for each of them, head width (diff: both maps' channels side by side)
   fmt                   "int8" or "fp8" (e4m3); dtype: of queries ("bf16", "f16")
-  shared, diff: window  tokens that a query sees, itself included; 0: all up to itself
   diff: tokens          query tokens of a row; chunk, chunk_rows: so many of the rows have `chunk` of them instead
+        window          tokens that a query sees, itself included; 0: all up to itself
         lam             "head": a lambda for each query head; "token": for each token and query head
 """
 from __future__ import annotations
@@ -53,8 +51,6 @@ def _case(name, kind, **kw):
         c.update(take=1)
     if kind == "compact":
         c.update(leave=0.3, room=100)
-    if kind == "shared":
-        c.update(group=4, dtype="bf16", family=8, own=200, window=0)
     if kind == "diff":
         c.update(group=4, dtype="bf16", tokens=1, chunk=0, chunk_rows=0, window=0, lam="head")
     c.update(kw)
@@ -65,23 +61,23 @@ def _case(name, kind, **kw):
 
 def listed():
     return [
+        # one worker: every prompt is sampled eight times
+        _case("fork_samples", "fork"),
         # beams of all workers of a replay trade places at a step: all rows at once, each family's among themselves
         _case("fork_beams", "fork", workers=512, rows=144, block=64, how="beams", own=300, family=4, idle=4),
-        # one worker: every prompt is sampled eight times, and the samples get their first tokens: a row's last block is its own from here on
+        # the first tokens of those samples: each row's last block is its own from here on
         _case("branch_samples", "branch", len_lo=300, len_hi=4000),
         # a few workers with odd sizes; rows go back to a point inside what they share and go on from there with drafted tokens
         _case("branch_ragged", "branch", workers=13, rows=77, block=32, len_lo=1, len_hi=3000, how="beams", own=40, family=5, cut=90, add=5, heads=3, dim=96, fmt="fp8", idle=7),
+        # one short request to its neighbour: the smallest call
+        _case("copy_short", "copy", workers=2, rows=3, len_lo=100, len_hi=500),
         # requests that change workers when loads are evened out
         _case("copy_requests", "copy", workers=16, rows=6, block=64, len_lo=1024, len_hi=16384, take=2, fmt="fp8"),
         # a worker gives part of its memory away when its requests have become few
         _case("compact_worker", "compact", block=64, leave=0.6, fmt="fp8"),
         # the workers of a batch of small clusters
         _case("compact_workers", "compact", workers=300, rows=31, len_lo=20, len_hi=1000, heads=1, dim=64, room=10),
-        # the four beams of one prompt, in their first steps
-        _case("shared_beams", "shared", rows=4, len_lo=900, len_hi=900, family=4, own=30),
-        # a full worker: eight samples of each of twelve prompts
-        _case("shared_samples", "shared", block=64, len_lo=1024, len_hi=16384, group=8, own=400, fmt="fp8"),
-        # the smallest call: one short request
+        # the smallest attention: one short request
         _case("diff_one_short", "diff", rows=1, len_lo=500, len_hi=500),
         # a full worker of the throughput configuration
         _case("diff_batch", "diff", rows=144, block=64, group=8, fmt="fp8", idle=3),
@@ -97,7 +93,7 @@ def _log_int(rng, lo, hi):
 
 
 def draw(rng):
-    kind = rng.choice(["fork", "branch", "copy", "compact", "shared", "shared", "diff", "diff"])
+    kind = rng.choice(["fork", "branch", "copy", "compact", "diff", "diff", "diff"])
     block = rng.choice([16, 32, 64, 128])
     if kind == "fork":
         workers = _log_int(rng, 1, 2048)
@@ -118,24 +114,15 @@ def draw(rng):
             return _case(None, kind, rows=rows, len_lo=max(1, hi // 30), len_hi=hi, chunk=chunk, chunk_rows=1, **sizes)
         return _case(None, kind, rows=rows, len_lo=rng.randrange(5, 6 + min(hi - 10, 300)), len_hi=hi, tokens=rng.choice([1, 1, 1, 2, 5]), window=rng.choice([0, 0, 0, 100, 2048]),
                      idle=rng.randrange(0, 1 + rows // 8), **sizes)
-    if kind == "shared":
-        family, group = rng.randrange(1, 20), rng.choice([1, 2, 3, 4, 5, 6, 7, 8, 12, 16])
-        most = 100000000 // cells
-        rows = _log_int(rng, 1, 200)
-        firsts = _up(rows, family)
-        hi = _log_int(rng, 16, max(17, min(40960, most // firsts)))
-        return _case(None, kind, rows=rows, len_lo=rng.randrange(1, 2 + min(hi - 10, 300)), len_hi=hi, idle=rng.randrange(0, 1 + rows // 8), family=family, group=group,
-                     own=_log_int(rng, 1, max(2, min(600, most // rows))), dtype=rng.choice(["bf16", "f16"]), window=rng.choice([0, 0, 0, 0, 100, 2048]), **sizes)
     most = max(2000, 300000000 // cells)  # tokens of all rows together
     workers = _log_int(rng, 2 if kind == "copy" else 1, 200)
-    room = most // 40 if kind != "branch" else 300000000 // (cells * (block + 50))  # rows of all workers (branch: a block of each may be copied)
-    rows = _log_int(rng, 2, max(3, min(300, room // workers)))
+    rows = _log_int(rng, 2, max(3, min(300, most // (40 * workers))))
     hi = max(20, min(16384, most // (workers * rows)))
     lens = dict(len_lo=rng.randrange(1, 20), len_hi=_log_int(rng, 20, max(21, hi)))
     idle = rng.randrange(0, 1 + rows // 8)
     if kind == "branch":
         return _case(None, kind, workers=workers, rows=rows, idle=idle, family=rng.randrange(2, 13), how=rng.choice(["samples", "beams"]),
-                     own=rng.choice([0, 1, _log_int(rng, 2, 60)]), cut=rng.choice([100, 100, rng.randrange(1, 100)]), add=rng.choice([1, 1, 1, 3, 40]), **lens, **sizes)
+                     own=rng.choice([0, 1, _log_int(rng, 2, 400)]), cut=rng.choice([100, 100, rng.randrange(1, 100)]), add=rng.choice([1, 1, 1, 3, 40]), **lens, **sizes)
     if kind == "copy":
         return _case(None, kind, workers=workers, rows=rows, take=rng.randrange(1, 1 + min(4, rows)), **lens, **sizes)
     return _case(None, kind, workers=workers, rows=rows, idle=idle, leave=rng.uniform(0.05, 0.9), room=rng.choice([100, 50, 50, rng.randrange(1, 30)]), **lens, **sizes)
@@ -153,12 +140,7 @@ def _lengths(case):
         return _spread(n, case["len_lo"], case["len_hi"]) + [0] * case["idle"]
     f = case["family"]
     shared = _spread(_up(n, f), case["len_lo"], case["len_hi"])
-    return [shared[r // f] + _alone(case, r) for r in range(n)] + [0] * case["idle"]
-
-
-def _alone(case, r):
-    """Tokens of row r that the others of its family do not hold."""
-    return 1 + r * 7919 % case["own"] if case["kind"] == "shared" else case["own"]
+    return [shared[r // f] + case["own"] for r in range(n)] + [0] * case["idle"]
 
 
 def _up(x, m):
@@ -198,19 +180,16 @@ def _families(case, g):
     n_blocks, width = _blocks(case)
     n = R - case["idle"]
     lens = torch.tensor(_lengths(case), device=DEVICE)
-    alone = torch.tensor([_alone(case, r) for r in range(R)], device=DEVICE)
     row = torch.arange(R, device=DEVICE)
     first = torch.where(row < n, row // f * f, row)
     nb = (lens + b - 1) // b
-    together = torch.where(row == first, 0, (lens - alone).clamp(min=0) // b)  # blocks that are the first row's
+    together = torch.where(row == first, 0, (lens - case["own"]).clamp(min=0) // b)  # blocks that are the first row's
     if case["own"] == 0:
         together = torch.where(row == first, 0, nb)
     alone = _table((nb - together).expand(W, R), width, n_blocks, g)
     at = torch.arange(width, device=DEVICE)
     mine = alone.gather(2, (at - together[:, None]).clamp(0, width - 1).expand(W, R, width))
     table = torch.where(at < together[:, None], alone[:, first], torch.where(at < nb[:, None], mine, -1))
-    if case["kind"] == "shared":
-        return dict(lens=lens.expand(W, R).to(torch.int32).contiguous(), table=table.to(torch.int32).contiguous(), lead=first.expand(W, R).to(torch.int32).contiguous())
     take = first if case["how"] == "samples" else torch.minimum(first + (torch.rand((W, R), generator=g, device=DEVICE) * f).long(), torch.tensor(max(n - 1, 0), device=DEVICE))
     take = torch.where(row < n, take, -1).expand(W, R)
     cut = torch.where(row < n, _cut(case, lens), 0).expand(W, R)
@@ -246,8 +225,8 @@ def prepare(case, seed):
         s["add"] = torch.where(gone, s["lens"], 0).contiguous()
         s["none"], s["all"] = torch.zeros_like(s["add"]), torch.full_like(s["keep"], -1)
         s["cap"], s["room"] = sum(_lengths(case)), max(1, n_blocks * case["room"] // 100)
-    if kind in ("shared", "diff"):
-        _prepare_attention(s, g)
+    if kind == "diff":
+        _prepare_diff(s, g)
     elif kind != "fork":
         H, D, N = case["heads"], case["dim"], W * n_blocks
         top = 255 if case["fmt"] == "int8" else 127  # (codes below 127 are numbers of either type)
@@ -275,7 +254,7 @@ def _moves(s, g):
     return dict(src=i32(src), dst=i32(dst), src_worker=i32(giver[:, None].expand(src.shape)))
 
 
-def _prepare_attention(s, g):
+def _prepare_diff(s, g):
     c = s["case"]
     H, G, D, b, n_blocks, t = c["heads"], c["group"], c["dim"], c["block"], s["n_blocks"], TYPES[c["dtype"]]
     randn = lambda *shape: torch.randn(shape, generator=g, device=DEVICE)
@@ -287,27 +266,22 @@ def _prepare_attention(s, g):
     s["k"], s["v"] = k, v.transpose(2, 3).contiguous()
     del k, v
     lens = s["lens"][0].long()
-    count = torch.where(lens > 0, c.get("tokens", 1), 0)
-    if c.get("chunk_rows"):  # the longest rows
+    count = torch.where(lens > 0, c["tokens"], 0)
+    if c["chunk_rows"]:  # the longest rows
         count[lens.argsort(descending=True)[:c["chunk_rows"]]] = c["chunk"]
     s["count"] = count.to(torch.int32)
     s["start"] = (count.cumsum(0) - count).to(torch.int32)
+    s["max_count"] = max(c["tokens"], c["chunk"])
     s["T"] = sum(_counts(c))
     s["q"] = randn(s["T"], H * G, D).to(t)
-    s["out"], s["max_len"] = torch.empty_like(s["q"]), max(_lengths(c))
-    if c["kind"] == "shared":
-        s["lse"] = torch.empty((s["T"], H * G), device=DEVICE)
-        return
-    s["max_count"] = max(c["tokens"], c["chunk"])
     # what exp(a . b) - exp(c . d) + lambda_0 of trained vectors comes to; from the token: a gate
     s["lam"] = 0.5 + 0.2 * randn(H * G) if c["lam"] == "head" else torch.sigmoid(randn(s["T"], H * G))
-    s["lse"] = torch.empty((s["T"], H * G, 2), device=DEVICE)
+    s["out"], s["lse"] = torch.empty_like(s["q"]), torch.empty((s["T"], H * G, 2), device=DEVICE)
+    s["max_len"] = max(_lengths(c))
 
 
 def _counts(case):
     n = case["rows"] - case["idle"]
-    if case["kind"] == "shared":
-        return [1] * n
     return [case["chunk"]] * case["chunk_rows"] + [case["tokens"]] * (n - case["chunk_rows"])
 
 
@@ -335,10 +309,6 @@ def _run_own(s):
     if kind == "diff":
         cache.attend_diff_device(s["layer"], s["q"], s["out"], s["lam"], lse=s["lse"], start=s["start"], count=s["count"], max_count=s["max_count"], window=s["case"]["window"])
         return dict(out=s["out"], lse=s["lse"])
-    if kind == "shared":  # which rows go together is found once for all layers of a step
-        cache.plan_device(s["lead"], members=s["case"]["family"], start=s["start"], count=s["count"])
-        cache.attend_shared_device(s["layer"], s["q"], s["out"], lse=s["lse"], window=s["case"]["window"])
-        return dict(out=s["out"], lse=s["lse"])
     if kind in ("fork", "branch"):
         cache.fork_device(s["take"], s["cut"] if s["case"]["cut"] < 100 or kind == "branch" else None)
         if kind == "fork":
@@ -364,8 +334,8 @@ def _memory(s):
 def _run_plain(s):
     c = s["case"]
     kind = c["kind"]
-    if kind in ("shared", "diff"):
-        return _plain_attention(s)
+    if kind == "diff":
+        return _plain_diff(s)
     if kind in ("fork", "branch"):
         _plain_fork(s, s["cut"] if c["cut"] < 100 or kind == "branch" else None)
         if kind == "fork":
@@ -508,25 +478,25 @@ def _value(code, fmt):
 
 
 # -- plain form of the attention ----------------------------------------------------
-def _plain_attention(s):
+def _plain_diff(s):
     """The rows with a chunk, if any, and the others, each padded to their largest."""
     c = s["case"]
     q = s["q"].float()
-    out, lse = torch.empty_like(q), torch.empty((*q.shape[:2], 2 if c["kind"] == "diff" else 1), device=DEVICE)
-    by_count, chunks = s["lens"][0].argsort(descending=True), c.get("chunk_rows", 0)
-    if chunks:
-        _padded(s, by_count[:chunks], c["chunk"], q, out, lse)
-    _padded(s, by_count[chunks:c["rows"] - c["idle"]], c.get("tokens", 1), q, out, lse)
-    return dict(out=out.to(s["q"].dtype), lse=lse if c["kind"] == "diff" else lse[..., 0])
+    out, lse = torch.empty_like(q), torch.empty((*q.shape[:2], 2), device=DEVICE)
+    by_count = s["lens"][0].argsort(descending=True)
+    if c["chunk_rows"]:
+        _padded(s, by_count[:c["chunk_rows"]], c["chunk"], q, out, lse)
+    _padded(s, by_count[c["chunk_rows"]:c["rows"] - c["idle"]], c["tokens"], q, out, lse)
+    return dict(out=out.to(s["q"].dtype), lse=lse)
 
 
 def _padded(s, rows, n, q, out, lse):
-    """Attention of n query tokens of each of the given rows: one map, or two over half of the channels each."""
+    """Differential attention of n query tokens of each of the given rows."""
     c = s["case"]
     b, H, G, D, R = c["block"], c["heads"], c["group"], c["dim"], len(rows)
     if not R:
         return
-    nb, half = _up(s["max_len"], b), D // lse.shape[2]
+    nb, half = _up(s["max_len"], b), D // 2
     blocks = s["table"][0, rows, :nb].clamp(min=0).long()
     k = (_value(s["k"][blocks], c["fmt"]) * s["k_scale"][blocks][..., None, None]).permute(0, 2, 1, 3, 4).reshape(R * H, nb * b, D)
     token = s["start"][rows].long()[:, None] + torch.arange(n, device=DEVICE)
@@ -535,7 +505,7 @@ def _padded(s, rows, n, q, out, lse):
     p = (s["lens"][0, rows].long()[:, None] - n + torch.arange(n, device=DEVICE))[:, None, :, None, None]
     seen = (j <= p) & (j > p - c["window"]) if c["window"] else j <= p
     maps = []
-    for m in range(lse.shape[2]):
+    for m in range(2):
         part = slice(m * half, (m + 1) * half)
         score = torch.bmm(qs[:, :, part].contiguous(), k[:, :, part].transpose(1, 2).contiguous()).view(R, H, n, G, nb * b) / math.sqrt(half)
         score = score.masked_fill_(~seen, -math.inf)
@@ -547,10 +517,8 @@ def _padded(s, rows, n, q, out, lse):
         lse[..., m][token] = (top + total.log()).view(R, H, n, G).permute(0, 2, 1, 3).reshape(R, n, H * G)
         del e
     del k, qs
-    weight = maps[0]
-    if len(maps) == 2:
-        lam = (s["lam"][token] if c["lam"] == "token" else s["lam"].expand(R, n, H * G)).view(R, n, H, G).permute(0, 2, 1, 3)
-        weight = weight - lam[..., None] * maps[1]
+    lam = (s["lam"][token] if c["lam"] == "token" else s["lam"].expand(R, n, H * G)).view(R, n, H, G).permute(0, 2, 1, 3)
+    weight = maps[0] - lam[..., None] * maps[1]
     del maps
     v = (_value(s["v"][blocks], c["fmt"]) * s["v_scale"][blocks][..., None, None]).permute(0, 2, 1, 4, 3).reshape(R * H, nb * b, D)
     o = torch.bmm(weight.reshape(R * H, n * G, nb * b), v)
@@ -559,15 +527,14 @@ def _padded(s, rows, n, q, out, lse):
 
 # -- the definition in 64 bits ----------------------------------------------------------
 def exact(case, seed):
-    if case["kind"] not in ("shared", "diff"):
+    if case["kind"] != "diff":
         return None  # whole numbers, and bytes that are copied
     s = prepare(case, seed)
     b, H, G, D, fmt = case["block"], case["heads"], case["group"], case["dim"], case["fmt"]
     if sum(n * x for n, x in zip(_counts(case), sorted(_lengths(case), reverse=True))) * H * G * D > 6e11:
         return None
     out = torch.zeros((s["T"], H * G, D), dtype=torch.float64, device=DEVICE)
-    maps = 2 if case["kind"] == "diff" else 1
-    lse = torch.full((s["T"], H * G, maps), -math.inf, dtype=torch.float64, device=DEVICE)
+    lse = torch.full((s["T"], H * G, 2), -math.inf, dtype=torch.float64, device=DEVICE)
     for r, (n, length, t0) in enumerate(zip(s["count"].tolist(), s["lens"][0].tolist(), s["start"].tolist())):
         if not n:
             continue
@@ -579,18 +546,17 @@ def exact(case, seed):
         hidden = j > i
         if case["window"]:
             hidden = hidden | (j <= i - case["window"])
-        if maps == 2:
-            lam = s["lam"].double()
-            lam = (lam[t0:t0 + n] if case["lam"] == "token" else lam.expand(n, H * G)).view(n, H, G).permute(1, 0, 2).reshape(H, n * G, 1)
-        for m, (qm, km) in enumerate(zip(q.chunk(maps, -1), k.chunk(maps, -1))):
-            z = torch.matmul(qm.contiguous(), km.transpose(1, 2).contiguous()).view(H, n, G, length) * (D // maps) ** -0.5
+        lam = s["lam"].double()
+        lam = (lam[t0:t0 + n] if case["lam"] == "token" else lam.expand(n, H * G)).view(n, H, G).permute(1, 0, 2).reshape(H, n * G, 1)
+        for m, (qm, km) in enumerate(zip(q.chunk(2, -1), k.chunk(2, -1))):
+            z = torch.matmul(qm.contiguous(), km.transpose(1, 2).contiguous()).view(H, n, G, length) * (D // 2) ** -0.5
             z = z.masked_fill(hidden[:, None], -math.inf)
             w = torch.logsumexp(z, -1)
             a = torch.exp(z - torch.where(torch.isinf(w), 0.0, w)[..., None]).reshape(H, n * G, length)
             o = torch.matmul(a, v) * (1.0 if m == 0 else -lam)
             out[t0:t0 + n] += o.view(H, n, G, D).transpose(0, 1).reshape(n, H * G, D)
             lse[t0:t0 + n, :, m] = w.permute(1, 0, 2).reshape(n, H * G)
-    return dict(out=out, lse=lse if maps == 2 else lse[..., 0])
+    return dict(out=out, lse=lse)
 
 
 # -- what a pass cannot do without ------------------------------------------------------
@@ -620,16 +586,6 @@ def work(case):
         return dict(bytes=W * (2 * 28 * R + 16 * sum(lens) + n_blocks / 2 + 8 * held + moved * (8 + 4 * (cells * b + 4 * case["heads"]))), flops=0)
     counts = _counts(case)
     read = pairs = 0
-    if kind == "shared":
-        n, f = R - case["idle"], case["family"]
-        seen = lambda r: min(lens[r], case["window"] or lens[r])
-        pairs = sum(seen(r) for r in range(n))
-        for first in range(0, n, f):
-            rows = range(first, min(first + f, n))
-            together = (lens[first] - _alone(case, first)) // b * b  # read once, as far as any row of the family sees it
-            read += max(0, together - min(lens[r] - seen(r) for r in rows)) + sum(lens[r] - max(lens[r] - seen(r), together) for r in rows)
-        scales = 2 * 4 * case["heads"] * read / b
-        return dict(bytes=2 * cells * read + scales + n * (4 * _up(max(lens), b) + case["group"] * (4 * cells + 4 * case["heads"])), flops=4 * cells * case["group"] * pairs)
     for n, x in zip(counts, sorted(lens, reverse=True)):
         seen = [min(p + 1, case["window"] or p + 1) for p in range(max(0, x - n), x)]
         pairs += sum(seen)
