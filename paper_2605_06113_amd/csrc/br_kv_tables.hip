@@ -100,7 +100,8 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
   constexpr int ROWS = NT * RPT, IDS = NT * 8, AT_ONCE = 8;
   extern __shared__ unsigned used[];
   __shared__ int part[16 * (NT / 64)], give_n, need_before[ROWS], tok_before[ROWS], row_kp[ROWS], give[ROWS], row_tail[ROWS], ids[IDS];
-  __shared__ int row_in[SHARED ? ROWS : 1], dropped;  // 1: the row's first block comes in the place of its last one
+  __shared__ int dropped;
+  int *const row_in = give;  // 1: the row's first block comes in the place of its last one (whose blocks are given back is done with by then)
   const int w = blockIdx.x, tid = threadIdx.x, B = t.B, b1 = (1 << t.shift) - 1;
   int turn = 0;
   int *lens = t.lens + (long long)w * B;
