@@ -305,7 +305,8 @@ int32_t br_kv_copy(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_moves *
 
 /*
  * Rows whose single tokens are read together.  lead [n_workers][rows]: the row of the same worker that leads row r (itself, outside [0, rows), or NULL: it is
- * alone).  Rows of one leader are a family; what they hold together with it is found in the tables: whatever lead says, each row's result is
+ * alone).  Rows of one leader are a family; what they hold together is found in the tables, by comparing each with the leader, or, where that is not one of them
+ * or holds no token, with the first of them that does (a company with a row that has gone its own way holds nothing together): whatever lead says, each row's result is
  * that of its own tokens.  start, count: as br_kv_attention's, or both NULL; rows whose count is not 1 have no part in it.  members: a family's rows are
  * taken together, so many at most (and 64 query rows, of wide heads 32, where they have more heads than that allows).
  */

@@ -1,9 +1,27 @@
 // Which rows are read together (br_kv_plan): companies of rows whose tables begin with the same blocks.
 #include "br_kv_device.h"
 
-// How many of its tokens row r of worker w holds in the same blocks as the row that leads it: by a wave, 256 entries at a time.
-__device__ __forceinline__ int br_kv_common(const BrKvTables &t, const BrKvPlan &x, int w, int r) {
-  const int lane = threadIdx.x & 63, f = br_kv_leader(t, x, w, r), row0 = w * t.B;
+// The row that those of r's family are compared with: the one that leads them, if it is one of them and holds tokens, or the first of them that does (what leads
+// a family may have left, or go with another one).  By a wave; r itself if it holds none.
+__device__ __forceinline__ int br_kv_compared(const BrKvTables &t, const BrKvPlan &x, int w, int r) {
+  const int lane = threadIdx.x & 63, row0 = w * t.B, f = br_kv_leader(t, x, w, r);
+  const int len = br_kv_len(t, row0 + r);
+  auto one_of_them = [&](int k) {  // (asked for at once)
+    const int lead = br_kv_leader(t, x, w, k), count = x.count ? x.count[row0 + k] : 1, len = br_kv_len(t, row0 + k);
+    return (lead == f) & (count == 1) & (len > 0);
+  };
+  if (one_of_them(f)) return len == 0 ? r : f;
+  if (len == 0) return r;
+  for (int k = 0; k < r; k += 64) {
+    const unsigned long long some = __ballot(k + lane < r && one_of_them(min(k + lane, r)));
+    if (some) return k + __ffsll(some) - 1;
+  }
+  return r;
+}
+
+// How many of its tokens row r of worker w holds in the same blocks as row f: by a wave, 256 entries at a time.
+__device__ __forceinline__ int br_kv_common(const BrKvTables &t, int w, int r, int f) {
+  const int lane = threadIdx.x & 63, row0 = w * t.B;
   int same = br_kv_len(t, row0 + r);
   if (f == r) return same;
   same = min(same, br_kv_len(t, row0 + f));
@@ -31,12 +49,13 @@ __global__ __launch_bounds__(256) void br_kv_k_plan_common(BrKvTables t, BrKvPla
   const int rows = t.W * t.B;
   for (int at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); at < rows; at += gridDim.x * 4) {
     if (x.count && x.count[at] != 1) continue;
-    const int w = at / t.B, same = br_kv_common(t, x, w, at - w * t.B);
+    const int w = at / t.B, r = at - w * t.B, same = br_kv_common(t, w, r, br_kv_compared(t, x, w, r));
     if ((threadIdx.x & 63) == 0) x.common[at] = same;
   }
 }
 
-// One block for each worker, a thread for each row: a family's rows in companies of at most `most`, evenly, in the order of the rows.
+// One block for each worker, a thread for each row: a family's rows in companies of at most `most`, evenly, in the order of the rows.  Rows without tokens
+// are families of their own: they have nothing in common with any other.
 // ALONE: what rows have in common is found here too (else by br_kv_k_plan_common, before).  Bound by its chain of loads and barriers: four rows of one worker
 // 4.1 us, a launch that does nothing 3.9; 96 rows in two launches 4.8 and 5.2.
 template <int NT, bool ALONE>
@@ -46,15 +65,20 @@ __global__ __launch_bounds__(NT) void br_kv_k_plan(BrKvTables t, BrKvPlan x) {
   const int w = blockIdx.x, r = threadIdx.x, B = t.B;
   const long long at = (long long)w * B + r;
   int turn = 0;
-  const int f = r < B && (!x.count || x.count[at] == 1) ? br_kv_leader(t, x, w, r) : -1;
-  family[r] = f;
+  const int lead = r < B && (!x.count || x.count[at] == 1) ? br_kv_leader(t, x, w, r) : -1, tokens = lead >= 0 ? br_kv_len(t, (int)at) : 0;
   size[r] = n_of[r] = begin_of[r] = tiles[r] = 0, least[r] = INT32_MAX;
   by16[4 * r] = by16[4 * r + 1] = by16[4 * r + 2] = by16[4 * r + 3] = by32[2 * r] = by32[2 * r + 1] = 0;
   __syncthreads();
+  if (tokens > 0) atomicMin(&least[lead], r == lead ? -1 : r);
+  __syncthreads();
+  const int first = tokens > 0 ? least[lead] : r, f = lead < 0 ? -1 : first < 0 ? lead : first;  // (br_kv_compared)
+  family[r] = f;
+  __syncthreads();
+  least[r] = INT32_MAX;
   if (ALONE)
     for (int k = __builtin_amdgcn_readfirstlane(r >> 6); k < B; k += NT / 64) {
       if (family[k] < 0) continue;
-      const int same = br_kv_common(t, x, w, k);
+      const int same = br_kv_common(t, w, k, __builtin_amdgcn_readfirstlane(family[k]));
       if ((r & 63) == 0) common[k] = same;
     }
   int rank = 0;
@@ -71,11 +95,10 @@ __global__ __launch_bounds__(NT) void br_kv_k_plan(BrKvTables t, BrKvPlan x) {
   br_kv_scan<NT, 2>(sum, all, part, turn);
   before[r] = sum[0] - mine[0], first_of[r] = sum[1] - mine[1];
   __syncthreads();
-  int company = -1, tokens = 0, place = 0;
+  int company = -1, place = 0;
   if (f >= 0) {
     const int companies = (size[f] + x.most - 1) / x.most, per = (size[f] + companies - 1) / companies, k = rank / per;
     company = first_of[f] + k, place = rank - k * per;
-    tokens = br_kv_len(t, (int)at);
     atomicMin(&least[company], ALONE ? common[r] : x.common[at]);
     if (place == 0) n_of[company] = min(per, size[f] - k * per), begin_of[company] = before[f] + k * per;
     x.members[(long long)w * B + before[f] + rank] = make_int4((int)at, x.start ? x.start[at] : (int)at, tokens, 0);

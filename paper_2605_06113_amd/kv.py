@@ -425,7 +425,7 @@ class KvCache:
     def plan_device(self, lead, members: int, start=None, count=None) -> None:
         """Which rows attend_shared_device reads together (br_kv_plan), for all layers of a step: behind step_device.
 
-        lead [n_workers, rows] int32: the row that row r shares its first blocks with (its family's first, itself, or -1); at most `members` rows together:
+        lead [n_workers, rows] int32: the row that row r shares its first blocks with (its family's first, which may have left since, itself, or -1); at most `members` rows together:
         with 16 query rows of a key head short calls are fastest, with more those that read much.
         start, count: step_device's; rows whose count is not 1 are left out; none: token r belongs to row r."""
         self._is_shared()
