@@ -319,14 +319,16 @@ typedef struct {
 } br_kv_families;
 
 /*
- * Plans the attentions of a step, for all layers: of a context of br_kv_init_shared, behind the step and whatever else changes its tables or lengths.
+ * Plans the attentions of a step, for all layers: of a context of br_kv_init_shared, behind the step and the forks before it.  It holds until the next
+ * br_kv_step_shared or br_kv_fork (br_kv_compact, with its copies, may come between).
  */
 int32_t br_kv_plan(br_kv_ctx *ctx, const br_kv_families *in);
 
 /*
  * br_kv_attend of the planned rows' tokens (start, count, lens and table are NULL, max_count 1 or more): whole tiles of 64 tokens that the rows read together hold in
  * the same blocks are read once for all of them.  Results are br_kv_attend's but for the order of the sums, which the families have a say in; equal plans and inputs give
- * equal outputs.  Before the first plan: BR_EINVAL; behind one that was captured and has not run, no row has a part in it.
+ * equal outputs.  Before the first plan: BR_EINVAL.  Where no plan has run since the last br_kv_step_shared or br_kv_fork, also one that was captured only,
+ * no row has a part in it, and nothing is written.
  */
 int32_t br_kv_attend_shared(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_attention *args);
 

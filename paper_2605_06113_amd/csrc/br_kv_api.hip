@@ -59,7 +59,7 @@ Places make_layout(const br_kv_config &c, bool shared) {
     l.next_lens = take(2 * rows);
     l.next_table = take(rows * c.max_blocks);
     l.moved = take(blocks);
-    l.least = take((uint64_t)c.n_workers);
+    l.least = take((uint64_t)c.n_workers + 1);  // (the last: BrKvTables' `planned`)
     l.common = take(rows);
     l.companies = take(8 * rows);
     l.members = take(4 * rows);
@@ -251,6 +251,7 @@ static int32_t init_context(const br_kv_config *cfg, const br_kv_state *init, bo
   t.used = (unsigned *)(base + at.used);
   t.arrived = (int *)(base + at.arrived);
   t.holders = shared ? (int *)(base + at.holders) : nullptr;
+  t.planned = shared ? (int *)(base + at.least) + cfg->n_workers : nullptr;
   int32_t rc = enqueue(ctx, [&] { br_kv_launch_clear(t, shared ? (int4 *)(base + at.companies) : nullptr, ctx->st); });
   if (rc == BR_OK && init) rc = enqueue(ctx, [&] { br_kv_launch_load(t, init->lens, init->table, ctx->st); });
   if (rc != BR_OK) {
@@ -377,6 +378,7 @@ int32_t br_kv_attend_shared(br_kv_ctx *ctx, const br_kv_layer *layer, const br_k
   if (!attention_of(ctx, layer, a, 1, p)) return BR_EINVAL;
   p.companies = (const int4 *)((char *)ctx->cfg.workspace + ctx->at.companies);
   p.members = (const int4 *)((char *)ctx->cfg.workspace + ctx->at.members);
+  p.planned = ctx->t.planned;
   const int tile = ctx->plan_tile;
   return enqueue(ctx, [&] { BR_KV_BY_DIM(br_kv_launch_shared) });
 }

@@ -991,10 +991,11 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend(BrKvAttend p) {
   __shared__ BrKvShare chains[NR + 1];  // of the query tile that run k has begun; the last: of one that an earlier block has
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), rn = wv / SHARE, row = 16 * (wv % SHARE);  // the wave's run, its first query row of the tile
+  const bool planned = !br_kv_shared(MODE) || *p.planned;  // (companies of other rows than there are now have no part)
   Runs runs(p, shared, gridDim.x, LEAST);
   // runs that follow each other go to one XCD (blocks go round them), which has what they share in its L2
   const int blocks = (runs.workers + NR - 1) / NR, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
-  if (wg >= blocks) return;
+  if (wg >= blocks || !planned) return;
   if (tid <= NR) chains[tid].on = 0;
   __syncthreads();
   const int me = wg * NR + rn;
@@ -1327,9 +1328,10 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend_together(BrKvAt
   __shared__ int arrived;
   const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int phase = wv / NH, row = 16 * NQ * (wv % NH);
+  const bool planned = *p.planned;  // (companies of other rows than there are now have no part)
   Runs runs(p, shared, gridDim.x, LEAST);
   const int blocks = runs.workers, b8 = blockIdx.x, wg = b8 < (blocks & ~7) ? (b8 & 7) * (blocks >> 3) + (b8 >> 3) : b8;
-  if (wg >= blocks) return;
+  if (wg >= blocks || !planned) return;
   long long u = runs.begin_of(wg);
   const long long end = runs.begin_of(wg + 1);
   BrKvPlace<TQ, NT, Runs, MODE> at;

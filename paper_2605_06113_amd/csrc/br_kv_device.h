@@ -22,6 +22,7 @@ struct BrKvTables {
   unsigned *used;                                // [W][words]
   int *arrived;                                  // BrKvAttend's
   int *holders;                                  // [W][n_blocks] entries that name a block; null: a block has one holder at most
+  int *planned;                                  // of blocks with several holders: 1 if nothing has changed the rows since br_kv_plan
 };
 
 // What rows become (br_kv_fork) and where blocks go (br_kv_compact), from one launch to the next.
@@ -92,6 +93,7 @@ struct BrKvAttend {
   long long lambda_token;
   const int4 *companies;       // of rows that are read together, see br_kv_k_plan: n_rows of them
   const int4 *members;
+  const int *planned;          // BrKvTables'
 };
 
 void br_kv_launch_clear(const BrKvTables &t, int4 *companies, hipStream_t st);

@@ -102,6 +102,7 @@ __global__ __launch_bounds__(256) void br_kv_k_fork_put(BrKvTables t, BrKvNext x
       if (blocks == 0) t.tail[r] = -1;
     }
   });
+  if (blockIdx.x == 0 && threadIdx.x == 0) *t.planned = 0;
 }
 
 // Bound by the way to memory: 512 workers of 144 rows, up to 133 entries each, 19.6 us, some 45 MB of lines of own and others' rows, a launch and four dependent
@@ -155,6 +156,7 @@ __global__ __launch_bounds__(NT) void br_kv_k_fork(BrKvTables t, BrKvNext x, con
       if (blocks == 0) t.tail[row0 + r] = -1;
     }
   }
+  if (w == 0 && threadIdx.x == 0) *t.planned = 0;
 }
 
 // One block for each worker: which blocks go where, the used bits and the counts.  The used bits are in LDS.  Bound by four scans and the trips between them, not

@@ -114,6 +114,7 @@ __global__ __launch_bounds__(NT) void br_kv_k_plan(BrKvTables t, BrKvPlan x) {
   }
   __syncthreads();
   if (r >= B) return;
+  if (at == 0) *t.planned = 1;  // (a store before the loads would keep them from being what they are: 4096 workers of 96 rows 61 us and 76)
   const int together = n_of[r] > 1 ? least[r] / BR_KV_TILE : 0;
   int4 *to = x.companies + 2 * at;
   to[0] = make_int4(n_of[r], w * B + begin_of[r], together, together + tiles[r]);

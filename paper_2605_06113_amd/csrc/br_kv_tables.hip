@@ -15,8 +15,10 @@ __global__ __launch_bounds__(256) void br_kv_k_clear(BrKvTables t, int4 *compani
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < BR_KV_SPLIT_WGS; i += step) t.arrived[i] = 0;
   if (t.holders)
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)t.W * t.n_blocks; i += step) t.holders[i] = 0;
-  if (companies)  // (a plan that was captured and not run yet has planned nothing)
+  if (companies) {  // (a plan that was captured and not run yet has planned nothing)
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < 2ll * t.W * t.B; i += step) companies[i] = make_int4(0, 0, 0, 0);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *t.planned = 0;
+  }
 }
 
 // The rows held at the start (behind br_kv_k_clear).
@@ -303,6 +305,7 @@ __global__ __launch_bounds__(NT) void br_kv_k_step(BrKvTables t, BrKvStep s) {
       if (want[i] > 0 && in[i] && atomicSub(&holders[tail[i]], 1) == 1) atomicAnd(&used[tail[i] >> 5], ~(1u << (tail[i] & 31))), atomicAdd(&dropped, 1);
     __syncthreads();
     if (tid == 0 && s.stats) say(dropped);
+    if (w == 0 && tid == 0) *t.planned = 0;
   }
   for (int i = tid; i < t.words; i += NT) gused[i] = used[i];
   if (LIST && (s.slot || s.pos))

@@ -439,7 +439,9 @@ class KvCache:
             self._done(rc, "br_kv_plan")
 
     def attend_shared_device(self, layer: KvLayer, q, out, lse=None, scale: Optional[float] = None, window: int = 0) -> None:
-        """attend_device of the planned rows' tokens (br_kv_attend_shared): what rows hold together is read once for all of them."""
+        """attend_device of the planned rows' tokens (br_kv_attend_shared): what rows hold together is read once for all of them.
+
+        A plan holds until the next step_device or fork_device: behind those, without another plan_device, nothing is written."""
         self._is_shared()
         self._pack_attention(layer, q, out, lse, (), None, None, 1, scale, self._scale, window, None, None)
         rc = self.lib.br_kv_attend_shared(self.ctx, layer.at, self._at)

@@ -86,3 +86,93 @@ def test_a_leader_that_goes_with_others():
         got = _plan("led", wide(lens, np.full((1, more), 5)), wide(lead, np.arange(12, R)[None]), 20, 6, said=wide(said, np.arange(12, R)[None]))
         got = [c for c in got if c[1][0] < 12]
         assert (0, [1, 2, 3, 4, 5], 5) in got and (0, [9, 10, 11], 5) in got and sum(0 in c[1] for c in got) == 1 and sorted(r for c in got for r in c[1]) == list(range(12)), got
+
+
+@pytest.mark.parametrize("case", [(1, 16, 4, 64, 4), (1, 16, 16, 128, 2), (2, 40, 8, 192, 4), (1, 100, 4, 64, 4)], ids=str)
+def test_a_plan_of_other_rows_is_none(case):
+    """A step or a fork behind a plan, eager or replayed: the attention writes nothing until the next plan has run; compaction leaves it as it is."""
+    torch = _torch()
+    W, R, members, D, group = case
+    _say("older plan", case)
+    rng = np.random.default_rng(R)
+    lens, lead = 150 + rng.integers(0, 100, (W, R)), _families(R, 8).repeat(W, 0)
+    one, layer, h = _shared_cache(rng, "int8", W, R, 16, D, 2, group, lens, lead, np.full((W, R), 8))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    cache = kv.KvCache(one.cfg, lens=_i32(lens), table=_i32(h["table"]), stream=side)
+    lead, q = _i32(lead), torch.tensor(rng.normal(size=(W * R, 2 * group, D)), dtype=torch.float16, device="cuda:0")
+    out, lse = torch.empty_like(q), torch.empty((W * R, 2 * group), device="cuda:0")
+    every, none, step, moves = _i32(np.full((W, R), -1)), _i32(np.zeros((W, R))), cache.alloc_step(4), cache.alloc_moves(h["N"])
+    torch.cuda.synchronize()
+
+    def attend(tag, planned):
+        with torch.cuda.stream(side):
+            out.fill_(7.0), lse.fill_(7.0)
+        cache.attend_shared_device(layer, q, out, lse=lse)
+        torch.cuda.synchronize()
+        if not planned:
+            assert bool((out == 7.0).all()) and bool((lse == 7.0).all()), tag
+            return
+        k, v, ks, vs = (x.cpu().numpy() for x in (layer.k, layer.v, layer.k_scale, layer.v_scale))
+        now = dict(h, k=k, v=v, ks=ks, vs=vs, table=cache.table.cpu().numpy())
+        ref = _reference(q.double().cpu().numpy(), now, cache.lens.cpu().numpy(), np.arange(W * R), np.ones(W * R, np.int64), W, group, 16, "int8", 0, None)
+        _check_attention((case, tag), cache, q, out, lse, ref, "float16")
+
+    def stepped():
+        cache.step_device(every, none, step)
+
+    def forked():
+        cache.fork_device(every)
+
+    cache.plan_device(lead, members)
+    attend("first", True)
+    graphs = {}
+    for what in (stepped, forked):
+        what()
+        attend(("behind", what.__name__), False)
+        cache.plan_device(lead, members)
+        attend(("again", what.__name__), True)
+        graphs[what] = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graphs[what], stream=side):
+            what()
+        attend(("captured", what.__name__), True)
+    planning = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(planning, stream=side):
+        cache.plan_device(lead, members)
+    for what, graph in graphs.items():
+        for turn in range(2):
+            with torch.cuda.stream(side):
+                graph.replay()
+            attend(("replayed", what.__name__, turn), False)
+            with torch.cuda.stream(side):
+                planning.replay()
+            attend(("planned", what.__name__, turn), True)
+    cache.compact_device(moves)
+    cache.copy_device(layer, moves["src"], moves["dst"])
+    attend("compact", True)
+    one.close(), cache.close()
+
+
+@pytest.mark.parametrize("W,R,M", [(1, 8, 4), (300, 40, 200), (5000, 2, 4)], ids=str)
+def test_every_form_of_a_fork_ends_a_plan(W, R, M):
+    torch = _torch()
+    _say("forks and plans", W, R, M)
+    cache = kv.KvCache(kv.KvConfig(n_workers=W, rows=R, n_blocks=R, max_blocks=M, shared=True), lens=_i32(np.full((W, R), 16)),
+                       table=_i32(np.where(np.arange(M) == 0, np.arange(R)[:, None], -1)[None].repeat(W, 0)))
+    layer = cache.new_layer()
+    for x in (layer.k, layer.v):
+        x.fill_(1)
+    for x in (layer.k_scale, layer.v_scale):
+        x.fill_(1.0)
+    q = torch.ones((W * R, 1, 64), dtype=torch.float16, device="cuda:0")
+    out, lead = torch.zeros_like(q), _i32(np.zeros((W, R)))
+    cache.plan_device(lead, 4)
+    cache.attend_shared_device(layer, q, out)
+    assert bool((out == 1.0).all())
+    cache.fork_device(lead)
+    cache.attend_shared_device(layer, q, out.fill_(7.0))
+    assert bool((out == 7.0).all())
+    cache.plan_device(lead, 4)
+    cache.attend_shared_device(layer, q, out)
+    assert bool((out == 1.0).all())
+    cache.close()
