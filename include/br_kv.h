@@ -70,7 +70,7 @@ enum {
 
 /* slots of a worker's stats block (int64 each), after the step */
 enum {
-  BR_KV_ST_TOKENS = 0, /* cached tokens: the worker's load L_g */
+  BR_KV_ST_TOKENS = 0, /* cached tokens: the worker's load L_g; what several rows hold together counts for each of them (br_kv_attend_shared may read it once) */
   BR_KV_ST_USED = 1,   /* blocks in use */
   BR_KV_ST_FREE = 2,   /* blocks free */
   BR_KV_ST_ROWS = 3,   /* rows that hold tokens */
@@ -282,7 +282,8 @@ typedef struct {
  * br_kv_step of a context of br_kv_init_shared.  In its order, with what is different:
  *  1. a block that is given back is free once no row holds it;
  *  2. a row with add > 0 whose kp tokens end inside a block that other rows hold too, after 1, needs one block more: it comes to stand in that
- *     one's place in the row's table.  Each such row gets one, also if all holders of the block do; it is counted by the refusals and the stats as any other;
+ *     one's place in the row's table.  Each such row gets one, also if all holders of the block do (so that eight samples that
+ *     write into a block of their prompt need eight free ones, for the step); it is counted by the refusals and the stats as any other;
  *  3. the block taken in another's place is the row's first.  A block that lost its last holder in this way is free after the step.
  * copies (src, dst [n_workers][rows], n = rows): what row r needs copied, src the block that it held, dst the one that it holds now; -1, -1 if nothing.  br_kv_copy
  * with this list comes before the step's tokens are appended, for every layer.
@@ -299,7 +300,7 @@ int32_t br_kv_compact(br_kv_ctx *ctx, const br_kv_moves *out);
 
 /*
  * Codes and scales of blocks src to blocks dst, as they are.  A block that is dst of two pairs, or src of one and dst of another, of the same call: what it and
- * the latter's dst get is not said.  Takes every context.
+ * the latter's dst get is not said.  A list's places take time also where they are no pairs.  Takes every context.
  */
 int32_t br_kv_copy(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_moves *in);
 
@@ -307,7 +308,8 @@ int32_t br_kv_copy(br_kv_ctx *ctx, const br_kv_layer *layer, const br_kv_moves *
  * Rows whose single tokens are read together.  lead [n_workers][rows]: the row of the same worker that leads row r (itself, outside [0, rows), or NULL: it is
  * alone).  Rows of one leader are a family; what they hold together is found in the tables, by comparing each with the leader, or, where that is not one of them
  * or holds no token, with the first of them that does (a company with a row that has gone its own way holds nothing together): whatever lead says, each row's result is
- * that of its own tokens.  start, count: as br_kv_attention's, or both NULL; rows whose count is not 1 have no part in it.  members: a family's rows are
+ * that of its own tokens.  start, count: as br_kv_attention's, or both NULL; rows whose count is not 1 have no part in it (br_kv_attend serves them, given a count of
+ * 0 for the others).  members: a family's rows are
  * taken together, so many at most (and 64 query rows, of wide heads 32, where they have more heads than that allows).
  */
 typedef struct {
@@ -326,7 +328,8 @@ int32_t br_kv_plan(br_kv_ctx *ctx, const br_kv_families *in);
 
 /*
  * br_kv_attend of the planned rows' tokens (start, count, lens and table are NULL, max_count 1 or more): whole tiles of 64 tokens that the rows read together hold in
- * the same blocks are read once for all of them.  Results are br_kv_attend's but for the order of the sums, which the families have a say in; equal plans and inputs give
+ * the same blocks are read once for all of them.  Where little is held together (8 or 32 rows of some 500 tokens) br_kv_attend is faster: which of both is called is the
+ * caller's to say.  Results are br_kv_attend's but for the order of the sums, which the families have a say in; equal plans and inputs give
  * equal outputs.  Before the first plan: BR_EINVAL.  Where no plan has run since the last br_kv_step_shared or br_kv_fork, also one that was captured only,
  * no row has a part in it, and nothing is written.
  */

@@ -202,7 +202,8 @@ int32_t attend_by_rows(br_kv_ctx *ctx, BrKvAttend &p, int max_count, int few_row
   const int group = p.group;
   const int64_t rows = (int64_t)max_count * group;
   // One does where the tables span few tiles: 10 rows of up to 110 tokens and 6 key heads 13.4 us, in two launches 24; 30 rows of 470 and
-  // 8 key heads, near the line, 27 to 33 us and 38.
+  // 8 key heads, near the line, 27 to 33 us and 38.  (by64 * tiles: 32 for each compute unit; two maps, one row of 8000 tokens, 32 of them queries, 8 key heads of 128
+  // channels, groups of 4, 40.7 us, with 8 for each 65; two of 12000, 4 key heads, 51 and 90; with 128 as with 32.)
   const int64_t tiles = (int64_t)p.n_rows * c.n_kv_heads * ((((int64_t)c.max_blocks << ctx->t.shift) + BR_KV_TILE - 1) / BR_KV_TILE);
   const bool both = rows > 64 && (tiles > 8 * ctx->cus || (int64_t)p.n_rows * c.n_kv_heads > most_tiles);
   const int64_t by64 = (rows + 63) / 64;

@@ -128,7 +128,7 @@ __device__ __forceinline__ int br_kv_place(const BrKvAttend &p, const BrKvRow &w
   return br_kv_shared(MODE) ? p.members[w.start + min(i, max(w.n - 1, 0))].y : w.start + i;
 }
 
-// x times inv, and of DIFF less lambda times y times inv_y: zero where nothing was seen, whatever lambda is.
+// DIFF: what the second map of a head is multiplied by: zero where nothing was seen, whatever lambda is.
 __device__ __forceinline__ float br_kv_lambda(const BrKvAttend &p, int t, int head, float inv) {
   return inv == 0.0f ? 0.0f : p.lambda[(long long)t * p.lambda_token + head];
 }
@@ -791,14 +791,19 @@ struct BrKvRuns {
       // tile: 32 companies of 8 rows that hold 2000 tokens (D 128, 4 query heads) 30 us in runs, 21 so; two maps of 32 query heads on one key head, one row of 4000
       // tokens, 57 and 30; 96 rows of 8, 2000 tokens, 36 and 29, though a part is up to 12 tiles over the mean.  One block is better where K save less than JOIN.
       // The join goes over K pieces as the blocks go over most / K tiles, so K is about the root of `most`: one row of 40000 tokens, two maps of 32 query heads on a key
-      // head, 100 us with as many as there are blocks for, 54 with 32; of 12000 tokens 44 and, with 16, 36.
+      // head, 100 us with as many as there are blocks for, 54 with 32; of 12000 tokens 44 and, with 16, 36.  Pieces of 16 rows are smaller: the root of 6 most, with that of 2 most one
+      // row of 40000 tokens and 8 query rows to one key head 23.1 us and 24.6, of 12000 to two 19.5 and 20.3, but four beams of 30000 on one 26.1 and 23.8.
       const int k = whole > 1 && 2 * total_q <= workers_most ? max(1, min(min(workers_most / max(total_q, 1), (int)__builtin_amdgcn_sqrtf((TQ > 16 ? 2.0f : 6.0f) * most)), most / (NR * least))) : 1;
       const int split = k > 1 ? (most + NR * k - 1) / (NR * k) : whole;
       if (k > 1) parts = whole <= split + JOIN;
       parts *= NR;
+      // Where runs would have the same number of tiles, uneven parts are faster up to 16 tiles over the mean: 64 rows of 8 (1000 to 3000 tokens, 8 query heads) 31.3 us, with 4
+      // over the mean 42.4, 96 of 8 (2000, 4 query heads) with none 39.1, so 29.7; with 64 as with 16.
       if (k > 1 && !parts && split <= max((int)min(q, 1ll << 20), (int)((float)total * __builtin_amdgcn_rcpf((float)(total_q * k)))) + 16) parts = NR * k, total_q *= k, sum_q *= k;
       // More query tiles than blocks: whole ones, one after the other.  152 rows of 2 (300 tokens, D 128, 12 query heads, 5 key heads) 39 us in runs, 30 so; 1103 tokens 52 and 40;
       // with 40 over the mean for two waves to a tile too, 300 rows of 8 (1103, 8 query heads, 8 key heads) 57 and 67.
+      // Up to eight to a block: with two 300 rows of 2 (300 tokens, 12 query heads, 5 key heads) 54 us and 41.8 so, two maps of 100 rows of 64 queries in 300 tokens 156 and 134;
+      // with 64 to a block 1000 rows of 2 (100 tokens, 8 key heads) 159 and 172, the others the same (their count is exact below BR_KV_COUNTED only).
       if (NR == 1 && total_q > workers_most && total_q < min(8 * workers_most, BR_KV_COUNTED)) {
         const int rounds = (total_q + workers_most - 1) / workers_most;
         if (rounds * most <= (int)min(q, 1ll << 20) + ROUNDS) {
@@ -1310,7 +1315,7 @@ __global__ __launch_bounds__(256, WAVES) void br_kv_k_attend_rows(BrKvAttend p) 
 // between them before the run's end, where the P sums of a row are joined in LDS.  A tile is decoded TQ / (16 NQ) times.  The queries are in LDS: in
 // registers they drove others out to memory, and every reload of those waited for the codes on their way (96 rows of 8 to a company, groups of 8, up to 16384
 // tokens together, 8 key heads of 128 channels, fp8: 72 us, 66 with them in LDS; a tile through LDS for all four waves of a block, as for many rows above: 84, and 98 by
-// the kernel of few rows).  Such a call, 184 MB, out of memory 72 us: two waves on a SIMD, each waits for its values' codes about as long as it computes.  Calls of a few
+// the kernel of few rows).  Such a call, 217 MB, out of memory 72 us: two waves on a SIMD, each waits for its values' codes about as long as it computes.  Calls of a few
 // companies are bound by a chain instead: division and place 2.3 us, the members 1.2, queries and first codes 4.5, each tile of a wave 2.5 (some 900 vector
 // instructions, two waves to a SIMD), the join in LDS 2, through memory some 7 more.
 template <int D, int TQ, int NQ, bool FP8, int NW, int WAVES>
@@ -1319,6 +1324,8 @@ __global__ __launch_bounds__(64 * NW, WAVES) void br_kv_k_attend_together(BrKvAt
   // A block that has fewer than LEAST tiles pays more for its pieces than it saves: with 8 for all, 20 rows of 11 key heads that hold 4339 tokens
   // together (D 256, 6 query heads each, by 64 rows) 96 us, here 59; for one wave to a tile, 8 rows of 8 (500 tokens, D 128, 4 query heads) 22 and 19; with 2 for two, 8 rows of 8
   // (2000, 8 query heads) 29 and 27.  JOIN: 96 rows of 8 (500, 4 query heads) 25 us with 12 / NH, 23 so, 32 of them with 20 / NH 23, 20 so.
+  // ROUNDS of one wave to a tile: with 8 over the mean 152 rows of 2 (1103 tokens, D 128, 12 query heads, 5 key heads) 49.9 us, so 41.7, 200 of 4 (64 to 900, 8 query heads, 7) 50.1 and 42.2; with
+  // 160 the same.
   constexpr int LEAST = NH < 2 ? 4 : 8 / NH, SLACK = 20 / NH, JOIN = NH < 2 ? 16 : 12 / NH, ROUNDS = NH < 2 ? 40 : 20 / NH;
   using Runs = BrKvRuns<TQ, NT, 1, SLACK, MODE, JOIN, ROUNDS>;
   __shared__ typename Runs::Shared shared;

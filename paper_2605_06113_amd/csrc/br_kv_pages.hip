@@ -105,8 +105,8 @@ __global__ __launch_bounds__(256) void br_kv_k_fork_put(BrKvTables t, BrKvNext x
   if (blockIdx.x == 0 && threadIdx.x == 0) *t.planned = 0;
 }
 
-// Bound by the way to memory: 512 workers of 144 rows, up to 133 entries each, 19.6 us, some 45 MB of lines of own and others' rows, a launch and four dependent
-// trips.  The next four entries on their way beside these ones' work did not change that.
+// Bound by the way to memory: 512 workers of 144 rows, up to 133 entries each, a tenth of which change, 21.4 us, 58 MB of lines of own and others' rows (2.7 TB/s), a
+// launch and four dependent trips.  The next four entries on their way beside these ones' work did not change that.
 // Both for one worker by one block, 16 lanes to a row: no row's entries are written before all have been read.  A lane notes which of its first 60 entries
 // change: rows of one family differ in a few, and the others are not looked at again.
 template <int NT>
@@ -159,8 +159,9 @@ __global__ __launch_bounds__(NT) void br_kv_k_fork(BrKvTables t, BrKvNext x, con
   if (w == 0 && threadIdx.x == 0) *t.planned = 0;
 }
 
-// One block for each worker: which blocks go where, the used bits and the counts.  The used bits are in LDS.  Bound by four scans and the trips between them, not
-// by what they move: one worker of 96 rows 3.6 us, 300 of 31 rows 6.0, 80 to 87 % of the time waiting.
+// One block for each worker: which blocks go where, the used bits and the counts.  The used bits are in LDS.  Bound by four scans and the trips between them,
+// not by what they move: one worker of 96 rows and 3916 blocks, 856 of which move, 11.0 us, 2.8 if none does; 300 of 31 rows, 56 moves each, 12.1; 83 to 87 % of the
+// time waiting.
 template <int NT>
 __global__ __launch_bounds__(NT) void br_kv_k_compact(BrKvTables t, BrKvNext x, BrKvMoves m) {
   extern __shared__ unsigned used[];
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(NT) void br_kv_k_compact(BrKvTables t, BrKvNext x, 
     for (int i = tid; i < t.words; i += NT) gused[i] = used[i];
 }
 
-// The tables' entries, by where the blocks have gone (behind br_kv_k_compact): three dependent trips, 2.6 us of one worker, 4.1 of 300 of 31 rows.
+// The tables' entries, by where the blocks have gone (behind br_kv_k_compact): three dependent trips, 4.4 us of one worker, 5.2 of 300 of 31 rows.
 template <int G>
 __global__ __launch_bounds__(256) void br_kv_k_compact_tables(BrKvTables t, BrKvNext x, int slices) {
   br_kv_rows<G>(t, slices, [&](int r, int w, int first) {
@@ -247,7 +248,8 @@ __global__ __launch_bounds__(256) void br_kv_k_compact_tables(BrKvTables t, BrKv
 }
 
 // Large blocks: a block of threads has one piece of a pair's keys or values, all of it on its way at once; the scales go with the first.  Bound by memory: requests
-// of 64 KB a block, 1.39 GB read and written, 278 us = 5.0 TB/s (a large copy 5.1).
+// of 64 KB a block, 1.39 GB read and written, 278 us = 5.0 TB/s (a large copy 5.1); 856 such blocks out of 3916 places, 225 MB, 54 us = 4.2.  A place that is no
+// pair costs its turns all the same, each a wait for src and dst: 73728 of them 59 us (blocks of 16 KB), 113 (64 KB).
 template <int AT_ONCE>
 __global__ __launch_bounds__(256) void br_kv_k_copy(BrKvCache c, BrKvMoves m, int W, int chunks, long long units) {
   constexpr int CHUNK = AT_ONCE * 256 * 16;
@@ -275,7 +277,8 @@ __global__ __launch_bounds__(256) void br_kv_k_copy(BrKvCache c, BrKvMoves m, in
 }
 
 // Pairs' codes in pieces of 1 KB, 16 bytes a lane: a block's keys, its values, then its scales as one piece.  A wave has eight pieces on their way at once.  Bound by
-// memory: 69 MB in 13.6 us = 5.1 TB/s.
+// what a wave does before them, a division and three dependent loads for each piece: 16800 pairs, 69 MB, 26.9 us = 2.6 TB/s, 71 % of the time waiting; 73728 places
+// without a pair 28.
 __global__ __launch_bounds__(256) void br_kv_k_copy_small(BrKvCache c, BrKvMoves m, int W, int half, long long batches) {
   constexpr int AT_ONCE = 8;
   typedef unsigned u4 __attribute__((ext_vector_type(4)));

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void br_kv_k_plan_common(BrKvTables t, BrKvPla
 // One block for each worker, a thread for each row: a family's rows in companies of at most `most`, evenly, in the order of the rows.  Rows without tokens
 // are families of their own: they have nothing in common with any other.
 // ALONE: what rows have in common is found here too (else by br_kv_k_plan_common, before).  Bound by its chain of loads and barriers: four rows of one worker
-// 4.1 us, a launch that does nothing 3.9; 96 rows in two launches 4.8 and 5.2.
+// 3.9 us; 96 rows in two launches 4.8 and 5.5.
 template <int NT, bool ALONE>
 __global__ __launch_bounds__(NT) void br_kv_k_plan(BrKvTables t, BrKvPlan x) {
   __shared__ __attribute__((aligned(16))) int family[NT];
@@ -123,8 +123,8 @@ __global__ __launch_bounds__(NT) void br_kv_k_plan(BrKvTables t, BrKvPlan x) {
 
 void br_kv_launch_plan(const BrKvTables &t, const BrKvPlan &x, hipStream_t st) {
   // A wave takes some 1.2 us for what a row has in common with its leader.  One worker's rows by its one block, in one launch, or by the card, in two: 16 rows
-  // 5.1 us and 8.5, 64 rows (a block of 16 waves) 6.7 and 8.7, 96 rows with tables out of memory 11.6 and 9.6, 256 rows 16 and 11.  Many workers fill the card by
-  // themselves, with blocks of four waves if they are very many: 512 of 144 rows 23 us and 28, 4096 of 32 rows 27, 67 with 16 waves each, and 46.
+  // 5.3 us and 9.0, 64 rows (a block of 16 waves) 6.5 and 8.6, 96 rows behind an attention, plan and attention together, 81.3 and 79.4, 256 rows 15.4 and 11.5.  Many workers
+  // fill the card by themselves, with blocks of four waves if they are very many: 512 of 144 rows 17.5 us and 32, 4096 of 32 rows 24.5, 45 with 16 waves each, and 54.
   if (t.B <= 16 || (t.W >= 1024 && t.B <= 256)) {
     br_kv_k_plan<256, true><<<t.W, 256, 0, st>>>(t, x);
     return;

@@ -348,7 +348,8 @@ class KvCache:
             self._done(rc, "br_kv_compact")
 
     def copy_device(self, layer: KvLayer, src, dst, src_worker=None) -> None:
-        """What blocks src hold to blocks dst (br_kv_copy): [n_workers, n] block ids of each worker, -1: none; src_worker: whose block src is, if another worker's."""
+        """What blocks src hold to blocks dst (br_kv_copy): [n_workers, n] block ids of each worker, -1: none (but passed over one by one); src_worker: whose block src
+        is, if another worker's."""
         if layer.sizes != self._layer:
             raise BrError("the layer is one of another cache's sizes")
         self._pack_moves(src, dst, src_worker)
@@ -426,8 +427,9 @@ class KvCache:
         """Which rows attend_shared_device reads together (br_kv_plan), for all layers of a step: behind step_device.
 
         lead [n_workers, rows] int32: the row that row r shares its first blocks with (its family's first, which may have left since, itself, or -1); at most `members` rows together:
-        with 16 query rows of a key head short calls are fastest, with more those that read much.
-        start, count: step_device's; rows whose count is not 1 are left out; none: token r belongs to row r."""
+        with 16 query rows of a key head short calls are fastest, with more those that read much.  Where rows hold little together (8 or 32 of them some 500 tokens)
+        attend_device alone is faster than both calls; from some 1000 tokens, or for a hundred rows, reading together is.
+        start, count: step_device's; rows whose count is not 1 are left out (attend_device serves them, with a count of 0 for the others); none: token r belongs to row r."""
         self._is_shared()
         at = (self._check(lead, "lead", self._rows, self._i32), *self._check_lists(start, count))
         try:
